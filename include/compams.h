@@ -341,6 +341,135 @@ int compams_inplace_probe(float* const* arrays, int n_arrays, size_t count, int 
 int compams_step_static(const compams_config* cfg, const float* g, float lr, int32_t* idx_out, float* val_out,
                         void* hip_stream);
 
+/* ---- Operators of the workers' models --------------------------------------------------------------------
+ * What the forward and backward pass that fills the gradient rows g of Algorithm 2 needs around its matrix products:
+ * layer norm, dropout from a counter-based generator, the join of a transformer block (both together with the residual
+ * add) and the softmax cross-entropy.  They need no context.
+ *
+ *   - Activations are matrices of n * rows rows: n workers (as in compams_config) of `rows` rows each, worker after
+ *     worker; row r starts r * ld elements after the first, its `cols` entries follow one another, and whatever lies
+ *     between two rows is never touched.  ld >= cols; pointers need the alignment of their type only (16 bytes, in rows
+ *     too, stream faster).  A length of zero rows is legal.
+ *   - Weights are float[cols], their gradients one float[cols] per worker, `ld_d...` elements apart: a parameter's place
+ *     in a worker's row of g and that row's stride (theta + offset, g + offset and ld).  What a worker's rows add up to
+ *     does not depend on the other workers, and on no order of execution: two calls on the same inputs give the same
+ *     bits.
+ *   - Sums, statistics and everything in between are fp32; every output is rounded once.
+ *   - Entry points only enqueue kernels on hip_stream (no allocation, no synchronisation, no memset or copy node), on
+ *     the device that is current, so a call may be recorded into a HIP graph.  Device memory is the caller's, the
+ *     workspace included; ordering calls that share buffers on different streams is the caller's.  Status codes as
+ *     above; nothing is enqueued by a call that returns COMPAMS_INVALID_ARG, COMPAMS_BAD_ALIGNMENT or
+ *     COMPAMS_WORKSPACE_TOO_SMALL.
+ *   - An output may be an input's own buffer where both have the same type and stride and the input is named beside it
+ *     ("may be"); otherwise buffers must not overlap. */
+enum {
+  COMPAMS_F32 = 0,  /* float */
+  COMPAMS_F16 = 1,  /* IEEE binary16; results beyond its range become infinite */
+  COMPAMS_BF16 = 2, /* bfloat16 */
+  COMPAMS_I32 = 3,  /* int32_t (targets) */
+  COMPAMS_I64 = 4   /* int64_t (targets) */
+};
+
+/* Dropout: entry (r, c) of a matrix is kept where u(r, c) >= T and then multiplied by 65536 / (65536 - T), else it is
+ * replaced by 0 (whatever it was), with T = floor(65536 p + 1/2): p is rounded to the nearest 65536th, and the factor is
+ * the exact one for the rounded p.  u(r, c) is a number of 16 bits from Philox-4x32 with ten rounds (Salmon, Moraes,
+ * Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): counter words (c div 8, r, low and high half of
+ * the offset), key = low and high half of the seed, column c taking bits 16 (c mod 2) and up of word (c mod 8) div 2.
+ * The mask is a function of seed, offset, r and c alone - of no type, stride or launch - and is never stored: the
+ * backward pass makes it again.  Give every use within a step, and every step, an offset (or a seed) of its own. */
+typedef struct compams_drop {
+  double p;              /* 0 <= p <= 1 */
+  uint64_t seed, offset;
+  const uint64_t* step;  /* DEVICE, or NULL: a number that is added to offset when the kernel runs (so that replays of
+                            a HIP graph can differ) */
+} compams_drop;
+
+/* y = dropout(x), or residual + dropout(x); its own backward pass: dx = dropout(dy).
+ *   x: n * rows x cols of type x_type.  residual: the same of type y_type, or NULL.  y: of type y_type; may be x or
+ *   residual.  x_type and y_type: equal, or one of them COMPAMS_F32. */
+int compams_dropout(int32_t n, int64_t rows, int64_t cols, int32_t x_type, int32_t y_type, const void* x, int64_t ld_x,
+                    const void* residual, int64_t ld_residual, void* y, int64_t ld_y, const compams_drop* drop,
+                    void* hip_stream);
+
+/* Layer norm, and the join between two branches of a transformer block.  For every row, with sums over its C = cols
+ * entries:
+ *   join only:  h = residual + dropout(x + bias)
+ *   mean = sum(h) / C,  rstd = 1 / sqrt(sum((h - mean)^2) / C + eps),  z = (h - mean) rstd,  y = gamma z + beta
+ * and backward, with the gradients dy of y and (join only) dh of h, u = gamma dy:
+ *   d = rstd (u - sum(u) / C - z sum(u z) / C) (+ dh)
+ *   dgamma = sum over the worker's rows of dy z,  dbeta = sum of dy
+ *   layer norm: dresidual = d;  join: dresidual = d, dx = dropout(d), dbias = sum over the worker's rows of dx
+ * The norm is taken of h before h is rounded to its type; the backward pass reads h as it was stored, with the saved
+ * statistics. */
+typedef struct compams_norm {
+  int32_t n;           /* workers, 1 <= n <= 65535 */
+  int64_t rows;        /* rows per worker, >= 0; n * rows < 2^31 */
+  int64_t cols;        /* 1 <= cols < 2^31 */
+  int32_t type;        /* of x, y, dy, dx */
+  int32_t stream_type; /* of h, residual, dh, dresidual: `type` or COMPAMS_F32 */
+  float eps;           /* >= 0 */
+  compams_drop drop;   /* join only */
+  const float* gamma;  /* cols, or NULL: all 1 */
+  const float* beta;   /* cols, or NULL: all 0 (forward) */
+  const float* bias;   /* cols, or NULL: all 0 (join, forward) */
+  /* forward */
+  const void* x;        int64_t ld_x;        /* join: the branch */
+  const void* residual; int64_t ld_residual; /* join: the residual stream, or NULL: all 0 */
+  void* h;              int64_t ld_h;        /* layer norm: its input, not written.  join: receives h, or NULL; may be
+                                                residual.  backward: h as it was stored */
+  void* y;              int64_t ld_y;        /* may be x; layer norm with one type: may be h */
+  float* mean;                               /* n * rows each; forward: receive the statistics, or NULL */
+  float* rstd;
+  /* backward */
+  const void* dy; int64_t ld_dy;
+  const void* dh; int64_t ld_dh;             /* join: the gradient of h from elsewhere, or NULL: all 0 */
+  void* dx;        int64_t ld_dx;            /* join: gradient of x, or NULL; may be dy */
+  void* dresidual; int64_t ld_dresidual;     /* gradient of h (layer norm) or of residual (join), or NULL; may be dh */
+  float* dgamma; int64_t ld_dgamma;          /* per worker, or NULL */
+  float* dbeta;  int64_t ld_dbeta;
+  float* dbias;  int64_t ld_dbias;           /* join */
+  int32_t accumulate;                        /* 1: the three gradients above are added to what is there; 0: written */
+  void* workspace;                           /* DEVICE, 256-byte aligned (backward) */
+  size_t workspace_bytes;
+} compams_norm;
+
+/* Bytes of workspace that the backward call with these fields takes (n, rows, cols, types, and which of the gradients
+ * are asked for); 0 if it takes none, and for an invalid configuration.  Host-only.  The workspace holds nothing from
+ * one call to the next. */
+size_t compams_norm_workspace_size(const compams_norm* a);
+int compams_layer_norm_forward(const compams_norm* a, void* hip_stream);
+int compams_layer_norm_backward(const compams_norm* a, void* hip_stream);
+int compams_dropout_add_norm_forward(const compams_norm* a, void* hip_stream);
+int compams_dropout_add_norm_backward(const compams_norm* a, void* hip_stream);
+
+/* Softmax cross-entropy and its gradient, every worker's loss the mean over its tokens.  For row r with target t:
+ *   losses[r] = log(sum_c exp(l_c - max l)) + max l - l_t,  dlogits = grad_scale / count (softmax(l) - [c = t])
+ *   mean_loss[i] = sum of worker i's losses / count
+ * with count = the worker's rows whose target is not ignore_index; ignored rows have loss 0 and gradient 0 whatever
+ * their logits are, and a worker without any other row has mean_loss 0.  Logits of minus infinity have probability 0
+ * (the loss is infinite where the target's is).  A row without a finite logit or with a NaN or plus infinity has no
+ * softmax, and a target outside [0, vocab) no loss: loss and gradient of such a row are NaN. */
+typedef struct compams_loss {
+  int32_t n;           /* workers, 1 <= n <= 65535 */
+  int64_t rows;        /* rows per worker, >= 0; n * rows < 2^31 */
+  int64_t vocab;       /* 1 <= vocab < 2^31 */
+  int32_t type;        /* of logits and dlogits */
+  int32_t target_type; /* COMPAMS_I32 or COMPAMS_I64 */
+  const void* logits; int64_t ld_logits;
+  const void* targets;                   /* n * rows */
+  int64_t ignore_index;
+  float grad_scale;                      /* factor of the gradient alone (a scaled loss) */
+  float* mean_loss;                      /* n, or NULL */
+  float* losses;                         /* n * rows, or NULL */
+  void* dlogits; int64_t ld_dlogits;     /* or NULL: the loss alone; may be logits */
+  void* workspace;                       /* DEVICE, 256-byte aligned */
+  size_t workspace_bytes;
+} compams_loss;
+
+/* Bytes of workspace that the call with these fields takes; 0 if none, and for an invalid configuration. */
+size_t compams_loss_workspace_size(const compams_loss* a);
+int compams_cross_entropy(const compams_loss* a, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,7 +28,9 @@ _STATE_DTYPE = {"last_idx": torch.int32, "last_signbits": torch.int32, "last_thr
 EXPORTS = ["compams_workspace_size", "compams_init", "compams_step", "compams_state", "compams_set_option",
            "compams_profile_enable", "compams_profile_read", "compams_destroy", "compams_strerror", "compams_copy", "compams_inplace_probe", "compams_cached_state_arrays",
            "compams_wire_capacity", "compams_encode", "compams_decode", "compams_worker_step", "compams_server_step",
-           "compams_step_static"]
+           "compams_step_static", "compams_dropout", "compams_norm_workspace_size", "compams_layer_norm_forward",
+           "compams_layer_norm_backward", "compams_dropout_add_norm_forward", "compams_dropout_add_norm_backward",
+           "compams_loss_workspace_size", "compams_cross_entropy"]
 STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -87,6 +89,14 @@ def lib():
                                           ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p]
         L.compams_step_static.argtypes = [cfgp, ctypes.c_void_p, ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p,
                                           ctypes.c_void_p]
+        # the operators of the workers' models (operators.py)
+        i32, i64, ptr = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
+        L.compams_dropout.argtypes = [i32, i64, i64, i32, i32, ptr, i64, ptr, i64, ptr, i64, ptr, ptr]
+        for f in (L.compams_norm_workspace_size, L.compams_loss_workspace_size):
+            f.restype, f.argtypes = ctypes.c_size_t, [ptr]
+        for f in (L.compams_layer_norm_forward, L.compams_layer_norm_backward, L.compams_dropout_add_norm_forward,
+                  L.compams_dropout_add_norm_backward, L.compams_cross_entropy):
+            f.argtypes = [ptr, ptr]
         _lib = L
     return _lib
 

@@ -1,0 +1,88 @@
+// Dropout from a counter-based generator, alone or added to a residual stream.
+#include "compams_rows.h"
+
+namespace compams {
+namespace {
+
+struct DropoutArgs {
+  uint32_t total, cols;
+  uint32_t across;  // workgroups side by side in a row
+  uint32_t wide;    // lanes side by side in a workgroup: a power of two
+  const void *x, *residual;
+  void* y;
+  int64_t ld_x, ld_residual, ld_y;
+  Drop drop;
+};
+constexpr uint32_t kThreads = 256;
+
+template <typename X, typename Y>
+__global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a) {
+  const uint32_t tall = kThreads / a.wide;
+  const uint32_t c = (blockIdx.x % a.across * a.wide + threadIdx.x % a.wide) * kGroup;
+  if (c >= a.cols) return;
+  const uint64_t offset = drop_offset(a.drop);
+  const uint32_t step = gridDim.x / a.across * tall;
+  for (uint64_t r = blockIdx.x / a.across * tall + threadIdx.x / a.wide; r < a.total; r += step) {
+    float v[kGroup];
+    load_group(v, static_cast<const X*>(a.x) + static_cast<int64_t>(r) * a.ld_x, c, a.cols);
+    drop_group(v, a.drop, offset, static_cast<uint32_t>(r), c);
+    if (a.residual) {
+      float w[kGroup];
+      load_group(w, static_cast<const Y*>(a.residual) + static_cast<int64_t>(r) * a.ld_residual, c, a.cols);
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) v[j] = w[j] + v[j];
+    }
+    store_group(static_cast<Y*>(a.y) + static_cast<int64_t>(r) * a.ld_y, c, a.cols, v);
+  }
+}
+
+template <typename X, typename Y>
+hipError_t launch_dropout(const DropoutArgs& a, uint32_t blocks, hipStream_t stream) {
+  hipLaunchKernelGGL((k_dropout<X, Y>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace compams
+
+extern "C" int compams_dropout(int32_t n, int64_t rows, int64_t cols, int32_t x_type, int32_t y_type, const void* x,
+                               int64_t ld_x, const void* residual, int64_t ld_residual, void* y, int64_t ld_y,
+                               const compams_drop* drop, void* hip_stream) {
+  using namespace compams;
+  if (!rows_valid(n, rows, cols) || !float_type(x_type) || !float_type(y_type) || !drop || !drop_valid(*drop))
+    return COMPAMS_INVALID_ARG;
+  if (x_type != y_type && x_type != COMPAMS_F32 && y_type != COMPAMS_F32) return COMPAMS_INVALID_ARG;
+  if (rows == 0) return COMPAMS_OK;
+  if (!x || !y || !stride_valid(ld_x, cols) || !stride_valid(ld_y, cols) || (residual && !stride_valid(ld_residual, cols)))
+    return COMPAMS_INVALID_ARG;
+  if (!aligned_to(x, type_size(x_type)) || !aligned_to(y, type_size(y_type)) || !aligned_to(residual, type_size(y_type)) ||
+      !aligned_to(drop->step, 8))
+    return COMPAMS_BAD_ALIGNMENT;
+  DropoutArgs a = {};
+  a.total = static_cast<uint32_t>(n * rows);
+  a.cols = static_cast<uint32_t>(cols);
+  a.x = x; a.residual = residual; a.y = y;
+  a.ld_x = ld_x; a.ld_residual = ld_residual; a.ld_y = ld_y;
+  a.drop = make_drop(*drop);
+  const uint32_t groups = (a.cols + kGroup - 1) / kGroup;
+  a.wide = 1;
+  while (a.wide < groups && a.wide < kThreads) a.wide *= 2;
+  a.across = (groups + a.wide - 1) / a.wide;
+  const uint32_t tall = kThreads / a.wide;
+  // (a dimension has room for 2^32 threads: rows beyond are taken in further turns)
+  const uint64_t down = (static_cast<uint64_t>(a.total) + tall - 1) / tall, most = (1u << 23) / a.across;
+  const uint32_t blocks = static_cast<uint32_t>(down < most ? down : most > 0 ? most : 1) * a.across;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipError_t err;
+  if (x_type == COMPAMS_F32)
+    err = y_type == COMPAMS_F32   ? launch_dropout<float, float>(a, blocks, stream)
+          : y_type == COMPAMS_F16 ? launch_dropout<float, half_t>(a, blocks, stream)
+                                  : launch_dropout<float, bfloat_t>(a, blocks, stream);
+  else if (x_type == COMPAMS_F16)
+    err = y_type == COMPAMS_F32 ? launch_dropout<half_t, float>(a, blocks, stream)
+                                : launch_dropout<half_t, half_t>(a, blocks, stream);
+  else
+    err = y_type == COMPAMS_F32 ? launch_dropout<bfloat_t, float>(a, blocks, stream)
+                                : launch_dropout<bfloat_t, bfloat_t>(a, blocks, stream);
+  return err == hipSuccess ? COMPAMS_OK : COMPAMS_HIP_ERROR;
+}
