@@ -1,0 +1,373 @@
+// Layer norm and the join of a transformer block, backward, with the gradients of the weights per worker.
+#include <math.h>
+
+#include "compams_norm.h"
+
+namespace compams {
+namespace {
+
+// One column's sum over a part, to where it belongs: the partial sums, or where a worker has one part, the gradient.
+__device__ __forceinline__ void emit_gradient(const NormArgs& a, uint32_t worker, uint32_t part, uint32_t which, uint32_t c,
+                                              float sum) {
+  if (a.parts > 1) {
+    a.partial[((static_cast<size_t>(worker) * a.parts + part) * kGradients + which) * a.cols + c] = sum;
+  } else {
+    float* const p = a.grad[which] + static_cast<int64_t>(worker) * a.ld_grad[which] + c;
+    *p = a.accumulate ? *p + sum : sum;
+  }
+}
+
+// ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
+// As in the forward pass, a team is 8 to 64 lanes of a wavefront (WAVE) or a whole workgroup, and a lane keeps to its
+// columns: it adds up the weights' gradients of the rows that its team takes.  A workgroup takes one part of a worker's
+// rows and leaves one sum per column.
+constexpr uint32_t kTeamThreads = 256;
+
+// v summed over the teams of a wavefront: over the lanes that are multiples of `lanes` apart.
+__device__ __forceinline__ float sum_teams(float v, uint32_t lanes) {
+  if (lanes <= 8) v += dpp<0x128>(v);  // a row's lanes turned by 8
+  if (lanes <= 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  if (lanes <= 32) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  return v;
+}
+
+template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN>
+__global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_backward(NormArgs a, uint32_t lanes) {
+  constexpr uint32_t kOf = JOIN ? 3 : 2;
+  __shared__ float slots[2][2][16];
+  extern __shared__ float tile[];  // WAVE: a row of columns for each wavefront
+  const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
+  const uint32_t together = WAVE ? kTeamThreads / lanes : 1u;
+  const uint32_t team = WAVE ? threadIdx.x / lanes : 0u;
+  const uint64_t offset = JOIN ? drop_offset(a.drop) : 0u;
+  const float count = static_cast<float>(a.cols);
+  float g[NG][kGroup];
+#pragma unroll
+  for (uint32_t k = 0; k < NG; ++k) load_weight(g[k], a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+  uint32_t turn = 0;
+  for (uint32_t job = blockIdx.x; job < a.n * a.parts; job += gridDim.x) {
+    const uint32_t w = job / a.parts, part = job % a.parts;
+    const uint32_t first = part * a.part_rows, left = a.rows - first, rows = left < a.part_rows ? left : a.part_rows;
+    float sum[kOf][NG][kGroup] = {};
+    for (uint32_t i = team; i < rows; i += together, turn ^= 1) {
+      const uint32_t r = w * a.rows + first + i;
+      typename Group<T>::type raw_y[NG];
+      typename Group<H>::type raw_h[NG], raw_g[NG];
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) {
+        const uint32_t c = (k * lanes + lane) * kGroup;
+        raw_y[k] = load_raw(row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
+        raw_h[k] = load_raw(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), c, a.cols);
+        if (JOIN && a.dh) raw_g[k] = load_raw(row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
+      }
+      const float mean = a.mean[r], rstd = a.rstd[r];
+      float s[2] = {0.0f, 0.0f};
+      float z[NG][kGroup], u[NG][kGroup];
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) {
+        unpack(u[k], raw_y[k]);
+        unpack(z[k], raw_h[k]);
+#pragma unroll
+        for (uint32_t j = 0; j < kGroup; ++j) {
+          // (columns beyond the last: dy and, read from gamma's end, the weight are 0)
+          z[k][j] = (z[k][j] - mean) * rstd;
+          sum[0][k][j] = fmaf(u[k][j], z[k][j], sum[0][k][j]);
+          sum[1][k][j] += u[k][j];
+          u[k][j] *= g[k][j];
+          s[0] += u[k][j];
+          s[1] = fmaf(u[k][j], z[k][j], s[1]);
+        }
+      }
+      if constexpr (WAVE) {
+        s[0] = sum_lanes(s[0], lanes);
+        s[1] = sum_lanes(s[1], lanes);
+      } else {
+        sum_block(s, slots[turn], lanes / 64);
+      }
+      const float s0 = s[0] / count, s1 = s[1] / count;
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) {
+        const uint32_t c = (k * lanes + lane) * kGroup;
+#pragma unroll
+        for (uint32_t j = 0; j < kGroup; ++j) u[k][j] = (u[k][j] - s0 - z[k][j] * s1) * rstd;
+        if constexpr (JOIN) {
+          if (a.dh) {
+            unpack(z[k], raw_g[k]);
+#pragma unroll
+            for (uint32_t j = 0; j < kGroup; ++j) u[k][j] += z[k][j];
+          }
+        }
+        if (a.dresidual) store_group(row_of<H>(a.dresidual, a.ld_dresidual, r), c, a.cols, u[k]);
+        if constexpr (JOIN) {
+          if (a.dx || a.grad[2]) {
+            drop_group(u[k], a.drop, offset, r, c);
+            if (a.dx) store_group(row_of<T>(a.dx, a.ld_dx, r), c, a.cols, u[k]);
+#pragma unroll
+            for (uint32_t j = 0; j < kGroup; ++j) sum[2][k][j] += u[k][j];
+          }
+        }
+      }
+    }
+    for (uint32_t which = 0; which < kOf; ++which) {
+      if (!a.grad[which]) continue;
+      if constexpr (WAVE) {
+        const uint32_t across = NG * lanes * kGroup;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t k = 0; k < NG; ++k)
+#pragma unroll
+          for (uint32_t j = 0; j < kGroup; ++j) {
+            const float v = sum_teams(which == 0 ? sum[0][k][j] : which == 1 ? sum[1][k][j] : sum[kOf - 1][k][j], lanes);
+            if ((threadIdx.x & 63u) < lanes) tile[(threadIdx.x >> 6) * across + (k * lanes + lane) * kGroup + j] = v;
+          }
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < a.cols; c += kTeamThreads)
+          emit_gradient(a, w, part, which, c, (tile[c] + tile[across + c]) + (tile[2 * across + c] + tile[3 * across + c]));
+      } else {
+#pragma unroll
+        for (uint32_t k = 0; k < NG; ++k)
+#pragma unroll
+          for (uint32_t j = 0; j < kGroup; ++j) {
+            const uint32_t c = (k * lanes + lane) * kGroup + j;
+            if (c < a.cols)
+              emit_gradient(a, w, part, which, c, which == 0 ? sum[0][k][j] : which == 1 ? sum[1][k][j] : sum[kOf - 1][k][j]);
+          }
+      }
+    }
+  }
+}
+
+// ---- Rows of any width: a pass for the rows' sums, one for the columns' and one for the outputs --------------------
+constexpr uint32_t kWideThreads = 1024;
+
+// z of a group from h as it was stored.
+template <typename H>
+__device__ __forceinline__ void load_z(float (&z)[kGroup], const NormArgs& a, uint32_t r, uint32_t c, float mean, float rstd) {
+  load_group(z, row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), c, a.cols);
+#pragma unroll
+  for (uint32_t j = 0; j < kGroup; ++j) z[j] = (z[j] - mean) * rstd;
+}
+
+template <typename T, typename H>
+__global__ __launch_bounds__(kWideThreads) void k_norm_sums_wide(NormArgs a) {
+  __shared__ float slots[2][2][16];
+  uint32_t turn = 0;
+  const float count = static_cast<float>(a.cols);
+  for (uint32_t r = blockIdx.x; r < a.total; r += gridDim.x, turn ^= 1) {
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    float s[2] = {0.0f, 0.0f};
+    for (uint32_t c = threadIdx.x * kGroup; c < a.cols; c += kWideThreads * kGroup) {
+      float u[kGroup], z[kGroup], g[kGroup];
+      load_group(u, row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
+      load_weight(g, a.gamma, c, a.cols, 1.0f);
+      load_z<H>(z, a, r, c, mean, rstd);
+      for (uint32_t j = 0; j < kGroup; ++j) {
+        u[j] *= g[j];
+        s[0] += c + j < a.cols ? u[j] : 0.0f;
+        s[1] += c + j < a.cols ? u[j] * z[j] : 0.0f;
+      }
+    }
+    sum_block(s, slots[turn], kWideThreads / 64);
+    if (threadIdx.x == 0) a.sums[r] = make_float2(s[0] / count, s[1] / count);
+  }
+}
+
+// The gradient of h in a group, from the two sums of its row: dy and z are left in u and z.
+template <typename T, typename H>
+__device__ __forceinline__ void form_d(float (&d)[kGroup], float (&u)[kGroup], float (&z)[kGroup], const NormArgs& a,
+                                       uint32_t r, uint32_t c) {
+  const float mean = a.mean[r], rstd = a.rstd[r];
+  const float2 s = a.sums[r];
+  float g[kGroup];
+  load_group(u, row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
+  load_weight(g, a.gamma, c, a.cols, 1.0f);
+  load_z<H>(z, a, r, c, mean, rstd);
+#pragma unroll
+  for (uint32_t j = 0; j < kGroup; ++j) d[j] = (u[j] * g[j] - s.x - z[j] * s.y) * rstd;
+  if (a.dh) {
+    load_group(g, row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
+#pragma unroll
+    for (uint32_t j = 0; j < kGroup; ++j) d[j] += g[j];
+  }
+}
+
+// The weights' gradients: 256 columns by one part of a worker's rows to a workgroup, eight of them at a time.
+constexpr uint32_t kTileGroups = 32, kTileRows = 8;
+
+template <typename T, typename H>
+__global__ __launch_bounds__(kTileGroups * kTileRows) void k_norm_columns_wide(NormArgs a) {
+  __shared__ float tile[kTileRows][kTileGroups * kGroup];
+  const uint32_t c = (blockIdx.x * kTileGroups + threadIdx.x % kTileGroups) * kGroup, lane_row = threadIdx.x / kTileGroups;
+  const uint64_t offset = a.join ? drop_offset(a.drop) : 0u;
+  const uint32_t w = blockIdx.z;
+  for (uint32_t part = blockIdx.y; part < a.parts; part += gridDim.y) {
+    float sum[kGradients][kGroup] = {};
+    const uint32_t first = part * a.part_rows, left = a.rows - first;
+    const uint32_t rows = left < a.part_rows ? left : a.part_rows;
+    if (c < a.cols) {
+      for (uint32_t i = lane_row; i < rows; i += kTileRows) {
+        const uint32_t r = w * a.rows + first + i;
+        float d[kGroup], u[kGroup], z[kGroup];
+        form_d<T, H>(d, u, z, a, r, c);
+        if (a.grad[2]) drop_group(d, a.drop, offset, r, c);
+#pragma unroll
+        for (uint32_t j = 0; j < kGroup; ++j) {
+          sum[0][j] += u[j] * z[j];
+          sum[1][j] += u[j];
+          sum[2][j] += d[j];
+        }
+      }
+    }
+    for (uint32_t k = 0; k < kGradients; ++k) {
+      if (!a.grad[k]) continue;
+      __syncthreads();
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) tile[lane_row][threadIdx.x % kTileGroups * kGroup + j] = sum[k][j];
+      __syncthreads();
+      const uint32_t col = blockIdx.x * kTileGroups * kGroup + threadIdx.x;
+      if (col < a.cols) {
+        float s = 0.0f;
+        for (uint32_t i = 0; i < kTileRows; ++i) s += tile[i][threadIdx.x];
+        emit_gradient(a, w, part, k, col, s);
+      }
+    }
+  }
+}
+
+template <typename T, typename H>
+__global__ __launch_bounds__(kWideThreads) void k_norm_backward_wide(NormArgs a) {
+  const uint64_t offset = a.join ? drop_offset(a.drop) : 0u;
+  for (uint32_t r = blockIdx.x; r < a.total; r += gridDim.x) {
+    for (uint32_t c = threadIdx.x * kGroup; c < a.cols; c += kWideThreads * kGroup) {
+      float d[kGroup], u[kGroup], z[kGroup];
+      form_d<T, H>(d, u, z, a, r, c);
+      if (a.dresidual) store_group(row_of<H>(a.dresidual, a.ld_dresidual, r), c, a.cols, d);
+      if (a.dx) {
+        drop_group(d, a.drop, offset, r, c);
+        store_group(row_of<T>(a.dx, a.ld_dx, r), c, a.cols, d);
+      }
+    }
+  }
+}
+
+// ---- What both take ------------------------------------------------------------------------------------------------
+// The parts' sums added up in their order: 64 columns to a workgroup, a quarter of the parts to each wavefront.
+__global__ __launch_bounds__(256) void k_norm_join_parts(NormArgs a) {
+  __shared__ float tile[4][64];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, which = blockIdx.y;
+  if (!a.grad[which]) return;
+  const uint32_t tiles = (a.cols + 63) / 64;
+  for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const uint32_t c = t * 64 + lane, w = blockIdx.z;
+    float s = 0.0f;
+    if (c < a.cols) {
+      const float* p = a.partial + (static_cast<size_t>(w) * a.parts * kGradients + which) * a.cols + c;
+      const size_t step = static_cast<size_t>(kGradients) * a.cols;
+      const uint32_t share = (a.parts + 3) / 4, from = wave * share, to = from + share < a.parts ? from + share : a.parts;
+      for (uint32_t i = from; i < to; ++i) s += p[i * step];
+    }
+    __syncthreads();
+    tile[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < a.cols) {
+      s = (tile[0][lane] + tile[1][lane]) + (tile[2][lane] + tile[3][lane]);
+      float* const out = a.grad[which] + static_cast<int64_t>(w) * a.ld_grad[which] + c;
+      *out = a.accumulate ? *out + s : s;
+    }
+  }
+}
+
+// No row at all: the gradients are sums over nothing.
+__global__ __launch_bounds__(256) void k_norm_no_rows(NormArgs a) {
+  const uint32_t which = blockIdx.y;
+  if (!a.grad[which]) return;
+  for (uint32_t c = blockIdx.x * 256 + threadIdx.x; c < a.cols; c += gridDim.x * 256)
+    a.grad[which][static_cast<int64_t>(blockIdx.z) * a.ld_grad[which] + c] = 0.0f;
+}
+
+// The team and the number of groups per lane that a row of `groups` groups is given (0 groups per lane: none).
+struct Team {
+  bool wave;
+  uint32_t lanes, each;
+};
+Team backward_team(uint32_t groups) {
+  if (groups <= 64) {
+    uint32_t lanes = 8;
+    while (lanes < groups) lanes *= 2;
+    return {true, lanes, 1};
+  }
+  if (groups <= 128) return {true, 64, 2};
+  const uint32_t each = groups <= 1024 ? 1 : groups <= 2048 ? 2 : 0;
+  return {false, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
+}
+
+template <typename T, typename H, bool JOIN>
+void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
+  const dim3 grid(blocks_for(static_cast<uint64_t>(k.n) * k.parts)), block(t.wave ? kTeamThreads : t.lanes);
+  const size_t lds = t.wave ? kTeamThreads / 64 * t.each * t.lanes * kGroup * sizeof(float) : 0;
+#define COMPAMS_BACKWARD(NG, WAVE) \
+  hipLaunchKernelGGL((k_norm_backward<T, H, NG, WAVE, JOIN>), grid, block, lds, stream, k, t.lanes)
+  if (t.wave) {
+    if (t.each == 1) COMPAMS_BACKWARD(1, true);
+    else COMPAMS_BACKWARD(2, true);
+  } else {
+    if (t.each == 1) COMPAMS_BACKWARD(1, false);
+    else COMPAMS_BACKWARD(2, false);
+  }
+#undef COMPAMS_BACKWARD
+}
+
+inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+}  // namespace
+
+// Parts are a function of a worker's rows alone, so that its sums do not depend on the other workers.
+Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool gradients) {
+  Cut c = {};
+  if (rows == 0) return c;
+  c.part_rows = rows <= 2048 ? 16 : rows <= 8192 ? 32 : 64;
+  c.parts = (rows + c.part_rows - 1) / c.part_rows;
+  if (backward_team((cols + kGroup - 1) / kGroup).each == 0) c.sums_bytes = up256(static_cast<size_t>(n) * rows * sizeof(float2));
+  if (gradients && c.parts > 1)
+    c.partial_bytes = up256(static_cast<size_t>(n) * c.parts * kGradients * cols * sizeof(float));
+  return c;
+}
+
+hipError_t norm_backward(const NormArgs& k, int32_t type, int32_t stream_type, hipStream_t stream) {
+  const bool gradients = k.grad[0] || k.grad[1] || k.grad[2];
+  if (k.rows == 0) {
+    if (k.accumulate || !gradients) return hipSuccess;
+    hipLaunchKernelGGL(k_norm_no_rows, dim3(at_most((k.cols + 255) / 256, 4096), kGradients, k.n), dim3(256), 0, stream, k);
+    return hipGetLastError();
+  }
+  const Team team = backward_team((k.cols + kGroup - 1) / kGroup);
+  return by_types(type, stream_type, [&](auto t, auto h) {
+    using T = decltype(t);
+    using H = decltype(h);
+    if (team.each == 0) {
+      hipLaunchKernelGGL((k_norm_sums_wide<T, H>), dim3(blocks_for(k.total)), dim3(kWideThreads), 0, stream, k);
+      constexpr uint32_t kTileCols = kTileGroups * kGroup;
+      if (gradients)
+        hipLaunchKernelGGL((k_norm_columns_wide<T, H>), dim3((k.cols + kTileCols - 1) / kTileCols, at_most(k.parts, 32768), k.n),
+                           dim3(kTileGroups * kTileRows), 0, stream, k);
+      // (the outputs last: they may be the inputs' own buffers)
+      if (k.dx || k.dresidual)
+        hipLaunchKernelGGL((k_norm_backward_wide<T, H>), dim3(blocks_for(k.total)), dim3(kWideThreads), 0, stream, k);
+    } else if (k.join) {
+      launch_team<T, H, true>(team, k, stream);
+    } else {
+      launch_team<T, H, false>(team, k, stream);
+    }
+    if (gradients && k.parts > 1)
+      hipLaunchKernelGGL(k_norm_join_parts, dim3(at_most((k.cols + 63) / 64, 4096), kGradients, k.n), dim3(256), 0, stream, k);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace compams

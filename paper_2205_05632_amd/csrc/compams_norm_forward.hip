@@ -1,0 +1,203 @@
+// Layer norm and the join of a transformer block, forward.
+#include <math.h>
+
+#include "compams_norm.h"
+
+namespace compams {
+namespace {
+
+// ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
+// A team is 8 to 64 lanes of a wavefront (WAVE) or a whole workgroup.  Its lanes take the row's groups of eight columns in
+// turn, NG of them each; the row is read once, and mean and variance are two sums over what the registers hold.
+constexpr uint32_t kTeamThreads = 256;
+
+template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN>
+__global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(NormArgs a, uint32_t lanes) {
+  __shared__ float slots[2][1][16];
+  const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
+  const uint32_t together = WAVE ? kTeamThreads / lanes : 1u;
+  const uint32_t first = WAVE ? blockIdx.x * together + threadIdx.x / lanes : blockIdx.x;
+  const uint64_t offset = JOIN ? drop_offset(a.drop) : 0u;
+  const float count = static_cast<float>(a.cols);
+  for (uint32_t r = first; r < a.total; r += gridDim.x * together) {
+    float v[NG][kGroup], g[NG][kGroup], b[NG][kGroup];
+    if constexpr (JOIN) {
+      typename Group<T>::type x[NG];
+      typename Group<H>::type res[NG];
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) x[k] = load_raw(row_of<T>(a.x, a.ld_x, r), (k * lanes + lane) * kGroup, a.cols);
+      if (a.residual) {
+#pragma unroll
+        for (uint32_t k = 0; k < NG; ++k)
+          res[k] = load_raw(row_of<H>(a.residual, a.ld_residual, r), (k * lanes + lane) * kGroup, a.cols);
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) {
+        load_weight(g[k], a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+        load_weight(b[k], a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) {
+        const uint32_t c = (k * lanes + lane) * kGroup;
+        float w[kGroup];
+        load_weight(w, a.bias, c, a.cols, 0.0f);
+        unpack(v[k], x[k]);
+#pragma unroll
+        for (uint32_t j = 0; j < kGroup; ++j) v[k][j] += w[j];
+        drop_group(v[k], a.drop, offset, r, c);
+        if (a.residual) {
+          unpack(w, res[k]);
+#pragma unroll
+          for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = w[j] + v[k][j];
+        }
+      }
+    } else {
+      typename Group<H>::type x[NG];
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k)
+        x[k] = load_raw(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), (k * lanes + lane) * kGroup, a.cols);
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) {
+        load_weight(g[k], a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+        load_weight(b[k], a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) unpack(v[k], x[k]);
+    }
+    // (columns beyond the last hold 0)
+    float s[1] = {0.0f};
+#pragma unroll
+    for (uint32_t k = 0; k < NG; ++k)
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) s[0] += v[k][j];
+    if constexpr (WAVE) s[0] = sum_lanes(s[0], lanes);
+    else sum_block(s, slots[0], lanes / 64);
+    const float mean = s[0] / count;
+    s[0] = 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < NG; ++k) {
+      const uint32_t c = (k * lanes + lane) * kGroup;
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) {
+        const float d = c + j < a.cols ? v[k][j] - mean : 0.0f;
+        s[0] = fmaf(d, d, s[0]);
+      }
+    }
+    if constexpr (WAVE) s[0] = sum_lanes(s[0], lanes);
+    else sum_block(s, slots[1], lanes / 64);
+    const float rstd = 1.0f / sqrtf(s[0] / count + a.eps);
+#pragma unroll
+    for (uint32_t k = 0; k < NG; ++k) {
+      const uint32_t c = (k * lanes + lane) * kGroup;
+      if (JOIN && a.h) store_group(row_of<H>(a.h, a.ld_h, r), c, a.cols, v[k]);
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = fmaf((v[k][j] - mean) * rstd, g[k][j], b[k][j]);
+      store_group(row_of<T>(a.y, a.ld_y, r), c, a.cols, v[k]);
+    }
+    if (lane == 0) {
+      if (a.mean) a.mean[r] = mean;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+  }
+}
+
+// ---- Rows of any width: a workgroup goes over its row once for every sum ---------------------------------------
+constexpr uint32_t kWideThreads = 1024;
+
+template <typename T, typename H>
+__global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) {
+  __shared__ float slots[2][1][16];
+  const uint64_t offset = a.join ? drop_offset(a.drop) : 0u;
+  const float count = static_cast<float>(a.cols);
+  for (uint32_t r = blockIdx.x; r < a.total; r += gridDim.x) {
+    float s[1] = {0.0f};
+    for (uint32_t c = threadIdx.x * kGroup; c < a.cols; c += kWideThreads * kGroup) {
+      float v[kGroup];
+      form_h<T, H>(v, a, offset, r, c);
+      for (uint32_t j = 0; j < kGroup; ++j) s[0] += c + j < a.cols ? v[j] : 0.0f;
+    }
+    sum_block(s, slots[0], kWideThreads / 64);
+    const float mean = s[0] / count;
+    s[0] = 0.0f;
+    for (uint32_t c = threadIdx.x * kGroup; c < a.cols; c += kWideThreads * kGroup) {
+      float v[kGroup];
+      form_h<T, H>(v, a, offset, r, c);
+      for (uint32_t j = 0; j < kGroup; ++j) {
+        const float d = v[j] - mean;
+        s[0] += c + j < a.cols ? d * d : 0.0f;
+      }
+    }
+    sum_block(s, slots[1], kWideThreads / 64);
+    const float rstd = 1.0f / sqrtf(s[0] / count + a.eps);
+    for (uint32_t c = threadIdx.x * kGroup; c < a.cols; c += kWideThreads * kGroup) {
+      float v[kGroup], g[kGroup], b[kGroup];
+      form_h<T, H>(v, a, offset, r, c);
+      if (a.join && a.h) store_group(row_of<H>(a.h, a.ld_h, r), c, a.cols, v);
+      load_weight(g, a.gamma, c, a.cols, 1.0f);
+      load_weight(b, a.beta, c, a.cols, 0.0f);
+      for (uint32_t j = 0; j < kGroup; ++j) v[j] = (v[j] - mean) * rstd * g[j] + b[j];
+      store_group(row_of<T>(a.y, a.ld_y, r), c, a.cols, v);
+    }
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[r] = mean;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+  }
+}
+
+// The team and the number of groups per lane that a row of `groups` groups is given (0 groups per lane: none).
+struct Team {
+  bool wave;
+  uint32_t lanes, each;
+};
+Team forward_team(uint32_t groups) {
+  if (groups <= 64) {
+    uint32_t lanes = 8;
+    while (lanes < groups) lanes *= 2;
+    return {true, lanes, 1};
+  }
+  if (groups <= 96) return {true, 32, 3};
+  if (groups <= 256) return {true, 64, (groups + 63) / 64};
+  const uint32_t each = groups <= 1024 ? 1 : groups <= 2048 ? 2 : groups <= 4096 ? 4 : 0;
+  return {false, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
+}
+
+template <typename T, typename H, bool JOIN>
+void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
+  const uint32_t together = t.wave ? kTeamThreads / t.lanes : 1;
+  const dim3 grid(blocks_for((static_cast<uint64_t>(k.total) + together - 1) / together));
+  const dim3 block(t.wave ? kTeamThreads : t.lanes);
+#define COMPAMS_FORWARD(NG, WAVE) \
+  hipLaunchKernelGGL((k_norm_forward<T, H, NG, WAVE, JOIN>), grid, block, 0, stream, k, t.lanes)
+  if (t.wave) {
+    switch (t.each) {
+      case 1: COMPAMS_FORWARD(1, true); break;
+      case 2: COMPAMS_FORWARD(2, true); break;
+      case 3: COMPAMS_FORWARD(3, true); break;
+      default: COMPAMS_FORWARD(4, true); break;
+    }
+  } else {
+    switch (t.each) {
+      case 1: COMPAMS_FORWARD(1, false); break;
+      case 2: COMPAMS_FORWARD(2, false); break;
+      default: COMPAMS_FORWARD(4, false); break;
+    }
+  }
+#undef COMPAMS_FORWARD
+}
+
+}  // namespace
+
+hipError_t norm_forward(const NormArgs& k, int32_t type, int32_t stream_type, hipStream_t stream) {
+  const Team team = forward_team((k.cols + kGroup - 1) / kGroup);
+  return by_types(type, stream_type, [&](auto t, auto h) {
+    using T = decltype(t);
+    using H = decltype(h);
+    if (team.each == 0) hipLaunchKernelGGL((k_norm_forward_wide<T, H>), dim3(blocks_for(k.total)), dim3(kWideThreads), 0, stream, k);
+    else if (k.join) launch_team<T, H, true>(team, k, stream);
+    else launch_team<T, H, false>(team, k, stream);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace compams

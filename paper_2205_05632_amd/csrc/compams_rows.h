@@ -28,16 +28,24 @@ struct Group {
 // Columns c .. c + 7 of a row of `cols` columns; those at or beyond `cols` are not read and come out as 0.  Rows may
 // start at any multiple of the element's size: the loads are wide all the same (unaligned accesses are the processor's).
 template <typename T>
-__device__ __forceinline__ void load_group(float (&v)[kGroup], const T* row, uint32_t c, uint32_t cols) {
+__device__ __forceinline__ typename Group<T>::type load_raw(const T* row, uint32_t c, uint32_t cols) {
+  typename Group<T>::type raw;
   if (c + kGroup <= cols) {
-    typename Group<T>::type raw;
     __builtin_memcpy(&raw, row + c, sizeof(raw));
-#pragma unroll
-    for (uint32_t j = 0; j < kGroup; ++j) v[j] = to_float(raw[j]);
   } else {
 #pragma unroll
-    for (uint32_t j = 0; j < kGroup; ++j) v[j] = c + j < cols ? to_float(row[c + j]) : 0.0f;
+    for (uint32_t j = 0; j < kGroup; ++j) raw[j] = c + j < cols ? row[c + j] : static_cast<T>(0.0f);
   }
+  return raw;
+}
+template <typename V>
+__device__ __forceinline__ void unpack(float (&v)[kGroup], const V& raw) {
+#pragma unroll
+  for (uint32_t j = 0; j < kGroup; ++j) v[j] = to_float(raw[j]);
+}
+template <typename T>
+__device__ __forceinline__ void load_group(float (&v)[kGroup], const T* row, uint32_t c, uint32_t cols) {
+  unpack(v, load_raw(row, c, cols));
 }
 
 // Each value rounded to T once, to the nearest.
