@@ -16,7 +16,8 @@ struct LossArgs {
   int64_t ignore;
   float grad_scale;
   float *mean_loss, *losses;
-  uint32_t* counts;  // per worker: rows that are learnt from
+  bool stream;       // the gradient is written past the memory-side cache
+  uint32_t* counts;  // per worker: rows that are learnt from; NULL where whoever asks counts them
 };
 
 __device__ __forceinline__ int64_t target_of(const LossArgs& a, uint32_t r) {
@@ -31,11 +32,17 @@ struct Max {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 
+// The rows of a worker that are learnt from, counted by the `lanes` lanes of a team (or of a wavefront of one).
+__device__ __forceinline__ uint32_t count_rows(const LossArgs& a, uint32_t w, uint32_t lane, uint32_t lanes) {
+  uint32_t mine = 0;
+  for (uint32_t i = lane; i < a.rows; i += lanes) mine += target_of(a, w * a.rows + i) != a.ignore;
+  return mine;
+}
+
 __global__ __launch_bounds__(kLossThreads) void k_loss_count(LossArgs a) {
   __shared__ float slots[1][16];
   for (uint32_t w = blockIdx.x; w < a.n; w += gridDim.x) {
-    uint32_t mine = 0;
-    for (uint32_t i = threadIdx.x; i < a.rows; i += kLossThreads) mine += target_of(a, w * a.rows + i) != a.ignore;
+    const uint32_t mine = count_rows(a, w, threadIdx.x, kLossThreads);
     // two halves, each exact in fp32 (a worker has fewer than 2^31 rows, a lane at most 2^21 of them)
     __syncthreads();
     float s[1] = {static_cast<float>(mine & 0xfffu)};
@@ -47,7 +54,171 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_count(LossArgs a) {
   }
 }
 
-// Rows of any width: a workgroup goes over its row twice, once for the running maximum and sum, once for the gradient.
+// exp(v - top) for v <= top as a power of two with one multiply-add; results below 2^-126 are 0.
+struct Exponent {
+  float scale, shift;  // v scale + shift
+};
+__device__ __forceinline__ Exponent exponent_of(float top) {
+  // From 1e38 on log2(e) top could overflow.  Two different numbers of that size are more than 1e30 apart, so that any
+  // scale that keeps them far below 0 does.
+  const float scale = fabsf(top) < 1e38f ? 1.44269504088896340736f : 0x1p-60f;
+  return {scale, -top * scale};
+}
+__device__ __forceinline__ float exp_below(float v, const Exponent& x) { return __builtin_amdgcn_exp2f(fmaf(v, x.scale, x.shift)); }
+
+// ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
+// A team is 16 to 64 lanes of a wavefront (WAVE) or a whole workgroup.  The row is read once and kept as it came, in
+// groups of 16 bytes; its maximum, the sum of its exponentials and its gradient are three passes over registers.  (The
+// exponentials are formed twice: kept in fp32 they would take up to two times the row's registers again, and what hides
+// one row's reads and reductions is the other rows that fit a compute unit.)
+//
+// The groups start at the row's first multiple of 16 bytes: rows of an odd vocabulary, one after another, start anywhere,
+// and accesses across cache lines cost a sixth of the time.  What is left at the row's two ends, up to seven columns
+// each, goes one by one to the first sixteen lanes.
+template <typename T>
+struct Logits {
+  static constexpr uint32_t kEach = 16 / sizeof(T);
+  typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
+};
+
+// Makes the compiler forget what it knows of a value, so that it unpacks a group again instead of keeping it in fp32
+// beside (with 16 groups of bfloat16 that spilled 178 registers), and forms an address again.
+__device__ __forceinline__ void forget(uint32_t& v) { asm volatile("" : "+v"(v)); }
+template <typename V>
+__device__ __forceinline__ void forget(V& raw) {
+  typedef uint32_t Words __attribute__((ext_vector_type(4)));
+  Words w;
+  __builtin_memcpy(&w, &raw, 16);
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) {
+    uint32_t v = w[i];
+    forget(v);
+    w[i] = v;
+  }
+  __builtin_memcpy(&raw, &w, 16);
+}
+
+constexpr uint32_t kTeamThreads = 256, kRowThreads = 512;
+constexpr uint64_t kStreamBytes = 32u << 20;
+
+template <typename T, uint32_t NG, bool WAVE>
+__global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(LossArgs a, uint32_t lanes) {
+  constexpr uint32_t kEach = Logits<T>::kEach;
+  typedef typename Logits<T>::type V;
+  __shared__ float tops[2][kLossWaves];
+  __shared__ float slots[2][2][kLossWaves];
+  const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
+  const uint32_t together = WAVE ? kTeamThreads / lanes : 1u, waves = lanes / 64;
+  uint32_t turn = 0;
+  for (uint32_t r = WAVE ? blockIdx.x * together + threadIdx.x / lanes : blockIdx.x; r < a.total; r += gridDim.x * together) {
+    const T* const logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(r) * a.ld_logits;
+    T* const out = a.dlogits ? static_cast<T*>(a.dlogits) + static_cast<int64_t>(r) * a.ld_dlogits : nullptr;
+    const int64_t target = target_of(a, r);
+    if (target == a.ignore) {  // nothing is read, whatever stands there
+      if (a.losses && lane == 0) a.losses[r] = 0.0f;
+      if (out)
+        for (uint32_t c = lane * kGroup; c < a.vocab; c += lanes * kGroup) {
+          const float zero[kGroup] = {};
+          store_group(out, c, a.vocab, zero);
+        }
+      continue;
+    }
+    uint32_t head = static_cast<uint32_t>(-reinterpret_cast<uintptr_t>(logits) % 16 / sizeof(T));
+    head = head < a.vocab ? head : a.vocab;
+    const uint32_t groups = (a.vocab - head) / kEach, tail = head + groups * kEach;
+    const char* const inner = reinterpret_cast<const char*>(logits + head);
+    V raw[NG] = {};
+    if (groups) {
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) {  // (lanes beyond the last group read that one, and leave it out below)
+        const uint32_t g = k * lanes + lane;
+        raw[k] = *reinterpret_cast<const V*>(inner + (g < groups ? g : groups - 1) * 16u);
+      }
+    }
+    const uint32_t end = lane < 8 ? (lane < head ? lane : a.vocab) : lane < 16 ? tail + (lane - 8) : a.vocab;
+    const float at_end = end < a.vocab ? to_float(logits[end]) : -INFINITY;
+    const uint32_t w = r / a.rows;
+    // (less than 2^24 of them: exact in fp32; a.counts is there where there may be more)
+    const float count = a.counts ? 0.0f : static_cast<float>(count_rows(a, w, lane, lanes));
+    const bool inside = target >= 0 && target < static_cast<int64_t>(a.vocab);
+    const float of_target = inside ? to_float(logits[target]) : 0.0f;
+    float top = at_end;
+    if (groups) {
+#pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) {
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j) top = fmaxf(top, to_float(raw[k][j]));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    top = over_lanes(top, WAVE ? lanes : 64u, Max());
+    if (!WAVE && waves > 1) {
+      if ((threadIdx.x & 63u) == 0) tops[turn][threadIdx.x >> 6] = top;
+      __syncthreads();
+      for (uint32_t i = 0; i < waves; ++i) top = fmaxf(top, tops[turn][i]);
+    }
+    const Exponent x = exponent_of(top);
+    uint32_t again = lane;
+    forget(again);
+    float s[2] = {exp_below(at_end, x), count};
+#pragma unroll
+    for (uint32_t k = 0; k < NG; ++k) {
+      forget(raw[k]);
+      float e[kEach];
+#pragma unroll
+      for (uint32_t j = 0; j < kEach; ++j) e[j] = exp_below(to_float(raw[k][j]), x);
+#pragma unroll
+      for (uint32_t n = kEach / 2; n > 0; n /= 2)
+#pragma unroll
+        for (uint32_t j = 0; j < n; ++j) e[j] += e[j + n];
+      s[0] += k * lanes + again < groups ? e[0] : 0.0f;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (WAVE) {
+      s[0] = sum_lanes(s[0], lanes);
+      s[1] = sum_lanes(s[1], lanes);
+    } else {
+      sum_block(s, slots[turn], waves);
+    }
+    turn ^= 1;
+    const bool none = !inside || top == -INFINITY;
+    if (a.losses && lane == 0) a.losses[r] = none ? __builtin_nanf("") : logf(s[0]) + top - of_target;
+    if (!out) continue;
+    if (a.counts) s[1] = static_cast<float>(a.counts[w]);
+    // a row without a softmax or a loss has no gradient
+    const float factor = none ? __builtin_nanf("") : a.grad_scale / s[1];
+    const float share = factor / s[0];
+    const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == reinterpret_cast<uintptr_t>(logits) % 16;
+    const uint32_t hot = inside ? static_cast<uint32_t>(target) : a.vocab;
+    char* const inner_out = reinterpret_cast<char*>(out + head);
+    forget(again);
+#pragma unroll
+    for (uint32_t k = 0; k < NG; ++k) {
+      const uint32_t g = k * lanes + again;
+      forget(raw[k]);
+      float v[kEach];
+#pragma unroll
+      for (uint32_t j = 0; j < kEach; ++j) v[j] = exp_below(to_float(raw[k][j]), x) * share;
+      const uint32_t at = hot - head - g * kEach;
+      if (at < kEach) {
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j) v[j] -= at == j ? factor : 0.0f;
+      }
+      V o;
+#pragma unroll
+      for (uint32_t j = 0; j < kEach; ++j) o[j] = static_cast<T>(v[j]);
+      if (g < groups) {
+        if (!aligned) __builtin_memcpy(inner_out + g * 16u, &o, 16);
+        else if (a.stream) __builtin_nontemporal_store(o, reinterpret_cast<V*>(inner_out + g * 16u));
+        else *reinterpret_cast<V*>(inner_out + g * 16u) = o;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (end < a.vocab) out[end] = static_cast<T>(exp_below(at_end, x) * share - (end == hot ? factor : 0.0f));
+  }
+}
+
+// ---- Rows of any width: a workgroup goes over its row twice, once for the running maximum and sum, once for the gradient.
 template <typename T>
 __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
   __shared__ float slots[2][kLossWaves];
@@ -108,16 +279,65 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
   }
 }
 
-// A worker's losses added up and divided.
+// A worker's losses added up and divided by their count.
 __global__ __launch_bounds__(kLossThreads) void k_loss_mean(LossArgs a) {
-  __shared__ float slots[2][1][16];
+  __shared__ float slots[2][2][16];
   uint32_t turn = 0;
   for (uint32_t w = blockIdx.x; w < a.n; w += gridDim.x, turn ^= 1) {
-    float s[1] = {0.0f};
+    float s[2] = {0.0f, a.counts ? 0.0f : static_cast<float>(count_rows(a, w, threadIdx.x, kLossThreads))};
     for (uint32_t i = threadIdx.x; i < a.rows; i += kLossThreads) s[0] += a.losses[static_cast<size_t>(w) * a.rows + i];
     sum_block(s, slots[turn], kLossWaves);
-    if (threadIdx.x == 0) a.mean_loss[w] = a.counts[w] ? s[0] / static_cast<float>(a.counts[w]) : 0.0f;
+    if (a.counts) s[1] = static_cast<float>(a.counts[w]);
+    if (threadIdx.x == 0) a.mean_loss[w] = s[1] > 0.0f ? s[0] / s[1] : 0.0f;
   }
+}
+
+// The team and the number of groups per lane that a row of `groups` groups is given (0 groups per lane: none).  A workgroup
+// of at most 512 threads leaves room for two rows and more on a compute unit, so that one row's reads are under way while
+// another's exponentials are formed: 8192 rows of bfloat16, us by threads x groups:
+//   vocabulary  4096: 256 x 2 32.5, 128 x 4 30.3, 64 x 8 31.9      8192: 256 x 4 56.8, 128 x 8 58.3, 64 x 16 58.8
+//              16384: 1024 x 2 152, 512 x 4 97, 256 x 8 101, 128 x 16 110      32000: 512 x 8 182, 256 x 16 193
+//              50257: 832 x 8 400, 448 x 16 312, 256 x 32 311, 320 x 20 467 (waves that do not go evenly into four)
+struct Team {
+  bool wave;
+  uint32_t lanes, each;
+};
+Team loss_team(uint32_t groups) {
+  if (groups <= 64) {
+    uint32_t lanes = 16;  // (as many as the two ends may have columns)
+    while (lanes < groups) lanes *= 2;
+    return {true, lanes, 1};
+  }
+  if (groups <= 128) return {true, 64, 2};
+  const uint32_t each = groups <= 2048 ? 4 : groups <= 4096 ? 8 : groups <= 8192 ? 16 : groups <= 16384 ? 32 : 0;
+  return {false, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
+}
+
+template <typename T>
+void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
+  constexpr uint64_t kMost = 1u << 21;  // workgroups: a dimension has room for 2^32 threads in all
+  const uint64_t together = t.wave ? kTeamThreads / t.lanes : 1, wanted = (k.total + together - 1) / together;
+  const dim3 grid(static_cast<uint32_t>(wanted < kMost ? wanted : kMost)), block(t.wave ? kTeamThreads : t.lanes);
+#define COMPAMS_LOSS(NG, WAVE) hipLaunchKernelGGL((k_loss<T, NG, WAVE>), grid, block, 0, stream, k, t.lanes)
+  if (t.wave) {
+    if (t.each == 1) COMPAMS_LOSS(1, true);
+    else COMPAMS_LOSS(2, true);
+  } else {
+    switch (t.each) {
+      case 0: hipLaunchKernelGGL(k_loss_wide<T>, grid, dim3(kLossThreads), 0, stream, k); break;
+      case 4: COMPAMS_LOSS(4, false); break;
+      case 8: COMPAMS_LOSS(8, false); break;
+      case 16: COMPAMS_LOSS(16, false); break;
+      default: COMPAMS_LOSS(32, false); break;
+    }
+  }
+#undef COMPAMS_LOSS
+}
+
+// Whether every row's team counts its worker's targets by itself: where they are few bytes beside the row's logits.  (They
+// are then counted in fp32, exactly: fewer than 2^24.)
+bool counts_inside(const LossArgs& k, const Team& t) {
+  return t.each != 0 && (k.rows <= 64 || k.rows <= k.vocab / 4) && k.rows < (1u << 24);
 }
 
 bool loss_valid(const compams_loss* a) {
@@ -166,16 +386,22 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream) {
   k.ignore = a->ignore_index;
   k.grad_scale = a->grad_scale;
   k.mean_loss = a->mean_loss;
-  k.counts = static_cast<uint32_t*>(a->workspace);
+  // What does not stay in the memory-side cache until it is read again need not pass through it (8192 rows of bfloat16,
+  // streamed / not: vocabulary 4096 30.3 / 39.6 us, 16384 97 / 110, 50257 312 / 317).
+  k.stream = static_cast<uint64_t>(a->n) * a->rows * a->vocab * type_size(a->type) > kStreamBytes;
   k.losses = a->losses ? a->losses
              : a->mean_loss ? reinterpret_cast<float*>(static_cast<char*>(a->workspace) + counts_bytes(*a)) : nullptr;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(k_loss_count, dim3(k.n), dim3(kLossThreads), 0, stream, k);
+  const uint32_t each = 16 / static_cast<uint32_t>(type_size(a->type));
+  const Team team = loss_team((k.vocab + each - 1) / each);
+  if (!counts_inside(k, team)) {
+    k.counts = static_cast<uint32_t*>(a->workspace);
+    hipLaunchKernelGGL(k_loss_count, dim3(k.n), dim3(kLossThreads), 0, stream, k);
+  }
   if (k.total) {
-    const dim3 grid(k.total < (1u << 21) ? k.total : (1u << 21));
-    if (a->type == COMPAMS_F32) hipLaunchKernelGGL(k_loss_wide<float>, grid, dim3(kLossThreads), 0, stream, k);
-    else if (a->type == COMPAMS_F16) hipLaunchKernelGGL(k_loss_wide<half_t>, grid, dim3(kLossThreads), 0, stream, k);
-    else hipLaunchKernelGGL(k_loss_wide<bfloat_t>, grid, dim3(kLossThreads), 0, stream, k);
+    if (a->type == COMPAMS_F32) launch_loss<float>(team, k, stream);
+    else if (a->type == COMPAMS_F16) launch_loss<half_t>(team, k, stream);
+    else launch_loss<bfloat_t>(team, k, stream);
   }
   if (k.mean_loss) hipLaunchKernelGGL(k_loss_mean, dim3(k.n), dim3(kLossThreads), 0, stream, k);
   return hipGetLastError() == hipSuccess ? COMPAMS_OK : COMPAMS_HIP_ERROR;

@@ -25,16 +25,16 @@ struct Group {
   typedef T type __attribute__((ext_vector_type(8)));
 };
 
-// Columns c .. c + 7 of a row of `cols` columns; those at or beyond `cols` are not read and come out as 0.  Rows may
-// start at any multiple of the element's size: the loads are wide all the same (unaligned accesses are the processor's).
+// Columns c .. c + 7 of a row of `cols` columns; those at or beyond `cols` are not read and come out as
+// `beyond`.  Rows may // start at any multiple of the element's size: the loads are wide all the same (unaligned accesses are the processor's).
 template <typename T>
-__device__ __forceinline__ typename Group<T>::type load_raw(const T* row, uint32_t c, uint32_t cols) {
+__device__ __forceinline__ typename Group<T>::type load_raw(const T* row, uint32_t c, uint32_t cols, float beyond = 0.0f) {
   typename Group<T>::type raw;
   if (c + kGroup <= cols) {
     __builtin_memcpy(&raw, row + c, sizeof(raw));
   } else {
 #pragma unroll
-    for (uint32_t j = 0; j < kGroup; ++j) raw[j] = c + j < cols ? row[c + j] : static_cast<T>(0.0f);
+    for (uint32_t j = 0; j < kGroup; ++j) raw[j] = c + j < cols ? row[c + j] : static_cast<T>(beyond);
   }
   return raw;
 }
