@@ -46,6 +46,15 @@ __device__ __forceinline__ void load_weight(float (&v)[kGroup], const float* w, 
   }
 }
 
+// The same in two steps (see load_early).
+__device__ __forceinline__ Group<float>::type load_weight_early(const float* w, uint32_t c, uint32_t cols, float absent) {
+  if (w) return load_early(w, c, cols);
+  Group<float>::type raw;
+#pragma unroll
+  for (uint32_t j = 0; j < kGroup; ++j) raw[j] = absent;
+  return raw;
+}
+
 // h of a group before it is rounded: the input of a layer norm, or residual + dropout(x + bias).
 template <typename T, typename H>
 __device__ __forceinline__ void form_h(float (&v)[kGroup], const NormArgs& a, uint64_t offset, uint32_t r, uint32_t c) {

@@ -37,79 +37,107 @@ __device__ __forceinline__ float sum_teams(float v, uint32_t lanes) {
   return v;
 }
 
-template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN>
+template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN, uint32_t ROWS>
 __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_backward(NormArgs a, uint32_t lanes) {
   constexpr uint32_t kOf = JOIN ? 3 : 2;
-  __shared__ float slots[2][2][16];
+  __shared__ float slots[2][2 * ROWS][16];
   extern __shared__ float tile[];  // WAVE: a row of columns for each wavefront
   const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
   const uint32_t together = WAVE ? kTeamThreads / lanes : 1u;
   const uint32_t team = WAVE ? threadIdx.x / lanes : 0u;
   const uint64_t offset = JOIN ? drop_offset(a.drop) : 0u;
-  const float count = static_cast<float>(a.cols);
-  float g[NG][kGroup];
+  const float one_by_count = 1.0f / static_cast<float>(a.cols);
+  typename Group<float>::type g[NG];
 #pragma unroll
-  for (uint32_t k = 0; k < NG; ++k) load_weight(g[k], a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+  for (uint32_t k = 0; k < NG; ++k) {
+    const uint32_t c = (k * lanes + lane) * kGroup;
+    g[k] = load_weight_early(a.gamma, c, a.cols, 1.0f);
+    settle<float>(g[k], c, a.cols);
+  }
   uint32_t turn = 0;
   for (uint32_t job = blockIdx.x; job < a.n * a.parts; job += gridDim.x) {
     const uint32_t w = job / a.parts, part = job % a.parts;
     const uint32_t first = part * a.part_rows, left = a.rows - first, rows = left < a.part_rows ? left : a.part_rows;
     float sum[kOf][NG][kGroup] = {};
-    for (uint32_t i = team; i < rows; i += together, turn ^= 1) {
-      const uint32_t r = w * a.rows + first + i;
-      typename Group<T>::type raw_y[NG];
-      typename Group<H>::type raw_h[NG], raw_g[NG];
+    for (uint32_t i = team; i < rows; i += together * ROWS, turn ^= 1) {
+      typename Group<T>::type raw_y[ROWS][NG];
+      typename Group<H>::type raw_h[ROWS][NG], raw_g[ROWS][NG];
+      float mean[ROWS], rstd[ROWS];
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) {
-        const uint32_t c = (k * lanes + lane) * kGroup;
-        raw_y[k] = load_raw(row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
-        raw_h[k] = load_raw(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), c, a.cols);
-        if (JOIN && a.dh) raw_g[k] = load_raw(row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
+      for (uint32_t q = 0; q < ROWS; ++q) {
+        // (a row beyond the part's last one: the last one again, left out below)
+        const uint32_t in = i + q * together, r = w * a.rows + first + (in < rows ? in : rows - 1);
+#pragma unroll
+        for (uint32_t k = 0; k < NG; ++k) {
+          const uint32_t c = (k * lanes + lane) * kGroup;
+          raw_y[q][k] = load_early(row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
+          raw_h[q][k] = load_early(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), c, a.cols);
+          if (JOIN && a.dh) raw_g[q][k] = load_early(row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
+        }
+        mean[q] = a.mean[r];
+        rstd[q] = a.rstd[r];
       }
-      const float mean = a.mean[r], rstd = a.rstd[r];
-      float s[2] = {0.0f, 0.0f};
-      float z[NG][kGroup], u[NG][kGroup];
+      float s[2 * ROWS];
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) {
-        unpack(u[k], raw_y[k]);
-        unpack(z[k], raw_h[k]);
+      for (uint32_t q = 0; q < ROWS; ++q) {
+        s[2 * q] = s[2 * q + 1] = 0.0f;
 #pragma unroll
-        for (uint32_t j = 0; j < kGroup; ++j) {
-          // (columns beyond the last: dy and, read from gamma's end, the weight are 0)
-          z[k][j] = (z[k][j] - mean) * rstd;
-          sum[0][k][j] = fmaf(u[k][j], z[k][j], sum[0][k][j]);
-          sum[1][k][j] += u[k][j];
-          u[k][j] *= g[k][j];
-          s[0] += u[k][j];
-          s[1] = fmaf(u[k][j], z[k][j], s[1]);
+        for (uint32_t k = 0; k < NG; ++k) {
+          const uint32_t c = (k * lanes + lane) * kGroup;
+          float z[kGroup], u[kGroup];
+          settle<T>(raw_y[q][k], c, a.cols);
+          settle<H>(raw_h[q][k], c, a.cols);
+          unpack(u, raw_y[q][k]);
+          unpack(z, raw_h[q][k]);
+#pragma unroll
+          for (uint32_t j = 0; j < kGroup; ++j) {
+            // (columns beyond the last: dy and, read from gamma's end, the weight are 0)
+            u[j] *= g[k][j];
+            s[2 * q] += u[j];
+            s[2 * q + 1] = fmaf(u[j], (z[j] - mean[q]) * rstd[q], s[2 * q + 1]);
+          }
         }
       }
       if constexpr (WAVE) {
-        s[0] = sum_lanes(s[0], lanes);
-        s[1] = sum_lanes(s[1], lanes);
+#pragma unroll
+        for (uint32_t q = 0; q < 2 * ROWS; ++q) s[q] = sum_lanes(s[q], lanes);
       } else {
         sum_block(s, slots[turn], lanes / 64);
       }
-      const float s0 = s[0] / count, s1 = s[1] / count;
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) {
-        const uint32_t c = (k * lanes + lane) * kGroup;
+      for (uint32_t q = 0; q < ROWS; ++q) {
+        const uint32_t in = i + q * together, r = w * a.rows + first + in;
+        if (ROWS > 1 && in >= rows) break;
+        const float s0 = s[2 * q] * one_by_count, s1 = s[2 * q + 1] * one_by_count;
 #pragma unroll
-        for (uint32_t j = 0; j < kGroup; ++j) u[k][j] = (u[k][j] - s0 - z[k][j] * s1) * rstd;
-        if constexpr (JOIN) {
-          if (a.dh) {
-            unpack(z[k], raw_g[k]);
+        for (uint32_t k = 0; k < NG; ++k) {
+          const uint32_t c = (k * lanes + lane) * kGroup;
+          float z[kGroup], u[kGroup];
+          unpack(u, raw_y[q][k]);
+          unpack(z, raw_h[q][k]);
 #pragma unroll
-            for (uint32_t j = 0; j < kGroup; ++j) u[k][j] += z[k][j];
+          for (uint32_t j = 0; j < kGroup; ++j) {
+            z[j] = (z[j] - mean[q]) * rstd[q];
+            sum[0][k][j] = fmaf(u[j], z[j], sum[0][k][j]);
+            sum[1][k][j] += u[j];
+            u[j] = (fmaf(u[j], g[k][j], -s0) - z[j] * s1) * rstd[q];
           }
-        }
-        if (a.dresidual) store_group(row_of<H>(a.dresidual, a.ld_dresidual, r), c, a.cols, u[k]);
-        if constexpr (JOIN) {
-          if (a.dx || a.grad[2]) {
-            drop_group(u[k], a.drop, offset, r, c);
-            if (a.dx) store_group(row_of<T>(a.dx, a.ld_dx, r), c, a.cols, u[k]);
+          if constexpr (JOIN) {
+            if (a.dh) {
+              settle<H>(raw_g[q][k], c, a.cols);
+              unpack(z, raw_g[q][k]);
 #pragma unroll
-            for (uint32_t j = 0; j < kGroup; ++j) sum[2][k][j] += u[k][j];
+              for (uint32_t j = 0; j < kGroup; ++j) u[j] += z[j];
+            }
+          }
+          if (a.dresidual) store_group(row_of<H>(a.dresidual, a.ld_dresidual, r), c, a.cols, u);
+          if constexpr (JOIN) {
+            if (a.dx || a.grad[2]) {
+              drop_group(u, a.drop, offset, r, c);
+              if (a.dx) store_group(row_of<T>(a.dx, a.ld_dx, r), c, a.cols, u);
+#pragma unroll
+              for (uint32_t j = 0; j < kGroup; ++j) sum[2][k][j] += u[j];
+            }
           }
         }
       }
@@ -257,26 +285,30 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_backward_wide(NormArgs a)
 }
 
 // ---- What both take ------------------------------------------------------------------------------------------------
-// The parts' sums added up in their order: 64 columns to a workgroup, a quarter of the parts to each wavefront.
-__global__ __launch_bounds__(256) void k_norm_join_parts(NormArgs a) {
-  __shared__ float tile[4][64];
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, which = blockIdx.y;
+// The parts' sums added up in their order: 64 columns to a workgroup, a sixteenth of the parts to each wavefront.
+constexpr uint32_t kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
+__global__ __launch_bounds__(kJoinThreads) void k_norm_join_parts(NormArgs a) {
+  __shared__ float tile[kJoinWaves][64];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, which = blockIdx.y, w = blockIdx.z;
   if (!a.grad[which]) return;
   const uint32_t tiles = (a.cols + 63) / 64;
   for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const uint32_t c = t * 64 + lane, w = blockIdx.z;
+    const uint32_t c = t * 64 + lane;
     float s = 0.0f;
     if (c < a.cols) {
-      const float* p = a.partial + (static_cast<size_t>(w) * a.parts * kGradients + which) * a.cols + c;
+      const float* const p = a.partial + (static_cast<size_t>(w) * a.parts * kGradients + which) * a.cols + c;
       const size_t step = static_cast<size_t>(kGradients) * a.cols;
-      const uint32_t share = (a.parts + 3) / 4, from = wave * share, to = from + share < a.parts ? from + share : a.parts;
+      const uint32_t share = (a.parts + kJoinWaves - 1) / kJoinWaves, from = wave * share;
+      const uint32_t to = from + share < a.parts ? from + share : a.parts;
+#pragma unroll 8
       for (uint32_t i = from; i < to; ++i) s += p[i * step];
     }
     __syncthreads();
     tile[wave][lane] = s;
     __syncthreads();
     if (wave == 0 && c < a.cols) {
-      s = (tile[0][lane] + tile[1][lane]) + (tile[2][lane] + tile[3][lane]);
+      s = 0.0f;
+      for (uint32_t i = 0; i < kJoinWaves; ++i) s += tile[i][lane];
       float* const out = a.grad[which] + static_cast<int64_t>(w) * a.ld_grad[which] + c;
       *out = a.accumulate ? *out + s : s;
     }
@@ -312,7 +344,7 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
   const dim3 grid(blocks_for(static_cast<uint64_t>(k.n) * k.parts)), block(t.wave ? kTeamThreads : t.lanes);
   const size_t lds = t.wave ? kTeamThreads / 64 * t.each * t.lanes * kGroup * sizeof(float) : 0;
 #define COMPAMS_BACKWARD(NG, WAVE) \
-  hipLaunchKernelGGL((k_norm_backward<T, H, NG, WAVE, JOIN>), grid, block, lds, stream, k, t.lanes)
+  hipLaunchKernelGGL((k_norm_backward<T, H, NG, WAVE, JOIN, 1>), grid, block, lds, stream, k, t.lanes)
   if (t.wave) {
     if (t.each == 1) COMPAMS_BACKWARD(1, true);
     else COMPAMS_BACKWARD(2, true);
@@ -322,6 +354,9 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
   }
 #undef COMPAMS_BACKWARD
 }
+
+// (a row shorter than a group has no wide load)
+Team team_of(uint32_t cols) { return cols < kGroup ? Team{false, 0, 0} : backward_team((cols + kGroup - 1) / kGroup); }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -333,7 +368,7 @@ Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool gradients) {
   if (rows == 0) return c;
   c.part_rows = rows <= 2048 ? 16 : rows <= 8192 ? 32 : 64;
   c.parts = (rows + c.part_rows - 1) / c.part_rows;
-  if (backward_team((cols + kGroup - 1) / kGroup).each == 0) c.sums_bytes = up256(static_cast<size_t>(n) * rows * sizeof(float2));
+  if (team_of(cols).each == 0) c.sums_bytes = up256(static_cast<size_t>(n) * rows * sizeof(float2));
   if (gradients && c.parts > 1)
     c.partial_bytes = up256(static_cast<size_t>(n) * c.parts * kGradients * cols * sizeof(float));
   return c;
@@ -346,7 +381,7 @@ hipError_t norm_backward(const NormArgs& k, int32_t type, int32_t stream_type, h
     hipLaunchKernelGGL(k_norm_no_rows, dim3(at_most((k.cols + 255) / 256, 4096), kGradients, k.n), dim3(256), 0, stream, k);
     return hipGetLastError();
   }
-  const Team team = backward_team((k.cols + kGroup - 1) / kGroup);
+  const Team team = team_of(k.cols);
   return by_types(type, stream_type, [&](auto t, auto h) {
     using T = decltype(t);
     using H = decltype(h);
@@ -365,7 +400,8 @@ hipError_t norm_backward(const NormArgs& k, int32_t type, int32_t stream_type, h
       launch_team<T, H, false>(team, k, stream);
     }
     if (gradients && k.parts > 1)
-      hipLaunchKernelGGL(k_norm_join_parts, dim3(at_most((k.cols + 63) / 64, 4096), kGradients, k.n), dim3(256), 0, stream, k);
+      hipLaunchKernelGGL(k_norm_join_parts, dim3(at_most((k.cols + 63) / 64, 4096), kGradients, k.n),
+                         dim3(kJoinThreads), 0, stream, k);
     return hipGetLastError();
   });
 }

@@ -20,32 +20,38 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(Nor
   const uint64_t offset = JOIN ? drop_offset(a.drop) : 0u;
   const float count = static_cast<float>(a.cols);
   for (uint32_t r = first; r < a.total; r += gridDim.x * together) {
-    float v[NG][kGroup], g[NG][kGroup], b[NG][kGroup];
+    typename Group<float>::type g[NG], b[NG];
+    float v[NG][kGroup];
     if constexpr (JOIN) {
       typename Group<T>::type x[NG];
       typename Group<H>::type res[NG];
+      typename Group<float>::type bias[NG];
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) x[k] = load_raw(row_of<T>(a.x, a.ld_x, r), (k * lanes + lane) * kGroup, a.cols);
+      for (uint32_t k = 0; k < NG; ++k) x[k] = load_early(row_of<T>(a.x, a.ld_x, r), (k * lanes + lane) * kGroup, a.cols);
       if (a.residual) {
 #pragma unroll
         for (uint32_t k = 0; k < NG; ++k)
-          res[k] = load_raw(row_of<H>(a.residual, a.ld_residual, r), (k * lanes + lane) * kGroup, a.cols);
+          res[k] = load_early(row_of<H>(a.residual, a.ld_residual, r), (k * lanes + lane) * kGroup, a.cols);
       }
 #pragma unroll
+      for (uint32_t k = 0; k < NG; ++k) bias[k] = load_weight_early(a.bias, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+#pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
-        load_weight(g[k], a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
-        load_weight(b[k], a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+        g[k] = load_weight_early(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+        b[k] = load_weight_early(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
       }
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
         const uint32_t c = (k * lanes + lane) * kGroup;
-        float w[kGroup];
-        load_weight(w, a.bias, c, a.cols, 0.0f);
+        settle<T>(x[k], c, a.cols);
+        settle<float>(bias[k], c, a.cols);
         unpack(v[k], x[k]);
 #pragma unroll
-        for (uint32_t j = 0; j < kGroup; ++j) v[k][j] += w[j];
+        for (uint32_t j = 0; j < kGroup; ++j) v[k][j] += bias[k][j];
         drop_group(v[k], a.drop, offset, r, c);
         if (a.residual) {
+          float w[kGroup];
+          settle<H>(res[k], c, a.cols);
           unpack(w, res[k]);
 #pragma unroll
           for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = w[j] + v[k][j];
@@ -55,14 +61,17 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(Nor
       typename Group<H>::type x[NG];
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k)
-        x[k] = load_raw(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), (k * lanes + lane) * kGroup, a.cols);
+        x[k] = load_early(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), (k * lanes + lane) * kGroup, a.cols);
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
-        load_weight(g[k], a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
-        load_weight(b[k], a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+        g[k] = load_weight_early(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+        b[k] = load_weight_early(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
       }
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) unpack(v[k], x[k]);
+      for (uint32_t k = 0; k < NG; ++k) {
+        settle<H>(x[k], (k * lanes + lane) * kGroup, a.cols);
+        unpack(v[k], x[k]);
+      }
     }
     // (columns beyond the last hold 0)
     float s[1] = {0.0f};
@@ -90,6 +99,8 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(Nor
     for (uint32_t k = 0; k < NG; ++k) {
       const uint32_t c = (k * lanes + lane) * kGroup;
       if (JOIN && a.h) store_group(row_of<H>(a.h, a.ld_h, r), c, a.cols, v[k]);
+      settle<float>(g[k], c, a.cols);
+      settle<float>(b[k], c, a.cols);
 #pragma unroll
       for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = fmaf((v[k][j] - mean) * rstd, g[k][j], b[k][j]);
       store_group(row_of<T>(a.y, a.ld_y, r), c, a.cols, v[k]);
@@ -189,7 +200,8 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
 }  // namespace
 
 hipError_t norm_forward(const NormArgs& k, int32_t type, int32_t stream_type, hipStream_t stream) {
-  const Team team = forward_team((k.cols + kGroup - 1) / kGroup);
+  // (a row shorter than a group has no wide load)
+  const Team team = k.cols < kGroup ? Team{false, 0, 0} : forward_team((k.cols + kGroup - 1) / kGroup);
   return by_types(type, stream_type, [&](auto t, auto h) {
     using T = decltype(t);
     using H = decltype(h);

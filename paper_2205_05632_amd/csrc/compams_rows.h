@@ -25,16 +25,58 @@ struct Group {
   typedef T type __attribute__((ext_vector_type(8)));
 };
 
-// Columns c .. c + 7 of a row of `cols` columns; those at or beyond `cols` are not read and come out as
-// `beyond`.  Rows may // start at any multiple of the element's size: the loads are wide all the same (unaligned accesses are the processor's).
+// A group's words moved down by S elements, where bit S of `by` is set.
+template <uint32_t S, typename T, typename Words>
+__device__ __forceinline__ void move_down(Words& w, uint32_t by) {
+  constexpr uint32_t kPerWord = 4 / sizeof(T), kWords = kGroup / kPerWord, kStep = S / kPerWord;
+  Words moved = {};
+#pragma unroll
+  for (uint32_t i = 0; i < kWords; ++i) {
+    if constexpr (S >= kPerWord) {
+      if (i + kStep < kWords) moved[i] = w[i + kStep];
+    } else {  // half a word
+      moved[i] = (w[i] >> 16) | (i + 1 < kWords ? w[i + 1 < kWords ? i + 1 : i] << 16 : 0u);
+    }
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < kWords; ++i) w[i] = by & S ? moved[i] : w[i];
+}
+
+// Columns c .. c + 7 of a row of `cols` >= 8 columns, in two steps.  The load is one wide one whatever c is, of the row's
+// last eight columns where the group would reach beyond them; rows may start at any multiple of the element's size
+// (unaligned accesses are the processor's).  settle() then moves such a group into its place, with 0 beyond the last
+// column: apart from the load, so that all of a row's loads are under way before the first one is waited for.  (With the
+// groups at a row's end read one by one and at once, a row of 1601 columns took a workgroup 2.3 us in the backward pass.)
 template <typename T>
-__device__ __forceinline__ typename Group<T>::type load_raw(const T* row, uint32_t c, uint32_t cols, float beyond = 0.0f) {
+__device__ __forceinline__ typename Group<T>::type load_early(const T* row, uint32_t c, uint32_t cols) {
   typename Group<T>::type raw;
-  if (c + kGroup <= cols) {
-    __builtin_memcpy(&raw, row + c, sizeof(raw));
+  __builtin_memcpy(&raw, row + (c < cols - kGroup ? c : cols - kGroup), sizeof(raw));
+  return raw;
+}
+template <typename T>
+__device__ __forceinline__ void settle(typename Group<T>::type& raw, uint32_t c, uint32_t cols) {
+  if (c + kGroup <= cols) return;
+  const uint32_t by = c + kGroup - cols;
+  typedef uint32_t Words __attribute__((ext_vector_type(kGroup * sizeof(T) / 4)));
+  Words w;
+  __builtin_memcpy(&w, &raw, sizeof(w));
+  move_down<4, T>(w, by);
+  move_down<2, T>(w, by);
+  move_down<1, T>(w, by);
+#pragma unroll
+  for (uint32_t i = 0; i < kGroup * sizeof(T) / 4; ++i) w[i] = by < kGroup ? w[i] : 0u;
+  __builtin_memcpy(&raw, &w, sizeof(w));
+}
+// The same in one, for rows of any width.
+template <typename T>
+__device__ __forceinline__ typename Group<T>::type load_raw(const T* row, uint32_t c, uint32_t cols) {
+  typename Group<T>::type raw = {};
+  if (cols >= kGroup) {
+    raw = load_early(row, c, cols);
+    settle<T>(raw, c, cols);
   } else {
 #pragma unroll
-    for (uint32_t j = 0; j < kGroup; ++j) raw[j] = c + j < cols ? row[c + j] : static_cast<T>(beyond);
+    for (uint32_t j = 0; j < kGroup; ++j) raw[j] = c + j < cols ? row[c + j] : static_cast<T>(0.0f);
   }
   return raw;
 }
@@ -56,10 +98,19 @@ __device__ __forceinline__ void store_group(T* row, uint32_t c, uint32_t cols, c
 #pragma unroll
     for (uint32_t j = 0; j < kGroup; ++j) raw[j] = static_cast<T>(v[j]);
     __builtin_memcpy(row + c, &raw, sizeof(raw));
-  } else {
+  } else if (c < cols) {  // as four, two and one
+    const uint32_t left = cols - c;
+    typedef uint32_t Words __attribute__((ext_vector_type(kGroup * sizeof(T) / 4)));
+    typename Group<T>::type raw;
 #pragma unroll
-    for (uint32_t j = 0; j < kGroup; ++j)
-      if (c + j < cols) row[c + j] = static_cast<T>(v[j]);
+    for (uint32_t j = 0; j < kGroup; ++j) raw[j] = static_cast<T>(v[j]);
+    Words w;
+    __builtin_memcpy(&w, &raw, sizeof(raw));
+    if (left & 4u) __builtin_memcpy(row + c, &w, 4 * sizeof(T));
+    move_down<4, T>(w, left);
+    if (left & 2u) __builtin_memcpy(row + c + (left & 4u), &w, 2 * sizeof(T));
+    move_down<2, T>(w, left);
+    if (left & 1u) __builtin_memcpy(row + c + (left & 6u), &w, sizeof(T));
   }
 }
 

@@ -13,6 +13,7 @@ Every output may be given by name, and is then written in place and returned; wh
 is recorded for autograd.  Work is enqueued on the current stream of the tensors' device.
 """
 import ctypes
+import struct
 from typing import Optional
 
 import torch
@@ -55,7 +56,13 @@ class compams_loss(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
-_NO_DROP = (0.0, 0, 0, None)
+# The calls below lay the structures out with one pack each: a ctypes structure takes 50 ns for every field, and the
+# smallest calls are as long as their marshalling.  (The C compiler's own padding; a null pointer is 0.)
+_DROP = struct.Struct("@dQQP")
+_NORM = struct.Struct("@iqqiif dQQP PPP PqPqPqPq PP PqPqPqPq PqPqPqi PN")
+_LOSS = struct.Struct("@iqqii Pq Pqf PP Pq PN")
+_NO_DROP = (0.0, 0, 0, 0)
+_LOW64 = (1 << 64) - 1
 
 
 def _type(dtype: torch.dtype, what: str) -> int:
@@ -66,25 +73,25 @@ def _type(dtype: torch.dtype, what: str) -> int:
 
 
 def _matrix(t: Optional[torch.Tensor], what: str, shape, dtype: torch.dtype, device: torch.device):
-    """(pointer, row stride) of a matrix that has to have this shape, type and device; (None, 0) for None."""
+    """(pointer, row stride) of a matrix that has to have this shape, type and device; (0, 0) for None."""
     if t is None:
-        return None, 0
-    if t.dtype is not dtype or t.device != device or t.shape != shape:
-        raise ValueError(f"{what} must be {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    apart, beside = t.stride()
-    if beside != 1 and shape[1] > 1:
+        return 0, 0
+    if t.dtype is dtype and t.shape == shape and t.device == device:
+        apart, beside = t.stride()
+        total, cols = shape
+        if beside == 1 or cols == 1:
+            return t.data_ptr(), apart if total > 1 else cols
         raise ValueError(f"the entries of a row of {what} must be contiguous, got strides {t.stride()}")
-    return t.data_ptr(), apart if shape[0] > 1 else shape[1]
+    raise ValueError(f"{what} must be {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _vector(t: Optional[torch.Tensor], what: str, count: int, device: torch.device, dtype=torch.float32):
-    """Pointer of a contiguous vector; None for None."""
+def _vector(t: Optional[torch.Tensor], what: str, shape, device: torch.device, dtype=torch.float32):
+    """Pointer of a contiguous vector of this shape; 0 for None."""
     if t is None:
-        return None
-    if t.dtype is not dtype or t.device != device or t.dim() != 1 or t.shape[0] != count or not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous {dtype} ({count},) on {device}, got {t.dtype} {tuple(t.shape)} "
-                         f"on {t.device}")
-    return t.data_ptr()
+        return 0
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{what} must be contiguous {dtype} {shape} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _shape(x: torch.Tensor, what: str, n: int = 1):
@@ -98,14 +105,14 @@ def _shape(x: torch.Tensor, what: str, n: int = 1):
 
 
 def _drop(p: float, seed: int, offset: int, step: Optional[torch.Tensor], device: torch.device):
-    return p, seed, offset, None if step is None else _vector(step, "step", 1, device, torch.int64)
+    return p, seed & _LOW64, offset & _LOW64, _vector(step, "step", (1,), device, torch.int64)
 
 
 def _workspace(workspace: Optional[torch.Tensor], need: int, device: torch.device):
     """(tensor to keep, pointer, bytes) of the caller's workspace, or of one that is allocated."""
     if workspace is None:
         if need == 0:
-            return None, None, 0
+            return None, 0, 0
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
     elif workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous on {device}")
@@ -125,9 +132,8 @@ def compams_dropout(x: torch.Tensor, p: float, seed: int, offset: int = 0, *, re
     px, lx = _matrix(x, "x", x.shape, x.dtype, dev)
     pr, lr = _matrix(residual, "residual", x.shape, y.dtype, dev)
     py, ly = _matrix(y, "y", x.shape, y.dtype, dev)
-    drop = compams_drop(*_drop(p, seed, offset, step, dev))
     _check(_on_stream(dev, lib().compams_dropout, 1, rows, cols, _type(x.dtype, "x"), _type(y.dtype, "y"), px, lx, pr, lr,
-                      py, ly, ctypes.byref(drop)), "compams_dropout")
+                      py, ly, _DROP.pack(*_drop(p, seed, offset, step, dev))), "compams_dropout")
     return y
 
 
@@ -138,11 +144,13 @@ def _forward(call, what, x, residual, h, y, gamma, beta, bias, mean, rstd, eps, 
     pr, lr = _matrix(residual, "residual", shape, stream_dtype, dev)
     ph, lh = _matrix(h, "h" if x is not None else "x", shape, stream_dtype, dev)
     py, ly = _matrix(y, "y", shape, dtype, dev)
-    a = compams_norm(1, total, cols, _type(dtype, "y"), _type(stream_dtype, "the stream"), eps, drop,
-                     _vector(gamma, "gamma", cols, dev), _vector(beta, "beta", cols, dev),
-                     _vector(bias, "bias", cols, dev), px, lx, pr, lr, ph, lh, py, ly,
-                     _vector(mean, "mean", total, dev), _vector(rstd, "rstd", total, dev))
-    _check(_on_stream(dev, call, ctypes.byref(a)), what)
+    of_cols, of_rows = (cols,), (total,)
+    a = _NORM.pack(1, total, cols, _type(dtype, "y"), _type(stream_dtype, "the stream"), eps, *drop,
+                   _vector(gamma, "gamma", of_cols, dev), _vector(beta, "beta", of_cols, dev),
+                   _vector(bias, "bias", of_cols, dev), px, lx, pr, lr, ph, lh, py, ly,
+                   _vector(mean, "mean", of_rows, dev), _vector(rstd, "rstd", of_rows, dev),
+                   0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    _check(_on_stream(dev, call, a), what)
 
 
 def compams_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor],
@@ -198,13 +206,13 @@ def _backward(call, what, dy, dh, h, mean, rstd, gamma, dx, dresidual, dgamma, d
     p0, l0 = _matrix(dgamma, "dgamma", of_weights, torch.float32, dev)
     p1, l1 = _matrix(dbeta, "dbeta", of_weights, torch.float32, dev)
     p2, l2 = _matrix(dbias, "dbias", of_weights, torch.float32, dev)
-    a = compams_norm(n, rows, cols, _type(dtype, "dy"), _type(stream_dtype, "h"), 0.0, drop,
-                     _vector(gamma, "gamma", cols, dev), None, None, None, 0, None, 0, ph, lh, None, 0,
-                     _vector(mean, "mean", total, dev), _vector(rstd, "rstd", total, dev), py, ly, pg, lg, px, lx, pr, lr,
-                     p0, l0, p1, l1, p2, l2, bool(accumulate))
-    ref = ctypes.byref(a)
-    workspace, a.workspace, a.workspace_bytes = _workspace(workspace, lib().compams_norm_workspace_size(ref), dev)
-    _check(_on_stream(dev, call, ref), what)
+    of_cols, of_rows = (cols,), (total,)
+    a = (n, rows, cols, _type(dtype, "dy"), _type(stream_dtype, "h"), 0.0, *drop, _vector(gamma, "gamma", of_cols, dev),
+         0, 0, 0, 0, 0, 0, ph, lh, 0, 0, _vector(mean, "mean", of_rows, dev), _vector(rstd, "rstd", of_rows, dev),
+         py, ly, pg, lg, px, lx, pr, lr, p0, l0, p1, l1, p2, l2, 1 if accumulate else 0)
+    need = lib().compams_norm_workspace_size(_NORM.pack(*a, 0, 0))
+    workspace, at, size = _workspace(workspace, need, dev)
+    _check(_on_stream(dev, call, _NORM.pack(*a, at, size)), what)
 
 
 def compams_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -272,10 +280,10 @@ def compams_cross_entropy(logits: torch.Tensor, targets: torch.Tensor, n: int = 
         raise ValueError(f"targets must be int32 or int64, got {targets.dtype}")
     pl, ll = _matrix(logits, "logits", logits.shape, logits.dtype, dev)
     pd, ld = _matrix(dlogits, "dlogits", logits.shape, logits.dtype, dev)
-    a = compams_loss(n, rows, vocab, _type(logits.dtype, "logits"), target_type, pl, ll,
-                     _vector(targets, "targets", total, dev, targets.dtype), ignore_index, grad_scale,
-                     _vector(mean_loss, "mean_loss", n, dev), _vector(losses, "losses", total, dev), pd, ld)
-    ref = ctypes.byref(a)
-    workspace, a.workspace, a.workspace_bytes = _workspace(workspace, lib().compams_loss_workspace_size(ref), dev)
-    _check(_on_stream(dev, lib().compams_cross_entropy, ref), "compams_cross_entropy")
+    a = (n, rows, vocab, _type(logits.dtype, "logits"), target_type, pl, ll,
+         _vector(targets, "targets", (total,), dev, targets.dtype), ignore_index, grad_scale,
+         _vector(mean_loss, "mean_loss", (n,), dev), _vector(losses, "losses", (total,), dev), pd, ld)
+    need = lib().compams_loss_workspace_size(_LOSS.pack(*a, 0, 0))
+    workspace, at, size = _workspace(workspace, need, dev)
+    _check(_on_stream(dev, lib().compams_cross_entropy, _LOSS.pack(*a, at, size)), "compams_cross_entropy")
     return mean_loss, losses, dlogits

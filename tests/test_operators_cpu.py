@@ -30,6 +30,26 @@ def test_structures_match_the_header(tmp_path, name):
     assert out[1:] == [getattr(struct, f).offset for f in fields]
 
 
+@pytest.mark.parametrize("name", ["drop", "norm", "loss"])
+def test_packed_arguments_have_the_structures_layout(name):
+    packer, struct = getattr(ops, "_" + name.upper()), getattr(ops, "compams_" + name)
+    leaves = []
+
+    def walk(s, base):
+        for field, kind in s._fields_:
+            at = base + getattr(s, field).offset
+            if issubclass(kind, ctypes.Structure):
+                walk(kind, at)
+            else:
+                leaves.append((at, kind))
+
+    walk(struct, 0)
+    assert packer.size == ctypes.sizeof(struct)
+    values = [i + 1.5 if kind in (ctypes.c_float, ctypes.c_double) else i + 1 for i, (_, kind) in enumerate(leaves)]
+    raw = packer.pack(*values)
+    assert [kind.from_buffer_copy(raw, at).value for at, kind in leaves] == values
+
+
 def test_generator_of_the_reference():
     """The vectors published with the generator (Salmon, Moraes, Dror, Shaw 2011), and both forms against each other."""
     assert R.philox((0, 0, 0, 0), (0, 0)) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
