@@ -15,30 +15,62 @@ struct DropoutArgs {
 };
 constexpr uint32_t kThreads = 256;
 
-template <typename X, typename Y>
+constexpr uint32_t kRows = 4;  // rows that a lane takes, its columns in each
+
+// FULL: every lane has a whole group.  SAME: a wavefront's lanes are all in one row, whose number is a scalar then, and with
+// it two of the generator's twenty products.
+template <typename X, typename Y, bool FULL, bool SAME, bool ADD>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a) {
   const uint32_t tall = kThreads / a.wide;
-  const uint32_t c = (blockIdx.x % a.across * a.wide + threadIdx.x % a.wide) * kGroup;
-  if (c >= a.cols) return;
+  const uint32_t c = (blockIdx.x % a.across * a.wide + (threadIdx.x & (a.wide - 1))) * kGroup;
+  if (!FULL && c >= a.cols) return;
+  uint32_t down = threadIdx.x / a.wide;
+  if constexpr (SAME) down = __builtin_amdgcn_readfirstlane(down);
   const uint64_t offset = drop_offset(a.drop);
-  const uint32_t step = gridDim.x / a.across * tall;
-  for (uint64_t r = blockIdx.x / a.across * tall + threadIdx.x / a.wide; r < a.total; r += step) {
-    float v[kGroup];
-    load_group(v, static_cast<const X*>(a.x) + static_cast<int64_t>(r) * a.ld_x, c, a.cols);
-    drop_group(v, a.drop, offset, static_cast<uint32_t>(r), c);
-    if (a.residual) {
-      float w[kGroup];
-      load_group(w, static_cast<const Y*>(a.residual) + static_cast<int64_t>(r) * a.ld_residual, c, a.cols);
+  const uint32_t step = gridDim.x / a.across * tall * kRows;
+  for (uint64_t first = blockIdx.x / a.across * tall * kRows + down; first < a.total; first += step) {
+    typename Group<X>::type x[kRows];
+    typename Group<Y>::type res[kRows];
 #pragma unroll
-      for (uint32_t j = 0; j < kGroup; ++j) v[j] = w[j] + v[j];
+    for (uint32_t q = 0; q < kRows; ++q) {
+      // (a row beyond the last: the last one again, not stored below)
+      const uint64_t in = first + q * tall, r = in < a.total ? in : a.total - 1;
+      const X* const from = static_cast<const X*>(a.x) + static_cast<int64_t>(r) * a.ld_x;
+      x[q] = FULL ? load_early<true>(from, c, a.cols) : load_raw(from, c, a.cols);
+      if constexpr (ADD) {
+        const Y* const add = static_cast<const Y*>(a.residual) + static_cast<int64_t>(r) * a.ld_residual;
+        res[q] = FULL ? load_early<true>(add, c, a.cols) : load_raw(add, c, a.cols);
+      }
     }
-    store_group(static_cast<Y*>(a.y) + static_cast<int64_t>(r) * a.ld_y, c, a.cols, v);
+#pragma unroll
+    for (uint32_t q = 0; q < kRows; ++q) {
+      const uint64_t r = first + q * tall;
+      if (r >= a.total) break;
+      float v[kGroup];
+      unpack(v, x[q]);
+      drop_group(v, a.drop, offset, static_cast<uint32_t>(r), c);
+      if constexpr (ADD) {
+        float w[kGroup];
+        unpack(w, res[q]);
+#pragma unroll
+        for (uint32_t j = 0; j < kGroup; ++j) v[j] = w[j] + v[j];
+      }
+      store_group<Y, FULL>(static_cast<Y*>(a.y) + static_cast<int64_t>(r) * a.ld_y, c, a.cols, v);
+    }
   }
 }
 
+template <typename X, typename Y, bool ADD>
+void launch_by_width(const DropoutArgs& a, uint32_t blocks, hipStream_t stream) {
+  const bool full = a.cols == a.across * a.wide * kGroup;
+  if (full && a.wide >= 64) hipLaunchKernelGGL((k_dropout<X, Y, true, true, ADD>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  else if (full) hipLaunchKernelGGL((k_dropout<X, Y, true, false, ADD>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((k_dropout<X, Y, false, false, ADD>), dim3(blocks), dim3(kThreads), 0, stream, a);
+}
 template <typename X, typename Y>
 hipError_t launch_dropout(const DropoutArgs& a, uint32_t blocks, hipStream_t stream) {
-  hipLaunchKernelGGL((k_dropout<X, Y>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  if (a.residual) launch_by_width<X, Y, true>(a, blocks, stream);
+  else launch_by_width<X, Y, false>(a, blocks, stream);
   return hipGetLastError();
 }
 
@@ -65,12 +97,18 @@ extern "C" int compams_dropout(int32_t n, int64_t rows, int64_t cols, int32_t x_
   a.ld_x = ld_x; a.ld_residual = ld_residual; a.ld_y = ld_y;
   a.drop = make_drop(*drop);
   const uint32_t groups = (a.cols + kGroup - 1) / kGroup;
-  a.wide = 1;
-  while (a.wide < groups && a.wide < kThreads) a.wide *= 2;
+  // As many lanes side by side as divide a row into whole parts, if that is half a wavefront or more; else one part, or
+  // parts of a workgroup, with lanes to spare.
+  a.wide = kThreads;
+  while (a.wide > 1 && groups % a.wide != 0) a.wide /= 2;
+  if (a.wide < 32) {
+    a.wide = 1;
+    while (a.wide < groups && a.wide < kThreads) a.wide *= 2;
+  }
   a.across = (groups + a.wide - 1) / a.wide;
   const uint32_t tall = kThreads / a.wide;
   // (a dimension has room for 2^32 threads: rows beyond are taken in further turns)
-  const uint64_t down = (static_cast<uint64_t>(a.total) + tall - 1) / tall, most = (1u << 23) / a.across;
+  const uint64_t down = (static_cast<uint64_t>(a.total) + tall * kRows - 1) / (tall * kRows), most = (1u << 23) / a.across;
   const uint32_t blocks = static_cast<uint32_t>(down < most ? down : most > 0 ? most : 1) * a.across;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   hipError_t err;

@@ -81,11 +81,10 @@ struct Logits {
   typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
 };
 
-// Makes the compiler forget what it knows of a value, so that it unpacks a group again instead of keeping it in fp32
-// beside (with 16 groups of bfloat16 that spilled 178 registers), and forms an address again.
-__device__ __forceinline__ void forget(uint32_t& v) { asm volatile("" : "+v"(v)); }
+// A group is forgotten before every pass, so that it is unpacked again instead of kept in fp32 beside (with 16 groups of
+// bfloat16 that spilled 178 registers).
 template <typename V>
-__device__ __forceinline__ void forget(V& raw) {
+__device__ __forceinline__ void forget_group(V& raw) {
   typedef uint32_t Words __attribute__((ext_vector_type(4)));
   Words w;
   __builtin_memcpy(&w, &raw, 16);
@@ -163,7 +162,7 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
     float s[2] = {exp_below(at_end, x), count};
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
-      forget(raw[k]);
+      forget_group(raw[k]);
       float e[kEach];
 #pragma unroll
       for (uint32_t j = 0; j < kEach; ++j) e[j] = exp_below(to_float(raw[k][j]), x);
@@ -195,7 +194,7 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
       const uint32_t g = k * lanes + again;
-      forget(raw[k]);
+      forget_group(raw[k]);
       float v[kEach];
 #pragma unroll
       for (uint32_t j = 0; j < kEach; ++j) v[j] = exp_below(to_float(raw[k][j]), x) * share;

@@ -23,21 +23,35 @@ __device__ __forceinline__ void emit_gradient(const NormArgs& a, uint32_t worker
 // rows and leaves one sum per column.
 constexpr uint32_t kTeamThreads = 256;
 
-// v summed over the teams of a wavefront: over the lanes that are multiples of `lanes` apart.
-__device__ __forceinline__ float sum_teams(float v, uint32_t lanes) {
-  if (lanes <= 8) v += dpp<0x128>(v);  // a row's lanes turned by 8
+// Values summed over the teams of a wavefront: over the lanes that are multiples of `lanes` apart.
+template <uint32_t NG>
+__device__ __forceinline__ void sum_teams(float (&v)[NG][kGroup], uint32_t lanes) {
+  if (lanes == 64) return;
+  if (lanes <= 8) {
+#pragma unroll
+    for (uint32_t k = 0; k < NG; ++k)
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) v[k][j] += dpp<0x128>(v[k][j]);  // a row's lanes turned by 8
+  }
   if (lanes <= 16) {
-    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+#pragma unroll
+    for (uint32_t k = 0; k < NG; ++k)
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[k][j]), __float_as_uint(v[k][j]), false, false);
+        v[k][j] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+      }
   }
-  if (lanes <= 32) {
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-  }
-  return v;
+#pragma unroll
+  for (uint32_t k = 0; k < NG; ++k)
+#pragma unroll
+    for (uint32_t j = 0; j < kGroup; ++j) {
+      const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[k][j]), __float_as_uint(v[k][j]), false, false);
+      v[k][j] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
 }
 
-template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN, uint32_t ROWS>
+template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN, uint32_t ROWS, bool FULL>
 __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_backward(NormArgs a, uint32_t lanes) {
   constexpr uint32_t kOf = JOIN ? 3 : 2;
   __shared__ float slots[2][2 * ROWS][16];
@@ -51,8 +65,8 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_backward(No
 #pragma unroll
   for (uint32_t k = 0; k < NG; ++k) {
     const uint32_t c = (k * lanes + lane) * kGroup;
-    g[k] = load_weight_early(a.gamma, c, a.cols, 1.0f);
-    settle<float>(g[k], c, a.cols);
+    g[k] = load_weight_early<FULL>(a.gamma, c, a.cols, 1.0f);
+    settle_unless<FULL, float>(g[k], c, a.cols);
   }
   uint32_t turn = 0;
   for (uint32_t job = blockIdx.x; job < a.n * a.parts; job += gridDim.x) {
@@ -70,9 +84,9 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_backward(No
 #pragma unroll
         for (uint32_t k = 0; k < NG; ++k) {
           const uint32_t c = (k * lanes + lane) * kGroup;
-          raw_y[q][k] = load_early(row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
-          raw_h[q][k] = load_early(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), c, a.cols);
-          if (JOIN && a.dh) raw_g[q][k] = load_early(row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
+          raw_y[q][k] = load_early<FULL>(row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
+          raw_h[q][k] = load_early<FULL>(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), c, a.cols);
+          if (JOIN && (FULL || a.dh)) raw_g[q][k] = load_early<FULL>(row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
         }
         mean[q] = a.mean[r];
         rstd[q] = a.rstd[r];
@@ -85,8 +99,8 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_backward(No
         for (uint32_t k = 0; k < NG; ++k) {
           const uint32_t c = (k * lanes + lane) * kGroup;
           float z[kGroup], u[kGroup];
-          settle<T>(raw_y[q][k], c, a.cols);
-          settle<H>(raw_h[q][k], c, a.cols);
+          settle_unless<FULL, T>(raw_y[q][k], c, a.cols);
+          settle_unless<FULL, H>(raw_h[q][k], c, a.cols);
           unpack(u, raw_y[q][k]);
           unpack(z, raw_h[q][k]);
 #pragma unroll
@@ -123,18 +137,18 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_backward(No
             u[j] = (fmaf(u[j], g[k][j], -s0) - z[j] * s1) * rstd[q];
           }
           if constexpr (JOIN) {
-            if (a.dh) {
-              settle<H>(raw_g[q][k], c, a.cols);
+            if (FULL || a.dh) {
+              settle_unless<FULL, H>(raw_g[q][k], c, a.cols);
               unpack(z, raw_g[q][k]);
 #pragma unroll
               for (uint32_t j = 0; j < kGroup; ++j) u[j] += z[j];
             }
           }
-          if (a.dresidual) store_group(row_of<H>(a.dresidual, a.ld_dresidual, r), c, a.cols, u);
+          if (FULL || a.dresidual) store_group<H, FULL>(row_of<H>(a.dresidual, a.ld_dresidual, r), c, a.cols, u);
           if constexpr (JOIN) {
-            if (a.dx || a.grad[2]) {
+            if (FULL || a.dx || a.grad[2]) {
               drop_group(u, a.drop, offset, r, c);
-              if (a.dx) store_group(row_of<T>(a.dx, a.ld_dx, r), c, a.cols, u);
+              if (FULL || a.dx) store_group<T, FULL>(row_of<T>(a.dx, a.ld_dx, r), c, a.cols, u);
 #pragma unroll
               for (uint32_t j = 0; j < kGroup; ++j) sum[2][k][j] += u[j];
             }
@@ -142,29 +156,32 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_backward(No
         }
       }
     }
+#pragma unroll
     for (uint32_t which = 0; which < kOf; ++which) {
-      if (!a.grad[which]) continue;
+      if (!FULL && !a.grad[which]) continue;
       if constexpr (WAVE) {
         const uint32_t across = NG * lanes * kGroup;
+        sum_teams(sum[which], lanes);
         __syncthreads();
+        if ((threadIdx.x & 63u) < lanes) {
 #pragma unroll
-        for (uint32_t k = 0; k < NG; ++k)
-#pragma unroll
-          for (uint32_t j = 0; j < kGroup; ++j) {
-            const float v = sum_teams(which == 0 ? sum[0][k][j] : which == 1 ? sum[1][k][j] : sum[kOf - 1][k][j], lanes);
-            if ((threadIdx.x & 63u) < lanes) tile[(threadIdx.x >> 6) * across + (k * lanes + lane) * kGroup + j] = v;
-          }
+          for (uint32_t k = 0; k < NG; ++k)
+            __builtin_memcpy(&tile[(threadIdx.x >> 6) * across + (k * lanes + lane) * kGroup], sum[which][k], sizeof(sum[which][k]));
+        }
         __syncthreads();
         for (uint32_t c = threadIdx.x; c < a.cols; c += kTeamThreads)
           emit_gradient(a, w, part, which, c, (tile[c] + tile[across + c]) + (tile[2 * across + c] + tile[3 * across + c]));
+      } else if (a.parts > 1) {
+        float* const row = a.partial + ((static_cast<size_t>(w) * a.parts + part) * kGradients + which) * a.cols;
+#pragma unroll
+        for (uint32_t k = 0; k < NG; ++k) store_group<float, FULL>(row, (k * lanes + lane) * kGroup, a.cols, sum[which][k]);
       } else {
 #pragma unroll
         for (uint32_t k = 0; k < NG; ++k)
 #pragma unroll
           for (uint32_t j = 0; j < kGroup; ++j) {
             const uint32_t c = (k * lanes + lane) * kGroup + j;
-            if (c < a.cols)
-              emit_gradient(a, w, part, which, c, which == 0 ? sum[0][k][j] : which == 1 ? sum[1][k][j] : sum[kOf - 1][k][j]);
+            if (FULL || c < a.cols) emit_gradient(a, w, part, which, c, sum[which][k][j]);
           }
       }
     }
@@ -343,8 +360,13 @@ template <typename T, typename H, bool JOIN>
 void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
   const dim3 grid(blocks_for(static_cast<uint64_t>(k.n) * k.parts)), block(t.wave ? kTeamThreads : t.lanes);
   const size_t lds = t.wave ? kTeamThreads / 64 * t.each * t.lanes * kGroup * sizeof(float) : 0;
-#define COMPAMS_BACKWARD(NG, WAVE) \
-  hipLaunchKernelGGL((k_norm_backward<T, H, NG, WAVE, JOIN, 1>), grid, block, lds, stream, k, t.lanes)
+  const bool full = k.cols == t.lanes * t.each * kGroup && k.gamma && k.dresidual && k.grad[0] && k.grad[1] &&
+                    (!JOIN || (k.dh && k.dx && k.grad[2]));
+#define COMPAMS_BACKWARD(NG, WAVE)                                                                                          \
+  do {                                                                                                                      \
+    if (full) hipLaunchKernelGGL((k_norm_backward<T, H, NG, WAVE, JOIN, 1, true>), grid, block, lds, stream, k, t.lanes); \
+    else hipLaunchKernelGGL((k_norm_backward<T, H, NG, WAVE, JOIN, 1, false>), grid, block, lds, stream, k, t.lanes);     \
+  } while (0)
   if (t.wave) {
     if (t.each == 1) COMPAMS_BACKWARD(1, true);
     else COMPAMS_BACKWARD(2, true);

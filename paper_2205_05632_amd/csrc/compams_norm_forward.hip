@@ -9,16 +9,18 @@ namespace {
 // ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
 // A team is 8 to 64 lanes of a wavefront (WAVE) or a whole workgroup.  Its lanes take the row's groups of eight columns in
 // turn, NG of them each; the row is read once, and mean and variance are two sums over what the registers hold.
+// FULL: the team has no lane to spare and everything that a call may leave out is there - the usual widths and the usual
+// calls, without a test of any of it for every group (a join of rows of 768: 212 vector instructions a group for 494).
 constexpr uint32_t kTeamThreads = 256;
 
-template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN>
+template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN, bool FULL>
 __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(NormArgs a, uint32_t lanes) {
   __shared__ float slots[2][1][16];
   const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
   const uint32_t together = WAVE ? kTeamThreads / lanes : 1u;
   const uint32_t first = WAVE ? blockIdx.x * together + threadIdx.x / lanes : blockIdx.x;
   const uint64_t offset = JOIN ? drop_offset(a.drop) : 0u;
-  const float count = static_cast<float>(a.cols);
+  const float one_by_count = 1.0f / static_cast<float>(a.cols);
   for (uint32_t r = first; r < a.total; r += gridDim.x * together) {
     typename Group<float>::type g[NG], b[NG];
     float v[NG][kGroup];
@@ -27,31 +29,31 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(Nor
       typename Group<H>::type res[NG];
       typename Group<float>::type bias[NG];
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) x[k] = load_early(row_of<T>(a.x, a.ld_x, r), (k * lanes + lane) * kGroup, a.cols);
-      if (a.residual) {
+      for (uint32_t k = 0; k < NG; ++k) x[k] = load_early<FULL>(row_of<T>(a.x, a.ld_x, r), (k * lanes + lane) * kGroup, a.cols);
+      if (FULL || a.residual) {
 #pragma unroll
         for (uint32_t k = 0; k < NG; ++k)
-          res[k] = load_early(row_of<H>(a.residual, a.ld_residual, r), (k * lanes + lane) * kGroup, a.cols);
+          res[k] = load_early<FULL>(row_of<H>(a.residual, a.ld_residual, r), (k * lanes + lane) * kGroup, a.cols);
       }
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) bias[k] = load_weight_early(a.bias, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+      for (uint32_t k = 0; k < NG; ++k) bias[k] = load_weight_early<FULL>(a.bias, (k * lanes + lane) * kGroup, a.cols, 0.0f);
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
-        g[k] = load_weight_early(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
-        b[k] = load_weight_early(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+        g[k] = load_weight_early<FULL>(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+        b[k] = load_weight_early<FULL>(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
       }
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
         const uint32_t c = (k * lanes + lane) * kGroup;
-        settle<T>(x[k], c, a.cols);
-        settle<float>(bias[k], c, a.cols);
+        settle_unless<FULL, T>(x[k], c, a.cols);
+        settle_unless<FULL, float>(bias[k], c, a.cols);
         unpack(v[k], x[k]);
 #pragma unroll
         for (uint32_t j = 0; j < kGroup; ++j) v[k][j] += bias[k][j];
         drop_group(v[k], a.drop, offset, r, c);
-        if (a.residual) {
+        if (FULL || a.residual) {
           float w[kGroup];
-          settle<H>(res[k], c, a.cols);
+          settle_unless<FULL, H>(res[k], c, a.cols);
           unpack(w, res[k]);
 #pragma unroll
           for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = w[j] + v[k][j];
@@ -61,15 +63,15 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(Nor
       typename Group<H>::type x[NG];
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k)
-        x[k] = load_early(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), (k * lanes + lane) * kGroup, a.cols);
+        x[k] = load_early<FULL>(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), (k * lanes + lane) * kGroup, a.cols);
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
-        g[k] = load_weight_early(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
-        b[k] = load_weight_early(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+        g[k] = load_weight_early<FULL>(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+        b[k] = load_weight_early<FULL>(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
       }
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
-        settle<H>(x[k], (k * lanes + lane) * kGroup, a.cols);
+        settle_unless<FULL, H>(x[k], (k * lanes + lane) * kGroup, a.cols);
         unpack(v[k], x[k]);
       }
     }
@@ -81,33 +83,40 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(Nor
       for (uint32_t j = 0; j < kGroup; ++j) s[0] += v[k][j];
     if constexpr (WAVE) s[0] = sum_lanes(s[0], lanes);
     else sum_block(s, slots[0], lanes / 64);
-    const float mean = s[0] / count;
+    const float mean = s[0] * one_by_count;
     s[0] = 0.0f;
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
       const uint32_t c = (k * lanes + lane) * kGroup;
+      if (FULL || c + kGroup <= a.cols) {
 #pragma unroll
-      for (uint32_t j = 0; j < kGroup; ++j) {
-        const float d = c + j < a.cols ? v[k][j] - mean : 0.0f;
-        s[0] = fmaf(d, d, s[0]);
+        for (uint32_t j = 0; j < kGroup; ++j) s[0] = fmaf(v[k][j] - mean, v[k][j] - mean, s[0]);
+      } else {
+        uint32_t left = a.cols - c;  // (wraps around where no column is left: negative below)
+        forget(left);
+#pragma unroll
+        for (uint32_t j = 0; j < kGroup; ++j) {
+          const float d = static_cast<int32_t>(j) < static_cast<int32_t>(left) ? v[k][j] - mean : 0.0f;
+          s[0] = fmaf(d, d, s[0]);
+        }
       }
     }
     if constexpr (WAVE) s[0] = sum_lanes(s[0], lanes);
     else sum_block(s, slots[1], lanes / 64);
-    const float rstd = 1.0f / sqrtf(s[0] / count + a.eps);
+    const float rstd = rsqrtf(fmaf(s[0], one_by_count, a.eps));
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
       const uint32_t c = (k * lanes + lane) * kGroup;
-      if (JOIN && a.h) store_group(row_of<H>(a.h, a.ld_h, r), c, a.cols, v[k]);
-      settle<float>(g[k], c, a.cols);
-      settle<float>(b[k], c, a.cols);
+      if (JOIN && (FULL || a.h)) store_group<H, FULL>(row_of<H>(a.h, a.ld_h, r), c, a.cols, v[k]);
+      settle_unless<FULL, float>(g[k], c, a.cols);
+      settle_unless<FULL, float>(b[k], c, a.cols);
 #pragma unroll
       for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = fmaf((v[k][j] - mean) * rstd, g[k][j], b[k][j]);
-      store_group(row_of<T>(a.y, a.ld_y, r), c, a.cols, v[k]);
+      store_group<T, FULL>(row_of<T>(a.y, a.ld_y, r), c, a.cols, v[k]);
     }
     if (lane == 0) {
-      if (a.mean) a.mean[r] = mean;
-      if (a.rstd) a.rstd[r] = rstd;
+      if (FULL || a.mean) a.mean[r] = mean;
+      if (FULL || a.rstd) a.rstd[r] = rstd;
     }
   }
 }
@@ -178,8 +187,13 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
   const uint32_t together = t.wave ? kTeamThreads / t.lanes : 1;
   const dim3 grid(blocks_for((static_cast<uint64_t>(k.total) + together - 1) / together));
   const dim3 block(t.wave ? kTeamThreads : t.lanes);
-#define COMPAMS_FORWARD(NG, WAVE) \
-  hipLaunchKernelGGL((k_norm_forward<T, H, NG, WAVE, JOIN>), grid, block, 0, stream, k, t.lanes)
+  const bool full = k.cols == t.lanes * t.each * kGroup && k.gamma && k.beta && k.mean && k.rstd &&
+                    (!JOIN || (k.bias && k.residual && k.h));
+#define COMPAMS_FORWARD(NG, WAVE)                                                                            \
+  do {                                                                                                      \
+    if (full) hipLaunchKernelGGL((k_norm_forward<T, H, NG, WAVE, JOIN, true>), grid, block, 0, stream, k, t.lanes); \
+    else hipLaunchKernelGGL((k_norm_forward<T, H, NG, WAVE, JOIN, false>), grid, block, 0, stream, k, t.lanes);     \
+  } while (0)
   if (t.wave) {
     switch (t.each) {
       case 1: COMPAMS_FORWARD(1, true); break;

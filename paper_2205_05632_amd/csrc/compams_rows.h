@@ -25,6 +25,9 @@ struct Group {
   typedef T type __attribute__((ext_vector_type(8)));
 };
 
+// Makes the compiler forget what it knows of a value: what follows from it is formed where it is used.
+__device__ __forceinline__ void forget(uint32_t& v) { asm volatile("" : "+v"(v)); }
+
 // A group's words moved down by S elements, where bit S of `by` is set.
 template <uint32_t S, typename T, typename Words>
 __device__ __forceinline__ void move_down(Words& w, uint32_t by) {
@@ -47,16 +50,18 @@ __device__ __forceinline__ void move_down(Words& w, uint32_t by) {
 // (unaligned accesses are the processor's).  settle() then moves such a group into its place, with 0 beyond the last
 // column: apart from the load, so that all of a row's loads are under way before the first one is waited for.  (With the
 // groups at a row's end read one by one and at once, a row of 1601 columns took a workgroup 2.3 us in the backward pass.)
-template <typename T>
+// FULL: the caller knows that no group reaches beyond the last column.
+template <bool FULL = false, typename T>
 __device__ __forceinline__ typename Group<T>::type load_early(const T* row, uint32_t c, uint32_t cols) {
   typename Group<T>::type raw;
-  __builtin_memcpy(&raw, row + (c < cols - kGroup ? c : cols - kGroup), sizeof(raw));
+  __builtin_memcpy(&raw, row + (FULL || c < cols - kGroup ? c : cols - kGroup), sizeof(raw));
   return raw;
 }
 template <typename T>
 __device__ __forceinline__ void settle(typename Group<T>::type& raw, uint32_t c, uint32_t cols) {
   if (c + kGroup <= cols) return;
-  const uint32_t by = c + kGroup - cols;
+  uint32_t by = c + kGroup - cols;
+  forget(by);  // (its comparisons, the same for every row, would be kept in, and spilled from, scalar registers)
   typedef uint32_t Words __attribute__((ext_vector_type(kGroup * sizeof(T) / 4)));
   Words w;
   __builtin_memcpy(&w, &raw, sizeof(w));
@@ -66,6 +71,10 @@ __device__ __forceinline__ void settle(typename Group<T>::type& raw, uint32_t c,
 #pragma unroll
   for (uint32_t i = 0; i < kGroup * sizeof(T) / 4; ++i) w[i] = by < kGroup ? w[i] : 0u;
   __builtin_memcpy(&raw, &w, sizeof(w));
+}
+template <bool FULL, typename T>
+__device__ __forceinline__ void settle_unless(typename Group<T>::type& raw, uint32_t c, uint32_t cols) {
+  if constexpr (!FULL) settle<T>(raw, c, cols);
 }
 // The same in one, for rows of any width.
 template <typename T>
@@ -91,15 +100,16 @@ __device__ __forceinline__ void load_group(float (&v)[kGroup], const T* row, uin
 }
 
 // Each value rounded to T once, to the nearest.
-template <typename T>
+template <typename T, bool FULL = false>
 __device__ __forceinline__ void store_group(T* row, uint32_t c, uint32_t cols, const float (&v)[kGroup]) {
-  if (c + kGroup <= cols) {
+  if (FULL || c + kGroup <= cols) {
     typename Group<T>::type raw;
 #pragma unroll
     for (uint32_t j = 0; j < kGroup; ++j) raw[j] = static_cast<T>(v[j]);
     __builtin_memcpy(row + c, &raw, sizeof(raw));
   } else if (c < cols) {  // as four, two and one
-    const uint32_t left = cols - c;
+    uint32_t left = cols - c;
+    forget(left);
     typedef uint32_t Words __attribute__((ext_vector_type(kGroup * sizeof(T) / 4)));
     typename Group<T>::type raw;
 #pragma unroll
@@ -117,12 +127,13 @@ __device__ __forceinline__ void store_group(T* row, uint32_t c, uint32_t cols, c
 // ---- The generator -------------------------------------------------------------------------------------------
 // Philox-4x32 with ten rounds (Salmon, Moraes, Dror, Shaw 2011): w -> (hi(M1 w2) ^ w1 ^ k0, lo(M1 w2), hi(M0 w0) ^ w3 ^ k1,
 // lo(M0 w0)), the key stepping by the golden ratio and by sqrt(3) - 1.
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
 __device__ __forceinline__ void philox(uint32_t (&w)[4], uint32_t k0, uint32_t k1) {
 #pragma unroll
   for (int turn = 0; turn < 10; ++turn) {
     const uint64_t a = static_cast<uint64_t>(w[0]) * 0xD2511F53u, b = static_cast<uint64_t>(w[2]) * 0xCD9E8D57u;
-    w[0] = static_cast<uint32_t>(b >> 32) ^ w[1] ^ k0;
-    w[2] = static_cast<uint32_t>(a >> 32) ^ w[3] ^ k1;
+    w[0] = xor3(static_cast<uint32_t>(b >> 32), w[1], k0);
+    w[2] = xor3(static_cast<uint32_t>(a >> 32), w[3], k1);
     w[1] = static_cast<uint32_t>(b);
     w[3] = static_cast<uint32_t>(a);
     k0 += 0x9E3779B9u;
