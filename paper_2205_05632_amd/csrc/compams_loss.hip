@@ -40,7 +40,7 @@ __device__ __forceinline__ uint32_t count_rows(const LossArgs& a, uint32_t w, ui
 }
 
 __global__ __launch_bounds__(kLossThreads) void k_loss_count(LossArgs a) {
-  __shared__ float slots[1][16];
+  __shared__ float slots[1][kSlots];
   for (uint32_t w = blockIdx.x; w < a.n; w += gridDim.x) {
     const uint32_t mine = count_rows(a, w, threadIdx.x, kLossThreads);
     // two halves, each exact in fp32 (a worker has fewer than 2^31 rows, a lane at most 2^21 of them)
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
   constexpr uint32_t kEach = Logits<T>::kEach;
   typedef typename Logits<T>::type V;
   __shared__ float tops[2][kLossWaves];
-  __shared__ float slots[2][2][kLossWaves];
+  __shared__ float slots[2][2][kSlots];
   const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
   const uint32_t together = WAVE ? kTeamThreads / lanes : 1u, waves = lanes / 64;
   uint32_t turn = 0;
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
 
 // A worker's losses added up and divided by their count.
 __global__ __launch_bounds__(kLossThreads) void k_loss_mean(LossArgs a) {
-  __shared__ float slots[2][2][16];
+  __shared__ float slots[2][2][kSlots];
   uint32_t turn = 0;
   for (uint32_t w = blockIdx.x; w < a.n; w += gridDim.x, turn ^= 1) {
     float s[2] = {0.0f, a.counts ? 0.0f : static_cast<float>(count_rows(a, w, threadIdx.x, kLossThreads))};

@@ -76,6 +76,44 @@ __device__ __forceinline__ void form_h(float (&v)[kGroup], const NormArgs& a, ui
   }
 }
 
+// How a row's team of lanes is made up.
+enum TeamKind {
+  kInWave = 0,  // 8, 16, 32 or 64 lanes of a wavefront; a workgroup of 256 threads has several teams
+  kBlock = 1,   // a whole workgroup
+  kPair = 2     // an odd number of half wavefronts, two such teams to a workgroup
+};
+constexpr uint32_t kTeamThreads = 256;  // of a workgroup of kInWave
+struct Team {
+  TeamKind kind;
+  uint32_t lanes, each;  // lanes of a team; groups that a lane takes (0: rows are not held in registers)
+};
+inline uint32_t team_threads(const Team& t) { return t.kind == kInWave ? kTeamThreads : t.kind == kBlock ? t.lanes : 2 * t.lanes; }
+// This lane's team within the workgroup, its place there, and the teams of a workgroup.
+template <TeamKind KIND>
+__device__ __forceinline__ uint32_t team_of_lane(uint32_t lanes) {
+  return KIND == kInWave ? threadIdx.x / lanes : KIND == kBlock ? 0u : threadIdx.x >= lanes ? 1u : 0u;
+}
+template <TeamKind KIND>
+__device__ __forceinline__ uint32_t lane_of_team(uint32_t lanes, uint32_t team) {
+  return KIND == kInWave ? threadIdx.x & (lanes - 1) : KIND == kBlock ? threadIdx.x : threadIdx.x - team * lanes;
+}
+template <TeamKind KIND>
+__device__ __forceinline__ uint32_t teams_together(uint32_t lanes) {
+  return KIND == kInWave ? kTeamThreads / lanes : KIND == kBlock ? 1u : 2u;
+}
+// Sums over the lanes of a team.
+template <TeamKind KIND, int N>
+__device__ __forceinline__ void sum_over_team(float (&v)[N], float (*slots)[kSlots], uint32_t lanes, uint32_t team) {
+  if constexpr (KIND == kInWave) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = sum_lanes(v[i], lanes);
+  } else if constexpr (KIND == kBlock) {
+    sum_team<false>(v, slots, 0, lanes / 64);
+  } else {
+    sum_team<true>(v, slots, team * (lanes / 32), lanes / 32);
+  }
+}
+
 // ---- Host ------------------------------------------------------------------------------------------------------
 template <typename F>
 inline hipError_t by_types(int32_t type, int32_t stream_type, F f) {

@@ -7,21 +7,22 @@ namespace compams {
 namespace {
 
 // ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
-// A team is 8 to 64 lanes of a wavefront (WAVE) or a whole workgroup.  Its lanes take the row's groups of eight columns in
+// Its lanes take the row's groups of eight columns in
 // turn, NG of them each; the row is read once, and mean and variance are two sums over what the registers hold.
 // FULL: the team has no lane to spare and everything that a call may leave out is there - the usual widths and the usual
 // calls, without a test of any of it for every group (a join of rows of 768: 212 vector instructions a group for 494).
-constexpr uint32_t kTeamThreads = 256;
-
-template <typename T, typename H, uint32_t NG, bool WAVE, bool JOIN, bool FULL>
-__global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(NormArgs a, uint32_t lanes) {
-  __shared__ float slots[2][1][16];
-  const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
-  const uint32_t together = WAVE ? kTeamThreads / lanes : 1u;
-  const uint32_t first = WAVE ? blockIdx.x * together + threadIdx.x / lanes : blockIdx.x;
+template <typename T, typename H, uint32_t NG, TeamKind KIND, bool JOIN, bool FULL>
+__global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_forward(NormArgs a, uint32_t lanes) {
+  __shared__ float slots[2][1][kSlots];
+  const uint32_t team = team_of_lane<KIND>(lanes), lane = lane_of_team<KIND>(lanes, team);
+  const uint32_t together = teams_together<KIND>(lanes);
   const uint64_t offset = JOIN ? drop_offset(a.drop) : 0u;
   const float one_by_count = 1.0f / static_cast<float>(a.cols);
-  for (uint32_t r = first; r < a.total; r += gridDim.x * together) {
+  for (uint32_t first = blockIdx.x * together; first < a.total; first += gridDim.x * together) {
+    // (a team without a row of its own goes over the last one again: the teams of a pair meet at barriers)
+    const bool spare = KIND != kBlock && first + team >= a.total;
+    if (KIND == kInWave && spare) break;
+    const uint32_t r = spare ? a.total - 1 : first + team;
     typename Group<float>::type g[NG], b[NG];
     float v[NG][kGroup];
     if constexpr (JOIN) {
@@ -81,8 +82,7 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(Nor
     for (uint32_t k = 0; k < NG; ++k)
 #pragma unroll
       for (uint32_t j = 0; j < kGroup; ++j) s[0] += v[k][j];
-    if constexpr (WAVE) s[0] = sum_lanes(s[0], lanes);
-    else sum_block(s, slots[0], lanes / 64);
+    sum_over_team<KIND>(s, slots[0], lanes, team);
     const float mean = s[0] * one_by_count;
     s[0] = 0.0f;
 #pragma unroll
@@ -101,8 +101,8 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : 1024) void k_norm_forward(Nor
         }
       }
     }
-    if constexpr (WAVE) s[0] = sum_lanes(s[0], lanes);
-    else sum_block(s, slots[1], lanes / 64);
+    sum_over_team<KIND>(s, slots[1], lanes, team);
+    if (KIND == kPair && spare) continue;
     const float rstd = rsqrtf(fmaf(s[0], one_by_count, a.eps));
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
@@ -126,7 +126,7 @@ constexpr uint32_t kWideThreads = 1024;
 
 template <typename T, typename H>
 __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) {
-  __shared__ float slots[2][1][16];
+  __shared__ float slots[2][1][kSlots];
   const uint64_t offset = a.join ? drop_offset(a.drop) : 0u;
   const float count = static_cast<float>(a.cols);
   for (uint32_t r = blockIdx.x; r < a.total; r += gridDim.x) {
@@ -165,47 +165,52 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) 
   }
 }
 
-// The team and the number of groups per lane that a row of `groups` groups is given (0 groups per lane: none).
-struct Team {
-  bool wave;
-  uint32_t lanes, each;
-};
-Team forward_team(uint32_t groups) {
+// The team that a row of `groups` groups is given.  No lane to spare counts most, then few registers; the best and the next
+// best, us, 8 x 4096 rows (65536 of 768) from bfloat16 and a stream in fp32, norm / join:
+//    768: 32 x 3 53.8 / 115, pair of 96 53.8 / 120, 128 56 / 127        1000: 64 x 2 37.7 / 80, 128 37.8 / 86
+//   1280: pair of 160 46 / 105, 64 x 3 49 / 124                         2048: 256 76 / 168, 64 x 4 79 / 151
+//   1601 (bfloat16 stream): pair of 224 57 / 126, 256 61 / 117
+Team forward_team(uint32_t groups, bool join) {
   if (groups <= 64) {
     uint32_t lanes = 8;
     while (lanes < groups) lanes *= 2;
-    return {true, lanes, 1};
+    return {kInWave, lanes, 1};
   }
-  if (groups <= 96) return {true, 32, 3};
-  if (groups <= 256) return {true, 64, (groups + 63) / 64};
+  if (groups <= 96) return {kInWave, 32, 3};
+  if (groups <= 128) return {kInWave, 64, 2};
+  const uint32_t halves = (groups + 31) / 32;
+  if (halves == 5 || (halves == 7 && !join)) return {kPair, halves * 32, 1};
+  if (halves == 8 && join) return {kInWave, 64, 4};
   const uint32_t each = groups <= 1024 ? 1 : groups <= 2048 ? 2 : groups <= 4096 ? 4 : 0;
-  return {false, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
+  return {kBlock, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
 }
 
 template <typename T, typename H, bool JOIN>
 void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
-  const uint32_t together = t.wave ? kTeamThreads / t.lanes : 1;
+  const uint32_t threads = team_threads(t), together = threads / t.lanes;
   const dim3 grid(blocks_for((static_cast<uint64_t>(k.total) + together - 1) / together));
-  const dim3 block(t.wave ? kTeamThreads : t.lanes);
+  const dim3 block(threads);
   const bool full = k.cols == t.lanes * t.each * kGroup && k.gamma && k.beta && k.mean && k.rstd &&
                     (!JOIN || (k.bias && k.residual && k.h));
-#define COMPAMS_FORWARD(NG, WAVE)                                                                            \
+#define COMPAMS_FORWARD(NG, KIND)                                                                            \
   do {                                                                                                      \
-    if (full) hipLaunchKernelGGL((k_norm_forward<T, H, NG, WAVE, JOIN, true>), grid, block, 0, stream, k, t.lanes); \
-    else hipLaunchKernelGGL((k_norm_forward<T, H, NG, WAVE, JOIN, false>), grid, block, 0, stream, k, t.lanes);     \
+    if (full) hipLaunchKernelGGL((k_norm_forward<T, H, NG, KIND, JOIN, true>), grid, block, 0, stream, k, t.lanes); \
+    else hipLaunchKernelGGL((k_norm_forward<T, H, NG, KIND, JOIN, false>), grid, block, 0, stream, k, t.lanes);     \
   } while (0)
-  if (t.wave) {
+  if (t.kind == kInWave) {
     switch (t.each) {
-      case 1: COMPAMS_FORWARD(1, true); break;
-      case 2: COMPAMS_FORWARD(2, true); break;
-      case 3: COMPAMS_FORWARD(3, true); break;
-      default: COMPAMS_FORWARD(4, true); break;
+      case 1: COMPAMS_FORWARD(1, kInWave); break;
+      case 2: COMPAMS_FORWARD(2, kInWave); break;
+      case 3: COMPAMS_FORWARD(3, kInWave); break;
+      default: COMPAMS_FORWARD(4, kInWave); break;
     }
+  } else if (t.kind == kPair) {
+    COMPAMS_FORWARD(1, kPair);
   } else {
     switch (t.each) {
-      case 1: COMPAMS_FORWARD(1, false); break;
-      case 2: COMPAMS_FORWARD(2, false); break;
-      default: COMPAMS_FORWARD(4, false); break;
+      case 1: COMPAMS_FORWARD(1, kBlock); break;
+      case 2: COMPAMS_FORWARD(2, kBlock); break;
+      default: COMPAMS_FORWARD(4, kBlock); break;
     }
   }
 #undef COMPAMS_FORWARD
@@ -215,7 +220,7 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
 
 hipError_t norm_forward(const NormArgs& k, int32_t type, int32_t stream_type, hipStream_t stream) {
   // (a row shorter than a group has no wide load)
-  const Team team = k.cols < kGroup ? Team{false, 0, 0} : forward_team((k.cols + kGroup - 1) / kGroup);
+  const Team team = k.cols < kGroup ? Team{kBlock, 0, 0} : forward_team((k.cols + kGroup - 1) / kGroup, k.join);
   return by_types(type, stream_type, [&](auto t, auto h) {
     using T = decltype(t);
     using H = decltype(h);

@@ -200,26 +200,31 @@ struct Add {
 };
 __device__ __forceinline__ float sum_lanes(float v, uint32_t lanes) { return over_lanes(v, lanes, Add()); }
 
-// Sums of N numbers over the whole workgroup (`waves` wavefronts, 16 at most), the same bits in every lane.  `slots` is
-// used again by the next call, so calls that follow each other take two of them in turn: then one barrier is enough (a
+// Sums of N numbers over a team of several wavefronts, or of an odd number of half wavefronts (HALVES), the same bits in
+// every lane of it: `parts` wavefronts or halves, 16 at most, the team's first being number `first` of the workgroup.  Every
+// lane takes one part's sum and they are added across lanes: one read instead of `parts` that wait for each other.  `slots`
+// is used again by the next call, so calls that follow each other take two of them in turn: then one barrier is enough (a
 // wavefront can be one call ahead of the slowest reader, not two).
-template <int N>
-__device__ __forceinline__ void sum_block(float (&v)[N], float (*slots)[16], uint32_t waves) {
+constexpr uint32_t kSlots = 32;
+template <bool HALVES, int N>
+__device__ __forceinline__ void sum_team(float (&v)[N], float (*slots)[kSlots], uint32_t first, uint32_t parts) {
+  constexpr uint32_t kLanes = HALVES ? 32 : 64;
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = sum_lanes(v[i], 64);
-  if (waves == 1) return;
-  const uint32_t wave = threadIdx.x >> 6;
-  if ((threadIdx.x & 63u) == 0) {
+  for (int i = 0; i < N; ++i) v[i] = sum_lanes(v[i], kLanes);
+  if (!HALVES && parts == 1) return;
+  if (threadIdx.x % kLanes == 0) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) slots[i][wave] = v[i];
+    for (int i = 0; i < N; ++i) slots[i][threadIdx.x / kLanes] = v[i];
   }
   __syncthreads();
+  const uint32_t mine = threadIdx.x & 15u;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float s = 0.0f;
-    for (uint32_t w = 0; w < waves; ++w) s += slots[i][w];
-    v[i] = s;
-  }
+  for (int i = 0; i < N; ++i) v[i] = sum_lanes(mine < parts ? slots[i][first + mine] : 0.0f, 16);
+}
+// Over the whole workgroup.
+template <int N>
+__device__ __forceinline__ void sum_block(float (&v)[N], float (*slots)[kSlots], uint32_t waves) {
+  sum_team<false>(v, slots, 0, waves);
 }
 
 // ---- Argument checks that the entry points share ---------------------------------------------------------------
