@@ -18,8 +18,10 @@ __device__ __forceinline__ void emit_gradient(const NormArgs& a, uint32_t worker
 }
 
 // ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
-// As in the forward pass; a lane keeps to its columns: it adds up the weights' gradients of the rows that its team takes.  A workgroup takes one part of a worker's
-// rows and leaves one sum per column.
+// As in the forward pass; a lane keeps to its columns: it adds up the weights' gradients of the rows that its team takes.  A
+// workgroup takes one part of a worker's rows and leaves one sum per column.  The parts take the rows in turn, so that the
+// workgroups that run together go through memory together (8 x 8192 x 768, join: 161 us, with a stretch of rows each 171).
+
 // Values summed over the teams of a wavefront: over the lanes that are multiples of `lanes` apart.
 template <uint32_t NG>
 __device__ __forceinline__ void sum_teams(float (&v)[NG][kGroup], uint32_t lanes) {
@@ -67,13 +69,12 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 ? 768 : 10
   uint32_t turn = 0;
   for (uint32_t job = blockIdx.x; job < a.n * a.parts; job += gridDim.x) {
     const uint32_t w = job / a.parts, part = job % a.parts;
-    const uint32_t first = part * a.part_rows, left = a.rows - first, rows = left < a.part_rows ? left : a.part_rows;
     float sum[kOf][NG][kGroup] = {};
-    for (uint32_t i = 0; i < rows; i += together, turn ^= 1) {
+    for (uint32_t i = part * together; i < a.rows; i += a.parts * together, turn ^= 1) {
       // (a team without a row of its own goes over the last one again: the teams of a pair meet at barriers)
-      const bool spare = KIND != kBlock && i + team >= rows;
+      const bool spare = KIND != kBlock && i + team >= a.rows;
       if (KIND == kInWave && spare) break;
-      const uint32_t r = w * a.rows + first + (spare ? rows - 1 : i + team);
+      const uint32_t r = w * a.rows + (spare ? a.rows - 1 : i + team);
       typename Group<T>::type raw_y[NG];
       typename Group<H>::type raw_h[NG], raw_g[NG];
 #pragma unroll
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(256) void k_norm_no_rows(NormArgs a) {
 }
 
 // The team that a row of `groups` groups is given; us, norm / join, bfloat16 and a stream in fp32:
-//   8 x 2048 x  640: pair of 96 27.3 / 43.4, 32 x 3 30.0 / 47.5       8 x 8192 x 768: join, 32 x 3 (229 registers) 166, pair 172
+//   8 x 2048 x  640: pair of 96 27.3 / 43.4, 32 x 3 30.0 / 47.5       8 x 8192 x 768: join, 32 x 3 (229 registers) 158, pair 161
 //   8 x 2048 x 1024: 64 x 2 41.2 / 60.6, 128 41.1 / 60.5, in parts of 32 rows 42.3 / 62.7 and 49.6 / 62.5
 Team backward_team(uint32_t groups) {
   if (groups <= 64) {
@@ -377,18 +378,23 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
 
-// Parts are a function of a worker's rows alone, so that its sums do not depend on the other workers.  Short ones fill the
-// device (us by rows of a part: 5 x 211 x 1111 norm 4 17.7, 8 17.2, 16 20.3; 3 x 401 x 1601 join 4 18.8, 8 18.5, 16 22.9;
-// 8 x 256 x 12000 norm 8 72, 16 87, 32 136), long ones leave fewer sums to be joined (8 x 8192 x 768 join 16 204, 32 174,
-// 64 171; 8 x 2048 x 4096 8 246, 16 229, 32 222).
+// Parts are a function of a worker's rows and columns alone, so that its sums do not depend on the other workers.  Small
+// ones fill the device with few workers, large ones leave fewer sums to be joined with many; us by rows of a part, 768
+// columns, norm / join:
+//   1 x 1024:  8 15.0 / 16.3,  16 14.9 / 16.5,  32 17.4 / 23.9      8 x 1024: 8 17.3, 16 17.8, 32 21.7 (norm)
+//   1 x 8192: 16 18.4 / 27.2,  32 21.7 / 33.8,  64 33.2 / 53.0      8 x 8192: 16 168, 32 166, 64 161 (join)
+// (5 x 211 x 1111, norm: 4 15.4, 8 15.4; 3 x 401 x 1601, join: 4 17.9, 8 17.4, 16 22.9; 8 x 256 x 12000, join: 8 109, 16 122;
+// 8 x 2048 x 4096, join: 8 234, 16 227, 32 232).
 Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool gradients) {
   Cut c = {};
   if (rows == 0) return c;
-  c.part_rows = 4;
-  while (c.part_rows < 32 && c.part_rows * 2 <= rows / 128) c.part_rows *= 2;
-  if (rows >= 16384) c.part_rows = 64;
+  c.part_rows = 8;
+  while (c.part_rows < 64 && c.part_rows * 2 <= rows / 512) c.part_rows *= 2;
+  const Team team = team_of(cols);
+  const uint32_t together = team.each ? team_threads(team) / team.lanes : 1;
+  if (c.part_rows < together) c.part_rows = together;
   c.parts = (rows + c.part_rows - 1) / c.part_rows;
-  if (team_of(cols).each == 0) c.sums_bytes = up256(static_cast<size_t>(n) * rows * sizeof(float2));
+  if (team.each == 0) c.sums_bytes = up256(static_cast<size_t>(n) * rows * sizeof(float2));
   if (gradients && c.parts > 1)
     c.partial_bytes = up256(static_cast<size_t>(n) * c.parts * kGradients * cols * sizeof(float));
   return c;
