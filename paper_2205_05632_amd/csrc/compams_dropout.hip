@@ -36,10 +36,10 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a) {
       // (a row beyond the last: the last one again, not stored below)
       const uint64_t in = first + q * tall, r = in < a.total ? in : a.total - 1;
       const X* const from = static_cast<const X*>(a.x) + static_cast<int64_t>(r) * a.ld_x;
-      x[q] = FULL ? load_early<true>(from, c, a.cols) : load_raw(from, c, a.cols);
+      x[q] = FULL ? load_early<kFullGroups>(from, c, a.cols) : load_raw(from, c, a.cols);
       if constexpr (ADD) {
         const Y* const add = static_cast<const Y*>(a.residual) + static_cast<int64_t>(r) * a.ld_residual;
-        res[q] = FULL ? load_early<true>(add, c, a.cols) : load_raw(add, c, a.cols);
+        res[q] = FULL ? load_early<kFullGroups>(add, c, a.cols) : load_raw(add, c, a.cols);
       }
     }
 #pragma unroll
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a) {
 #pragma unroll
         for (uint32_t j = 0; j < kGroup; ++j) v[j] = w[j] + v[j];
       }
-      store_group<Y, FULL>(static_cast<Y*>(a.y) + static_cast<int64_t>(r) * a.ld_y, c, a.cols, v);
+      store_group<Y, FULL ? kFullGroups : kAnyWidth>(static_cast<Y*>(a.y) + static_cast<int64_t>(r) * a.ld_y, c, a.cols, v);
     }
   }
 }

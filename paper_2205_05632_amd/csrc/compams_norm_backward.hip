@@ -50,8 +50,9 @@ __device__ __forceinline__ void sum_teams(float (&v)[NG][kGroup], uint32_t lanes
     }
 }
 
-template <typename T, typename H, uint32_t NG, TeamKind KIND, bool JOIN, bool FULL>
+template <typename T, typename H, uint32_t NG, TeamKind KIND, bool JOIN, Width WIDTH>
 __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 ? 768 : 1024) void k_norm_backward(NormArgs a, uint32_t lanes) {
+  constexpr bool FULL = WIDTH == kFullGroups;  // and nothing is left out of the call
   constexpr uint32_t kOf = JOIN ? 3 : 2;
   __shared__ float slots[2][2][kSlots];
   extern __shared__ float tile[];  // a row of columns for each wavefront (kInWave), or one (kPair)
@@ -63,8 +64,8 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 ? 768 : 10
 #pragma unroll
   for (uint32_t k = 0; k < NG; ++k) {
     const uint32_t c = (k * lanes + lane) * kGroup;
-    g[k] = load_weight_early<FULL>(a.gamma, c, a.cols, 1.0f);
-    settle_unless<FULL, float>(g[k], c, a.cols);
+    g[k] = load_weight_early<WIDTH>(a.gamma, c, a.cols, 1.0f);
+    settle_if<WIDTH, float>(g[k], c, a.cols);
   }
   uint32_t turn = 0;
   for (uint32_t job = blockIdx.x; job < a.n * a.parts; job += gridDim.x) {
@@ -80,9 +81,9 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 ? 768 : 10
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
         const uint32_t c = (k * lanes + lane) * kGroup;
-        raw_y[k] = load_early<FULL>(row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
-        raw_h[k] = load_early<FULL>(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), c, a.cols);
-        if (JOIN && (FULL || a.dh)) raw_g[k] = load_early<FULL>(row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
+        raw_y[k] = load_early<WIDTH>(row_of<T>(a.dy, a.ld_dy, r), c, a.cols);
+        raw_h[k] = load_early<WIDTH>(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), c, a.cols);
+        if (JOIN && (FULL || a.dh)) raw_g[k] = load_early<WIDTH>(row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
       }
       const float mean = a.mean[r], rstd = a.rstd[r];
       float s[2] = {0.0f, 0.0f};
@@ -90,8 +91,8 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 ? 768 : 10
       for (uint32_t k = 0; k < NG; ++k) {
         const uint32_t c = (k * lanes + lane) * kGroup;
         float z[kGroup], u[kGroup];
-        settle_unless<FULL, T>(raw_y[k], c, a.cols);
-        settle_unless<FULL, H>(raw_h[k], c, a.cols);
+        settle_if<WIDTH, T>(raw_y[k], c, a.cols);
+        settle_if<WIDTH, H>(raw_h[k], c, a.cols);
         unpack(u, raw_y[k]);
         unpack(z, raw_h[k]);
 #pragma unroll
@@ -120,17 +121,17 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 ? 768 : 10
         }
         if constexpr (JOIN) {
           if (FULL || a.dh) {
-            settle_unless<FULL, H>(raw_g[k], c, a.cols);
+            settle_if<WIDTH, H>(raw_g[k], c, a.cols);
             unpack(z, raw_g[k]);
 #pragma unroll
             for (uint32_t j = 0; j < kGroup; ++j) u[j] += z[j];
           }
         }
-        if (FULL || a.dresidual) store_group<H, FULL>(row_of<H>(a.dresidual, a.ld_dresidual, r), c, a.cols, u);
+        if (FULL || a.dresidual) store_group<H, WIDTH>(row_of<H>(a.dresidual, a.ld_dresidual, r), c, a.cols, u);
         if constexpr (JOIN) {
           if (FULL || a.dx || a.grad[2]) {
             drop_group(u, a.drop, offset, r, c);
-            if (FULL || a.dx) store_group<T, FULL>(row_of<T>(a.dx, a.ld_dx, r), c, a.cols, u);
+            if (FULL || a.dx) store_group<T, WIDTH>(row_of<T>(a.dx, a.ld_dx, r), c, a.cols, u);
 #pragma unroll
             for (uint32_t j = 0; j < kGroup; ++j) sum[2][k][j] += u[j];
           }
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 ? 768 : 10
         if (a.parts > 1) {
           float* const row = a.partial + ((static_cast<size_t>(w) * a.parts + part) * kGradients + which) * a.cols;
 #pragma unroll
-          for (uint32_t k = 0; k < NG; ++k) store_group<float, FULL>(row, (k * lanes + lane) * kGroup, a.cols, sum[which][k]);
+          for (uint32_t k = 0; k < NG; ++k) store_group<float, WIDTH>(row, (k * lanes + lane) * kGroup, a.cols, sum[which][k]);
         } else {
 #pragma unroll
           for (uint32_t k = 0; k < NG; ++k)
@@ -356,11 +357,13 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
                     (!JOIN || (k.dh && k.dx && k.grad[2]));
 #define COMPAMS_BACKWARD(NG, KIND)                                                                                          \
   do {                                                                                                                      \
-    if (full) hipLaunchKernelGGL((k_norm_backward<T, H, NG, KIND, JOIN, true>), grid, block, lds, stream, k, t.lanes); \
-    else hipLaunchKernelGGL((k_norm_backward<T, H, NG, KIND, JOIN, false>), grid, block, lds, stream, k, t.lanes);     \
+    if (full) hipLaunchKernelGGL((k_norm_backward<T, H, NG, KIND, JOIN, kFullGroups>), grid, block, lds, stream, k, t.lanes); \
+    else hipLaunchKernelGGL((k_norm_backward<T, H, NG, KIND, JOIN, kAnyWidth>), grid, block, lds, stream, k, t.lanes);     \
   } while (0)
   if (t.kind == kInWave) {
-    if (t.each == 1) COMPAMS_BACKWARD(1, kInWave);
+    if (k.cols < kGroup)
+      hipLaunchKernelGGL((k_norm_backward<T, H, 1, kInWave, JOIN, kOneGroup>), grid, block, lds, stream, k, t.lanes);
+    else if (t.each == 1) COMPAMS_BACKWARD(1, kInWave);
     else COMPAMS_BACKWARD(2, kInWave);
   } else if (t.kind == kPair) {
     COMPAMS_BACKWARD(1, kPair);
@@ -371,8 +374,7 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
 #undef COMPAMS_BACKWARD
 }
 
-// (a row shorter than a group has no wide load)
-Team team_of(uint32_t cols) { return cols < kGroup ? Team{kBlock, 0, 0} : backward_team((cols + kGroup - 1) / kGroup); }
+Team team_of(uint32_t cols) { return backward_team((cols + kGroup - 1) / kGroup); }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 

@@ -9,10 +9,11 @@ namespace {
 // ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
 // Its lanes take the row's groups of eight columns in
 // turn, NG of them each; the row is read once, and mean and variance are two sums over what the registers hold.
-// FULL: the team has no lane to spare and everything that a call may leave out is there - the usual widths and the usual
+// kFullGroups: the team has no lane to spare and everything that a call may leave out is there - the usual widths and the usual
 // calls, without a test of any of it for every group (a join of rows of 768: 212 vector instructions a group for 494).
-template <typename T, typename H, uint32_t NG, TeamKind KIND, bool JOIN, bool FULL>
+template <typename T, typename H, uint32_t NG, TeamKind KIND, bool JOIN, Width WIDTH>
 __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_forward(NormArgs a, uint32_t lanes) {
+  constexpr bool FULL = WIDTH == kFullGroups;  // and nothing is left out of the call
   __shared__ float slots[2][1][kSlots];
   const uint32_t team = team_of_lane<KIND>(lanes), lane = lane_of_team<KIND>(lanes, team);
   const uint32_t together = teams_together<KIND>(lanes);
@@ -30,31 +31,31 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_
       typename Group<H>::type res[NG];
       typename Group<float>::type bias[NG];
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) x[k] = load_early<FULL>(row_of<T>(a.x, a.ld_x, r), (k * lanes + lane) * kGroup, a.cols);
+      for (uint32_t k = 0; k < NG; ++k) x[k] = load_early<WIDTH>(row_of<T>(a.x, a.ld_x, r), (k * lanes + lane) * kGroup, a.cols);
       if (FULL || a.residual) {
 #pragma unroll
         for (uint32_t k = 0; k < NG; ++k)
-          res[k] = load_early<FULL>(row_of<H>(a.residual, a.ld_residual, r), (k * lanes + lane) * kGroup, a.cols);
+          res[k] = load_early<WIDTH>(row_of<H>(a.residual, a.ld_residual, r), (k * lanes + lane) * kGroup, a.cols);
       }
 #pragma unroll
-      for (uint32_t k = 0; k < NG; ++k) bias[k] = load_weight_early<FULL>(a.bias, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+      for (uint32_t k = 0; k < NG; ++k) bias[k] = load_weight_early<WIDTH>(a.bias, (k * lanes + lane) * kGroup, a.cols, 0.0f);
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
-        g[k] = load_weight_early<FULL>(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
-        b[k] = load_weight_early<FULL>(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+        g[k] = load_weight_early<WIDTH>(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+        b[k] = load_weight_early<WIDTH>(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
       }
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
         const uint32_t c = (k * lanes + lane) * kGroup;
-        settle_unless<FULL, T>(x[k], c, a.cols);
-        settle_unless<FULL, float>(bias[k], c, a.cols);
+        settle_if<WIDTH, T>(x[k], c, a.cols);
+        settle_if<WIDTH, float>(bias[k], c, a.cols);
         unpack(v[k], x[k]);
 #pragma unroll
         for (uint32_t j = 0; j < kGroup; ++j) v[k][j] += bias[k][j];
         drop_group(v[k], a.drop, offset, r, c);
         if (FULL || a.residual) {
           float w[kGroup];
-          settle_unless<FULL, H>(res[k], c, a.cols);
+          settle_if<WIDTH, H>(res[k], c, a.cols);
           unpack(w, res[k]);
 #pragma unroll
           for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = w[j] + v[k][j];
@@ -64,15 +65,15 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_
       typename Group<H>::type x[NG];
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k)
-        x[k] = load_early<FULL>(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), (k * lanes + lane) * kGroup, a.cols);
+        x[k] = load_early<WIDTH>(row_of<H>(static_cast<const void*>(a.h), a.ld_h, r), (k * lanes + lane) * kGroup, a.cols);
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
-        g[k] = load_weight_early<FULL>(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
-        b[k] = load_weight_early<FULL>(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
+        g[k] = load_weight_early<WIDTH>(a.gamma, (k * lanes + lane) * kGroup, a.cols, 1.0f);
+        b[k] = load_weight_early<WIDTH>(a.beta, (k * lanes + lane) * kGroup, a.cols, 0.0f);
       }
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
-        settle_unless<FULL, H>(x[k], (k * lanes + lane) * kGroup, a.cols);
+        settle_if<WIDTH, H>(x[k], (k * lanes + lane) * kGroup, a.cols);
         unpack(v[k], x[k]);
       }
     }
@@ -107,12 +108,12 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
       const uint32_t c = (k * lanes + lane) * kGroup;
-      if (JOIN && (FULL || a.h)) store_group<H, FULL>(row_of<H>(a.h, a.ld_h, r), c, a.cols, v[k]);
-      settle_unless<FULL, float>(g[k], c, a.cols);
-      settle_unless<FULL, float>(b[k], c, a.cols);
+      if (JOIN && (FULL || a.h)) store_group<H, WIDTH>(row_of<H>(a.h, a.ld_h, r), c, a.cols, v[k]);
+      settle_if<WIDTH, float>(g[k], c, a.cols);
+      settle_if<WIDTH, float>(b[k], c, a.cols);
 #pragma unroll
       for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = fmaf((v[k][j] - mean) * rstd, g[k][j], b[k][j]);
-      store_group<T, FULL>(row_of<T>(a.y, a.ld_y, r), c, a.cols, v[k]);
+      store_group<T, WIDTH>(row_of<T>(a.y, a.ld_y, r), c, a.cols, v[k]);
     }
     if (lane == 0) {
       if (FULL || a.mean) a.mean[r] = mean;
@@ -194,12 +195,16 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
                     (!JOIN || (k.bias && k.residual && k.h));
 #define COMPAMS_FORWARD(NG, KIND)                                                                            \
   do {                                                                                                      \
-    if (full) hipLaunchKernelGGL((k_norm_forward<T, H, NG, KIND, JOIN, true>), grid, block, 0, stream, k, t.lanes); \
-    else hipLaunchKernelGGL((k_norm_forward<T, H, NG, KIND, JOIN, false>), grid, block, 0, stream, k, t.lanes);     \
+    if (full) hipLaunchKernelGGL((k_norm_forward<T, H, NG, KIND, JOIN, kFullGroups>), grid, block, 0, stream, k, t.lanes); \
+    else hipLaunchKernelGGL((k_norm_forward<T, H, NG, KIND, JOIN, kAnyWidth>), grid, block, 0, stream, k, t.lanes);     \
   } while (0)
   if (t.kind == kInWave) {
     switch (t.each) {
-      case 1: COMPAMS_FORWARD(1, kInWave); break;
+      case 1:
+        if (k.cols < kGroup)
+          hipLaunchKernelGGL((k_norm_forward<T, H, 1, kInWave, JOIN, kOneGroup>), grid, block, 0, stream, k, t.lanes);
+        else COMPAMS_FORWARD(1, kInWave);
+        break;
       case 2: COMPAMS_FORWARD(2, kInWave); break;
       case 3: COMPAMS_FORWARD(3, kInWave); break;
       default: COMPAMS_FORWARD(4, kInWave); break;
@@ -219,8 +224,7 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
 }  // namespace
 
 hipError_t norm_forward(const NormArgs& k, int32_t type, int32_t stream_type, hipStream_t stream) {
-  // (a row shorter than a group has no wide load)
-  const Team team = k.cols < kGroup ? Team{kBlock, 0, 0} : forward_team((k.cols + kGroup - 1) / kGroup, k.join);
+  const Team team = forward_team((k.cols + kGroup - 1) / kGroup, k.join);
   return by_types(type, stream_type, [&](auto t, auto h) {
     using T = decltype(t);
     using H = decltype(h);

@@ -50,11 +50,21 @@ __device__ __forceinline__ void move_down(Words& w, uint32_t by) {
 // (unaligned accesses are the processor's).  settle() then moves such a group into its place, with 0 beyond the last
 // column: apart from the load, so that all of a row's loads are under way before the first one is waited for.  (With the
 // groups at a row's end read one by one and at once, a row of 1601 columns took a workgroup 2.3 us in the backward pass.)
-// FULL: the caller knows that no group reaches beyond the last column.
-template <bool FULL = false, typename T>
+// What a kernel knows of its rows' width.
+enum Width {
+  kAnyWidth = 0,   // at least eight columns
+  kFullGroups = 1, // no lane has a group that reaches beyond the last column
+  kOneGroup = 2    // fewer than eight columns: no wide load fits, and one lane has all of them
+};
+template <Width WIDTH = kAnyWidth, typename T>
 __device__ __forceinline__ typename Group<T>::type load_early(const T* row, uint32_t c, uint32_t cols) {
   typename Group<T>::type raw;
-  __builtin_memcpy(&raw, row + (FULL || c < cols - kGroup ? c : cols - kGroup), sizeof(raw));
+  if constexpr (WIDTH == kOneGroup) {
+#pragma unroll
+    for (uint32_t j = 0; j < kGroup; ++j) raw[j] = c + j < cols ? row[c + j] : static_cast<T>(0.0f);
+  } else {
+    __builtin_memcpy(&raw, row + (WIDTH == kFullGroups || c < cols - kGroup ? c : cols - kGroup), sizeof(raw));
+  }
   return raw;
 }
 template <typename T>
@@ -72,20 +82,19 @@ __device__ __forceinline__ void settle(typename Group<T>::type& raw, uint32_t c,
   for (uint32_t i = 0; i < kGroup * sizeof(T) / 4; ++i) w[i] = by < kGroup ? w[i] : 0u;
   __builtin_memcpy(&raw, &w, sizeof(w));
 }
-template <bool FULL, typename T>
-__device__ __forceinline__ void settle_unless(typename Group<T>::type& raw, uint32_t c, uint32_t cols) {
-  if constexpr (!FULL) settle<T>(raw, c, cols);
+template <Width WIDTH, typename T>
+__device__ __forceinline__ void settle_if(typename Group<T>::type& raw, uint32_t c, uint32_t cols) {
+  if constexpr (WIDTH == kAnyWidth) settle<T>(raw, c, cols);
 }
 // The same in one, for rows of any width.
 template <typename T>
 __device__ __forceinline__ typename Group<T>::type load_raw(const T* row, uint32_t c, uint32_t cols) {
-  typename Group<T>::type raw = {};
+  typename Group<T>::type raw;
   if (cols >= kGroup) {
     raw = load_early(row, c, cols);
     settle<T>(raw, c, cols);
   } else {
-#pragma unroll
-    for (uint32_t j = 0; j < kGroup; ++j) raw[j] = c + j < cols ? row[c + j] : static_cast<T>(0.0f);
+    raw = load_early<kOneGroup>(row, c, cols);
   }
   return raw;
 }
@@ -100,9 +109,9 @@ __device__ __forceinline__ void load_group(float (&v)[kGroup], const T* row, uin
 }
 
 // Each value rounded to T once, to the nearest.
-template <typename T, bool FULL = false>
+template <typename T, Width WIDTH = kAnyWidth>
 __device__ __forceinline__ void store_group(T* row, uint32_t c, uint32_t cols, const float (&v)[kGroup]) {
-  if (FULL || c + kGroup <= cols) {
+  if (WIDTH == kFullGroups || c + kGroup <= cols) {
     typename Group<T>::type raw;
 #pragma unroll
     for (uint32_t j = 0; j < kGroup; ++j) raw[j] = static_cast<T>(v[j]);
