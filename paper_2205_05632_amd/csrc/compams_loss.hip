@@ -65,6 +65,15 @@ __device__ __forceinline__ Exponent exponent_of(float top) {
   return {scale, -top * scale};
 }
 __device__ __forceinline__ float exp_below(float v, const Exponent& x) { return __builtin_amdgcn_exp2f(fmaf(v, x.scale, x.shift)); }
+// The shift is rounded: with a top of 65504 all exponentials are off by the same 2^(half of 2^-7).  That cancels in the
+// softmax as long as they come from one shift; from one to another they change by the difference of the shifts ...
+__device__ __forceinline__ float from_to(const Exponent& from, const Exponent& to) {
+  return from.scale == to.scale ? __builtin_amdgcn_exp2f(to.shift - from.shift) : 0.0f;
+}
+// ... and a logarithm of their sum is set right by what is left at the top (exact in one multiply-add).
+__device__ __forceinline__ float log_of_sum(float sum, float top, const Exponent& x) {
+  return logf(sum) - 0.693147180559945309417f * fmaf(top, x.scale, x.shift);
+}
 
 // ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
 // A team is 16 to 64 lanes of a wavefront (WAVE) or a whole workgroup.  The row is read once and kept as it came, in
@@ -181,7 +190,7 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
     }
     turn ^= 1;
     const bool none = !inside || top == -INFINITY;
-    if (a.losses && lane == 0) a.losses[r] = none ? __builtin_nanf("") : logf(s[0]) + top - of_target;
+    if (a.losses && lane == 0) a.losses[r] = none ? __builtin_nanf("") : log_of_sum(s[0], top, x) + top - of_target;
     if (!out) continue;
     if (a.counts) s[1] = static_cast<float>(a.counts[w]);
     // a row without a softmax or a loss has no gradient
@@ -217,10 +226,28 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
   }
 }
 
-// ---- Rows of any width: a workgroup goes over its row twice, once for the running maximum and sum, once for the gradient.
+// ---- Rows of any width: a workgroup goes over its row twice, once for a running maximum and sum, once for the gradient.
+constexpr uint32_t kAhead = 4;  // groups that a lane requests at once
+
+// One more value to a lane's maximum and sum.  What the sum counts from moves up rarely after the first few.
+struct Running {
+  float top = -INFINITY, sum = 0.0f;
+  Exponent x = {0.0f, 0.0f};
+  __device__ __forceinline__ void raise(float m) {
+    if (!(m > top)) return;
+    const Exponent to = exponent_of(m);
+    sum = top == -INFINITY ? sum : sum * from_to(x, to);  // (without a finite entry so far it is 0 or NaN)
+    top = m;
+    x = to;
+  }
+  __device__ __forceinline__ void add(float v) { sum += top == -INFINITY ? (v != v ? v : 0.0f) : exp_below(v, x); }
+};
+
 template <typename T>
 __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
-  __shared__ float slots[2][kLossWaves];
+  constexpr uint32_t kEach = Logits<T>::kEach;
+  typedef typename Logits<T>::type V;
+  __shared__ float tops[kLossWaves], sums[kLossWaves];
   for (uint32_t r = blockIdx.x; r < a.total; r += gridDim.x) {
     const int64_t target = target_of(a, r);
     const T* const row = static_cast<const T*>(a.logits) + static_cast<int64_t>(r) * a.ld_logits;
@@ -233,48 +260,81 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
       continue;
     }
     const bool inside = target >= 0 && target < static_cast<int64_t>(a.vocab);
-    const float of_target = inside ? to_float(row[target]) : __builtin_nanf("");
-    float top = -INFINITY, sum = 0.0f;
-    for (uint32_t c = threadIdx.x * kGroup; c < a.vocab; c += kLossThreads * kGroup) {
-      float v[kGroup];
-      load_group(v, row, c, a.vocab);
-      float m = top;
-#pragma unroll
-      for (uint32_t j = 0; j < kGroup; ++j) m = c + j < a.vocab ? fmaxf(m, v[j]) : m;
-      // (no finite entry so far: a lane's sum stays 0, or becomes NaN with one)
-      sum = top == -INFINITY ? sum : sum * expf(top - m);
-      top = m;
-#pragma unroll
-      for (uint32_t j = 0; j < kGroup; ++j)
-        if (c + j < a.vocab) sum += v[j] == -INFINITY ? 0.0f : expf(v[j] - top);
+    const float of_target = inside ? to_float(row[target]) : 0.0f;
+    // groups from the row's first multiple of 16 bytes, and its two ends, as above
+    uint32_t head = static_cast<uint32_t>(-reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
+    head = head < a.vocab ? head : a.vocab;
+    const uint32_t groups = (a.vocab - head) / kEach, tail = head + groups * kEach, lane = threadIdx.x;
+    const uint32_t end = lane < 8 ? (lane < head ? lane : a.vocab) : lane < 16 ? tail + (lane - 8) : a.vocab;
+    const float at_end = end < a.vocab ? to_float(row[end]) : -INFINITY;
+    const V* const inner = reinterpret_cast<const V*>(row + head);
+    Running run;
+    if (end < a.vocab) {
+      run.raise(at_end);
+      run.add(at_end);
     }
-    const float wave_top = over_lanes(top, 64, Max());
+    for (uint32_t first = lane; first < groups; first += kLossThreads * kAhead) {
+      V raw[kAhead];
+#pragma unroll
+      for (uint32_t k = 0; k < kAhead; ++k) {  // (beyond the last group: that one, left out below)
+        const uint32_t g = first + k * kLossThreads;
+        raw[k] = inner[g < groups ? g : groups - 1];
+      }
+      float m = -INFINITY;
+#pragma unroll
+      for (uint32_t k = 0; k < kAhead; ++k)
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j) m = fmaxf(m, to_float(raw[k][j]));
+      run.raise(m);
+#pragma unroll
+      for (uint32_t k = 0; k < kAhead; ++k) {
+        if (first + k * kLossThreads >= groups) break;
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j) run.add(to_float(raw[k][j]));
+      }
+    }
+    const float wave_top = over_lanes(run.top, 64, Max());
     __syncthreads();  // the slots may still be read for the row before
-    if ((threadIdx.x & 63u) == 0) slots[0][threadIdx.x >> 6] = wave_top;
+    if (lane % 64 == 0) tops[lane / 64] = wave_top;
     __syncthreads();
-    float all_top = slots[0][0];
-    for (uint32_t w = 1; w < kLossWaves; ++w) all_top = fmaxf(all_top, slots[0][w]);
-    sum = sum_lanes(top == -INFINITY ? sum : sum * expf(top - all_top), 64);
-    if ((threadIdx.x & 63u) == 0) slots[1][threadIdx.x >> 6] = sum;
+    float top = tops[0];
+    for (uint32_t w = 1; w < kLossWaves; ++w) top = fmaxf(top, tops[w]);
+    const Exponent x = exponent_of(top);
+    const float mine = sum_lanes(run.top == -INFINITY ? run.sum : run.sum * from_to(run.x, x), 64);
+    if (lane % 64 == 0) sums[lane / 64] = mine;
     __syncthreads();
-    float all_sum = 0.0f;
-    for (uint32_t w = 0; w < kLossWaves; ++w) all_sum += slots[1][w];
-    // a row without any finite entry, or with a target that is none, has no softmax and no loss
-    const float log_sum = logf(all_sum) + all_top;
-    const bool none = !inside || all_top == -INFINITY;
-    if (a.losses && threadIdx.x == 0) a.losses[r] = none ? __builtin_nanf("") : log_sum - of_target;
+    float sum = 0.0f;
+    for (uint32_t w = 0; w < kLossWaves; ++w) sum += sums[w];
+    const bool none = !inside || top == -INFINITY;
+    if (a.losses && lane == 0) a.losses[r] = none ? __builtin_nanf("") : log_of_sum(sum, top, x) + top - of_target;
     if (!out) continue;
-    const float count = static_cast<float>(a.counts[r / a.rows]);
-    const float factor = none ? __builtin_nanf("") : a.grad_scale / count;
-    const float share = factor / all_sum;
-    for (uint32_t c = threadIdx.x * kGroup; c < a.vocab; c += kLossThreads * kGroup) {
-      float v[kGroup];
-      load_group(v, row, c, a.vocab);
+    const float factor = none ? __builtin_nanf("") : a.grad_scale / static_cast<float>(a.counts[r / a.rows]);
+    const float share = factor / sum;
+    const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == reinterpret_cast<uintptr_t>(row) % 16;
+    const uint32_t hot = inside ? static_cast<uint32_t>(target) : a.vocab;
+    char* const inner_out = reinterpret_cast<char*>(out + head);
+    for (uint32_t first = lane; first < groups; first += kLossThreads * kAhead) {
+      V raw[kAhead];
 #pragma unroll
-      for (uint32_t j = 0; j < kGroup; ++j)
-        v[j] = expf(v[j] - all_top) * share - (static_cast<int64_t>(c + j) == target ? factor : 0.0f);
-      store_group(out, c, a.vocab, v);
+      for (uint32_t k = 0; k < kAhead; ++k) {
+        const uint32_t g = first + k * kLossThreads;
+        raw[k] = inner[g < groups ? g : groups - 1];
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < kAhead; ++k) {
+        const uint32_t g = first + k * kLossThreads, at = hot - head - g * kEach;
+        if (g >= groups) break;
+        V o;
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j)
+          o[j] = static_cast<T>(exp_below(to_float(raw[k][j]), x) * share - (at == j ? factor : 0.0f));
+        char* const p = inner_out + static_cast<size_t>(g) * 16;
+        if (!aligned) __builtin_memcpy(p, &o, 16);
+        else if (a.stream) __builtin_nontemporal_store(o, reinterpret_cast<V*>(p));
+        else *reinterpret_cast<V*>(p) = o;
+      }
     }
+    if (end < a.vocab) out[end] = static_cast<T>(exp_below(at_end, x) * share - (end == hot ? factor : 0.0f));
   }
 }
 

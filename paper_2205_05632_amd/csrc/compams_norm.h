@@ -131,7 +131,7 @@ struct Cut {
   uint32_t parts, part_rows;
   size_t sums_bytes, partial_bytes;
 };
-Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool gradients);
+Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool join, bool gradients);
 
 hipError_t norm_forward(const NormArgs& a, int32_t type, int32_t stream_type, hipStream_t stream);
 hipError_t norm_backward(const NormArgs& a, int32_t type, int32_t stream_type, hipStream_t stream);

@@ -84,7 +84,7 @@ int backward(const compams_norm* a, bool join, hipStream_t stream) {
                                check_matrix(a->dresidual, a->ld_dresidual, *a, a->stream_type), check_vectors(*a, join)});
     if (bad != COMPAMS_OK) return bad;
   }
-  const Cut cut = norm_cut(k.n, k.rows, k.cols, any_gradient(*a));
+  const Cut cut = norm_cut(k.n, k.rows, k.cols, join, any_gradient(*a));
   if (cut.sums_bytes + cut.partial_bytes > 0) {
     if (!a->workspace) return COMPAMS_INVALID_ARG;
     if (!aligned_to(a->workspace, 256)) return COMPAMS_BAD_ALIGNMENT;
@@ -105,8 +105,9 @@ extern "C" {
 
 size_t compams_norm_workspace_size(const compams_norm* a) {
   if (!compams::norm_valid(a, false)) return 0;
-  const compams::Cut c =
-      compams::norm_cut(static_cast<uint32_t>(a->n), static_cast<uint32_t>(a->rows), static_cast<uint32_t>(a->cols), compams::any_gradient(*a));
+  // (for either of the two calls: a join's cut is the one that takes more)
+  const compams::Cut c = compams::norm_cut(static_cast<uint32_t>(a->n), static_cast<uint32_t>(a->rows),
+                                           static_cast<uint32_t>(a->cols), true, compams::any_gradient(*a));
   return c.sums_bytes + c.partial_bytes;
 }
 int compams_layer_norm_forward(const compams_norm* a, void* hip_stream) {

@@ -51,7 +51,7 @@ __device__ __forceinline__ void sum_teams(float (&v)[NG][kGroup], uint32_t lanes
 }
 
 template <typename T, typename H, uint32_t NG, TeamKind KIND, bool JOIN, Width WIDTH>
-__global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 ? 768 : 1024) void k_norm_backward(NormArgs a, uint32_t lanes) {
+__global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 && JOIN ? 768 : 1024) void k_norm_backward(NormArgs a, uint32_t lanes) {
   constexpr bool FULL = WIDTH == kFullGroups;  // and nothing is left out of the call
   constexpr uint32_t kOf = JOIN ? 3 : 2;
   __shared__ float slots[2][2][kSlots];
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(256) void k_norm_no_rows(NormArgs a) {
 // The team that a row of `groups` groups is given; us, norm / join, bfloat16 and a stream in fp32:
 //   8 x 2048 x  640: pair of 96 27.3 / 43.4, 32 x 3 30.0 / 47.5       8 x 8192 x 768: join, 32 x 3 (229 registers) 158, pair 161
 //   8 x 2048 x 1024: 64 x 2 41.2 / 60.6, 128 41.1 / 60.5, in parts of 32 rows 42.3 / 62.7 and 49.6 / 62.5
-Team backward_team(uint32_t groups) {
+Team backward_team(uint32_t groups, bool join) {
   if (groups <= 64) {
     uint32_t lanes = 8;
     while (lanes < groups) lanes *= 2;
@@ -344,8 +344,8 @@ Team backward_team(uint32_t groups) {
   const uint32_t halves = (groups + 31) / 32;
   if (halves == 3 || halves == 5 || halves == 7) return {kPair, halves * 32, 1};
   if (groups <= 128) return {kInWave, 64, 2};
-  // (two groups a lane need 170 registers: twelve wavefronts at most)
-  const uint32_t each = groups <= 1024 ? 1 : groups <= 1536 ? 2 : 0;
+  // (two groups a lane take a join 168 registers: twelve wavefronts at most)
+  const uint32_t each = groups <= 1024 ? 1 : groups <= (join ? 1536 : 2048) ? 2 : 0;
   return {kBlock, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
 }
 
@@ -374,7 +374,7 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
 #undef COMPAMS_BACKWARD
 }
 
-Team team_of(uint32_t cols) { return backward_team((cols + kGroup - 1) / kGroup); }
+Team team_of(uint32_t cols, bool join) { return backward_team((cols + kGroup - 1) / kGroup, join); }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -387,12 +387,12 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 //   1 x 8192: 16 18.4 / 27.2,  32 21.7 / 33.8,  64 33.2 / 53.0      8 x 8192: 16 168, 32 166, 64 161 (join)
 // (5 x 211 x 1111, norm: 4 15.4, 8 15.4; 3 x 401 x 1601, join: 4 17.9, 8 17.4, 16 22.9; 8 x 256 x 12000, join: 8 109, 16 122;
 // 8 x 2048 x 4096, join: 8 234, 16 227, 32 232).
-Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool gradients) {
+Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool join, bool gradients) {
   Cut c = {};
   if (rows == 0) return c;
   c.part_rows = 8;
   while (c.part_rows < 64 && c.part_rows * 2 <= rows / 512) c.part_rows *= 2;
-  const Team team = team_of(cols);
+  const Team team = team_of(cols, join);
   const uint32_t together = team.each ? team_threads(team) / team.lanes : 1;
   if (c.part_rows < together) c.part_rows = together;
   c.parts = (rows + c.part_rows - 1) / c.part_rows;
@@ -409,7 +409,7 @@ hipError_t norm_backward(const NormArgs& k, int32_t type, int32_t stream_type, h
     hipLaunchKernelGGL(k_norm_no_rows, dim3(at_most((k.cols + 255) / 256, 4096), kGradients, k.n), dim3(256), 0, stream, k);
     return hipGetLastError();
   }
-  const Team team = team_of(k.cols);
+  const Team team = team_of(k.cols, k.join);
   return by_types(type, stream_type, [&](auto t, auto h) {
     using T = decltype(t);
     using H = decltype(h);
