@@ -148,7 +148,7 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
     // (less than 2^24 of them: exact in fp32; a.counts is there where there may be more)
     const float count = a.counts ? 0.0f : static_cast<float>(count_rows(a, w, lane, lanes));
     const bool inside = target >= 0 && target < static_cast<int64_t>(a.vocab);
-    const float of_target = inside ? to_float(logits[target]) : 0.0f;
+    float of_target = inside ? to_float(logits[target]) : 0.0f;
     float top = at_end;
     if (groups) {
 #pragma unroll
@@ -181,6 +181,8 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
       s[0] += k * lanes + again < groups ? e[0] : 0.0f;
       __builtin_amdgcn_sched_barrier(0);
     }
+    // The target's logit is here before the last barrier: behind it another wavefront may write the gradient over it.
+    asm volatile("" : "+v"(of_target));
     if constexpr (WAVE) {
       s[0] = sum_lanes(s[0], lanes);
       s[1] = sum_lanes(s[1], lanes);
