@@ -108,16 +108,31 @@ __device__ __forceinline__ void forget_group(V& raw) {
 constexpr uint32_t kTeamThreads = 256, kRowThreads = 512;
 constexpr uint64_t kStreamBytes = 32u << 20;
 
-template <typename T, uint32_t NG, bool WAVE, bool STREAM>
-__global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(LossArgs a, uint32_t lanes) {
+enum RowKind {
+  kWaveRows = 0,   // a team of 16 to 64 lanes to a row, 256 threads to a workgroup
+  kBlockRow = 1,   // a workgroup to a row
+  kWorkerRows = 2  // a wavefront to a row, a workgroup to all rows of a worker, whose mean it forms as well
+};
+
+template <typename T, uint32_t NG, RowKind KIND, bool STREAM>
+__global__ __launch_bounds__(KIND == kWaveRows ? kTeamThreads : KIND == kBlockRow ? kRowThreads : kLossThreads) void k_loss(LossArgs a, uint32_t lanes) {
   constexpr uint32_t kEach = Logits<T>::kEach;
   typedef typename Logits<T>::type V;
   __shared__ float tops[2][kLossWaves];
   __shared__ float slots[2][2][kSlots];
-  const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
-  const uint32_t together = WAVE ? kTeamThreads / lanes : 1u, waves = lanes / 64;
+  constexpr bool WAVE = KIND != kBlockRow;
+  const uint32_t lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x, team = WAVE ? threadIdx.x / lanes : 0u;
+  const uint32_t together = KIND == kWaveRows ? kTeamThreads / lanes : KIND == kBlockRow ? 1u : kLossWaves, waves = lanes / 64;
   uint32_t turn = 0;
-  for (uint32_t r = WAVE ? blockIdx.x * together + threadIdx.x / lanes : blockIdx.x; r < a.total; r += gridDim.x * together) {
+  float of_worker[2] = {0.0f, 0.0f};  // kWorkerRows: losses, and rows that are learnt from
+  if constexpr (KIND == kWorkerRows) {
+    float c[1] = {static_cast<float>(count_rows(a, blockIdx.x, threadIdx.x, kLossThreads))};
+    sum_block(c, slots[0], kLossWaves);
+    of_worker[1] = c[0];
+  }
+  const uint32_t from = (KIND == kWorkerRows ? blockIdx.x * a.rows : blockIdx.x * together) + team;
+  const uint32_t to = KIND == kWorkerRows ? blockIdx.x * a.rows + a.rows : a.total;
+  for (uint32_t r = from; r < to; r += KIND == kWorkerRows ? together : gridDim.x * together) {
     const T* const logits = static_cast<const T*>(a.logits) + static_cast<int64_t>(r) * a.ld_logits;
     T* const out = a.dlogits ? static_cast<T*>(a.dlogits) + static_cast<int64_t>(r) * a.ld_dlogits : nullptr;
     const int64_t target = target_of(a, r);
@@ -146,7 +161,7 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
     const float at_end = end < a.vocab ? to_float(logits[end]) : -INFINITY;
     const uint32_t w = r / a.rows;
     // (less than 2^24 of them: exact in fp32; a.counts is there where there may be more)
-    const float count = a.counts ? 0.0f : static_cast<float>(count_rows(a, w, lane, lanes));
+    const float count = a.counts || KIND == kWorkerRows ? 0.0f : static_cast<float>(count_rows(a, w, lane, lanes));
     const bool inside = target >= 0 && target < static_cast<int64_t>(a.vocab);
     float of_target = inside ? to_float(logits[target]) : 0.0f;
     float top = at_end;
@@ -191,9 +206,12 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
     }
     turn ^= 1;
     const bool none = !inside || top == -INFINITY;
-    if (a.losses && lane == 0) a.losses[r] = none ? __builtin_nanf("") : log_of_sum(s[0], top, x) + top - of_target;
+    const float loss = none ? __builtin_nanf("") : log_of_sum(s[0], top, x) + top - of_target;
+    of_worker[0] += loss;
+    if (a.losses && lane == 0) a.losses[r] = loss;
     if (!out) continue;
     if (a.counts) s[1] = static_cast<float>(a.counts[w]);
+    if (KIND == kWorkerRows) s[1] = of_worker[1];
     // a row without a softmax or a loss has no gradient
     const float factor = none ? __builtin_nanf("") : a.grad_scale / s[1];
     const float share = factor / s[0];
@@ -224,6 +242,16 @@ __global__ __launch_bounds__(WAVE ? kTeamThreads : kRowThreads) void k_loss(Loss
       __builtin_amdgcn_sched_barrier(0);
     }
     if (end < a.vocab) out[end] = static_cast<T>(exp_below(at_end, x) * share - (end == hot ? factor : 0.0f));
+  }
+  if constexpr (KIND == kWorkerRows) {
+    // (the same in all lanes of a wavefront: one of them counts)
+    if (lane == 0) slots[1][0][team] = of_worker[0];
+    __syncthreads();
+    if (threadIdx.x == 0 && a.mean_loss) {
+      float sum = 0.0f;
+      for (uint32_t i = 0; i < kLossWaves; ++i) sum += slots[1][0][i];
+      a.mean_loss[blockIdx.x] = of_worker[1] > 0.0f ? sum / of_worker[1] : 0.0f;
+    }
   }
 }
 
@@ -359,18 +387,21 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_mean(LossArgs a) {
 //              16384: 1024 x 2 152, 512 x 4 97, 256 x 8 101, 128 x 16 110      32000: 512 x 8 182, 256 x 16 193
 //              50257: 832 x 8 400, 448 x 16 312, 256 x 32 311, 320 x 20 467 (waves that do not go evenly into four)
 struct Team {
-  bool wave;
+  RowKind kind;
   uint32_t lanes, each;
 };
-Team loss_team(uint32_t groups) {
+Team loss_team(uint32_t n, uint32_t rows, uint32_t groups) {
+  // A few short rows of each worker: the launch that would form the means costs more than going over them one after another
+  // (8 x 32 x 1000 fp32: 10.5 us a call, with a launch more 12.5; on the device 8.2 and 4.0 + 2.8 and a gap).
+  if (n <= 256 && rows <= 2 * kLossWaves && groups <= 256) return {kWorkerRows, 64, groups <= 64 ? 1u : groups <= 128 ? 2u : 4u};
   if (groups <= 64) {
     uint32_t lanes = 16;  // (as many as the two ends may have columns)
     while (lanes < groups) lanes *= 2;
-    return {true, lanes, 1};
+    return {kWaveRows, lanes, 1};
   }
-  if (groups <= 128) return {true, 64, 2};
+  if (groups <= 128) return {kWaveRows, 64, 2};
   const uint32_t each = groups <= 2048 ? 4 : groups <= 4096 ? 8 : groups <= 8192 ? 16 : groups <= 16384 ? 32 : 0;
-  return {false, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
+  return {kBlockRow, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
 }
 
 // STREAM: the gradient is written past the memory-side cache.  (A template parameter: between two stores that differ in
@@ -378,19 +409,25 @@ Team loss_team(uint32_t groups) {
 template <typename T, bool STREAM>
 void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
   constexpr uint64_t kMost = 1u << 21;  // workgroups: a dimension has room for 2^32 threads in all
-  const uint64_t together = t.wave ? kTeamThreads / t.lanes : 1, wanted = (k.total + together - 1) / together;
-  const dim3 grid(static_cast<uint32_t>(wanted < kMost ? wanted : kMost)), block(t.wave ? kTeamThreads : t.lanes);
-#define COMPAMS_LOSS(NG, WAVE) hipLaunchKernelGGL((k_loss<T, NG, WAVE, STREAM>), grid, block, 0, stream, k, t.lanes)
-  if (t.wave) {
-    if (t.each == 1) COMPAMS_LOSS(1, true);
-    else COMPAMS_LOSS(2, true);
+  const uint64_t together = t.kind == kWaveRows ? kTeamThreads / t.lanes : 1;
+  const uint64_t wanted = t.kind == kWorkerRows ? k.n : (k.total + together - 1) / together;
+  const dim3 grid(static_cast<uint32_t>(wanted < kMost ? wanted : kMost));
+  const dim3 block(t.kind == kWaveRows ? kTeamThreads : t.kind == kWorkerRows ? kLossThreads : t.lanes);
+#define COMPAMS_LOSS(NG, KIND) hipLaunchKernelGGL((k_loss<T, NG, KIND, STREAM>), grid, block, 0, stream, k, t.lanes)
+  if (t.kind == kWorkerRows) {
+    if (t.each == 1) COMPAMS_LOSS(1, kWorkerRows);
+    else if (t.each == 2) COMPAMS_LOSS(2, kWorkerRows);
+    else COMPAMS_LOSS(4, kWorkerRows);
+  } else if (t.kind == kWaveRows) {
+    if (t.each == 1) COMPAMS_LOSS(1, kWaveRows);
+    else COMPAMS_LOSS(2, kWaveRows);
   } else {
     switch (t.each) {
       case 0: hipLaunchKernelGGL((k_loss_wide<T, STREAM>), grid, dim3(kLossThreads), 0, stream, k); break;
-      case 4: COMPAMS_LOSS(4, false); break;
-      case 8: COMPAMS_LOSS(8, false); break;
-      case 16: COMPAMS_LOSS(16, false); break;
-      default: COMPAMS_LOSS(32, false); break;
+      case 4: COMPAMS_LOSS(4, kBlockRow); break;
+      case 8: COMPAMS_LOSS(8, kBlockRow); break;
+      case 16: COMPAMS_LOSS(16, kBlockRow); break;
+      default: COMPAMS_LOSS(32, kBlockRow); break;
     }
   }
 #undef COMPAMS_LOSS
@@ -452,7 +489,7 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream) {
              : a->mean_loss ? reinterpret_cast<float*>(static_cast<char*>(a->workspace) + counts_bytes(*a)) : nullptr;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const uint32_t each = 16 / static_cast<uint32_t>(type_size(a->type));
-  const Team team = loss_team((k.vocab + each - 1) / each);
+  const Team team = loss_team(k.n, k.rows, (k.vocab + each - 1) / each);
   if (!counts_inside(k, team)) {
     k.counts = static_cast<uint32_t*>(a->workspace);
     hipLaunchKernelGGL(k_loss_count, dim3(k.n), dim3(kLossThreads), 0, stream, k);
@@ -469,7 +506,7 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream) {
     else if (a->type == COMPAMS_F16) launch(half_t());
     else launch(bfloat_t());
   }
-  if (k.mean_loss) hipLaunchKernelGGL(k_loss_mean, dim3(k.n), dim3(kLossThreads), 0, stream, k);
+  if (k.mean_loss && (team.kind != kWorkerRows || k.total == 0)) hipLaunchKernelGGL(k_loss_mean, dim3(k.n), dim3(kLossThreads), 0, stream, k);
   return hipGetLastError() == hipSuccess ? COMPAMS_OK : COMPAMS_HIP_ERROR;
 }
 
