@@ -110,6 +110,28 @@ def test_join(cols, types):
         R.close(g, w, b, what)
 
 
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, F32)], ids=["f32", "bf16_f32"])
+@pytest.mark.parametrize("cols", [3, 7, 8, 24, 128, 512, 640, 900, 1024, 1280, 1700, 2000, 2048, 8192, 8193, 12288, 13000, 16400])
+def test_join_of_every_kind_of_team(cols, types):
+    test_join(cols, types)
+
+
+@pytest.mark.parametrize("n,rows,vocab", [(1, 32, 1000), (3, 32, 1000), (3, 33, 1000), (257, 4, 40), (2, 1, 2048), (5, 17, 500),
+                                          (4, 100, 300), (1, 3000, 64), (2, 400, 90)])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_cross_entropy_of_many_shapes(n, rows, vocab, dtype):
+    """Few and many rows to a worker, among them workers that learn from none."""
+    rng = np.random.default_rng(n * 100 + rows + vocab)
+    x, x64 = matrix(rng, n * rows, vocab, dtype, 3, 1, 2.0)
+    t = torch.from_numpy(rng.integers(0, vocab, n * rows))
+    t[torch.from_numpy(rng.random(n * rows) < 0.3)] = -100
+    t[(n - 1) * rows:] = -100
+    got = ops.compams_cross_entropy(x, t.cuda(), n)
+    want, bound = R.cross_entropy(x64, t, n, -100, 1.0, dtype)
+    for g, w, b, what in zip(got, want, bound, ("mean_loss", "losses", "dlogits")):
+        R.close(g, w, b, what)
+
+
 @pytest.mark.parametrize("n,rows", [(1, 1), (5, 1), (2, 2), (1, 31), (2, 63), (2, 64), (2, 65), (3, 129), (1, 1000), (16, 300),
                                     (1, 4097), (300, 3)])
 @pytest.mark.parametrize("cols", [24, 768, 2080])
