@@ -15,6 +15,8 @@ struct DropoutArgs {
 };
 constexpr uint32_t kThreads = 256;
 
+// Bound by memory, with the generator close behind: 20 products of 32 x 32 bits for eight columns (one row a lane, its place
+// formed for itself, 82 % of the vector unit's time).  49152 x 1024 bfloat16: 36.7 us, 5.5 TB/s; without arithmetic 35.5.
 constexpr uint32_t kRows = 4;  // rows that a lane takes, its columns in each
 
 // FULL: every lane has a whole group.  SAME: a wavefront's lanes are all in one row, whose number is a scalar then, and with

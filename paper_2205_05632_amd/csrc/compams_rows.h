@@ -45,17 +45,18 @@ __device__ __forceinline__ void move_down(Words& w, uint32_t by) {
   for (uint32_t i = 0; i < kWords; ++i) w[i] = by & S ? moved[i] : w[i];
 }
 
-// Columns c .. c + 7 of a row of `cols` >= 8 columns, in two steps.  The load is one wide one whatever c is, of the row's
-// last eight columns where the group would reach beyond them; rows may start at any multiple of the element's size
-// (unaligned accesses are the processor's).  settle() then moves such a group into its place, with 0 beyond the last
-// column: apart from the load, so that all of a row's loads are under way before the first one is waited for.  (With the
-// groups at a row's end read one by one and at once, a row of 1601 columns took a workgroup 2.3 us in the backward pass.)
 // What a kernel knows of its rows' width.
 enum Width {
   kAnyWidth = 0,   // at least eight columns
   kFullGroups = 1, // no lane has a group that reaches beyond the last column
   kOneGroup = 2    // fewer than eight columns: no wide load fits, and one lane has all of them
 };
+
+// Columns c .. c + 7 of a row of `cols` >= 8 columns, in two steps.  The load is one wide one whatever c is, of the row's
+// last eight columns where the group would reach beyond them; rows may start at any multiple of the element's size
+// (unaligned accesses are the processor's).  settle() then moves such a group into its place, with 0 beyond the last
+// column: apart from the load, so that all of a row's loads are under way before the first one is waited for.  (With the
+// groups at a row's end read one by one and at once, a row of 1601 columns took a workgroup 2.3 us in the backward pass.)
 template <Width WIDTH = kAnyWidth, typename T>
 __device__ __forceinline__ typename Group<T>::type load_early(const T* row, uint32_t c, uint32_t cols) {
   typename Group<T>::type raw;
@@ -136,7 +137,9 @@ __device__ __forceinline__ void store_group(T* row, uint32_t c, uint32_t cols, c
 // ---- The generator -------------------------------------------------------------------------------------------
 // Philox-4x32 with ten rounds (Salmon, Moraes, Dror, Shaw 2011): w -> (hi(M1 w2) ^ w1 ^ k0, lo(M1 w2), hi(M0 w0) ^ w3 ^ k1,
 // lo(M0 w0)), the key stepping by the golden ratio and by sqrt(3) - 1.
-__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+}
 __device__ __forceinline__ void philox(uint32_t (&w)[4], uint32_t k0, uint32_t k1) {
 #pragma unroll
   for (int turn = 0; turn < 10; ++turn) {

@@ -367,6 +367,25 @@ def test_cross_entropy_of_strange_rows(vocab, dtype):
     assert bool((got[2][9:11] == 0).all()) and bool(torch.isnan(got[2][7:9]).all())
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("vocab", [40, 1500, 20000, 140000])
+def test_cross_entropy_far_from_zero(vocab, dtype):
+    """Rows whose logits are a few steps of the type apart, at every magnitude that the type has."""
+    tops = [1e3, 3e4, -6e4] if dtype is F16 else [1e3, 1e6, 1e8, 1e9, 4e9, 1e10, 3e12, 1e20, 1e30, 3e38, -1e6, -1e9, -1e10, -1e25, -3e38]
+    rng = np.random.default_rng(vocab)
+    rows = len(tops)
+    v = torch.tensor(tops, dtype=torch.float64)[:, None].expand(rows, vocab).to(dtype).clone()
+    for _ in range(8):
+        down = torch.from_numpy(rng.random((rows, vocab)) < 0.5)
+        v = torch.where(down, torch.nextafter(v, torch.tensor(-math.inf, dtype=dtype)), v)
+    v = torch.where(torch.isfinite(v), v, torch.finfo(dtype).min)
+    t = torch.from_numpy(rng.integers(0, vocab, rows))
+    got = ops.compams_cross_entropy(v.cuda(), t.cuda(), 1, grad_scale=64.0)
+    want, bound = R.cross_entropy(v.double(), t, 1, -100, 64.0, dtype)
+    for g, w, b, what in zip(got, want, bound, ("mean_loss", "losses", "dlogits")):
+        R.close(g, w, b, what)
+
+
 def test_workers_without_tokens():
     x = torch.randn(6, 40, device="cuda")
     t = torch.tensor([1, 2, 7, 7, 7, 3], device="cuda")
