@@ -31,17 +31,34 @@ struct Max {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 
-// The rows of a worker that are learnt from, counted by the `lanes` lanes of a team (or of a wavefront of one).
-__device__ __forceinline__ uint32_t count_rows(const LossArgs& a, uint32_t w, uint32_t lane, uint32_t lanes) {
+// The rows of a worker that are learnt from, counted by the `lanes` lanes of a team (or of a wavefront of one), `AT_ONCE`
+// loads under way in each.
+template <uint32_t AT_ONCE, typename I>
+__device__ __forceinline__ uint32_t count_targets(const I* targets, uint32_t rows, int64_t ignore, uint32_t lane, uint32_t lanes) {
   uint32_t mine = 0;
-  for (uint32_t i = lane; i < a.rows; i += lanes) mine += target_of(a, w * a.rows + i) != a.ignore;
+  for (uint32_t first = lane; first < rows; first += lanes * AT_ONCE) {
+    I t[AT_ONCE];
+#pragma unroll
+    for (uint32_t k = 0; k < AT_ONCE; ++k) {  // (beyond the last row: that one, left out below)
+      const uint32_t i = first + k * lanes;
+      t[k] = targets[i < rows ? i : rows - 1];
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < AT_ONCE; ++k) mine += first + k * lanes < rows && t[k] != ignore;
+  }
   return mine;
+}
+template <uint32_t AT_ONCE>
+__device__ __forceinline__ uint32_t count_rows(const LossArgs& a, uint32_t w, uint32_t lane, uint32_t lanes) {
+  const size_t from = static_cast<size_t>(w) * a.rows;
+  return a.wide_targets ? count_targets<AT_ONCE>(static_cast<const int64_t*>(a.targets) + from, a.rows, a.ignore, lane, lanes)
+                        : count_targets<AT_ONCE>(static_cast<const int32_t*>(a.targets) + from, a.rows, a.ignore, lane, lanes);
 }
 
 __global__ __launch_bounds__(kLossThreads) void k_loss_count(LossArgs a) {
   __shared__ float slots[1][kSlots];
   for (uint32_t w = blockIdx.x; w < a.n; w += gridDim.x) {
-    const uint32_t mine = count_rows(a, w, threadIdx.x, kLossThreads);
+    const uint32_t mine = count_rows<8>(a, w, threadIdx.x, kLossThreads);
     // two halves, each exact in fp32 (a worker has fewer than 2^31 rows, a lane at most 2^21 of them)
     __syncthreads();
     float s[1] = {static_cast<float>(mine & 0xfffu)};
@@ -112,7 +129,7 @@ __global__ __launch_bounds__(KIND == kWaveRows ? kTeamThreads : KIND == kBlockRo
   uint32_t turn = 0;
   float of_worker[2] = {0.0f, 0.0f};  // kWorkerRows: losses, and rows that are learnt from
   if constexpr (KIND == kWorkerRows) {
-    float c[1] = {static_cast<float>(count_rows(a, blockIdx.x, threadIdx.x, kLossThreads))};
+    float c[1] = {static_cast<float>(count_rows<1>(a, blockIdx.x, threadIdx.x, kLossThreads))};
     sum_block(c, slots[0], kLossWaves);
     of_worker[1] = c[0];
   }
@@ -147,7 +164,7 @@ __global__ __launch_bounds__(KIND == kWaveRows ? kTeamThreads : KIND == kBlockRo
     const float at_end = end < a.vocab ? to_float(logits[end]) : -INFINITY;
     const uint32_t w = r / a.rows;
     // (less than 2^24 of them: exact in fp32; a.counts is there where there may be more)
-    const float count = a.counts || KIND == kWorkerRows ? 0.0f : static_cast<float>(count_rows(a, w, lane, lanes));
+    const float count = a.counts || KIND == kWorkerRows ? 0.0f : static_cast<float>(count_rows<4>(a, w, lane, lanes));
     const bool inside = target >= 0 && target < static_cast<int64_t>(a.vocab);
     float of_target = inside ? to_float(logits[target]) : 0.0f;
     float top = at_end;
@@ -353,8 +370,18 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_mean(LossArgs a) {
   __shared__ float slots[2][2][kSlots];
   uint32_t turn = 0;
   for (uint32_t w = blockIdx.x; w < a.n; w += gridDim.x, turn ^= 1) {
-    float s[2] = {0.0f, a.counts ? 0.0f : static_cast<float>(count_rows(a, w, threadIdx.x, kLossThreads))};
-    for (uint32_t i = threadIdx.x; i < a.rows; i += kLossThreads) s[0] += a.losses[static_cast<size_t>(w) * a.rows + i];
+    float s[2] = {0.0f, a.counts ? 0.0f : static_cast<float>(count_rows<8>(a, w, threadIdx.x, kLossThreads))};
+    const float* const losses = a.losses + static_cast<size_t>(w) * a.rows;
+    for (uint32_t first = threadIdx.x; first < a.rows; first += kLossThreads * 8) {
+      float l[8];
+#pragma unroll
+      for (uint32_t k = 0; k < 8; ++k) {  // (eight loads under way in each lane)
+        const uint32_t i = first + k * kLossThreads;
+        l[k] = losses[i < a.rows ? i : a.rows - 1];
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < 8; ++k) s[0] += first + k * kLossThreads < a.rows ? l[k] : 0.0f;
+    }
     sum_block(s, slots[turn], kLossWaves);
     if (a.counts) s[1] = static_cast<float>(a.counts[w]);
     if (threadIdx.x == 0) a.mean_loss[w] = s[1] > 0.0f ? s[0] / s[1] : 0.0f;
@@ -375,12 +402,16 @@ Team loss_team(uint32_t n, uint32_t rows, uint32_t groups) {
   // A few short rows of each worker: the launch that would form the means costs more than going over them one after another
   // (8 x 32 x 1000 fp32: 10.5 us a call, with a launch more 12.5; on the device 8.2 and 4.0 + 2.8 and a gap).
   if (n <= 256 && rows <= 2 * kLossWaves && groups <= 256) return {kWorkerRows, 64, groups <= 64 ? 1u : groups <= 128 ? 2u : 4u};
-  if (groups <= 64) {
-    uint32_t lanes = 16;  // (as many as the two ends may have columns)
-    while (lanes < groups) lanes *= 2;
-    return {kWaveRows, lanes, 1};
+  // Short rows: few lanes with up to four groups, so that what a row costs besides its columns (its reductions, logarithm and
+  // quotients) is shared by the rows of a wavefront.  (16 x 9882 rows of float16, us on the device and the two small launches:
+  // 133 columns 32 x 1 52.3, 16 x 2 43.6, 16 x 4 55.4; 260 columns 64 x 1 92.5, 32 x 2 75.3, 16 x 4 63.0, 16 x 8 90.0;
+  // 512 columns 64 x 1 99.7, 32 x 2 85.3, 16 x 4 73.3; 8 x 9882 x 1000: 64 x 2 81.8, 32 x 4 73.7, 16 x 8 86.0.)
+  if (groups <= 256) {
+    uint32_t lanes = 16, each = 1;  // (as many lanes as the two ends may have columns)
+    while (each < 4 && lanes * each < groups) each *= 2;
+    while (lanes * each < groups) lanes *= 2;
+    return {kWaveRows, lanes, each};
   }
-  if (groups <= 128) return {kWaveRows, 64, 2};
   const uint32_t each = groups <= 2048 ? 4 : groups <= 4096 ? 8 : groups <= 8192 ? 16 : groups <= 16384 ? 32 : 0;
   return {kBlockRow, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
 }
@@ -401,7 +432,8 @@ void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
     else COMPAMS_LOSS(4, kWorkerRows);
   } else if (t.kind == kWaveRows) {
     if (t.each == 1) COMPAMS_LOSS(1, kWaveRows);
-    else COMPAMS_LOSS(2, kWaveRows);
+    else if (t.each == 2) COMPAMS_LOSS(2, kWaveRows);
+    else COMPAMS_LOSS(4, kWaveRows);
   } else {
     switch (t.each) {
       case 0: hipLaunchKernelGGL((k_loss_wide<T, STREAM>), grid, dim3(kLossThreads), 0, stream, k); break;
