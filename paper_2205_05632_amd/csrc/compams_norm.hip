@@ -105,10 +105,14 @@ extern "C" {
 
 size_t compams_norm_workspace_size(const compams_norm* a) {
   if (!compams::norm_valid(a, false)) return 0;
-  // (for either of the two calls: a join's cut is the one that takes more)
-  const compams::Cut c = compams::norm_cut(static_cast<uint32_t>(a->n), static_cast<uint32_t>(a->rows),
-                                           static_cast<uint32_t>(a->cols), true, compams::any_gradient(*a));
-  return c.sums_bytes + c.partial_bytes;
+  // (for either of the two calls)
+  size_t most = 0;
+  for (const bool join : {false, true}) {
+    const compams::Cut c = compams::norm_cut(static_cast<uint32_t>(a->n), static_cast<uint32_t>(a->rows),
+                                             static_cast<uint32_t>(a->cols), join, compams::any_gradient(*a));
+    if (c.sums_bytes + c.partial_bytes > most) most = c.sums_bytes + c.partial_bytes;
+  }
+  return most;
 }
 int compams_layer_norm_forward(const compams_norm* a, void* hip_stream) {
   return compams::forward(a, false, static_cast<hipStream_t>(hip_stream));

@@ -299,11 +299,12 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_backward_wide(NormArgs a)
 }
 
 // ---- What both take ------------------------------------------------------------------------------------------------
-// The parts' sums added up in their order: 64 columns to a workgroup, a sixteenth of the parts to each wavefront.
+// The parts' sums added up in their order: 64 columns to a workgroup, a sixteenth of the parts to each wavefront.  (Where there
+// are fewer than sixteen, as many wavefronts; 8 x 24 x 9062, three parts: 35.8 us a call, with sixteen 43.4.)
 constexpr uint32_t kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
 __global__ __launch_bounds__(kJoinThreads) void k_norm_join_parts(NormArgs a) {
   __shared__ float tile[kJoinWaves][64];
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, which = blockIdx.y, w = blockIdx.z;
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, waves = blockDim.x / 64, which = blockIdx.y, w = blockIdx.z;
   if (!a.grad[which]) return;
   const uint32_t tiles = (a.cols + 63) / 64;
   for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_norm_join_parts(NormArgs a) {
     if (c < a.cols) {
       const float* const p = a.partial + (static_cast<size_t>(w) * a.parts * kGradients + which) * a.cols + c;
       const size_t step = static_cast<size_t>(kGradients) * a.cols;
-      const uint32_t share = (a.parts + kJoinWaves - 1) / kJoinWaves, from = wave * share;
+      const uint32_t share = (a.parts + waves - 1) / waves, from = wave * share;
       const uint32_t to = from + share < a.parts ? from + share : a.parts;
 #pragma unroll 8
       for (uint32_t i = from; i < to; ++i) s += p[i * step];
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_norm_join_parts(NormArgs a) {
     __syncthreads();
     if (wave == 0 && c < a.cols) {
       s = 0.0f;
-      for (uint32_t i = 0; i < kJoinWaves; ++i) s += tile[i][lane];
+      for (uint32_t i = 0; i < waves; ++i) s += tile[i][lane];
       float* const out = a.grad[which] + static_cast<int64_t>(w) * a.ld_grad[which] + c;
       *out = a.accumulate ? *out + s : s;
     }
@@ -393,15 +394,18 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 //   1 x 1024:  8 15.0 / 16.3,  16 14.9 / 16.5,  32 17.4 / 23.9      8 x 1024: 8 17.3, 16 17.8, 32 21.7 (norm)
 //   1 x 8192: 16 18.4 / 27.2,  32 21.7 / 33.8,  64 33.2 / 53.0      8 x 8192: 16 168, 32 166, 64 161 (join)
 // (5 x 211 x 1111, norm: 4 15.4, 8 15.4; 3 x 401 x 1601, join: 4 17.9, 8 17.4, 16 22.9; 8 x 256 x 12000, join: 8 109, 16 122;
-// 8 x 2048 x 4096, join: 8 234, 16 227, 32 232).
+// 8 x 2048 x 4096, join: 8 234, 16 227, 32 232.)  Short rows are cheap and their teams many: two turns for each (join, 8 x 6167
+// x 173, 8 teams: 8 41.7, 16 32.7; 8 x 13028 x 68, 16 teams: 16 41.9, 32 31.4; 1 x 6167 x 256: 8 16.9, 16 17.0).  A few rows
+// of a workgroup each take a compute unit 2 to 4 us apiece (join, 8 x 24 x 9062: 4 27.4, 8 35.9; 5 x 61 x 7431: 4 28.2, 8 34.6;
+// 8 x 128 x 6000: 4 30.1, 8 31.6; beyond that the sums weigh more: 8 x 256 x 12000 4 91.8, 8 82.6).
 Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool join, bool gradients) {
   Cut c = {};
   if (rows == 0) return c;
-  c.part_rows = 8;
-  while (c.part_rows < 64 && c.part_rows * 2 <= rows / 512) c.part_rows *= 2;
   const Team team = team_of(cols, join);
   const uint32_t together = team.each ? team_threads(team) / team.lanes : 1;
-  if (c.part_rows < together) c.part_rows = together;
+  c.part_rows = team.each && team.kind == kBlock && rows <= 128 ? 4 : 8;
+  while (c.part_rows < 64 && c.part_rows * 2 <= rows / 512) c.part_rows *= 2;
+  if (team.kind == kInWave && team.lanes < 64 && c.part_rows < 2 * together) c.part_rows = 2 * together;
   if (rows <= 4 * together) c.part_rows = rows;  // a few turns, and no launch to join (8 x 16 x 1000 15.8 -> 11.1 us)
   c.parts = (rows + c.part_rows - 1) / c.part_rows;
   if (team.each == 0) c.sums_bytes = up256(static_cast<size_t>(n) * rows * sizeof(float2));
@@ -437,7 +441,7 @@ hipError_t norm_backward(const NormArgs& k, int32_t type, int32_t stream_type, h
     }
     if (gradients && k.parts > 1)
       hipLaunchKernelGGL(k_norm_join_parts, dim3(at_most((k.cols + 63) / 64, 4096), kGradients, k.n),
-                         dim3(kJoinThreads), 0, stream, k);
+                         dim3(64 * at_most(k.parts, kJoinWaves)), 0, stream, k);
     return hipGetLastError();
   });
 }
