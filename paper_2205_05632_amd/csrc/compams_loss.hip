@@ -446,10 +446,13 @@ void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
 #undef COMPAMS_LOSS
 }
 
-// Whether every row's team counts its worker's targets by itself: where they are few bytes beside the row's logits.  (They
-// are then counted in fp32, exactly: fewer than 2^24.)
+// Whether every row's team counts its worker's targets by itself: where they are few bytes beside the row's logits, or few in
+// all, and the launch that would count them costs more (float16 and bfloat16, us a call with it / without: 8 x 105 x 83 16.5 /
+// 14.2, 8 x 256 x 512 17.1 / 14.3, 16 x 512 x 1000 16.7 / 15.5; 16 x 1024 x 1000 22.3 / 25.3).  (They are then counted in
+// fp32, exactly: fewer than 2^24.)
 bool counts_inside(const LossArgs& k, const Team& t) {
-  return t.each != 0 && (k.rows <= 64 || k.rows <= k.vocab / 4) && k.rows < (1u << 24);
+  const bool few = k.rows <= 512 && static_cast<uint64_t>(k.total) * k.rows <= 1u << 22;
+  return t.each != 0 && (few || k.rows <= k.vocab / 4) && k.rows < (1u << 24);
 }
 
 bool loss_valid(const compams_loss* a) {
