@@ -340,6 +340,7 @@ __global__ __launch_bounds__(256) void k_norm_no_rows(NormArgs a) {
 
 // The team that a row of `groups` groups is given; us, norm / join, bfloat16 and a stream in fp32:
 //   8 x 2048 x  640: pair of 96 27.3 / 43.4, 32 x 3 30.0 / 47.5       8 x 8192 x 768: join, 32 x 3 (229 registers) 158, pair 161
+//   8 x 3117 x 1280, float16: pair of 160 51.5 / 100, 192 53.4 / 81.6; x 1600: pair of 224 66.1 / 108, 256 63.7 / 103
 //   8 x 2048 x 1024: 64 x 2 41.2 / 60.6, 128 41.1 / 60.5, in parts of 32 rows 42.3 / 62.7 and 49.6 / 62.5
 Team backward_team(uint32_t groups, bool join) {
   if (groups <= 64) {
@@ -348,7 +349,8 @@ Team backward_team(uint32_t groups, bool join) {
     return {kInWave, lanes, 1};
   }
   const uint32_t halves = (groups + 31) / 32;
-  if (halves == 3 || halves == 5 || halves == 7) return {kPair, halves * 32, 1};
+  // (a join's four wavefronts to a SIMD seldom hold three workgroups of five: a row of 3 wavefronts instead of two of 5)
+  if (halves == 3 || (!join && (halves == 5 || halves == 7))) return {kPair, halves * 32, 1};
   if (groups <= 128) return {kInWave, 64, 2};
   // (two groups a lane take a join 168 registers: twelve wavefronts at most)
   const uint32_t each = groups <= 1024 ? 1 : groups <= (join ? 1536 : 2048) ? 2 : 0;
