@@ -342,8 +342,10 @@ __global__ __launch_bounds__(256) void k_norm_no_rows(NormArgs a) {
 //   8 x 2048 x  640: pair of 96 27.3 / 43.4, 32 x 3 30.0 / 47.5       8 x 8192 x 768: join, 32 x 3 (229 registers) 158, pair 161
 //   8 x 3117 x 1280, float16: pair of 160 51.5 / 100, 192 53.4 / 81.6; x 1600: pair of 224 66.1 / 108, 256 63.7 / 103
 //   8 x 2048 x 1024: 64 x 2 41.2 / 60.6, 128 41.1 / 60.5, in parts of 32 rows 42.3 / 62.7 and 49.6 / 62.5
+//   8 x 6167 x  512: 64 58.5 / 88.1, all float16 40.2 / 60.8; 32 x 2 55.9 / 84.7 and 38.8 / 57.9
 Team backward_team(uint32_t groups, bool join) {
-  if (groups <= 64) {
+  if (groups > 48 && groups <= 64) return {kInWave, 32, 2};
+  if (groups <= 48) {
     uint32_t lanes = 8;
     while (lanes < groups) lanes *= 2;
     return {kInWave, lanes, 1};
