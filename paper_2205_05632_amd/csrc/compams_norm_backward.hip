@@ -343,7 +343,7 @@ __global__ __launch_bounds__(256) void k_norm_no_rows(NormArgs a) {
 //   8 x 3117 x 1280, float16: pair of 160 51.5 / 100, 192 53.4 / 81.6; x 1600: pair of 224 66.1 / 108, 256 63.7 / 103
 //   8 x 2048 x 1024: 64 x 2 41.2 / 60.6, 128 41.1 / 60.5, in parts of 32 rows 42.3 / 62.7 and 49.6 / 62.5
 //   8 x 6167 x  512: 64 58.5 / 88.1, all float16 40.2 / 60.8; 32 x 2 55.9 / 84.7 and 38.8 / 57.9
-Team backward_team(uint32_t groups, bool join) {
+Team backward_team(uint32_t rows, uint32_t groups, bool join) {
   if (groups > 48 && groups <= 64) return {kInWave, 32, 2};
   if (groups <= 48) {
     uint32_t lanes = 8;
@@ -351,8 +351,9 @@ Team backward_team(uint32_t groups, bool join) {
     return {kInWave, lanes, 1};
   }
   const uint32_t halves = (groups + 31) / 32;
-  // (a join's four wavefronts to a SIMD seldom hold three workgroups of five: a row of 3 wavefronts instead of two of 5)
-  if (halves == 3 || (!join && (halves == 5 || halves == 7))) return {kPair, halves * 32, 1};
+  // (a join's four wavefronts to a SIMD seldom hold three workgroups of five: a row of three wavefronts instead of two of five,
+  // but where a worker has few rows: 8 x 400 x 1280 pair 18.5, 192 22.1; 3 x 401 x 1601 17.4 and 21.2; 8 x 1000 x 1280 41.9 and 33.3)
+  if (halves == 3 || ((!join || rows <= 512) && (halves == 5 || halves == 7))) return {kPair, halves * 32, 1};
   if (groups <= 128) return {kInWave, 64, 2};
   // (two groups a lane take a join 168 registers: twelve wavefronts at most)
   const uint32_t each = groups <= 1024 ? 1 : groups <= (join ? 1536 : 2048) ? 2 : 0;
@@ -386,7 +387,7 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
 #undef COMPAMS_BACKWARD_OF
 }
 
-Team team_of(uint32_t cols, bool join) { return backward_team((cols + kGroup - 1) / kGroup, join); }
+Team team_of(uint32_t rows, uint32_t cols, bool join) { return backward_team(rows, (cols + kGroup - 1) / kGroup, join); }
 
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -405,7 +406,7 @@ inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 Cut norm_cut(uint32_t n, uint32_t rows, uint32_t cols, bool join, bool gradients) {
   Cut c = {};
   if (rows == 0) return c;
-  const Team team = team_of(cols, join);
+  const Team team = team_of(rows, cols, join);
   const uint32_t together = team.each ? team_threads(team) / team.lanes : 1;
   c.part_rows = team.each && team.kind == kBlock && rows <= 128 ? 4 : 8;
   while (c.part_rows < 64 && c.part_rows * 2 <= rows / 512) c.part_rows *= 2;
@@ -425,7 +426,7 @@ hipError_t norm_backward(const NormArgs& k, int32_t type, int32_t stream_type, h
     hipLaunchKernelGGL(k_norm_no_rows, dim3(at_most((k.cols + 255) / 256, 4096), kGradients, k.n), dim3(256), 0, stream, k);
     return hipGetLastError();
   }
-  const Team team = team_of(k.cols, k.join);
+  const Team team = team_of(k.rows, k.cols, k.join);
   return by_types(type, stream_type, [&](auto t, auto h) {
     using T = decltype(t);
     using H = decltype(h);
