@@ -394,6 +394,8 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_mean(LossArgs a) {
 //   vocabulary  4096: 256 x 2 32.5, 128 x 4 30.3, 64 x 8 31.9      8192: 256 x 4 56.8, 128 x 8 58.3, 64 x 16 58.8
 //              16384: 1024 x 2 152, 512 x 4 97, 256 x 8 101, 128 x 16 110      32000: 512 x 8 182, 256 x 16 193
 //              50257: 832 x 8 400, 448 x 16 312, 256 x 32 311, 320 x 20 467 (waves that do not go evenly into four)
+// and 2048 rows of  40000: 448 x 12 66.9, 320 x 16 77.6; 1078 rows of 67875: 448 x 20 89, 320 x 32 114; of 80387: 512 x 20 96,
+// 320 x 32 120; of 98000: 512 x 24 113, 384 x 32 130; of 33000 fp32: 448 x 20 68.9, 320 x 32 78.4.
 struct Team {
   RowKind kind;
   uint32_t lanes, each;
@@ -412,7 +414,9 @@ Team loss_team(uint32_t n, uint32_t rows, uint32_t groups) {
     while (lanes * each < groups) lanes *= 2;
     return {kWaveRows, lanes, each};
   }
-  const uint32_t each = groups <= 2048 ? 4 : groups <= 4096 ? 8 : groups <= 8192 ? 16 : groups <= 16384 ? 32 : 0;
+  uint32_t each = 0;
+  for (const uint32_t k : {4u, 8u, 12u, 16u, 20u, 24u, 32u})
+    if (each == 0 && groups <= k * kRowThreads) each = k;
   return {kBlockRow, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
 }
 
@@ -439,7 +443,10 @@ void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
       case 0: hipLaunchKernelGGL((k_loss_wide<T, STREAM>), grid, dim3(kLossThreads), 0, stream, k); break;
       case 4: COMPAMS_LOSS(4, kBlockRow); break;
       case 8: COMPAMS_LOSS(8, kBlockRow); break;
+      case 12: COMPAMS_LOSS(12, kBlockRow); break;
       case 16: COMPAMS_LOSS(16, kBlockRow); break;
+      case 20: COMPAMS_LOSS(20, kBlockRow); break;
+      case 24: COMPAMS_LOSS(24, kBlockRow); break;
       default: COMPAMS_LOSS(32, kBlockRow); break;
     }
   }
