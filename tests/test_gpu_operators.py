@@ -554,3 +554,34 @@ def test_refusals():
                  lambda: ops.compams_cross_entropy(x, t, gradient=False, dlogits=x)):
         with pytest.raises((ValueError, B.CompamsError)):
             call()
+
+
+@pytest.mark.parametrize("types", [(F16, F16), (BF16, F32)], ids=["f16", "bf16_f32"])
+@pytest.mark.parametrize("cols", [68, 72, 173, 200, 300, 321, 330, 384, 385, 450, 512, 2304, 2500, 2900, 3008, 5400, 6144, 7169,
+                                  10484, 16384, 20479, 20480])
+def test_layer_norm_of_every_kind_of_team(cols, types):
+    test_layer_norm(cols, types)
+
+
+@pytest.mark.parametrize("types", [(F16, F16), (BF16, F32)], ids=["f16", "bf16_f32"])
+@pytest.mark.parametrize("cols", [68, 173, 200, 300, 321, 330, 384, 450, 512, 1111, 1280, 1792, 2304, 2900, 7169, 16384, 20480])
+def test_join_between_the_teams_widths(cols, types):
+    test_join(cols, types)
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 513, 1111), (2, 600, 1280), (2, 512, 1600), (2, 513, 1792), (3, 128, 2500), (3, 129, 2500),
+                                         (2, 40, 200), (2, 200, 68), (2, 70, 512), (2, 9, 8300), (2, 3, 4100), (1, 5, 9000)])
+def test_sums_of_parts_of_every_size(n, rows, cols):
+    test_sums_over_any_number_of_rows(n, rows, cols)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("vocab", [64, 65, 127, 129, 250, 260, 385, 500, 1030, 2047, 2050, 33000, 40007, 49160, 70001, 81930, 98304])
+def test_cross_entropy_of_every_kind_of_team(vocab, dtype):
+    test_cross_entropy(vocab, dtype)
+
+
+@pytest.mark.parametrize("n,rows,vocab", [(2, 512, 90), (2, 513, 90), (1, 1100, 260), (3, 8200, 24), (9, 700, 130), (1, 530, 2200)])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_cross_entropy_of_many_rows(n, rows, vocab, dtype):
+    test_cross_entropy_of_many_shapes(n, rows, vocab, dtype)
