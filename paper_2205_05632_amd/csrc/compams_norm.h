@@ -49,7 +49,7 @@ __device__ __forceinline__ void load_weight(float (&v)[kGroup], const float* w, 
 // The same in two steps (see load_early).
 template <Width WIDTH = kAnyWidth>
 __device__ __forceinline__ Group<float>::type load_weight_early(const float* w, uint32_t c, uint32_t cols, float absent) {
-  if (WIDTH == kFullGroups || w) return load_early<WIDTH>(w, c, cols);
+  if (WIDTH == kFullGroups || WIDTH == kWholeGroups || w) return load_early<WIDTH>(w, c, cols);
   Group<float>::type raw;
 #pragma unroll
   for (uint32_t j = 0; j < kGroup; ++j) raw[j] = absent;

@@ -56,7 +56,7 @@ __device__ __forceinline__ void sum_teams(float (&v)[NG][kGroup], uint32_t lanes
 template <typename T, typename H, uint32_t NG, TeamKind KIND, bool JOIN, Width WIDTH>
 __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 && JOIN ? 768 : 1024) void k_norm_backward(NormArgs a,
                                                                                                           uint32_t lanes) {
-  constexpr bool FULL = WIDTH == kFullGroups;  // and nothing is left out of the call
+  constexpr bool FULL = WIDTH == kFullGroups || WIDTH == kWholeGroups;  // nothing is left out of the call
   constexpr uint32_t kOf = JOIN ? 3 : 2;
   __shared__ float slots[2][2][kSlots];
   extern __shared__ float tile[];  // a row of columns for each wavefront (kInWave), or one (kPair)
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 && JOIN ? 
 #pragma unroll
             for (uint32_t j = 0; j < kGroup; ++j) {
               const uint32_t c = (k * lanes + lane) * kGroup + j;
-              if (FULL || c < a.cols) emit_gradient(a, w, part, which, c, sum[which][k][j]);
+              if (WIDTH == kFullGroups || c < a.cols) emit_gradient(a, w, part, which, c, sum[which][k][j]);
             }
         }
       }
@@ -364,13 +364,14 @@ template <typename T, typename H, bool JOIN>
 void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
   const dim3 grid(blocks_for(static_cast<uint64_t>(k.n) * k.parts)), block(team_threads(t));
   const size_t lds = (t.kind == kInWave ? kTeamThreads / 64 : t.kind == kPair ? 1 : 0) * t.each * t.lanes * kGroup * sizeof(float);
-  const bool full = k.cols == t.lanes * t.each * kGroup && k.gamma && k.dresidual && k.grad[0] && k.grad[1] &&
-                    (!JOIN || (k.dh && k.dx && k.grad[2]));
+  const bool all = k.gamma && k.dresidual && k.grad[0] && k.grad[1] && (!JOIN || (k.dh && k.dx && k.grad[2]));
+  const bool full = all && k.cols == t.lanes * t.each * kGroup, whole = all && k.cols % kGroup == 0;
 #define COMPAMS_BACKWARD_OF(NG, KIND, WIDTH) \
   hipLaunchKernelGGL((k_norm_backward<T, H, NG, KIND, JOIN, WIDTH>), grid, block, lds, stream, k, t.lanes)
 #define COMPAMS_BACKWARD(NG, KIND)                         \
   do {                                                     \
     if (full) COMPAMS_BACKWARD_OF(NG, KIND, kFullGroups);  \
+    else if (whole) COMPAMS_BACKWARD_OF(NG, KIND, kWholeGroups); \
     else COMPAMS_BACKWARD_OF(NG, KIND, kAnyWidth);         \
   } while (0)
   if (t.kind == kInWave) {

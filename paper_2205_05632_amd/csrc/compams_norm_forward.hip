@@ -14,7 +14,7 @@ namespace {
 // usual calls, without a test of any of it for every group (a join of rows of 768: 177 vector instructions a group for 494).
 template <typename T, typename H, uint32_t NG, TeamKind KIND, bool JOIN, Width WIDTH>
 __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_forward(NormArgs a, uint32_t lanes) {
-  constexpr bool FULL = WIDTH == kFullGroups;  // and nothing is left out of the call
+  constexpr bool FULL = WIDTH == kFullGroups || WIDTH == kWholeGroups;  // nothing is left out of the call
   __shared__ float slots[2][1][kSlots];
   const uint32_t team = team_of_lane<KIND>(lanes), lane = lane_of_team<KIND>(lanes, team);
   const uint32_t together = teams_together<KIND>(lanes);
@@ -90,10 +90,10 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
       const uint32_t c = (k * lanes + lane) * kGroup;
-      if (FULL || c + kGroup <= a.cols) {
+      if (WIDTH == kFullGroups || c + kGroup <= a.cols) {
 #pragma unroll
         for (uint32_t j = 0; j < kGroup; ++j) s[0] = fmaf(v[k][j] - mean, v[k][j] - mean, s[0]);
-      } else {
+      } else if constexpr (WIDTH != kWholeGroups) {
         uint32_t left = a.cols - c;  // (wraps around where no column is left: negative below)
         forget(left);
 #pragma unroll
@@ -110,8 +110,10 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_
     for (uint32_t k = 0; k < NG; ++k) {
       const uint32_t c = (k * lanes + lane) * kGroup;
       if (JOIN && (FULL || a.h)) store_group<H, WIDTH>(row_of<H>(a.h, a.ld_h, r), c, a.cols, v[k]);
-      settle_if<WIDTH, float>(g[k], c, a.cols);
-      settle_if<WIDTH, float>(b[k], c, a.cols);
+      if constexpr (WIDTH != kWholeGroups) {  // (lanes without a group store none)
+        settle_if<WIDTH, float>(g[k], c, a.cols);
+        settle_if<WIDTH, float>(b[k], c, a.cols);
+      }
 #pragma unroll
       for (uint32_t j = 0; j < kGroup; ++j) v[k][j] = fmaf((v[k][j] - mean) * rstd, g[k][j], b[k][j]);
       store_group<T, WIDTH>(row_of<T>(a.y, a.ld_y, r), c, a.cols, v[k]);
@@ -207,13 +209,14 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
   const uint32_t threads = team_threads(t), together = threads / t.lanes;
   const dim3 grid(blocks_for((static_cast<uint64_t>(k.total) + together - 1) / together));
   const dim3 block(threads);
-  const bool full = k.cols == t.lanes * t.each * kGroup && k.gamma && k.beta && k.mean && k.rstd &&
-                    (!JOIN || (k.bias && k.residual && k.h));
+  const bool all = k.gamma && k.beta && k.mean && k.rstd && (!JOIN || (k.bias && k.residual && k.h));
+  const bool full = all && k.cols == t.lanes * t.each * kGroup, whole = all && k.cols % kGroup == 0;
 #define COMPAMS_FORWARD_OF(NG, KIND, WIDTH) \
   hipLaunchKernelGGL((k_norm_forward<T, H, NG, KIND, JOIN, WIDTH>), grid, block, 0, stream, k, t.lanes)
 #define COMPAMS_FORWARD(NG, KIND)                           \
   do {                                                      \
     if (full) COMPAMS_FORWARD_OF(NG, KIND, kFullGroups);    \
+    else if (whole) COMPAMS_FORWARD_OF(NG, KIND, kWholeGroups); \
     else COMPAMS_FORWARD_OF(NG, KIND, kAnyWidth);           \
   } while (0)
   if (t.kind == kInWave) {

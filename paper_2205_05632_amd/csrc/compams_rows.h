@@ -49,7 +49,8 @@ __device__ __forceinline__ void move_down(Words& w, uint32_t by) {
 enum Width {
   kAnyWidth = 0,   // at least eight columns
   kFullGroups = 1, // no lane has a group that reaches beyond the last column
-  kOneGroup = 2    // fewer than eight columns: no wide load fits, and one lane has all of them
+  kOneGroup = 2,   // fewer than eight columns: no wide load fits, and one lane has all of them
+  kWholeGroups = 3 // a multiple of eight columns: lanes have a group of the row or, beyond its last, none
 };
 
 // Columns c .. c + 7 of a row of `cols` >= 8 columns, in two steps.  The load is one wide one whatever c is, of the row's
@@ -86,6 +87,14 @@ __device__ __forceinline__ void settle(typename Group<T>::type& raw, uint32_t c,
 template <Width WIDTH, typename T>
 __device__ __forceinline__ void settle_if(typename Group<T>::type& raw, uint32_t c, uint32_t cols) {
   if constexpr (WIDTH == kAnyWidth) settle<T>(raw, c, cols);
+  if constexpr (WIDTH == kWholeGroups) {
+    typedef uint32_t Words __attribute__((ext_vector_type(kGroup * sizeof(T) / 4)));
+    Words w;
+    __builtin_memcpy(&w, &raw, sizeof(w));
+#pragma unroll
+    for (uint32_t i = 0; i < kGroup * sizeof(T) / 4; ++i) w[i] = c < cols ? w[i] : 0u;
+    __builtin_memcpy(&raw, &w, sizeof(w));
+  }
 }
 // The same in one, for rows of any width.
 template <typename T>
@@ -112,12 +121,12 @@ __device__ __forceinline__ void load_group(float (&v)[kGroup], const T* row, uin
 // Each value rounded to T once, to the nearest.
 template <typename T, Width WIDTH = kAnyWidth>
 __device__ __forceinline__ void store_group(T* row, uint32_t c, uint32_t cols, const float (&v)[kGroup]) {
-  if (WIDTH == kFullGroups || c + kGroup <= cols) {
+  if (WIDTH == kFullGroups || (WIDTH == kWholeGroups ? c < cols : c + kGroup <= cols)) {
     typename Group<T>::type raw;
 #pragma unroll
     for (uint32_t j = 0; j < kGroup; ++j) raw[j] = static_cast<T>(v[j]);
     __builtin_memcpy(row + c, &raw, sizeof(raw));
-  } else if (c < cols) {  // as four, two and one
+  } else if (WIDTH != kWholeGroups && c < cols) {  // as four, two and one
     uint32_t left = cols - c;
     forget(left);
     typedef uint32_t Words __attribute__((ext_vector_type(kGroup * sizeof(T) / 4)));
