@@ -174,17 +174,19 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) 
 // 8 x 4096 rows (65536 of 768) from bfloat16 and a stream in fp32
 //    768: 32 x 3 53.8 / 115, pair of 96 53.8 / 120, 128 56 / 127        1000: 64 x 2 37.7 / 80, 128 37.8 / 86
 //   1280: pair of 160 46 / 105, 64 x 3 49 / 124                         2048: 256 76 / 168, 64 x 4 79 / 151
-//   1601 (bfloat16 stream): pair of 224 57 / 126, 256 61 / 117
+//   1601 (bfloat16 stream): pair of 224 57 / 126, 256 61 / 117          8 x 3117 x 1600: pair of 224 46.6 / 101, 256 47.0 / 107
 // 8 x 6167 rows (13028 of 68, 2048 of 2304 and 2900, 1000 of 6144 and 7168), all float16 | bfloat16 and fp32
 //     68: 8 x 2 11.6 / 21.4 | 12.0 / 22.4, 16 13.9 / 24.4 | 14.0 / 24.5
 //    200: 16 x 2 11.3 / 19.9 | 12.5 / 29.5, 32 13.5 / 22.8 | 14.1 / 28.9     300: 16 x 3 15.0 / 34.8 | 19.0 / 51.7, 64 23.2 / 43.1 | 24.8 / 46.2
 //    384: 16 x 3 14.8 / 31.4 | 21.3 / 45.1, 64 23.6 / 42.4 | 26.4 / 50.0     512: 32 x 2 20.6 / 38.6 | 28.3 / 57.8, 64 21.0 / 39.1 | 28.1 / 60.1
 //   2304: 192 x 2 39.3 / 73.6 | 47.0 / 98.0, 320 41.4 / 77.8 | 48.2 / 100    2900: 192 x 2 49.5 / 88.9 | 59.8 / 127, 384 54.4 / 101 | 61.2 / 128
 //   6144: 384 x 2 53.7 / 107 | 62.8 / 132, 768 59.7 / 83.8 | 65.8 / 122      7168: 512 x 2 60.9 / 115 | 69.7 / 144, 896 70.8 / 108 | 78.6 / 160
-// (8 x 300 x 16384 norm: 512 x 4 43.5 | 51.4, 1024 x 2 49.0 | 57.6, but 600 x 10484: 384 x 4 121, 704 x 2 66.9: four groups and
-// the masks of a row's end do not fit the registers, and neither do four groups of a join, 8 x 200 x 32768 258 | 322; the route
-// of wide rows 178 | 227, norm 83.7 | 103, 1024 x 4 62.5 | 76.7.)
-Team forward_team(uint32_t groups, bool join) {
+// Beyond 16384 columns four groups a lane, norm, whole groups: 8 x 300 x 20000 69.4 | 82.4, the route of wide rows 74.5 | 88.3,
+// x 30008 95.7 | 118 and 108 | 136.  With the masks of a row's end they do not fit the registers (600 x 10484 as 384 x
+// 4 121, as 704 x 2 66.9), and a join's never (8 x 200 x 32768 258 | 322, the route of wide rows 178 | 227).
+Team forward_team(uint32_t cols, bool join) {
+  const uint32_t groups = (cols + kGroup - 1) / kGroup;
+  const bool whole = cols % kGroup == 0;
   if (groups <= 64) {
     if (groups <= 8) return {kInWave, 8, 1};
     if (groups <= 16) return {kInWave, 8, 2};
@@ -195,11 +197,11 @@ Team forward_team(uint32_t groups, bool join) {
   if (groups <= 96) return {kInWave, 32, 3};
   if (groups <= 128) return {kInWave, 64, 2};
   const uint32_t halves = (groups + 31) / 32;
-  if (halves == 5 || (halves == 7 && !join)) return {kPair, halves * 32, 1};
+  if (halves == 5 || (halves == 7 && (!join || whole))) return {kPair, halves * 32, 1};
   if (halves == 8 && join) return {kInWave, 64, 4};
   if (groups > 256 && groups <= 384) return {kBlock, 192, 2};
   if (!join && groups > 640 && groups <= 2048) return {kBlock, (groups + 255) / 256 * 128, 2};
-  if (groups > 2048 && groups <= 4096 && groups % 256 == 0 && !join) return {kBlock, groups / 4, 4};
+  if (groups > 2048 && groups <= 4096 && whole && !join) return {kBlock, (groups + 255) / 256 * 64, 4};
   const uint32_t each = groups <= 1024 ? 1 : groups <= 2048 ? 2 : 0;
   return {kBlock, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
 }
@@ -249,7 +251,7 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
 }  // namespace
 
 hipError_t norm_forward(const NormArgs& k, int32_t type, int32_t stream_type, hipStream_t stream) {
-  const Team team = forward_team((k.cols + kGroup - 1) / kGroup, k.join);
+  const Team team = forward_team(k.cols, k.join);
   return by_types(type, stream_type, [&](auto t, auto h) {
     using T = decltype(t);
     using H = decltype(h);
