@@ -409,11 +409,11 @@ Team loss_team(uint32_t n, uint32_t rows, uint32_t groups) {
   // 133 columns 32 x 1 52.3, 16 x 2 43.6, 16 x 4 55.4; 260 columns 64 x 1 92.5, 32 x 2 75.3, 16 x 4 63.0, 16 x 8 90.0;
   // 512 columns 64 x 1 99.7, 32 x 2 85.3, 16 x 4 73.3; 8 x 9882 x 1000: 64 x 2 81.8, 32 x 4 73.7, 16 x 8 86.0.)
   if (groups <= 256) {
-    uint32_t lanes = 16, each = 1;  // (as many lanes as the two ends may have columns)
-    while (each < 4 && lanes * each < groups) each *= 2;
-    while (lanes * each < groups) lanes *= 2;
-    return {kWaveRows, lanes, each};
+    uint32_t lanes = 16;  // (as many as the two ends may have columns)
+    while (lanes * 4 < groups) lanes *= 2;
+    return {kWaveRows, lanes, groups <= lanes ? 1 : (groups + lanes - 1) / lanes};
   }
+  if (groups <= 384) return {kBlockRow, 128, 3};
   uint32_t each = 0;
   for (const uint32_t k : {4u, 8u, 12u, 16u, 20u, 24u, 32u})
     if (each == 0 && groups <= k * kRowThreads) each = k;
@@ -437,10 +437,12 @@ void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
   } else if (t.kind == kWaveRows) {
     if (t.each == 1) COMPAMS_LOSS(1, kWaveRows);
     else if (t.each == 2) COMPAMS_LOSS(2, kWaveRows);
+    else if (t.each == 3) COMPAMS_LOSS(3, kWaveRows);
     else COMPAMS_LOSS(4, kWaveRows);
   } else {
     switch (t.each) {
       case 0: hipLaunchKernelGGL((k_loss_wide<T, STREAM>), grid, dim3(kLossThreads), 0, stream, k); break;
+      case 3: COMPAMS_LOSS(3, kBlockRow); break;
       case 4: COMPAMS_LOSS(4, kBlockRow); break;
       case 8: COMPAMS_LOSS(8, kBlockRow); break;
       case 12: COMPAMS_LOSS(12, kBlockRow); break;
