@@ -394,6 +394,8 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_mean(LossArgs a) {
 //   vocabulary  4096: 256 x 2 32.5, 128 x 4 30.3, 64 x 8 31.9      8192: 256 x 4 56.8, 128 x 8 58.3, 64 x 16 58.8
 //              16384: 1024 x 2 152, 512 x 4 97, 256 x 8 101, 128 x 16 110      32000: 512 x 8 182, 256 x 16 193
 //              50257: 832 x 8 400, 448 x 16 312, 256 x 32 311, 320 x 20 467 (waves that do not go evenly into four)
+// 8 x 6284 rows of 2268 float16: 64 x 5 91.0, 128 x 3 111, 192 x 2 135; 8 x 3000 rows of 5000 bfloat16: 128 x 5 89.8, 192 x 4
+// 93.9; of 10000: 256 x 5 170, 320 x 4 191
 // and 2048 rows of  40000: 448 x 12 66.9, 320 x 16 77.6; 1078 rows of 67875: 448 x 20 89, 320 x 32 114; of 80387: 512 x 20 96,
 // 320 x 32 120; of 98000: 512 x 24 113, 384 x 32 130; of 33000 fp32: 448 x 20 68.9, 320 x 32 78.4.
 struct Team {
@@ -413,7 +415,9 @@ Team loss_team(uint32_t n, uint32_t rows, uint32_t groups) {
     while (lanes * 4 < groups) lanes *= 2;
     return {kWaveRows, lanes, groups <= lanes ? 1 : (groups + lanes - 1) / lanes};
   }
-  if (groups <= 384) return {kBlockRow, 128, 3};
+  if (groups <= 384) return {kWaveRows, 64, (groups + 63) / 64};
+  if (groups > 512 && groups <= 640) return {kBlockRow, 128, 5};
+  if (groups > 1024 && groups <= 1280) return {kBlockRow, 256, 5};
   uint32_t each = 0;
   for (const uint32_t k : {4u, 8u, 12u, 16u, 20u, 24u, 32u})
     if (each == 0 && groups <= k * kRowThreads) each = k;
@@ -438,12 +442,14 @@ void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
     if (t.each == 1) COMPAMS_LOSS(1, kWaveRows);
     else if (t.each == 2) COMPAMS_LOSS(2, kWaveRows);
     else if (t.each == 3) COMPAMS_LOSS(3, kWaveRows);
-    else COMPAMS_LOSS(4, kWaveRows);
+    else if (t.each == 4) COMPAMS_LOSS(4, kWaveRows);
+    else if (t.each == 5) COMPAMS_LOSS(5, kWaveRows);
+    else COMPAMS_LOSS(6, kWaveRows);
   } else {
     switch (t.each) {
       case 0: hipLaunchKernelGGL((k_loss_wide<T, STREAM>), grid, dim3(kLossThreads), 0, stream, k); break;
-      case 3: COMPAMS_LOSS(3, kBlockRow); break;
       case 4: COMPAMS_LOSS(4, kBlockRow); break;
+      case 5: COMPAMS_LOSS(5, kBlockRow); break;
       case 8: COMPAMS_LOSS(8, kBlockRow); break;
       case 12: COMPAMS_LOSS(12, kBlockRow); break;
       case 16: COMPAMS_LOSS(16, kBlockRow); break;
