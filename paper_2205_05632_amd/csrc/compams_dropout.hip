@@ -19,8 +19,9 @@ constexpr uint32_t kThreads = 256;
 // formed for itself, 82 % of the vector unit's time).  49152 x 1024 bfloat16: 36.7 us, 5.5 TB/s; without arithmetic 35.5.
 constexpr uint32_t kRows = 4;  // rows that a lane takes, its columns in each
 
-// FULL: a multiple of eight columns, a lane has a whole group or none.  SAME: a wavefront's lanes are all in one row, whose number is a scalar then, and with
-// it two of the generator's twenty products.
+// FULL: a multiple of eight columns, a lane has a whole group or none (8 x 1127 x 1816 added to an fp32 stream 39.0 us, 1812
+// 47.3).  SAME: a wavefront's lanes are all in one row, whose number is a scalar then, and with it two of the generator's
+// twenty products.
 template <typename X, typename Y, bool FULL, bool SAME, bool ADD>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutArgs a) {
   const uint32_t tall = kThreads / a.wide;

@@ -34,7 +34,8 @@ struct Max {
 // The rows of a worker that are learnt from, counted by the `lanes` lanes of a team (or of a wavefront of one), `AT_ONCE`
 // loads under way in each.
 template <uint32_t AT_ONCE, typename I>
-__device__ __forceinline__ uint32_t count_targets(const I* targets, uint32_t rows, int64_t ignore, uint32_t lane, uint32_t lanes) {
+__device__ __forceinline__ uint32_t count_targets(const I* targets, uint32_t rows, int64_t ignore, uint32_t lane,
+                                                  uint32_t lanes) {
   uint32_t mine = 0;
   for (uint32_t first = lane; first < rows; first += lanes * AT_ONCE) {
     I t[AT_ONCE];
@@ -118,7 +119,8 @@ enum RowKind {
 };
 
 template <typename T, uint32_t NG, RowKind KIND, bool STREAM>
-__global__ __launch_bounds__(KIND == kWaveRows ? kTeamThreads : KIND == kBlockRow ? kRowThreads : kLossThreads) void k_loss(LossArgs a, uint32_t lanes) {
+__global__ __launch_bounds__(KIND == kWaveRows ? kTeamThreads : KIND == kBlockRow ? kRowThreads : kLossThreads)
+void k_loss(LossArgs a, uint32_t lanes) {
   constexpr uint32_t kEach = Logits<T>::kEach;
   typedef typename Logits<T>::type V;
   __shared__ float tops[2][kLossWaves];
@@ -537,7 +539,8 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream) {
     else if (a->type == COMPAMS_F16) launch(half_t());
     else launch(bfloat_t());
   }
-  if (k.mean_loss && (team.kind != kWorkerRows || k.total == 0)) hipLaunchKernelGGL(k_loss_mean, dim3(k.n), dim3(kLossThreads), 0, stream, k);
+  if (k.mean_loss && (team.kind != kWorkerRows || k.total == 0))
+    hipLaunchKernelGGL(k_loss_mean, dim3(k.n), dim3(kLossThreads), 0, stream, k);
   return hipGetLastError() == hipSuccess ? COMPAMS_OK : COMPAMS_HIP_ERROR;
 }
 

@@ -87,7 +87,9 @@ struct Team {
   TeamKind kind;
   uint32_t lanes, each;  // lanes of a team; groups that a lane takes (0: rows are not held in registers)
 };
-inline uint32_t team_threads(const Team& t) { return t.kind == kInWave ? kTeamThreads : t.kind == kBlock ? t.lanes : 2 * t.lanes; }
+inline uint32_t team_threads(const Team& t) {
+  return t.kind == kInWave ? kTeamThreads : t.kind == kBlock ? t.lanes : 2 * t.lanes;
+}
 // This lane's team within the workgroup, its place there, and the teams of a workgroup.
 template <TeamKind KIND>
 __device__ __forceinline__ uint32_t team_of_lane(uint32_t lanes) {

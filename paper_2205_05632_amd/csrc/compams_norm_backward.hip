@@ -352,7 +352,8 @@ Team backward_team(uint32_t rows, uint32_t groups, bool join) {
   }
   const uint32_t halves = (groups + 31) / 32;
   // (a join's four wavefronts to a SIMD seldom hold three workgroups of five: a row of three wavefronts instead of two of five,
-  // but where a worker has few rows: 8 x 400 x 1280 pair 18.5, 192 22.1; 3 x 401 x 1601 17.4 and 21.2; 8 x 1000 x 1280 41.9 and 33.3)
+  // but where a worker has few rows: 8 x 400 x 1280 pair 18.5, 192 22.1; 3 x 401 x 1601 17.4 and 21.2; 8 x 1000 x 1280 41.9
+  // and 33.3)
   if (halves == 3 || ((!join || rows <= 512) && (halves == 5 || halves == 7))) return {kPair, halves * 32, 1};
   if (groups <= 128) return {kInWave, 64, 2};
   // (two groups a lane take a join 168 registers: twelve wavefronts at most)
@@ -363,7 +364,8 @@ Team backward_team(uint32_t rows, uint32_t groups, bool join) {
 template <typename T, typename H, bool JOIN>
 void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
   const dim3 grid(blocks_for(static_cast<uint64_t>(k.n) * k.parts)), block(team_threads(t));
-  const size_t lds = (t.kind == kInWave ? kTeamThreads / 64 : t.kind == kPair ? 1 : 0) * t.each * t.lanes * kGroup * sizeof(float);
+  const size_t lines = t.kind == kInWave ? kTeamThreads / 64 : t.kind == kPair ? 1 : 0;
+  const size_t lds = lines * t.each * t.lanes * kGroup * sizeof(float);
   const bool all = k.gamma && k.dresidual && k.grad[0] && k.grad[1] && (!JOIN || (k.dh && k.dx && k.grad[2]));
   const bool full = all && k.cols == t.lanes * t.each * kGroup, whole = all && k.cols % kGroup == 0;
 #define COMPAMS_BACKWARD_OF(NG, KIND, WIDTH) \

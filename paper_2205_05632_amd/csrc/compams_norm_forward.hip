@@ -177,10 +177,15 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) 
 //   1601 (bfloat16 stream): pair of 224 57 / 126, 256 61 / 117          8 x 3117 x 1600: pair of 224 46.6 / 101, 256 47.0 / 107
 // 8 x 6167 rows (13028 of 68, 2048 of 2304 and 2900, 1000 of 6144 and 7168), all float16 | bfloat16 and fp32
 //     68: 8 x 2 11.6 / 21.4 | 12.0 / 22.4, 16 13.9 / 24.4 | 14.0 / 24.5
-//    200: 16 x 2 11.3 / 19.9 | 12.5 / 29.5, 32 13.5 / 22.8 | 14.1 / 28.9     300: 16 x 3 15.0 / 34.8 | 19.0 / 51.7, 64 23.2 / 43.1 | 24.8 / 46.2
-//    384: 16 x 3 14.8 / 31.4 | 21.3 / 45.1, 64 23.6 / 42.4 | 26.4 / 50.0     512: 32 x 2 20.6 / 38.6 | 28.3 / 57.8, 64 21.0 / 39.1 | 28.1 / 60.1
-//   2304: 192 x 2 39.3 / 73.6 | 47.0 / 98.0, 320 41.4 / 77.8 | 48.2 / 100    2900: 192 x 2 49.5 / 88.9 | 59.8 / 127, 384 54.4 / 101 | 61.2 / 128
-//   6144: 384 x 2 53.7 / 107 | 62.8 / 132, 768 59.7 / 83.8 | 65.8 / 122      7168: 512 x 2 60.9 / 115 | 69.7 / 144, 896 70.8 / 108 | 78.6 / 160
+//    200: 16 x 2 11.3 / 19.9 | 12.5 / 29.5, 32 13.5 / 22.8 | 14.1 / 28.9
+//    300: 16 x 3 15.0 / 34.8 | 19.0 / 51.7, 64 23.2 / 43.1 | 24.8 / 46.2
+//    384: 16 x 3 14.8 / 31.4 | 21.3 / 45.1, 64 23.6 / 42.4 | 26.4 / 50.0
+//    512: 32 x 2 20.6 / 38.6 | 28.3 / 57.8, 64 21.0 / 39.1 | 28.1 / 60.1
+//   2304: 192 x 2 39.3 / 73.6 | 47.0 / 98.0, 320 41.4 / 77.8 | 48.2 / 100
+//   2900: 192 x 2 49.5 / 88.9 | 59.8 / 127, 384 54.4 / 101 | 61.2 / 128
+//   6144: 384 x 2 53.7 / 107 | 62.8 / 132, 768 59.7 / 83.8 | 65.8 / 122
+//   7168: 512 x 2 60.9 / 115 | 69.7 / 144, 896 70.8 / 108 | 78.6 / 160
+// (before whole groups had a variant of their own, which takes up to a quarter less: 8 x 6167 x 200, join, 15.7 | 27.8)
 // Beyond 16384 columns four groups a lane, norm, whole groups: 8 x 300 x 20000 69.4 | 82.4, the route of wide rows 74.5 | 88.3,
 // x 30008 95.7 | 118 and 108 | 136.  With the masks of a row's end they do not fit the registers (600 x 10484 as 384 x
 // 4 121, as 704 x 2 66.9), and a join's never (8 x 200 x 32768 258 | 322, the route of wide rows 178 | 227).

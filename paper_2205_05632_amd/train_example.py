@@ -55,7 +55,8 @@ class Model:
             if name.startswith("gamma"):
                 p.fill_(1.0)
             elif p.dim() == 2:
-                p.copy_(torch.randn(p.shape, generator=g) * (0.5 if name == "embed" else 1.0) / math.sqrt(p.shape[0 if name != "embed" else 1]))
+                fan, scale = (p.shape[1], 0.5) if name == "embed" else (p.shape[0], 1.0)
+                p.copy_(torch.randn(p.shape, generator=g) * scale / math.sqrt(fan))
         return flat
 
 
