@@ -406,8 +406,10 @@ struct Team {
 };
 Team loss_team(uint32_t n, uint32_t rows, uint32_t groups) {
   // A few short rows of each worker: the launch that would form the means costs more than going over them one after another
-  // (8 x 32 x 1000 fp32: 10.5 us a call, with a launch more 12.5; on the device 8.2 and 4.0 + 2.8 and a gap).
-  if (n <= 256 && rows <= 2 * kLossWaves && groups <= 256) return {kWorkerRows, 64, groups <= 64 ? 1u : groups <= 128 ? 2u : 4u};
+  // (8 x 32 x 1000 fp32: 10.5 us a call, with a launch more 12.5; on the device 8.2 and 4.0 + 2.8 and a gap).  However many
+  // workers there are, so that a worker's losses are the same bits beside any others (300 x 32 x 1000 fp32 16.6 and 16.9, 1000 x
+  // 4 x 40 11.1 and 13.1, 3000 x 32 x 256 bfloat16 47.5 and 35.2); a grid has room for a million.
+  if (n <= 1u << 20 && rows <= 2 * kLossWaves && groups <= 256) return {kWorkerRows, 64, groups <= 64 ? 1u : groups <= 128 ? 2u : 4u};
   // Short rows: few lanes with up to four groups, so that what a row costs besides its columns (its reductions, logarithm and
   // quotients) is shared by the rows of a wavefront.  (16 x 9882 rows of float16, us on the device and the two small launches:
   // 133 columns 32 x 1 52.3, 16 x 2 43.6, 16 x 4 55.4; 260 columns 64 x 1 92.5, 32 x 2 75.3, 16 x 4 63.0, 16 x 8 90.0;

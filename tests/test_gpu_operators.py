@@ -585,3 +585,19 @@ def test_cross_entropy_of_every_kind_of_team(vocab, dtype):
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_cross_entropy_of_many_rows(n, rows, vocab, dtype):
     test_cross_entropy_of_many_shapes(n, rows, vocab, dtype)
+
+
+@pytest.mark.parametrize("rows,vocab", [(4, 40), (32, 300), (3, 2000), (33, 40), (600, 24)])
+def test_a_worker_on_its_own_has_the_same_loss(rows, vocab):
+    """The bits of a worker's loss and gradient do not depend on how many workers stand beside it."""
+    rng = np.random.default_rng(rows * vocab)
+    n = 300 if rows <= 32 else 40
+    x, _ = matrix(rng, n * rows, vocab, BF16, 0, 0, 2.0)
+    t = torch.from_numpy(rng.integers(0, vocab, n * rows)).cuda()
+    t[::7] = -100
+    beside = ops.compams_cross_entropy(x, t, n)
+    for w in (0, n - 1):
+        part = slice(w * rows, (w + 1) * rows)
+        alone = ops.compams_cross_entropy(x[part], t[part], 1)
+        assert torch.equal(alone[0][0], beside[0][w])
+        assert torch.equal(alone[1], beside[1][part]) and torch.equal(alone[2], beside[2][part])
