@@ -443,7 +443,7 @@ int compams_dropout_add_norm_forward(const compams_norm* a, void* hip_stream);
 int compams_dropout_add_norm_backward(const compams_norm* a, void* hip_stream);
 
 /* Softmax cross-entropy and its gradient, every worker's loss the mean over its tokens.  For row r with target t:
- *   losses[r] = log(sum_c exp(l_c - max l)) + max l - l_t,  dlogits = grad_scale / count (softmax(l) - [c = t])
+ *   losses[r] = (max l - l_t) + log(sum_c exp(l_c - max l)),  dlogits = grad_scale / count (softmax(l) - [c = t])
  *   mean_loss[i] = sum of worker i's losses / count
  * with count = the worker's rows whose target is not ignore_index; ignored rows have loss 0 and gradient 0 whatever
  * their logits are, and a worker without any other row has mean_loss 0.  Logits of minus infinity have probability 0

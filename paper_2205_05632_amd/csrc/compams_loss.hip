@@ -210,7 +210,8 @@ void k_loss(LossArgs a, uint32_t lanes) {
     }
     turn ^= 1;
     const bool none = !inside || top == -INFINITY;
-    const float loss = none ? __builtin_nanf("") : logf(s[0]) + top - of_target;
+    // (the large numbers first: their difference is what the loss is made of, a sum of them would round it away)
+    const float loss = none ? __builtin_nanf("") : (top - of_target) + logf(s[0]);
     of_worker[0] += loss;
     if (a.losses && lane == 0) a.losses[r] = loss;
     if (!out) continue;
@@ -335,7 +336,7 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
     float sum = 0.0f;
     for (uint32_t w = 0; w < kLossWaves; ++w) sum += sums[w];
     const bool none = !inside || top == -INFINITY;
-    if (a.losses && lane == 0) a.losses[r] = none ? __builtin_nanf("") : logf(sum) + top - of_target;
+    if (a.losses && lane == 0) a.losses[r] = none ? __builtin_nanf("") : (top - of_target) + logf(sum);
     if (!out) continue;
     const float factor = none ? __builtin_nanf("") : a.grad_scale / static_cast<float>(a.counts[r / a.rows]);
     const float share = factor / sum;
