@@ -71,18 +71,37 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_count(LossArgs a) {
   }
 }
 
-// exp(v - top) for v <= top; results below 2^-126 are 0.  (The difference first: with log2(e) top taken off in one
-// multiply-add instead, 309 us for 316 below, tops from 1e9 on leave more of their rounding than an exponent holds.)
+// exp(v - top) = 2^((v - top) log2(e)) for v <= top.  (The difference first: with log2(e) top taken off in one multiply-add
+// instead, 2 % faster at 8192 x 50257, tops from 1e9 on leave more of their rounding than an exponent holds.)
+//
+// Rows of 32 bits: the exponent as a whole number and a part in -1/2 .. 1/2, which is formed with the product's and log2(e)'s own
+// rounding put right, so that the result is off by three units of 2^-24 at any distance.  (Rounded once, an exponent of -60 is
+// off by up to 2^-19: 22 such units of the result.)  Distances beyond 200 are taken as that: whatever they are, 0 is left.
+// Rows of 16 bits: the product rounded once, three instructions for ten.  With the difference's rounding an entry is off by
+// 2.3 (top - v) units of 2^-24, at a distance of 87, the largest that leaves a normal number, by 2^-16 of itself, where its
+// gradient is rounded to 2^-9 or 2^-12; of their sum it is the mean distance by weight, log(vocab) at most.  Results below
+// 2^-126 are 0.
+constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kShift = 0x1.8p23f;  // what is added to it is rounded to a whole number, which is in the low bits then
+constexpr float kLog2ERest = static_cast<float>(1.44269504088896340736 - static_cast<double>(kLog2E));
+template <typename T>
 __device__ __forceinline__ float exp_below(float v, float top) {
-  return __builtin_amdgcn_exp2f((v - top) * 1.44269504088896340736f);
+  if constexpr (sizeof(T) < 4) {
+    return __builtin_amdgcn_exp2f((v - top) * kLog2E);
+  } else {
+    const float away = __builtin_elementwise_maximum(v - top, -200.0f);  // (a NaN stays one)
+    const float shifted = fmaf(away, kLog2E, kShift), whole = shifted - kShift;
+    const float part = fmaf(away, kLog2ERest, fmaf(away, kLog2E, -whole));
+    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(part), static_cast<int16_t>(__float_as_uint(shifted)));
+  }
 }
 
 // ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
 // A team is 16 to 64 lanes of a wavefront or a whole workgroup.  The row is read once and kept as it came, in
 // groups of 16 bytes; its maximum, the sum of its exponentials and its gradient are three passes over registers.  (The
-// exponentials are formed twice: kept in fp32 they would take up to two times the row's registers again, and what hides
-// one row's reads and reductions is the other rows that fit a compute unit.)  8192 x 50257 bfloat16: 316 us, of which reading,
-// the barriers and writing alone take 298; 5.2 TB/s.
+// exponentials of 16-bit rows are formed twice: kept in fp32 they would take two times the row's registers again, and what
+// hides one row's reads and reductions is the other rows that fit a compute unit.  Those of fp32 rows take their logits'
+// place.)  8192 x 50257 bfloat16: 312 us, of which reading, the barriers and writing alone take 298; 5.3 TB/s.
 //
 // The groups start at the row's first multiple of 16 bytes: rows of an odd vocabulary, one after another, start anywhere,
 // and accesses across cache lines cost a sixth of the time.  What is left at the row's two ends, up to seven columns
@@ -118,10 +137,14 @@ enum RowKind {
   kWorkerRows = 2  // a wavefront to a row, a workgroup to all rows of a worker, whose mean it forms as well
 };
 
+// (20 groups of fp32 are kept to the registers that leave room for a second row: 8 x 500 x 33000 202 us for 224, 207 with
+// exponentials rounded as those of 16-bit rows are.)
 template <typename T, uint32_t NG, RowKind KIND, bool STREAM>
-__global__ __launch_bounds__(KIND == kWaveRows ? kTeamThreads : KIND == kBlockRow ? kRowThreads : kLossThreads)
+__global__ __launch_bounds__(KIND == kWaveRows ? kTeamThreads : KIND == kBlockRow ? kRowThreads : kLossThreads,
+                             NG == 20 && sizeof(T) == 4 ? 4 : 1)
 void k_loss(LossArgs a, uint32_t lanes) {
   constexpr uint32_t kEach = Logits<T>::kEach;
+  constexpr bool kKept = sizeof(T) == 4;
   typedef typename Logits<T>::type V;
   __shared__ float tops[2][kLossWaves];
   __shared__ float slots[2][2][kSlots];
@@ -186,13 +209,14 @@ void k_loss(LossArgs a, uint32_t lanes) {
     }
     uint32_t again = lane;
     forget(again);
-    float s[2] = {exp_below(at_end, top), count};
+    float s[2] = {exp_below<T>(at_end, top), count};
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
       forget_group(raw[k]);
       float e[kEach];
 #pragma unroll
-      for (uint32_t j = 0; j < kEach; ++j) e[j] = exp_below(to_float(raw[k][j]), top);
+      for (uint32_t j = 0; j < kEach; ++j) e[j] = exp_below<T>(to_float(raw[k][j]), top);
+      if constexpr (kKept) __builtin_memcpy(&raw[k], e, sizeof(raw[k]));
 #pragma unroll
       for (uint32_t n = kEach / 2; n > 0; n /= 2)
 #pragma unroll
@@ -230,7 +254,7 @@ void k_loss(LossArgs a, uint32_t lanes) {
       forget_group(raw[k]);
       float v[kEach];
 #pragma unroll
-      for (uint32_t j = 0; j < kEach; ++j) v[j] = exp_below(to_float(raw[k][j]), top) * share;
+      for (uint32_t j = 0; j < kEach; ++j) v[j] = (kKept ? to_float(raw[k][j]) : exp_below<T>(to_float(raw[k][j]), top)) * share;
       const uint32_t at = hot - head - g * kEach;
       if (at < kEach) {
 #pragma unroll
@@ -246,7 +270,7 @@ void k_loss(LossArgs a, uint32_t lanes) {
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (end < a.vocab) out[end] = static_cast<T>(exp_below(at_end, top) * share - (end == hot ? factor : 0.0f));
+    if (end < a.vocab) out[end] = static_cast<T>(exp_below<T>(at_end, top) * share - (end == hot ? factor : 0.0f));
   }
   if constexpr (KIND == kWorkerRows) {
     // (the same in all lanes of a wavefront: one of them counts)
@@ -264,14 +288,15 @@ void k_loss(LossArgs a, uint32_t lanes) {
 constexpr uint32_t kAhead = 4;  // groups that a lane requests at once
 
 // One more value to a lane's maximum and sum.  What the sum counts from moves up rarely after the first few.
+template <typename T>
 struct Running {
   float top = -INFINITY, sum = 0.0f;
   __device__ __forceinline__ void raise(float m) {
     if (!(m > top)) return;
-    sum = top == -INFINITY ? sum : sum * exp_below(top, m);  // (without a finite entry so far it is 0 or NaN)
+    sum = top == -INFINITY ? sum : sum * exp_below<T>(top, m);  // (without a finite entry so far it is 0 or NaN)
     top = m;
   }
-  __device__ __forceinline__ void add(float v) { sum += top == -INFINITY ? (v != v ? v : 0.0f) : exp_below(v, top); }
+  __device__ __forceinline__ void add(float v) { sum += top == -INFINITY ? (v != v ? v : 0.0f) : exp_below<T>(v, top); }
 };
 
 template <typename T, bool STREAM>
@@ -299,7 +324,7 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
     const uint32_t end = lane < 8 ? (lane < head ? lane : a.vocab) : lane < 16 ? tail + (lane - 8) : a.vocab;
     const float at_end = end < a.vocab ? to_float(row[end]) : -INFINITY;
     const V* const inner = reinterpret_cast<const V*>(row + head);
-    Running run;
+    Running<T> run;
     if (end < a.vocab) {
       run.raise(at_end);
       run.add(at_end);
@@ -330,7 +355,7 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
     __syncthreads();
     float top = tops[0];
     for (uint32_t w = 1; w < kLossWaves; ++w) top = fmaxf(top, tops[w]);
-    const float mine = sum_lanes(run.top == -INFINITY ? run.sum : run.sum * exp_below(run.top, top), 64);
+    const float mine = sum_lanes(run.top == -INFINITY ? run.sum : run.sum * exp_below<T>(run.top, top), 64);
     if (lane % 64 == 0) sums[lane / 64] = mine;
     __syncthreads();
     float sum = 0.0f;
@@ -357,14 +382,14 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
         V o;
 #pragma unroll
         for (uint32_t j = 0; j < kEach; ++j)
-          o[j] = static_cast<T>(exp_below(to_float(raw[k][j]), top) * share - (at == j ? factor : 0.0f));
+          o[j] = static_cast<T>(exp_below<T>(to_float(raw[k][j]), top) * share - (at == j ? factor : 0.0f));
         char* const p = inner_out + static_cast<size_t>(g) * 16;
         if (!aligned) __builtin_memcpy(p, &o, 16);
         else if (STREAM) __builtin_nontemporal_store(o, reinterpret_cast<V*>(p));
         else *reinterpret_cast<V*>(p) = o;
       }
     }
-    if (end < a.vocab) out[end] = static_cast<T>(exp_below(at_end, top) * share - (end == hot ? factor : 0.0f));
+    if (end < a.vocab) out[end] = static_cast<T>(exp_below<T>(at_end, top) * share - (end == hot ? factor : 0.0f));
   }
 }
 

@@ -37,3 +37,35 @@ def test_losses_do_not_depend_on_an_offset(rows, vocab, dtype):
     R.close(losses, want, bound, "losses")
     # (the mean: the losses' own errors, a sum of at most `rows` terms and a quotient)
     R.close(mean, want.mean(0, keepdim=True), bound.mean(0, keepdim=True) + 1.01 * U * (rows + 1) * want.mean(0, keepdim=True), "mean")
+
+
+ROUTES = [(1, 24), (40, 24), (1, 500), (700, 130), (3, 2000), (40, 5000), (40, 20000), (3, 140000)]    # (rows of one worker, columns)
+
+
+def few_entries(rng, rows, vocab, dtype, far):
+    """Rows of minus infinity but for six entries: the largest, 0, and five at whole and half distances up to `far` below, so
+    that every difference is exact and a row's sum has six terms.  (logits, targets: the largest or another of the six)"""
+    at = torch.from_numpy(np.stack([rng.choice(vocab, 6, replace=False) for _ in range(rows)]))
+    away = torch.from_numpy(rng.integers(0, 2 * far, (rows, 6)) / 2.0)
+    away[:, 0] = 0.0
+    v = torch.full((rows, vocab), -math.inf, dtype=torch.float64).scatter_(1, at, -away)
+    t = at[:, 0].clone()
+    t[1::3] = at[1::3, 1]
+    return v.to(dtype), t
+
+
+def gradient_of(v, t, scale):
+    """(gradient, probabilities, where the targets are), in 64 bits."""
+    p = torch.softmax(v.double(), 1)
+    hot = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
+    return (p - hot) * scale, p, hot
+
+
+@pytest.mark.parametrize("rows,vocab", ROUTES)
+def test_exponentials_at_every_distance(rows, vocab):
+    """Entries of fp32 rows keep their digits at any distance to the row's maximum: an exponential four units, the sum of six
+    of them those and six roundings, the quotient and the product one each."""
+    v, t = few_entries(np.random.default_rng(rows + vocab), rows, vocab, F32, 100)
+    _, _, d = ops.compams_cross_entropy(v.cuda(), t.cuda(), 1, grad_scale=float(rows))
+    want, p, hot = gradient_of(v, t, 1.0)
+    R.close(d, want, 16 * U * p + 2 * U * hot + 2.0 ** -149, "dlogits")
