@@ -15,6 +15,7 @@ struct LossArgs {
   bool wide_targets;  // 64 bits
   int64_t ignore;
   float grad_scale;
+  float lift;  // of the gradient's exponentials, see exp_below
   float *mean_loss, *losses;
   uint32_t* counts;  // per worker: rows that are learnt from; NULL where whoever asks counts them
 };
@@ -81,19 +82,28 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_count(LossArgs a) {
 // 2.3 (top - v) units of 2^-24, at a distance of 87, the largest that leaves a normal number, by 2^-16 of itself, where its
 // gradient is rounded to 2^-9 or 2^-12; of their sum it is the mean distance by weight, log(vocab) at most.  Results below
 // 2^-126 are 0.
+//
+// lift: the result is 2^lift times as large, so that no entry is lost that the gradient's scale makes a normal number again
+// (grad_scale < 2^lift; for 16 bits two more units for each power of two, the largest entry stays exact).
 constexpr float kLog2E = 1.44269504088896340736f;
 constexpr float kShift = 0x1.8p23f;  // what is added to it is rounded to a whole number, which is in the low bits then
 constexpr float kLog2ERest = static_cast<float>(1.44269504088896340736 - static_cast<double>(kLog2E));
 template <typename T>
-__device__ __forceinline__ float exp_below(float v, float top) {
+__device__ __forceinline__ float exp_below(float v, float top, float lift = 0.0f) {
   if constexpr (sizeof(T) < 4) {
-    return __builtin_amdgcn_exp2f((v - top) * kLog2E);
+    return __builtin_amdgcn_exp2f(fmaf(v - top, kLog2E, lift));
   } else {
     const float away = __builtin_elementwise_maximum(v - top, -200.0f);  // (a NaN stays one)
-    const float shifted = fmaf(away, kLog2E, kShift), whole = shifted - kShift;
+    const float shifted = fmaf(away, kLog2E, kShift + lift), whole = shifted - (kShift + lift);
     const float part = fmaf(away, kLog2ERest, fmaf(away, kLog2E, -whole));
     return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(part), static_cast<int16_t>(__float_as_uint(shifted)));
   }
+}
+
+// (With float16 no number that a gradient can hold comes from an exponential below 2^-126.)
+template <typename T>
+__device__ __forceinline__ float lift_of(const LossArgs& a) {
+  return __is_same(T, half_t) ? 0.0f : a.lift;
 }
 
 // ---- Rows that a team of lanes holds in registers ---------------------------------------------------------------
@@ -145,6 +155,7 @@ __global__ __launch_bounds__(KIND == kWaveRows ? kTeamThreads : KIND == kBlockRo
 void k_loss(LossArgs a, uint32_t lanes) {
   constexpr uint32_t kEach = Logits<T>::kEach;
   constexpr bool kKept = sizeof(T) == 4;
+  const float lift = lift_of<T>(a);
   typedef typename Logits<T>::type V;
   __shared__ float tops[2][kLossWaves];
   __shared__ float slots[2][2][kSlots];
@@ -208,14 +219,15 @@ void k_loss(LossArgs a, uint32_t lanes) {
       for (uint32_t i = 0; i < waves; ++i) top = fmaxf(top, tops[turn][i]);
     }
     uint32_t again = lane;
+    const float in_sum = kKept ? lift : 0.0f;  // (kept for the gradient)
     forget(again);
-    float s[2] = {exp_below<T>(at_end, top), count};
+    float s[2] = {exp_below<T>(at_end, top, in_sum), count};
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
       forget_group(raw[k]);
       float e[kEach];
 #pragma unroll
-      for (uint32_t j = 0; j < kEach; ++j) e[j] = exp_below<T>(to_float(raw[k][j]), top);
+      for (uint32_t j = 0; j < kEach; ++j) e[j] = exp_below<T>(to_float(raw[k][j]), top, in_sum);
       if constexpr (kKept) __builtin_memcpy(&raw[k], e, sizeof(raw[k]));
 #pragma unroll
       for (uint32_t n = kEach / 2; n > 0; n /= 2)
@@ -233,6 +245,7 @@ void k_loss(LossArgs a, uint32_t lanes) {
       sum_block(s, slots[turn], waves);
     }
     turn ^= 1;
+    if constexpr (kKept) s[0] = __builtin_amdgcn_ldexpf(s[0], -static_cast<int>(lift));
     const bool none = !inside || top == -INFINITY;
     // (the large numbers first: their difference is what the loss is made of, a sum of them would round it away)
     const float loss = none ? __builtin_nanf("") : (top - of_target) + logf(s[0]);
@@ -243,7 +256,7 @@ void k_loss(LossArgs a, uint32_t lanes) {
     if (KIND == kWorkerRows) s[1] = of_worker[1];
     // a row without a softmax or a loss has no gradient
     const float factor = none ? __builtin_nanf("") : a.grad_scale / s[1];
-    const float share = factor / s[0];
+    const float share = __builtin_amdgcn_ldexpf(factor / s[0], -static_cast<int>(lift));
     const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == reinterpret_cast<uintptr_t>(logits) % 16;
     const uint32_t hot = inside ? static_cast<uint32_t>(target) : a.vocab;
     char* const inner_out = reinterpret_cast<char*>(out + head);
@@ -254,7 +267,10 @@ void k_loss(LossArgs a, uint32_t lanes) {
       forget_group(raw[k]);
       float v[kEach];
 #pragma unroll
-      for (uint32_t j = 0; j < kEach; ++j) v[j] = (kKept ? to_float(raw[k][j]) : exp_below<T>(to_float(raw[k][j]), top)) * share;
+      for (uint32_t j = 0; j < kEach; ++j) {
+        const float l = to_float(raw[k][j]);
+        v[j] = (kKept ? l : exp_below<T>(l, top, lift)) * share;
+      }
       const uint32_t at = hot - head - g * kEach;
       if (at < kEach) {
 #pragma unroll
@@ -270,7 +286,7 @@ void k_loss(LossArgs a, uint32_t lanes) {
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (end < a.vocab) out[end] = static_cast<T>(exp_below<T>(at_end, top) * share - (end == hot ? factor : 0.0f));
+    if (end < a.vocab) out[end] = static_cast<T>(exp_below<T>(at_end, top, lift) * share - (end == hot ? factor : 0.0f));
   }
   if constexpr (KIND == kWorkerRows) {
     // (the same in all lanes of a wavefront: one of them counts)
@@ -304,6 +320,7 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
   constexpr uint32_t kEach = Logits<T>::kEach;
   typedef typename Logits<T>::type V;
   __shared__ float tops[kLossWaves], sums[kLossWaves];
+  const float lift = lift_of<T>(a);
   for (uint32_t r = blockIdx.x; r < a.total; r += gridDim.x) {
     const int64_t target = target_of(a, r);
     const T* const row = static_cast<const T*>(a.logits) + static_cast<int64_t>(r) * a.ld_logits;
@@ -364,7 +381,7 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
     if (a.losses && lane == 0) a.losses[r] = none ? __builtin_nanf("") : (top - of_target) + logf(sum);
     if (!out) continue;
     const float factor = none ? __builtin_nanf("") : a.grad_scale / static_cast<float>(a.counts[r / a.rows]);
-    const float share = factor / sum;
+    const float share = __builtin_amdgcn_ldexpf(factor / sum, -static_cast<int>(lift));
     const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == reinterpret_cast<uintptr_t>(row) % 16;
     const uint32_t hot = inside ? static_cast<uint32_t>(target) : a.vocab;
     char* const inner_out = reinterpret_cast<char*>(out + head);
@@ -382,14 +399,14 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_wide(LossArgs a) {
         V o;
 #pragma unroll
         for (uint32_t j = 0; j < kEach; ++j)
-          o[j] = static_cast<T>(exp_below<T>(to_float(raw[k][j]), top) * share - (at == j ? factor : 0.0f));
+          o[j] = static_cast<T>(exp_below<T>(to_float(raw[k][j]), top, lift) * share - (at == j ? factor : 0.0f));
         char* const p = inner_out + static_cast<size_t>(g) * 16;
         if (!aligned) __builtin_memcpy(p, &o, 16);
         else if (STREAM) __builtin_nontemporal_store(o, reinterpret_cast<V*>(p));
         else *reinterpret_cast<V*>(p) = o;
       }
     }
-    if (end < a.vocab) out[end] = static_cast<T>(exp_below<T>(at_end, top) * share - (end == hot ? factor : 0.0f));
+    if (end < a.vocab) out[end] = static_cast<T>(exp_below<T>(at_end, top, lift) * share - (end == hot ? factor : 0.0f));
   }
 }
 
@@ -545,6 +562,9 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream) {
   k.wide_targets = a->target_type == COMPAMS_I64;
   k.ignore = a->ignore_index;
   k.grad_scale = a->grad_scale;
+  // |factor| <= |grad_scale| < 2^lift.  (At most 96: the sum of an fp32 row is formed so too, with 2^31 entries.)
+  const float size = fabsf(k.grad_scale);
+  k.lift = size > 1.0f ? fminf(static_cast<float>(ilogbf(fminf(size, 0x1p96f)) + 1), 96.0f) : 0.0f;
   k.mean_loss = a->mean_loss;
   k.losses = a->losses ? a->losses
              : a->mean_loss ? reinterpret_cast<float*>(static_cast<char*>(a->workspace) + counts_bytes(*a)) : nullptr;

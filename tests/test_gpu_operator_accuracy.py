@@ -69,3 +69,21 @@ def test_exponentials_at_every_distance(rows, vocab):
     _, _, d = ops.compams_cross_entropy(v.cuda(), t.cuda(), 1, grad_scale=float(rows))
     want, p, hot = gradient_of(v, t, 1.0)
     R.close(d, want, 16 * U * p + 2 * U * hot + 2.0 ** -149, "dlogits")
+
+
+@pytest.mark.parametrize("dtype,scale", [(F32, 2.0 ** 15), (F32, -3.0 * 2.0 ** 40), (F32, 2.0 ** 110), (F16, 2.0 ** 15),
+                                         (BF16, 2.0 ** 15), (BF16, -3.0 * 2.0 ** 40), (BF16, 2.0 ** 110)],
+                         ids=["f32_15", "f32_41", "f32_110", "f16_15", "bf16_15", "bf16_41", "bf16_110"])
+@pytest.mark.parametrize("rows,vocab", ROUTES)
+def test_what_a_scale_brings_back(rows, vocab, dtype, scale):
+    """Of a scaled loss the gradient, not the probability, decides what is too small to be held, with scales up to 2^96 at
+    least.  (Of 16 bits an exponential is off by 2.3 units for each of the distance and two for each power of two of the
+    scale, and subnormal results may be 0.)"""
+    v, t = few_entries(np.random.default_rng(rows + vocab + 1), rows, vocab, dtype, 115)
+    _, _, d = ops.compams_cross_entropy(v.cuda(), t.cuda(), 1, grad_scale=scale * rows)
+    want, p, hot = gradient_of(v, t, scale)
+    units, least = 16.0, 2.0 ** -149
+    if dtype is not F32:
+        units, least = 16.0 + 2.3 * (-v.double()).clamp(max=200.0) + 2 * math.log2(abs(scale) * rows), 2.0 ** -126 + R.LEAST[dtype]
+    least = max(least, 2.0 ** -125 * abs(scale) / 2.0 ** 96)
+    R.close(d, want, (units * U * p + 2 * U * hot) * abs(scale) + R.UNIT[dtype] * 1.01 * want.abs() + least, "dlogits")
