@@ -39,6 +39,8 @@ NormArgs make_args(const compams_norm& a, bool join) {
   k.n = static_cast<uint32_t>(a.n);
   k.rows = static_cast<uint32_t>(a.rows);
   k.cols = static_cast<uint32_t>(a.cols);
+  k.count.n = static_cast<float>(k.cols);
+  k.count.inverse = 1.0f / k.count.n;
   k.total = k.n * k.rows;
   k.eps = a.eps;
   k.join = join;

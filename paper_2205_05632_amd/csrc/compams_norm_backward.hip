@@ -63,7 +63,6 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 && JOIN ? 
   const uint32_t team = team_of_lane<KIND>(lanes), lane = lane_of_team<KIND>(lanes, team);
   const uint32_t together = teams_together<KIND>(lanes);
   const uint64_t offset = JOIN ? drop_offset(a.drop) : 0u;
-  const float one_by_count = 1.0f / static_cast<float>(a.cols);
   typename Group<float>::type g[NG];
 #pragma unroll
   for (uint32_t k = 0; k < NG; ++k) {
@@ -109,7 +108,7 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 && JOIN ? 
       }
       sum_over_team<KIND>(s, slots[turn], lanes, team);
       if (KIND == kPair && spare) continue;
-      const float s0 = s[0] * one_by_count, s1 = s[1] * one_by_count;
+      const float s0 = mean_of(s[0], a.count), s1 = mean_of(s[1], a.count);
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
         const uint32_t c = (k * lanes + lane) * kGroup;
@@ -200,7 +199,6 @@ template <typename T, typename H>
 __global__ __launch_bounds__(kWideThreads) void k_norm_sums_wide(NormArgs a) {
   __shared__ float slots[2][2][kSlots];
   uint32_t turn = 0;
-  const float count = static_cast<float>(a.cols);
   for (uint32_t r = blockIdx.x; r < a.total; r += gridDim.x, turn ^= 1) {
     const float mean = a.mean[r], rstd = a.rstd[r];
     float s[2] = {0.0f, 0.0f};
@@ -216,7 +214,7 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_sums_wide(NormArgs a) {
       }
     }
     sum_block(s, slots[turn], kWideThreads / 64);
-    if (threadIdx.x == 0) a.sums[r] = make_float2(s[0] / count, s[1] / count);
+    if (threadIdx.x == 0) a.sums[r] = make_float2(mean_of(s[0], a.count), mean_of(s[1], a.count));
   }
 }
 

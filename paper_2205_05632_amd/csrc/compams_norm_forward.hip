@@ -21,7 +21,6 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_
   const uint32_t team = team_of_lane<KIND>(lanes), lane = lane_of_team<KIND>(lanes, team);
   const uint32_t together = teams_together<KIND>(lanes);
   const uint64_t offset = JOIN ? drop_offset(a.drop) : 0u;
-  const float one_by_count = 1.0f / static_cast<float>(a.cols);
   for (uint32_t first = blockIdx.x * together; first < a.total; first += gridDim.x * together) {
     // (a team without a row of its own goes over the last one again: the teams of a pair meet at barriers)
     const bool spare = KIND != kBlock && first + team >= a.total;
@@ -87,7 +86,7 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_
 #pragma unroll
       for (uint32_t j = 0; j < kGroup; ++j) s[0] += v[k][j];
     sum_over_team<KIND>(s, slots[0], lanes, team);
-    const float mean = s[0] * one_by_count;
+    const float mean = mean_of(s[0], a.count);
     s[0] = 0.0f;
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
@@ -107,7 +106,7 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : 1024) void k_norm_
     }
     sum_over_team<KIND>(s, slots[1], lanes, team);
     if (KIND == kPair && spare) continue;
-    const float rstd = rsqrtf(fmaf(s[0], one_by_count, a.eps));
+    const float rstd = rstd_of(s[0], a.count, a.eps);
 #pragma unroll
     for (uint32_t k = 0; k < NG; ++k) {
       const uint32_t c = (k * lanes + lane) * kGroup;
@@ -134,7 +133,6 @@ template <typename T, typename H>
 __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) {
   __shared__ float slots[2][1][kSlots];
   const uint64_t offset = a.join ? drop_offset(a.drop) : 0u;
-  const float count = static_cast<float>(a.cols);
   for (uint32_t r = blockIdx.x; r < a.total; r += gridDim.x) {
     float s[1] = {0.0f};
     for (uint32_t c = threadIdx.x * kGroup; c < a.cols; c += kWideThreads * kGroup) {
@@ -143,7 +141,7 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) 
       for (uint32_t j = 0; j < kGroup; ++j) s[0] += c + j < a.cols ? v[j] : 0.0f;
     }
     sum_block(s, slots[0], kWideThreads / 64);
-    const float mean = s[0] / count;
+    const float mean = mean_of(s[0], a.count);
     s[0] = 0.0f;
     for (uint32_t c = threadIdx.x * kGroup; c < a.cols; c += kWideThreads * kGroup) {
       float v[kGroup];
@@ -154,7 +152,7 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) 
       }
     }
     sum_block(s, slots[1], kWideThreads / 64);
-    const float rstd = 1.0f / sqrtf(s[0] / count + a.eps);
+    const float rstd = rstd_of(s[0], a.count, a.eps);
     for (uint32_t c = threadIdx.x * kGroup; c < a.cols; c += kWideThreads * kGroup) {
       float v[kGroup], g[kGroup], b[kGroup];
       form_h<T, H>(v, a, offset, r, c);

@@ -87,3 +87,28 @@ def test_what_a_scale_brings_back(rows, vocab, dtype, scale):
         units, least = 16.0 + 2.3 * (-v.double()).clamp(max=200.0) + 2 * math.log2(abs(scale) * rows), 2.0 ** -126 + R.LEAST[dtype]
     least = max(least, 2.0 ** -125 * abs(scale) / 2.0 ** 96)
     R.close(d, want, (units * U * p + 2 * U * hot) * abs(scale) + R.UNIT[dtype] * 1.01 * want.abs() + least, "dlogits")
+
+
+@pytest.mark.parametrize("join", [False, True], ids=["norm", "join"])
+@pytest.mark.parametrize("cols", [6, 10, 24, 100, 333, 768, 1000, 1601, 2304, 6144, 10484, 12288, 20000, 33000])
+def test_statistics_are_rounded_once(cols, join):
+    """Rows of whole numbers, whose sums are exact: the mean is the quotient to the nearest, on every route the same; where
+    the mean is whole the sum of squares is exact too, and rstd what correct rounding makes of the quotient and of eps
+    added, and then of the inverse root (half a unit in its last place, and a 64th for the residual's own rounding)."""
+    rng = np.random.default_rng(cols)
+    rows = 24
+    v = rng.integers(-20, 21, (rows, cols)).astype(np.float64)
+    short = (-v.sum(1)) % cols * (np.arange(rows) % 2)       # every other row: a whole mean
+    v += np.arange(cols)[None] < short[:, None]
+    x = torch.from_numpy(v).float().cuda()
+    if join:
+        _, _, mean, rstd = ops.compams_dropout_add_norm_forward(torch.zeros_like(x), x, None, None, 0.0, 1, eps=0.25)
+    else:
+        _, mean, rstd = ops.compams_layer_norm_forward(x, None, None, 0.25)
+    assert np.array_equal(mean.cpu().numpy(), np.float32(v.sum(1)) / np.float32(cols))
+    whole = v[1::2]
+    squares = ((whole - whole.mean(1, keepdims=True)) ** 2).sum(1)
+    assert squares.max() < 2 ** 24
+    var = (np.float32(squares) / np.float32(cols) + np.float32(0.25)).astype(np.float64)
+    got = rstd[1::2].cpu().numpy()
+    assert np.all(np.abs(got.astype(np.float64) - var ** -0.5) <= (0.5 + 1 / 64) * np.spacing(got))
