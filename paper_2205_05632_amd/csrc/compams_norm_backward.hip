@@ -89,6 +89,11 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 && JOIN ? 
         if (JOIN && (FULL || a.dh)) raw_g[k] = load_early<WIDTH>(row_of<H>(a.dh, a.ld_dh, r), c, a.cols);
       }
       const float mean = a.mean[r], rstd = a.rstd[r];
+      // Beyond the row's last column h and u are read as 0, and z is the mean's size: nothing in a product with u while that
+      // is a number.  Where it is none, the entries that these statistics belong to are the mean, and their z is 0.  (Telling
+      // those columns apart takes a join of 8 x 4096 x 773 a sixth longer; lanes without a group are left out below.)
+      constexpr bool kEnd = WIDTH == kAnyWidth || WIDTH == kOneGroup;
+      const float rstd_of_sums = !kEnd || fabsf(mean * rstd) < INFINITY ? rstd : 0.0f;
       float s[2] = {0.0f, 0.0f};
 #pragma unroll
       for (uint32_t k = 0; k < NG; ++k) {
@@ -98,13 +103,15 @@ __global__ __launch_bounds__(KIND == kInWave ? kTeamThreads : NG == 2 && JOIN ? 
         settle_if<WIDTH, H>(raw_h[k], c, a.cols);
         unpack(u, raw_y[k]);
         unpack(z, raw_h[k]);
+        const float before = s[1];
 #pragma unroll
         for (uint32_t j = 0; j < kGroup; ++j) {
           // (columns beyond the last: dy and, read from gamma's end, the weight are 0)
           u[j] *= g[k][j];
           s[0] += u[j];
-          s[1] = fmaf(u[j], (z[j] - mean) * rstd, s[1]);
+          s[1] = fmaf(u[j], (z[j] - mean) * rstd_of_sums, s[1]);
         }
+        if (WIDTH == kWholeGroups && c >= a.cols) s[1] = before;
       }
       sum_over_team<KIND>(s, slots[turn], lanes, team);
       if (KIND == kPair && spare) continue;

@@ -112,3 +112,28 @@ def test_statistics_are_rounded_once(cols, join):
     var = (np.float32(squares) / np.float32(cols) + np.float32(0.25)).astype(np.float64)
     got = rstd[1::2].cpu().numpy()
     assert np.all(np.abs(got.astype(np.float64) - var ** -0.5) <= (0.5 + 1 / 64) * np.spacing(got))
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["without_gamma", "with_gamma"])
+@pytest.mark.parametrize("join", [False, True], ids=["norm", "join"])
+@pytest.mark.parametrize("cols", [3, 7, 9, 72, 100, 333, 776, 1000, 1601, 2056, 2500, 6000, 6001, 9000, 20001])
+def test_gradients_of_equal_entries_of_any_size(cols, join, whole):
+    """Rows whose entries are all the same have z = 0 and a gradient of rstd (u - mean u), however large the entries are: what
+    stands beside the row's columns in a lane has no part in its sums."""
+    rng = np.random.default_rng(cols)
+    rows = 9
+    size = np.float32(10.0) ** np.linspace(0, 38, rows, dtype=np.float32)
+    x = torch.from_numpy(size)[:, None].expand(rows, cols).contiguous().cuda()
+    mean, rstd = torch.from_numpy(size).cuda(), torch.full((rows,), 300.0, device="cuda")
+    dy = torch.from_numpy(rng.standard_normal((rows, cols))).float()
+    one, gamma = torch.ones(cols), torch.ones(cols, device="cuda") if whole else None
+    if join:
+        dh = torch.zeros_like(x) if whole else None
+        _, dx, dgamma, dbeta, _ = ops.compams_dropout_add_norm_backward(dy.cuda(), dh, x, mean, rstd, gamma, 0.0, 1)
+    else:
+        dx, dgamma, dbeta = ops.compams_layer_norm_backward(dy.cuda(), x, mean, rstd, gamma)
+    want, bound = R.norm_backward(dy.double(), None, x.cpu().double(), mean.cpu().double(), rstd.cpu().double(), one.double(),
+                                  F32, F32, 1)
+    R.close(dx, want[1], bound[1], "dx")
+    R.close(dgamma, want[2], bound[2], "dgamma")
+    R.close(dbeta, want[3], bound[3], "dbeta")
