@@ -189,9 +189,11 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) 
 // Beyond 16384 columns four groups a lane, norm, whole groups: 8 x 300 x 20000 69.4 | 82.4, the route of wide rows 74.5 | 88.3,
 // x 30008 95.7 | 118 and 108 | 136.  With the masks of a row's end they do not fit the registers (600 x 10484 as 384 x
 // 4 121, as 704 x 2 66.9), and a join's never (8 x 200 x 32768 258 | 322, the route of wide rows 178 | 227).
-Team forward_team(uint32_t cols, bool join) {
+// `whole`: rows of whole groups and nothing left out of the call.  Anything else has the masks, whatever the width (without
+// beta 8 x 300 x 30008 float16 four groups a lane 124, the route of wide rows 87; a join without bias 8 x 3117 x 1600 pair 56,
+// 256 46).
+Team forward_team(uint32_t cols, bool join, bool whole) {
   const uint32_t groups = (cols + kGroup - 1) / kGroup;
-  const bool whole = cols % kGroup == 0;
   if (groups <= 64) {
     if (groups <= 8) return {kInWave, 8, 1};
     if (groups <= 16) return {kInWave, 8, 2};
@@ -211,13 +213,16 @@ Team forward_team(uint32_t cols, bool join) {
   return {kBlock, each ? (groups + 64 * each - 1) / (64 * each) * 64 : 0, each};
 }
 
+bool whole_groups(const NormArgs& k) {
+  return k.cols % kGroup == 0 && k.gamma && k.beta && k.mean && k.rstd && (!k.join || (k.bias && k.residual && k.h));
+}
+
 template <typename T, typename H, bool JOIN>
 void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
   const uint32_t threads = team_threads(t), together = threads / t.lanes;
   const dim3 grid(blocks_for((static_cast<uint64_t>(k.total) + together - 1) / together));
   const dim3 block(threads);
-  const bool all = k.gamma && k.beta && k.mean && k.rstd && (!JOIN || (k.bias && k.residual && k.h));
-  const bool full = all && k.cols == t.lanes * t.each * kGroup, whole = all && k.cols % kGroup == 0;
+  const bool whole = whole_groups(k), full = whole && k.cols == t.lanes * t.each * kGroup;
 #define COMPAMS_FORWARD_OF(NG, KIND, WIDTH) \
   hipLaunchKernelGGL((k_norm_forward<T, H, NG, KIND, JOIN, WIDTH>), grid, block, 0, stream, k, t.lanes)
 #define COMPAMS_FORWARD(NG, KIND)                           \
@@ -244,8 +249,11 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
     switch (t.each) {
       case 1: COMPAMS_FORWARD(1, kBlock); break;
       case 2: COMPAMS_FORWARD(2, kBlock); break;
-      default:
-        if constexpr (!JOIN) COMPAMS_FORWARD(4, kBlock);
+      default:  // (of whole groups alone)
+        if constexpr (!JOIN) {
+          if (full) COMPAMS_FORWARD_OF(4, kBlock, kFullGroups);
+          else COMPAMS_FORWARD_OF(4, kBlock, kWholeGroups);
+        }
         break;
     }
   }
@@ -256,7 +264,7 @@ void launch_team(const Team& t, const NormArgs& k, hipStream_t stream) {
 }  // namespace
 
 hipError_t norm_forward(const NormArgs& k, int32_t type, int32_t stream_type, hipStream_t stream) {
-  const Team team = forward_team(k.cols, k.join);
+  const Team team = forward_team(k.cols, k.join, whole_groups(k));
   return by_types(type, stream_type, [&](auto t, auto h) {
     using T = decltype(t);
     using H = decltype(h);

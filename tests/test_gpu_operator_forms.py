@@ -1,0 +1,77 @@
+"""Forms of the operators' kernels that a size, a type or an absent argument picks: each against the formulas in 64 bits."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import operator_reference as R
+from paper_2205_05632_amd import binding as B
+from paper_2205_05632_amd import operators as ops
+from test_gpu_operators import BF16, EPS, F16, F32, IDS, TYPES, matrix, room, untouched, vector
+
+pytestmark = pytest.mark.gpu
+
+
+def norm_without(what, cols, types, rows=5):
+    """A layer norm forward, through the C ABI, with the arguments in `what` left out."""
+    dtype, stream = types
+    rng = np.random.default_rng(cols + TYPES.index(types))
+    x, x64 = matrix(rng, rows, cols, stream, 8, 0, 2.0)
+    gamma, g64 = vector(rng, cols, 1.0)
+    beta, b64 = vector(rng, cols)
+    y, base = room(rows, cols, dtype, 8)
+    mean, rstd = (torch.full((rows,), 7.0, device="cuda") for _ in range(2))
+    given = {"gamma": gamma, "beta": beta, "mean": mean, "rstd": rstd}
+    a = ops.compams_norm(n=1, rows=rows, cols=cols, type=ops._TYPE[dtype], stream_type=ops._TYPE[stream], eps=EPS, h=x.data_ptr(),
+                         ld_h=cols + 8, y=y.data_ptr(), ld_y=cols + 8)
+    for k, t in given.items():
+        setattr(a, k, None if k in what else t.data_ptr())
+    assert B.lib().compams_layer_norm_forward(ctypes.byref(a), torch.cuda.current_stream().cuda_stream) == 0
+    g64 = torch.ones_like(g64) if "gamma" in what else g64
+    b64 = torch.zeros_like(b64) if "beta" in what else b64
+    want, bound = R.norm_forward(x64, g64, b64, EPS, dtype)
+    R.close(y, want[0], bound[0], "y")
+    untouched(base, 0, cols)
+    for k, w, b in zip(("mean", "rstd"), want[1:], bound[1:]):
+        if k in what:
+            assert bool((given[k] == 7.0).all())
+        else:
+            R.close(given[k], w, b, k)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("what", [(), ("gamma",), ("beta",), ("gamma", "beta"), ("mean",), ("mean", "rstd")],
+                         ids=lambda w: "without_" + "_".join(w) if w else "all")
+@pytest.mark.parametrize("cols", [1600, 16392, 20008, 30008, 32760, 32768])
+def test_wide_norms_of_whole_groups(cols, what, types):
+    """Rows that a workgroup holds four groups a lane of, lanes idle or none, and the same rows in calls that leave something
+    out, which another route takes."""
+    norm_without(what, cols, types)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("cols", [768, 1600, 1792])
+@pytest.mark.parametrize("what", ["bias", "residual", "gamma", "beta"])
+def test_joins_without(what, cols, types):
+    """Joins of whole groups that leave one argument out."""
+    dtype, stream = types
+    rng = np.random.default_rng(cols + TYPES.index(types))
+    total, p, seed = 21, 0.2, 77
+    x, x64 = matrix(rng, total, cols, dtype)
+    res, r64 = matrix(rng, total, cols, stream, 0, 0, 2.0)
+    (gamma, g64), (beta, b64), (bias, c64) = vector(rng, cols, 1.0), vector(rng, cols), vector(rng, cols)
+    h = torch.empty(total, cols, dtype=stream, device="cuda")
+    args = {"residual": res, "gamma": gamma, "beta": beta, "bias": bias}
+    args[what] = None
+    _, y, mean, rstd = ops.compams_dropout_add_norm_forward(x, args["residual"], args["gamma"], args["beta"], p, seed, bias=args["bias"],
+                                                            h=h)
+    one, zero = torch.ones_like(g64), torch.zeros_like(g64)
+    g64, b64, c64 = (one if what == "gamma" else g64), (zero if what == "beta" else b64), (zero if what == "bias" else c64)
+    r64 = torch.zeros_like(r64) if what == "residual" else r64
+    branch = torch.where(R.kept(total, cols, p, seed, 0), (x64 + c64) * R.factor(p), torch.zeros_like(x64))
+    h64 = r64 + branch
+    R.close(h, h64, R.rounding(h64, stream) + 4.04 * R.U * (branch.abs() + h64.abs()), "h")
+    want, bound = R.norm_forward(h64, g64, b64, EPS, dtype)
+    for got, w, b, name in zip((y, mean, rstd), want, bound, ("y", "mean", "rstd")):
+        R.close(got, w, b, name)
