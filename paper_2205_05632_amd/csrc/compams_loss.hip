@@ -199,7 +199,7 @@ void k_loss(LossArgs a, uint32_t lanes) {
     const uint32_t end = lane < 8 ? (lane < head ? lane : a.vocab) : lane < 16 ? tail + (lane - 8) : a.vocab;
     const float at_end = end < a.vocab ? to_float(logits[end]) : -INFINITY;
     const uint32_t w = r / a.rows;
-    // (less than 2^24 of them: exact in fp32; a.counts is there where there may be more)
+    // (2^12 of them at most: exact in fp32; a.counts is there where there may be more)
     const float count = a.counts || KIND == kWorkerRows ? 0.0f : static_cast<float>(count_rows<4>(a, w, lane, lanes));
     const bool inside = target >= 0 && target < static_cast<int64_t>(a.vocab);
     float of_target = inside ? to_float(logits[target]) : 0.0f;
@@ -508,13 +508,14 @@ void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
 #undef COMPAMS_LOSS
 }
 
-// Whether every row's team counts its worker's targets by itself: where they are few bytes beside the row's logits, or few in
-// all, and the launch that would count them costs more (float16 and bfloat16, us a call with it / without: 8 x 105 x 83 16.5 /
-// 14.2, 8 x 256 x 512 17.1 / 14.3, 16 x 512 x 1000 16.7 / 15.5; 16 x 1024 x 1000 22.3 / 25.3).  (They are then counted in
-// fp32, exactly: fewer than 2^24.)
+// Whether every row's team counts its worker's targets by itself: where they are few for a row, or few beside its logits, and
+// few in all, for a launch that counts them costs 2 to 3 us and then reads each only once (us a call with it / without, targets
+// of 64 bits; float16 and bfloat16: 8 x 105 x 83 16.5 / 14.2, 16 x 512 x 1000 16.7 / 15.5, 16 x 1024 x 1000 22.3 / 25.3, 1 x 2000 x
+// 50257 80.3 / 78.6, 8 x 1024 x 50257 303 / 307, 4 x 1500 x 20000 93.2 / 95.2, 1 x 4000 x 50257 158 / 168, 1 x 8000 x 50257 297 / 323;
+// fp32: 8 x 1024 x 8192 94.7 / 91.8, x 32000 350 / 344, 1 x 4000 x 50257 348 / 363).  (They are then counted in fp32, exactly.)
 bool counts_inside(const LossArgs& k, const Team& t) {
-  const bool few = k.rows <= 512 && static_cast<uint64_t>(k.total) * k.rows <= 1u << 22;
-  return t.each != 0 && (few || k.rows <= k.vocab / 4) && k.rows < (1u << 24);
+  const uint64_t in_all = static_cast<uint64_t>(k.total) * k.rows;
+  return t.each != 0 && ((k.rows <= 512 && in_all <= 1u << 22) || (k.rows <= k.vocab / 4 && in_all <= 1u << 23));
 }
 
 bool loss_valid(const compams_loss* a) {

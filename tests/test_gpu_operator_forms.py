@@ -75,3 +75,28 @@ def test_joins_without(what, cols, types):
     want, bound = R.norm_forward(h64, g64, b64, EPS, dtype)
     for got, w, b, name in zip((y, mean, rstd), want, bound, ("y", "mean", "rstd")):
         R.close(got, w, b, name)
+
+
+def counted_first(n, rows, vocab, dtype=BF16, targets=torch.int64):
+    """Whether a call counts the workers' targets in a launch of its own, which leaves the counts at its workspace's start; its
+    outputs are checked on the way."""
+    g = torch.Generator(device="cuda").manual_seed(n + rows + vocab)
+    x = torch.randn(n * rows, vocab, generator=g, device="cuda").to(dtype)
+    t = torch.randint(0, vocab, (n * rows,), generator=g, device="cuda").to(targets)
+    t[::3] = -100
+    ws = torch.full((1 << 16,), 0x5A, dtype=torch.uint8, device="cuda")
+    mean, losses, _ = ops.compams_cross_entropy(x, t, n, dlogits=x, workspace=ws)
+    count = (t != -100).reshape(n, rows).sum(1)
+    assert torch.allclose(mean.double() * count, losses.double().reshape(n, rows).sum(1), rtol=1e-5)
+    head = ws[:4 * n].view(torch.int32)
+    if bool((ws[:4 * n] == 0x5A).all()):
+        return False
+    assert torch.equal(head, count.int())
+    return True
+
+
+@pytest.mark.parametrize("n,rows,vocab,launch", [(1, 8000, 33000, True), (8, 1100, 8192, True), (1, 4100, 16500, True), (1, 2000, 8192, False),
+                                                 (8, 500, 1000, False), (1, 1100, 260, True)])
+def test_many_targets_are_counted_once(n, rows, vocab, launch):
+    """Every row's team counts its worker's targets only where those are few, and not because the rows are long."""
+    assert counted_first(n, rows, vocab) == launch
