@@ -447,12 +447,12 @@ struct Team {
   RowKind kind;
   uint32_t lanes, each;
 };
-Team loss_team(uint32_t n, uint32_t rows, uint32_t groups) {
+Team loss_team(uint32_t rows, uint32_t groups) {
   // A few short rows of each worker: the launch that would form the means costs more than going over them one after another
   // (8 x 32 x 1000 fp32: 10.5 us a call, with a launch more 12.5; on the device 8.2 and 4.0 + 2.8 and a gap).  However many
   // workers there are, so that a worker's losses are the same bits beside any others (300 x 32 x 1000 fp32 16.6 and 16.9, 1000 x
-  // 4 x 40 11.1 and 13.1, 3000 x 32 x 256 bfloat16 47.5 and 35.2); a grid has room for a million.
-  if (n <= 1u << 20 && rows <= 2 * kLossWaves && groups <= 256) return {kWorkerRows, 64, groups <= 64 ? 1u : groups <= 128 ? 2u : 4u};
+  // 4 x 40 11.1 and 13.1, 3000 x 32 x 256 bfloat16 47.5 and 35.2).
+  if (rows <= 2 * kLossWaves && groups <= 256) return {kWorkerRows, 64, groups <= 64 ? 1u : groups <= 128 ? 2u : 4u};
   // Short rows: few lanes with up to four groups, so that what a row costs besides its columns (its reductions, logarithm and
   // quotients) is shared by the rows of a wavefront.  (16 x 9882 rows of float16, us on the device and the two small launches:
   // 133 columns 32 x 1 52.3, 16 x 2 43.6, 16 x 4 55.4; 260 columns 64 x 1 92.5, 32 x 2 75.3, 16 x 4 63.0, 16 x 8 90.0;
@@ -514,6 +514,7 @@ void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
 // 50257 80.3 / 78.6, 8 x 1024 x 50257 303 / 307, 4 x 1500 x 20000 93.2 / 95.2, 1 x 4000 x 50257 158 / 168, 1 x 8000 x 50257 297 / 323;
 // fp32: 8 x 1024 x 8192 94.7 / 91.8, x 32000 350 / 344, 1 x 4000 x 50257 348 / 363).  (They are then counted in fp32, exactly.)
 bool counts_inside(const LossArgs& k, const Team& t) {
+  if (t.kind == kWorkerRows) return true;  // (the workgroup that has all of a worker's rows)
   const uint64_t in_all = static_cast<uint64_t>(k.total) * k.rows;
   return t.each != 0 && ((k.rows <= 512 && in_all <= 1u << 22) || (k.rows <= k.vocab / 4 && in_all <= 1u << 23));
 }
@@ -571,7 +572,7 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream) {
              : a->mean_loss ? reinterpret_cast<float*>(static_cast<char*>(a->workspace) + counts_bytes(*a)) : nullptr;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const uint32_t each = 16 / static_cast<uint32_t>(type_size(a->type));
-  const Team team = loss_team(k.n, k.rows, (k.vocab + each - 1) / each);
+  const Team team = loss_team(k.rows, (k.vocab + each - 1) / each);
   if (!counts_inside(k, team)) {
     k.counts = static_cast<uint32_t*>(a->workspace);
     hipLaunchKernelGGL(k_loss_count, dim3(k.n), dim3(kLossThreads), 0, stream, k);

@@ -100,3 +100,10 @@ def counted_first(n, rows, vocab, dtype=BF16, targets=torch.int64):
 def test_many_targets_are_counted_once(n, rows, vocab, launch):
     """Every row's team counts its worker's targets only where those are few, and not because the rows are long."""
     assert counted_first(n, rows, vocab) == launch
+
+
+@pytest.mark.parametrize("n,rows,vocab", [(5000, 32, 100), (5000, 30, 24), (300, 32, 1000)])
+@pytest.mark.parametrize("targets", [torch.int32, torch.int64], ids=["i32", "i64"])
+def test_few_rows_of_many_workers_are_one_launch(n, rows, vocab, targets):
+    """A workgroup that has all of a worker's rows counts them: no launch for that, however many workers there are."""
+    assert not counted_first(n, rows, vocab, targets=targets)
