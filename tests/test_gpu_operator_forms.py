@@ -8,7 +8,7 @@ import torch
 import operator_reference as R
 from paper_2205_05632_amd import binding as B
 from paper_2205_05632_amd import operators as ops
-from test_gpu_operators import BF16, EPS, F16, F32, IDS, TYPES, matrix, room, untouched, vector
+from test_gpu_operators import BF16, EPS, F16, F32, IDS, TYPES, matrix, room, test_dropout as dropout_test, untouched, vector
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,33 @@ def test_many_targets_are_counted_once(n, rows, vocab, launch):
 def test_few_rows_of_many_workers_are_one_launch(n, rows, vocab, targets):
     """A workgroup that has all of a worker's rows counts them: no launch for that, however many workers there are."""
     assert not counted_first(n, rows, vocab, targets=targets)
+
+
+@pytest.mark.parametrize("kinds", [(F32, F32), (F16, F16), (BF16, BF16), (F32, F16), (F32, BF16), (F16, F32), (BF16, F32)],
+                         ids=lambda k: f"{k[0]}_{k[1]}".replace("torch.", ""))
+@pytest.mark.parametrize("total,cols", [(37, 512), (9, 1000), (23, 1024), (37, 1536), (1, 2048), (11, 6000), (6, 16384)])
+def test_dropout_of_rows_that_fill_wavefronts(total, cols, kinds):
+    """Whole groups, 64 lanes side by side and more, rows that end within a workgroup's turn: alone and added to a stream."""
+    dropout_test(total, cols, kinds)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,rows,vocab,pad", [(1100, 32, 1000, 0), (7, 2500, 1000, 0), (8, 4096, 600, 1), (3, 1800, 4096, 0), (2, 1100, 9000, 8),
+                                              (2, 240, 50257, 0), (3, 90, 70001, 0), (2, 70, 140000, 0)])
+def test_gradients_that_do_not_fit_the_cache(n, rows, vocab, pad, dtype):
+    """Gradients of more than 32 MB are streamed past it: every kind of team, beside the logits and over them."""
+    assert n * rows * vocab * 2 > 32 << 20
+    rng = np.random.default_rng(vocab)
+    g = torch.Generator(device="cuda").manual_seed(vocab + n)
+    base = torch.randn(n * rows, vocab + pad, generator=g, device="cuda").mul_(2.5).to(dtype)
+    x = base[:, :vocab]
+    t = torch.from_numpy(rng.integers(0, vocab, n * rows)).cuda()
+    t[::5] = -100
+    dl, out = room(n * rows, vocab, dtype, pad)
+    got = ops.compams_cross_entropy(x, t, n, grad_scale=64.0, dlogits=dl)
+    want, bound = R.cross_entropy(x.double(), t, n, -100, 64.0, dtype)
+    for a, w, b, what in zip(got, want, bound, ("mean_loss", "losses", "dlogits")):
+        R.close(a, w.cpu(), b.cpu(), what)
+    untouched(out, 0, vocab)
+    over = ops.compams_cross_entropy(x, t, n, grad_scale=64.0, dlogits=x)
+    assert over[2].data_ptr() == x.data_ptr() and all(torch.equal(a, b) for a, b in zip(over, got))
