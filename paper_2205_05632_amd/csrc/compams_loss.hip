@@ -75,9 +75,9 @@ __global__ __launch_bounds__(kLossThreads) void k_loss_count(LossArgs a) {
 // exp(v - top) = 2^((v - top) log2(e)) for v <= top.  (The difference first: with log2(e) top taken off in one multiply-add
 // instead, 2 % faster at 8192 x 50257, tops from 1e9 on leave more of their rounding than an exponent holds.)
 //
-// Rows of 32 bits: the exponent as a whole number and a part in -1/2 .. 1/2, which is formed with the product's and log2(e)'s own
-// rounding put right, so that the result is off by three units of 2^-24 at any distance.  (Rounded once, an exponent of -60 is
-// off by up to 2^-19: 22 such units of the result.)  Distances beyond 200 are taken as that: whatever they are, 0 is left.
+// Rows of 32 bits: the exponent as a whole number and a part in -1/2 .. 1/2, which is formed with the rounding of the product
+// and of log2(e) put right, so that the result is off by three units of 2^-24 at any distance.  (Rounded once, an exponent of
+// -60 is off by up to 2^-19: 22 such units of the result.)  Distances beyond 200 are taken as that: whatever they are, 0 is left.
 // Rows of 16 bits: the product rounded once, three instructions for ten.  With the difference's rounding an entry is off by
 // 2.3 (top - v) units of 2^-24, at a distance of 87, the largest that leaves a normal number, by 2^-16 of itself, where its
 // gradient is rounded to 2^-9 or 2^-12; of their sum it is the mean distance by weight, log(vocab) at most.  Results below
@@ -510,9 +510,9 @@ void launch_loss(const Team& t, const LossArgs& k, hipStream_t stream) {
 
 // Whether every row's team counts its worker's targets by itself: where they are few for a row, or few beside its logits, and
 // few in all, for a launch that counts them costs 2 to 3 us and then reads each only once (us a call with it / without, targets
-// of 64 bits; float16 and bfloat16: 8 x 105 x 83 16.5 / 14.2, 16 x 512 x 1000 16.7 / 15.5, 16 x 1024 x 1000 22.3 / 25.3, 1 x 2000 x
-// 50257 80.3 / 78.6, 8 x 1024 x 50257 303 / 307, 4 x 1500 x 20000 93.2 / 95.2, 1 x 4000 x 50257 158 / 168, 1 x 8000 x 50257 297 / 323;
-// fp32: 8 x 1024 x 8192 94.7 / 91.8, x 32000 350 / 344, 1 x 4000 x 50257 348 / 363).  (They are then counted in fp32, exactly.)
+// of 64 bits; float16 and bfloat16: 8 x 105 x 83 16.5 / 14.2, 16 x 512 x 1000 16.7 / 15.5, 16 x 1024 x 1000 22.3 / 25.3,
+// 1 x 2000 x 50257 80.3 / 78.6, 4 x 1500 x 20000 93.2 / 95.2, 1 x 4000 x 50257 158 / 168, 1 x 8000 x 50257 297 / 323; fp32:
+// 8 x 1024 x 8192 94.7 / 91.8, 8 x 1024 x 32000 350 / 344, 1 x 4000 x 50257 348 / 363).  (They are counted in fp32, exactly.)
 bool counts_inside(const LossArgs& k, const Team& t) {
   if (t.kind == kWorkerRows) return true;  // (the workgroup that has all of a worker's rows)
   const uint64_t in_all = static_cast<uint64_t>(k.total) * k.rows;
@@ -579,7 +579,7 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream) {
   }
   if (k.total) {
     // What does not stay in the memory-side cache until it is read again need not pass through it (8192 rows of bfloat16,
-    // streamed / not: vocabulary 4096 30.1 / 39.6 us, 16384 95.6 / 100, 32000 180 / 188, 50257 308 / 313).
+    // streamed / not: vocabulary 4096 29.5 / 35.8 us, 16384 98.3 / 102, 32000 182 / 189, 50257 312 / 317).
     const bool stream_out = static_cast<uint64_t>(k.total) * k.vocab * type_size(a->type) > kStreamBytes;
     const auto launch = [&](auto t) {
       if (stream_out) launch_loss<decltype(t), true>(team, k, stream);

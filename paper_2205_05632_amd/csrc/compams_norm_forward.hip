@@ -170,25 +170,28 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(NormArgs a) 
 }
 
 // The team that a row of `groups` groups is given.  No lane to spare counts most; then few lanes, so that a wavefront's rows
-// share what a row costs besides its columns; then few registers.  The best and the next best, us, norm / join:
-// 8 x 4096 rows (65536 of 768) from bfloat16 and a stream in fp32
-//    768: 32 x 3 53.8 / 115, pair of 96 53.8 / 120, 128 56 / 127        1000: 64 x 2 37.7 / 80, 128 37.8 / 86
-//   1280: pair of 160 46 / 105, 64 x 3 49 / 124                         2048: 256 76 / 168, 64 x 4 79 / 151
-//   1601 (bfloat16 stream): pair of 224 57 / 126, 256 61 / 117          8 x 3117 x 1600: pair of 224 46.6 / 101, 256 47.0 / 107
-// 8 x 6167 rows (13028 of 68, 2048 of 2304 and 2900, 1000 of 6144 and 7168), all float16 | bfloat16 and fp32
-//     68: 8 x 2 11.6 / 21.4 | 12.0 / 22.4, 16 13.9 / 24.4 | 14.0 / 24.5
-//    200: 16 x 2 11.3 / 19.9 | 12.5 / 29.5, 32 13.5 / 22.8 | 14.1 / 28.9
-//    300: 16 x 3 15.0 / 34.8 | 19.0 / 51.7, 64 23.2 / 43.1 | 24.8 / 46.2
-//    384: 16 x 3 14.8 / 31.4 | 21.3 / 45.1, 64 23.6 / 42.4 | 26.4 / 50.0
-//    512: 32 x 2 20.6 / 38.6 | 28.3 / 57.8, 64 21.0 / 39.1 | 28.1 / 60.1
-//   2304: 192 x 2 39.3 / 73.6 | 47.0 / 98.0, 320 41.4 / 77.8 | 48.2 / 100
-//   2900: 192 x 2 49.5 / 88.9 | 59.8 / 127, 384 54.4 / 101 | 61.2 / 128
-//   6144: 384 x 2 53.7 / 107 | 62.8 / 132, 768 59.7 / 83.8 | 65.8 / 122
-//   7168: 512 x 2 60.9 / 115 | 69.7 / 144, 896 70.8 / 108 | 78.6 / 160
-// (before whole groups had a variant of their own, which takes up to a quarter less: 8 x 6167 x 200, join, 15.7 | 27.8)
-// Beyond 16384 columns four groups a lane, norm, whole groups: 8 x 300 x 20000 69.4 | 82.4, the route of wide rows 74.5 | 88.3,
-// x 30008 95.7 | 118 and 108 | 136.  With the masks of a row's end they do not fit the registers (600 x 10484 as 384 x
-// 4 121, as 704 x 2 66.9), and a join's never (8 x 200 x 32768 258 | 322, the route of wide rows 178 | 227).
+// share what a row costs besides its columns; then few registers.  What is taken and another, us, norm / join, everything
+// there, all float16 | from bfloat16 and a stream in fp32:
+// 8 x 4096 rows (65536 of 768, 8 x 3117 of 1600 and 1601)
+//    768: 32 x 3 38.1 / 72.4 | 52.3 / 110, pair of 96 38.0 / 74.6 | 52.4 / 115, 128 43.5 / 79.6 | 53.9 / 125
+//   1000: 64 x 2 26.9 / 53.1 | 36.2 / 80.5, 128 27.3 / 55.6 | 36.7 / 82.6
+//   1280: pair of 160 36.2 / 66.7 | 45.5 / 100, 64 x 3 39.7 / 70.0 | 47.5 / 103, 192 35.4 / 70.5 | 46.9 / 105
+//   1600: pair of 224 36.2 / 67.5 | 46.3 / 96.6, 256 34.9 / 70.1 | 46.2 / 102
+//   1601: pair of 224 44.0 / 92.3 | 48.8 / 109, 256 45.3 / 84.5 | 47.9 / 106 (a join takes 256)
+//   2048: 256 56.0 / 108 | 74.8 / 159, 128 x 2 56.8 / 112 | 76.9 / 157, 64 x 4 (a join) 113 | 145
+// 8 x 6167 rows (13028 of 68, 2048 of 2304 and 2900, 1000 of 6144 and 7168)
+//     68: 8 x 2 11.5 / 20.0 | 11.9 / 21.3, 16 13.6 / 22.3 | 14.0 / 23.3
+//    200: 16 x 2 9.3 / 15.2 | 11.0 / 27.3, 32 9.3 / 14.4 | 10.9 / 25.6
+//    300: 16 x 3 15.1 / 33.8 | 17.9 / 50.3, 64 22.7 / 41.8 | 24.0 / 45.1 (a join takes 64)
+//    384: 16 x 3 13.3 / 30.7 | 21.1 / 43.6, 64 15.5 / 30.5 | 21.8 / 45.8
+//    512: 32 x 2 20.5 / 38.0 | 27.8 / 56.3, 64 21.0 / 38.5 | 27.6 / 58.5
+//   2304: 192 x 2 38.1 / 69.5 | 47.0 / 95.3, 320 38.8 / 68.3 | 46.7 / 97.0
+//   2900: 192 x 2 47.6 / 82.2 | 58.8 / 120, 384 52.4 / 95.0 | 60.3 / 121
+//   6144: 384 x 2 51.5 / 102 | 61.6 / 126, 768 58.8 / 79.9 | 64.4 / 118 (a join takes 768)
+//   7168: 512 x 2 62.3 / 113 | 70.5 / 139, 896 72.3 / 104 | 80.3 / 158 (a join takes 896)
+// Beyond 16384 columns four groups a lane, norm, whole groups: 8 x 300 x 20000 65.5 | 81.7, the route of wide rows 73.3 | 87.5,
+// x 30008 90.2 | 115 and 109 | 134 (six or seven registers do not fit).  With the masks of a row's end many more do not (600 x
+// 10484 as 384 x 4 121, as 704 x 2 66.9), nor with a join (8 x 200 x 32768 258 | 322, the route of wide rows 178 | 227).
 // `whole`: rows of whole groups and nothing left out of the call.  Anything else has the masks, whatever the width (without
 // beta 8 x 300 x 30008 float16 four groups a lane 124, the route of wide rows 87; a join without bias 8 x 3117 x 1600 pair 56,
 // 256 46).
