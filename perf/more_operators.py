@@ -209,7 +209,7 @@ def _run_own(s):
         got = ops.compams_linear_cross_entropy(s["x"], s["weight"], s["targets"], c["n"], IGNORE, s["grad_scale"],
                                                gradient=c["gradient"], **out)
         return got if c["gradient"] else got[:2]
-    _, norms, factors = ops.compams_clip(s["tensors"], s["max_norm"], c["n"], scale=c["scale"], **out)
+    _, norms, factors = ops.compams_clip_gradients(s["tensors"], s["max_norm"], c["n"], scale=c["scale"], **out)
     return s["rows"], norms, factors
 
 
