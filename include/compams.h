@@ -470,6 +470,145 @@ typedef struct compams_loss {
 size_t compams_loss_workspace_size(const compams_loss* a);
 int compams_cross_entropy(const compams_loss* a, void* hip_stream);
 
+/* ---- Operators that hold matrix products, and the bound of a gradient ----------------------------------------
+ * The conventions are those of the section above (activations, strides, weights' gradients, streams, status codes), and:
+ *
+ *   - Weights are matrices of the activations' type, a row for every output (`hidden` or `vocab` rows of `cols` entries), rows
+ *     any distance apart; their gradients are one float matrix per worker: worker i's row r begins i * stride + r * ld floats
+ *     after the first (a parameter's place in a worker's row of g, with ld = cols and stride = that row's).
+ *   - Products are formed from the operands as they are, with fp32 sums.
+ *   - cols and hidden are at most COMPAMS_MOST_ENTRIES.
+ *   - Operands whose rows do not all begin on 16 bytes and hold a multiple of 16 bytes are first copied into the workspace,
+ *     so the workspace's size depends on pointers and strides too: ask with the fields that the call gets. */
+#define COMPAMS_MOST_ENTRIES (1 << 20)
+enum {
+  COMPAMS_SILU = 0,      /* a / (1 + exp(-a)) */
+  COMPAMS_GELU = 1,      /* a (1 + erf(a / sqrt 2)) / 2 */
+  COMPAMS_GELU_TANH = 2, /* a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2 */
+  COMPAMS_RELU = 3,      /* max(a, 0), slope 0 at 0 */
+  COMPAMS_SIGMOID = 4    /* 1 / (1 + exp(-a)) */
+};
+
+/* A gated feed-forward block up to its product.  For every row x:
+ *   a = gate_weight x + gate_bias,  b = up_weight x + up_bias,  m = act(a) b
+ * m is formed from a and b before these are rounded; a and b are stored only where they are asked for (the backward pass
+ * takes them as they were stored).  Backward, with the gradient dm of m:
+ *   dgate = dm b act'(a),  dup = dm act(a),  dgate_bias and dup_bias = the sums of both over the worker's rows, before they
+ *   are rounded */
+typedef struct compams_gated {
+  int32_t n;          /* workers, 1 <= n <= 65535 */
+  int64_t rows;       /* rows per worker, >= 0; n * rows < 2^31 */
+  int64_t cols;       /* entries of x (forward) */
+  int64_t hidden;     /* entries of a, b and m */
+  int32_t type;       /* of all matrices */
+  int32_t activation;
+  /* forward */
+  const void* x;           int64_t ld_x;
+  const void* gate_weight; int64_t ld_gate_weight; /* hidden x cols */
+  const void* up_weight;   int64_t ld_up_weight;
+  const float* gate_bias;                          /* hidden, or NULL: all 0 */
+  const float* up_bias;
+  void* m;    int64_t ld_m;
+  void* gate; int64_t ld_gate; /* forward: receives a, or NULL.  backward: a as it was stored */
+  void* up;   int64_t ld_up;   /* the same of b */
+  /* backward */
+  const void* dm; int64_t ld_dm;
+  void* dgate;    int64_t ld_dgate; /* may be gate, up or dm */
+  void* dup;      int64_t ld_dup;   /* may be another of them */
+  float* dgate_bias; int64_t ld_dgate_bias; /* per worker, or NULL */
+  float* dup_bias;   int64_t ld_dup_bias;
+  int32_t accumulate; /* 1: the biases' gradients are added to what is there; 0: written */
+  void* workspace;    /* DEVICE, 256-byte aligned */
+  size_t workspace_bytes;
+} compams_gated;
+
+/* Bytes of workspace that the call with these fields takes; 0 if none, and for an invalid configuration.  Host-only. */
+size_t compams_gated_forward_workspace_size(const compams_gated* a);
+size_t compams_gated_backward_workspace_size(const compams_gated* a);
+int compams_gated_forward(const compams_gated* a, void* hip_stream);
+int compams_gated_backward(const compams_gated* a, void* hip_stream);
+
+/* The gradients behind one projection of x, or behind two that read the same x:
+ *   dx = gate_weight' dgate + up_weight' dup
+ *   dgate_weight = the sum over the worker's rows of dgate x',  dup_weight = the sum of dup x'
+ * With dup NULL there is one projection (up_weight and dup_weight are NULL then). */
+typedef struct compams_projections {
+  int32_t n;
+  int64_t rows, cols, hidden;
+  int32_t type;
+  const void* dgate; int64_t ld_dgate; /* n * rows x hidden */
+  const void* dup;   int64_t ld_dup;
+  const void* x;     int64_t ld_x;     /* n * rows x cols; NULL where no weight's gradient is asked for */
+  const void* gate_weight; int64_t ld_gate_weight; /* hidden x cols; NULL where dx is not asked for */
+  const void* up_weight;   int64_t ld_up_weight;
+  void* dx;          int64_t ld_dx;    /* n * rows x cols, or NULL */
+  float* dgate_weight; int64_t ld_dgate_weight, stride_dgate_weight; /* or NULL */
+  float* dup_weight;   int64_t ld_dup_weight, stride_dup_weight;
+  int32_t accumulate; /* 1: the weights' gradients are added to what is there; 0: written */
+  void* workspace;    /* DEVICE, 256-byte aligned */
+  size_t workspace_bytes;
+} compams_projections;
+
+size_t compams_projections_workspace_size(const compams_projections* a);
+int compams_projections_backward(const compams_projections* a, void* hip_stream);
+
+/* Softmax cross-entropy of an output layer, with logits weight x that are never stored: compams_cross_entropy's mean_loss and
+ * losses of these logits (in fp32), and, with its dlogits d in fp32,
+ *   dx = weight' d,  dweight = the sum over the worker's rows of d x'
+ * The vocabulary is gone over twice, in pieces the second time; a piece's gradients d are held in the workspace in as many digits as
+ * fp32 has (dx takes those of the type).  Ignored rows: loss and dx are 0 and nothing is added to dweight, whatever x
+ * holds there. */
+typedef struct compams_linear_loss {
+  int32_t n;
+  int64_t rows, cols;
+  int64_t vocab;       /* 1 <= vocab < 2^31 */
+  int32_t type;        /* of x, weight and dx */
+  int32_t target_type; /* COMPAMS_I32 or COMPAMS_I64 */
+  const void* x;      int64_t ld_x;
+  const void* weight; int64_t ld_weight; /* vocab x cols */
+  const void* targets;                   /* n * rows */
+  int64_t ignore_index;
+  float grad_scale;                      /* factor of the gradients alone (a scaled loss) */
+  float* mean_loss;                      /* n, or NULL */
+  float* losses;                         /* n * rows, or NULL */
+  void* dx; int64_t ld_dx;               /* or NULL */
+  float* dweight; int64_t ld_dweight, stride_dweight; /* vocab x cols per worker, or NULL */
+  int32_t accumulate;  /* 1: dweight is added to what is there; 0: written */
+  void* workspace;     /* DEVICE, 256-byte aligned */
+  size_t workspace_bytes;
+} compams_linear_loss;
+
+size_t compams_linear_loss_workspace_size(const compams_linear_loss* a);
+int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream);
+
+/* The norm of every worker's gradient over all its tensors, and the gradient cut to a largest norm:
+ *   norms[i] = scale * sqrt(sum of the squares of worker i's entries)
+ *   factors[i] = scale * min(1, max_norm / norms[i])   (scale where norms[i] is 0)
+ *   to = factors[i] * from
+ * A worker whose gradient holds a NaN or an infinity has a norm that says so, factors[i] = 0 and zeros in `to`: it takes no
+ * part in the step.  Squares and their sums are fp64, so no finite gradient has a norm beyond range or below it, in
+ * fp32 or narrower types, unless the norm itself is. */
+typedef struct compams_clip_tensor {
+  const void* from; int64_t ld_from; /* n rows of `count` entries, ld_from entries apart */
+  void* to;         int64_t ld_to;   /* the same, or NULL: nothing is written; may be `from` where both have one type */
+  int64_t count;                     /* >= 0 */
+  int32_t from_type, to_type;        /* equal, or to_type COMPAMS_F32 */
+} compams_clip_tensor;
+typedef struct compams_clip {
+  int32_t n;                            /* workers, 1 <= n <= 65535 */
+  int32_t tensors;                      /* >= 0 */
+  const compams_clip_tensor* tensor;    /* HOST, read before the call returns */
+  float max_norm;                       /* >= 0; infinity: nothing is cut */
+  float scale;                          /* > 0, finite: takes a loss's scale back */
+  float* norms;                         /* n, or NULL */
+  float* factors;                       /* n, or NULL */
+  void* workspace;                      /* DEVICE, 256-byte aligned */
+  size_t workspace_bytes;
+} compams_clip;
+
+size_t compams_clip_workspace_size(const compams_clip* a);
+int compams_clip_gradients(const compams_clip* a, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

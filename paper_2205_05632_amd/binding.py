@@ -30,7 +30,10 @@ EXPORTS = ["compams_workspace_size", "compams_init", "compams_step", "compams_st
            "compams_wire_capacity", "compams_encode", "compams_decode", "compams_worker_step", "compams_server_step",
            "compams_step_static", "compams_dropout", "compams_norm_workspace_size", "compams_layer_norm_forward",
            "compams_layer_norm_backward", "compams_dropout_add_norm_forward", "compams_dropout_add_norm_backward",
-           "compams_loss_workspace_size", "compams_cross_entropy"]
+           "compams_loss_workspace_size", "compams_cross_entropy", "compams_gated_forward_workspace_size",
+           "compams_gated_backward_workspace_size", "compams_gated_forward", "compams_gated_backward",
+           "compams_projections_workspace_size", "compams_projections_backward", "compams_linear_loss_workspace_size",
+           "compams_linear_cross_entropy", "compams_clip_workspace_size", "compams_clip_gradients"]
 STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -92,10 +95,14 @@ def lib():
         # the operators of the workers' models (operators.py)
         i32, i64, ptr = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
         L.compams_dropout.argtypes = [i32, i64, i64, i32, i32, ptr, i64, ptr, i64, ptr, i64, ptr, ptr]
-        for f in (L.compams_norm_workspace_size, L.compams_loss_workspace_size):
+        for f in (L.compams_norm_workspace_size, L.compams_loss_workspace_size, L.compams_gated_forward_workspace_size,
+                  L.compams_gated_backward_workspace_size, L.compams_projections_workspace_size,
+                  L.compams_linear_loss_workspace_size, L.compams_clip_workspace_size):
             f.restype, f.argtypes = ctypes.c_size_t, [ptr]
         for f in (L.compams_layer_norm_forward, L.compams_layer_norm_backward, L.compams_dropout_add_norm_forward,
-                  L.compams_dropout_add_norm_backward, L.compams_cross_entropy):
+                  L.compams_dropout_add_norm_backward, L.compams_cross_entropy, L.compams_gated_forward,
+                  L.compams_gated_backward, L.compams_projections_backward, L.compams_linear_cross_entropy,
+                  L.compams_clip_gradients):
             f.argtypes = [ptr, ptr]
         _lib = L
     return _lib

@@ -19,7 +19,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcompams.so")
 SOURCES = ["compams_api.hip", "compams_topk.hip", "compams_blocksign.hip", "compams_wire.hip", "compams_norm.hip",
-           "compams_norm_forward.hip", "compams_norm_backward.hip", "compams_dropout.hip", "compams_loss.hip"]
+           "compams_norm_forward.hip", "compams_norm_backward.hip", "compams_dropout.hip", "compams_loss.hip", "compams_tiles.hip",
+           "compams_gated.hip", "compams_projections.hip", "compams_linear_loss.hip", "compams_clip.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=off",

@@ -1,0 +1,376 @@
+// A gated feed-forward block up to its product, m = act(x Wg' + bg) * (x Wu' + bu), and the gradients of its two projections.
+#include "compams_tiles.h"
+
+#include <utility>
+
+namespace compams {
+namespace {
+
+// ---- Activations ---------------------------------------------------------------------------------------------
+// The processor's 2^x and 1 / x, a unit each; exp's argument z is off by |z| / 2 units after the product with log2 e.
+__device__ __forceinline__ float exp_fast(float z) { return __expf(z); }
+__device__ __forceinline__ float logistic(float a) { return __builtin_amdgcn_rcpf(1.0f + exp_fast(-a)); }
+
+// act(a), and its derivative where SLOPE.
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float activate(float a, float& slope) {
+  if constexpr (ACT == COMPAMS_RELU) {
+    if constexpr (SLOPE) slope = a > 0.0f ? 1.0f : a != a ? a : 0.0f;
+    return a > 0.0f || a != a ? a : 0.0f;
+  } else if constexpr (ACT == COMPAMS_SIGMOID) {
+    const float q = logistic(a);
+    if constexpr (SLOPE) slope = q * logistic(-a);  // (1 - q would lose its digits for large a)
+    return q;
+  } else if constexpr (ACT == COMPAMS_SILU) {
+    const float q = logistic(a), v = a < -88.0f ? -0.0f : a * q;  // (beyond it q is 0)
+    if constexpr (SLOPE) slope = q + v * logistic(-a);
+    return v;
+  } else if constexpr (ACT == COMPAMS_GELU) {
+    const float cdf = 0.5f * erfcf(a * -0.70710678118654752f);  // (1 + erf would lose its digits for negative a)
+    if constexpr (SLOPE) slope = a * a > 400.0f ? cdf : cdf + a * exp_fast(-0.5f * a * a) * 0.3989422804014327f;
+    return a < -14.0f ? -0.0f : a * cdf;
+  } else {
+    // (1 + tanh u) / 2 = logistic(2 u)
+    const float a2 = a * a, u2 = 1.5957691216057308f * a * (1.0f + 0.044715f * a2);
+    const float q = logistic(u2);
+    if constexpr (SLOPE) {
+      const float inner = 1.5957691216057308f * (1.0f + 3.0f * 0.044715f * a2);
+      slope = a2 > 400.0f ? q : q + a * q * logistic(-u2) * inner;
+    }
+    return a < -14.0f ? -0.0f : a * q;
+  }
+}
+
+// ---- Forward -------------------------------------------------------------------------------------------------
+struct ForwardArgs {
+  Read x, gate_weight, up_weight;
+  const float *gate_bias, *up_bias;
+  void *m, *gate, *up;
+  int64_t ld_m, ld_gate, ld_up;
+  uint32_t total, cols, hidden, tall, wide;
+  uint32_t aligned;  // whether four entries of an output's row can be stored at once
+};
+
+// A tile of 256 x 256 is 256 rows of x and 128 columns of each projection, which take turns of sixteen: what belongs together
+// is in one lane's registers.  Bound by the matrix cores and, with K = 768, by the tile's three outputs.
+template <typename TL, int ACT>
+__global__ __launch_bounds__(TL::kThreads) void k_gated_forward(ForwardArgs a) {
+  using T = typename TL::T;
+  COMPAMS_TILE_LDS(TL);
+  const uint32_t tiles = a.tall * a.wide, id = tile_id();
+  if (id >= tiles) return;
+  uint32_t down, across;
+  tile_at(by_die(id, tiles), a.tall, a.wide, down, across);
+  const uint32_t m0 = down * TL::kM, h0 = across * (TL::kN / 2);
+  TL t;
+  t.clear();
+  t.run([&](uint32_t, Side& x, Side& g, Side& u) {
+    x = side<T, kAlong>(a.x.p, a.x.ld, a.total, m0, a.cols);
+    g = side<T, kAlong>(a.gate_weight.p, a.gate_weight.ld, a.hidden, h0, a.cols);
+    u = side<T, kAlong>(a.up_weight.p, a.up_weight.ld, a.hidden, h0, a.cols);
+  }, 1, a.cols, COMPAMS_TILE_LDS_ARGS);
+  const uint32_t m1 = m0 + TL::first_m() + TL::lane_m(), h1 = h0 + TL::first_n() / 2 + TL::lane_n();
+#pragma unroll
+  for (uint32_t j = 0; j < TL::FN; j += 2) {
+    const uint32_t h = h1 + j * 8;
+    if (h >= a.hidden) continue;
+    const int64_t left = a.hidden - h;
+    f32x4 bg = {}, bu = {};
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q) {
+      if (a.gate_bias && q < left) bg[q] = a.gate_bias[h + q];
+      if (a.up_bias && q < left) bu[q] = a.up_bias[h + q];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < TL::FM; ++i) {
+      const uint32_t r = m1 + i * 16;
+      if (r >= a.total) continue;
+      const f32x4 g = t.sum[i][j] + bg, u = t.sum[i][j + 1] + bu;
+      f32x4 m;
+      float none;
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) m[q] = activate<ACT, false>(g[q], none) * u[q];
+      store4(static_cast<T*>(a.m) + static_cast<int64_t>(r) * a.ld_m + h, m, left, a.aligned & 1u);
+      if (a.gate) store4(static_cast<T*>(a.gate) + static_cast<int64_t>(r) * a.ld_gate + h, g, left, a.aligned & 2u);
+      if (a.up) store4(static_cast<T*>(a.up) + static_cast<int64_t>(r) * a.ld_up + h, u, left, a.aligned & 4u);
+    }
+  }
+}
+
+template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
+void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
+  using TL = Tiles<T, kAlong, kAlong, WM, WN, FM, FN, true>;
+  a.tall = static_cast<uint32_t>(tiles_of(a.total, TL::kM));
+  a.wide = static_cast<uint32_t>(tiles_of(a.hidden, TL::kN / 2));
+  const dim3 grid = tile_grid(static_cast<uint64_t>(a.tall) * a.wide), block(TL::kThreads);
+  switch (act) {
+    case COMPAMS_SILU: hipLaunchKernelGGL((k_gated_forward<TL, COMPAMS_SILU>), grid, block, 0, stream, a); break;
+    case COMPAMS_GELU: hipLaunchKernelGGL((k_gated_forward<TL, COMPAMS_GELU>), grid, block, 0, stream, a); break;
+    case COMPAMS_GELU_TANH: hipLaunchKernelGGL((k_gated_forward<TL, COMPAMS_GELU_TANH>), grid, block, 0, stream, a); break;
+    case COMPAMS_RELU: hipLaunchKernelGGL((k_gated_forward<TL, COMPAMS_RELU>), grid, block, 0, stream, a); break;
+    default: hipLaunchKernelGGL((k_gated_forward<TL, COMPAMS_SIGMOID>), grid, block, 0, stream, a); break;
+  }
+}
+template <typename T>
+void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
+  switch (tile_size(a.total, 2 * static_cast<uint64_t>(a.hidden), 1)) {
+    case kTile256: launch_forward<T, 2, 4, 8, 4>(a, act, stream); break;
+    case kTile128: launch_forward<T, 2, 2, 4, 4>(a, act, stream); break;
+    default: launch_forward<T, 2, 2, 2, 2>(a, act, stream); break;
+  }
+}
+
+// ---- Backward ------------------------------------------------------------------------------------------------
+struct BackwardArgs {
+  const void *dm, *gate, *up;
+  void *dgate, *dup;
+  int64_t ld_dm, ld_gate, ld_up, ld_dgate, ld_dup;
+  float* bias[2];       // of worker 0, or null
+  int64_t ld_bias[2];
+  float* partial;       // [worker][part][2][hidden], where there is more than one part
+  uint32_t n, rows, hidden;
+  uint32_t across, wide, parts, part_rows;
+  uint32_t accumulate;
+};
+constexpr uint32_t kThreads = 256;
+
+// A workgroup takes a part of a worker's rows and wide * 8 columns of them, a lane eight columns of every (256 / wide)-th row.
+// Bound by memory: three matrices read, two written.
+template <typename T, int ACT, bool BIAS>
+__global__ __launch_bounds__(kThreads) void k_gated_backward(BackwardArgs a) {
+  __shared__ float sums[BIAS ? 2 * kThreads * kGroup : 1];
+  const uint32_t tall = kThreads / a.wide;
+  const uint32_t strip = blockIdx.x % a.across, piece = blockIdx.x / a.across;
+  const uint32_t w = piece / a.parts, part = piece - w * a.parts;
+  const uint32_t lane = threadIdx.x & (a.wide - 1), down = threadIdx.x / a.wide;
+  const uint32_t c = (strip * a.wide + lane) * kGroup;
+  const uint32_t first = part * a.part_rows, last = min(first + a.part_rows, a.rows);
+  float sg[kGroup] = {}, su[kGroup] = {};
+  if (c < a.hidden) {
+    for (uint32_t in = first + down; in < last; in += tall) {
+      const int64_t r = static_cast<int64_t>(w) * a.rows + in;
+      float dm[kGroup], g[kGroup], u[kGroup], dg[kGroup], du[kGroup];
+      load_group(dm, static_cast<const T*>(a.dm) + r * a.ld_dm, c, a.hidden);
+      load_group(g, static_cast<const T*>(a.gate) + r * a.ld_gate, c, a.hidden);
+      load_group(u, static_cast<const T*>(a.up) + r * a.ld_up, c, a.hidden);
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) {
+        float slope;
+        const float v = activate<ACT, true>(g[j], slope);
+        dg[j] = dm[j] * u[j] * slope;
+        du[j] = dm[j] * v;
+        if constexpr (BIAS) {
+          sg[j] += dg[j];
+          su[j] += du[j];
+        }
+      }
+      store_group<T>(static_cast<T*>(a.dgate) + r * a.ld_dgate, c, a.hidden, dg);
+      store_group<T>(static_cast<T*>(a.dup) + r * a.ld_dup, c, a.hidden, du);
+    }
+  }
+  if constexpr (BIAS) {
+#pragma unroll
+    for (uint32_t j = 0; j < kGroup; ++j) {
+      sums[j * kThreads + threadIdx.x] = sg[j];
+      sums[(kGroup + j) * kThreads + threadIdx.x] = su[j];
+    }
+    __syncthreads();
+    // sixteen sums for each of `wide` groups
+    for (uint32_t i = threadIdx.x; i < 2 * kGroup * a.wide; i += kThreads) {
+      const uint32_t which = i / (kGroup * a.wide), of = i % (kGroup * a.wide), j = of % kGroup, l = of / kGroup;
+      const uint32_t column = (strip * a.wide + l) * kGroup + j;
+      float s = 0.0f;
+      for (uint32_t k = 0; k < tall; ++k) s += sums[(which * kGroup + j) * kThreads + k * a.wide + l];
+      if (column >= a.hidden) continue;
+      if (a.parts > 1) {
+        a.partial[((static_cast<uint64_t>(w) * a.parts + part) * 2 + which) * a.hidden + column] = s;
+      } else if (a.bias[which]) {
+        float* const to = a.bias[which] + static_cast<int64_t>(w) * a.ld_bias[which] + column;
+        *to = a.accumulate ? *to + s : s;
+      }
+    }
+  }
+}
+
+// The parts' sums of 32 columns, eight lanes to a column.
+__global__ __launch_bounds__(kThreads) void k_gated_bias(BackwardArgs a) {
+  __shared__ float sums[8][33];
+  const uint32_t l = threadIdx.x % 32, turn = threadIdx.x / 32;
+  const uint32_t column = blockIdx.x * 32 + l, which = blockIdx.z;
+  if (!a.bias[which]) return;
+  for (uint32_t w = blockIdx.y; w < a.n; w += gridDim.y) {
+    float s = 0.0f;
+    if (column < a.hidden)
+      for (uint32_t p = turn; p < a.parts; p += 8) s += a.partial[((static_cast<uint64_t>(w) * a.parts + p) * 2 + which) * a.hidden + column];
+    sums[turn][l] = s;
+    __syncthreads();
+    if (turn == 0 && column < a.hidden) {
+      float all = 0.0f;
+#pragma unroll
+      for (uint32_t k = 0; k < 8; ++k) all += sums[k][l];
+      float* const to = a.bias[which] + static_cast<int64_t>(w) * a.ld_bias[which] + column;
+      *to = a.accumulate ? *to + all : all;
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T, int ACT>
+void launch_backward(const BackwardArgs& a, uint32_t blocks, hipStream_t stream) {
+  if (a.bias[0] || a.bias[1]) hipLaunchKernelGGL((k_gated_backward<T, ACT, true>), dim3(blocks), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((k_gated_backward<T, ACT, false>), dim3(blocks), dim3(kThreads), 0, stream, a);
+}
+template <typename T>
+void launch_backward(const BackwardArgs& a, int act, uint32_t blocks, hipStream_t stream) {
+  switch (act) {
+    case COMPAMS_SILU: launch_backward<T, COMPAMS_SILU>(a, blocks, stream); break;
+    case COMPAMS_GELU: launch_backward<T, COMPAMS_GELU>(a, blocks, stream); break;
+    case COMPAMS_GELU_TANH: launch_backward<T, COMPAMS_GELU_TANH>(a, blocks, stream); break;
+    case COMPAMS_RELU: launch_backward<T, COMPAMS_RELU>(a, blocks, stream); break;
+    default: launch_backward<T, COMPAMS_SIGMOID>(a, blocks, stream); break;
+  }
+}
+
+// ---- Checks --------------------------------------------------------------------------------------------------
+bool gated_valid(const compams_gated* a) {
+  return a && rows_valid(a->n, a->rows, a->hidden) && a->hidden <= kMostEntries && float_type(a->type) &&
+         a->activation >= COMPAMS_SILU && a->activation <= COMPAMS_SIGMOID;
+}
+bool forward_valid(const compams_gated* a) {
+  return gated_valid(a) && a->cols >= 1 && a->cols <= kMostEntries && tiles_fit(a->n * a->rows, 2 * a->hidden, 1);
+}
+
+struct Operands {
+  Matrix x, gate, up;
+};
+Operands operands(const compams_gated& a) {
+  const size_t size = type_size(a.type);
+  return {{a.x, a.ld_x, a.n * a.rows, a.cols, size},
+          {a.gate_weight, a.ld_gate_weight, a.hidden, a.cols, size},
+          {a.up_weight, a.ld_up_weight, a.hidden, a.cols, size}};
+}
+size_t forward_bytes(const compams_gated& a) {
+  if (a.rows == 0) return 0;
+  const Operands o = operands(a);
+  return o.x.packed_bytes() + o.gate.packed_bytes() + o.up.packed_bytes();
+}
+
+// How a worker's rows are cut: the lanes side by side in a workgroup and the rows of a part.
+struct BackwardCut {
+  uint32_t wide, across, parts, part_rows;
+};
+BackwardCut backward_cut(const compams_gated& a) {
+  BackwardCut c;
+  const uint64_t groups = (static_cast<uint64_t>(a.hidden) + kGroup - 1) / kGroup;
+  c.wide = 1;
+  while (c.wide < groups && c.wide < kThreads) c.wide *= 2;
+  c.across = static_cast<uint32_t>((groups + c.wide - 1) / c.wide);
+  const uint64_t tall = kThreads / c.wide;
+  uint64_t rows = tall * 8;  // of a part
+  // (workgroups are 2^23 at most: a grid has room for 2^32 threads)
+  const uint64_t most = (1u << 23) / c.across / static_cast<uint64_t>(a.n) + 1;
+  if ((static_cast<uint64_t>(a.rows) + rows - 1) / rows > most) rows = (static_cast<uint64_t>(a.rows) + most - 1) / most;
+  c.part_rows = static_cast<uint32_t>(rows);
+  c.parts = static_cast<uint32_t>((static_cast<uint64_t>(a.rows) + rows - 1) / rows);
+  if (c.parts == 0) c.parts = 1;
+  return c;
+}
+size_t backward_bytes(const compams_gated& a) {
+  const BackwardCut c = backward_cut(a);
+  if (c.parts == 1 || (!a.dgate_bias && !a.dup_bias)) return 0;
+  return (static_cast<size_t>(a.n) * c.parts * 2 * a.hidden * sizeof(float) + 255) / 256 * 256;
+}
+}  // namespace
+}  // namespace compams
+
+extern "C" {
+
+size_t compams_gated_forward_workspace_size(const compams_gated* a) {
+  return compams::forward_valid(a) ? compams::forward_bytes(*a) : 0;
+}
+size_t compams_gated_backward_workspace_size(const compams_gated* a) {
+  return compams::gated_valid(a) ? compams::backward_bytes(*a) : 0;
+}
+
+int compams_gated_forward(const compams_gated* a, void* hip_stream) {
+  using namespace compams;
+  if (!forward_valid(a)) return COMPAMS_INVALID_ARG;
+  if (a->rows == 0) return COMPAMS_OK;
+  const size_t size = type_size(a->type);
+  if (!a->x || !a->gate_weight || !a->up_weight || !a->m || !stride_valid(a->ld_x, a->cols) ||
+      !stride_valid(a->ld_gate_weight, a->cols) || !stride_valid(a->ld_up_weight, a->cols) || !stride_valid(a->ld_m, a->hidden) ||
+      (a->gate && !stride_valid(a->ld_gate, a->hidden)) || (a->up && !stride_valid(a->ld_up, a->hidden)))
+    return COMPAMS_INVALID_ARG;
+  if (!aligned_to(a->x, size) || !aligned_to(a->gate_weight, size) || !aligned_to(a->up_weight, size) || !aligned_to(a->m, size) ||
+      !aligned_to(a->gate, size) || !aligned_to(a->up, size) || !aligned_to(a->gate_bias, 4) || !aligned_to(a->up_bias, 4))
+    return COMPAMS_BAD_ALIGNMENT;
+  const int status = workspace_status(a->workspace, a->workspace_bytes, forward_bytes(*a));
+  if (status != COMPAMS_OK) return status;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  ForwardArgs k = {};
+  const Operands o = operands(*a);
+  Packing packing;
+  char* room = static_cast<char*>(a->workspace);
+  k.x = packing.add(o.x, room);
+  k.gate_weight = packing.add(o.gate, room);
+  k.up_weight = packing.add(o.up, room);
+  run_packing(packing, size, stream);
+  k.gate_bias = a->gate_bias; k.up_bias = a->up_bias;
+  k.m = a->m; k.gate = a->gate; k.up = a->up;
+  k.ld_m = a->ld_m; k.ld_gate = a->ld_gate; k.ld_up = a->ld_up;
+  const auto four = [&](const void* p, int64_t ld) { return aligned_to(p, 4 * size) && ld % 4 == 0; };
+  k.aligned = four(k.m, k.ld_m) | four(k.gate, k.ld_gate) << 1 | four(k.up, k.ld_up) << 2;
+  k.total = static_cast<uint32_t>(a->n * a->rows);
+  k.cols = static_cast<uint32_t>(a->cols);
+  k.hidden = static_cast<uint32_t>(a->hidden);
+  if (a->type == COMPAMS_F32) launch_forward<float>(k, a->activation, stream);
+  else if (a->type == COMPAMS_F16) launch_forward<half_t>(k, a->activation, stream);
+  else launch_forward<bfloat_t>(k, a->activation, stream);
+  return hipGetLastError() == hipSuccess ? COMPAMS_OK : COMPAMS_HIP_ERROR;
+}
+
+int compams_gated_backward(const compams_gated* a, void* hip_stream) {
+  using namespace compams;
+  if (!gated_valid(a) || (a->accumulate != 0 && a->accumulate != 1)) return COMPAMS_INVALID_ARG;
+  const size_t size = type_size(a->type);
+  for (const auto& [p, ld] : {std::pair<float*, int64_t>{a->dgate_bias, a->ld_dgate_bias}, {a->dup_bias, a->ld_dup_bias}}) {
+    if (!p) continue;
+    if (a->n > 1 && (ld < a->hidden || ld >= (static_cast<int64_t>(1) << 40))) return COMPAMS_INVALID_ARG;
+    if (!aligned_to(p, 4)) return COMPAMS_BAD_ALIGNMENT;
+  }
+  if (a->rows > 0) {
+    if (!a->dm || !a->gate || !a->up || !a->dgate || !a->dup || !stride_valid(a->ld_dm, a->hidden) ||
+        !stride_valid(a->ld_gate, a->hidden) || !stride_valid(a->ld_up, a->hidden) || !stride_valid(a->ld_dgate, a->hidden) ||
+        !stride_valid(a->ld_dup, a->hidden))
+      return COMPAMS_INVALID_ARG;
+    if (!aligned_to(a->dm, size) || !aligned_to(a->gate, size) || !aligned_to(a->up, size) || !aligned_to(a->dgate, size) ||
+        !aligned_to(a->dup, size))
+      return COMPAMS_BAD_ALIGNMENT;
+  } else if (!a->dgate_bias && !a->dup_bias) {
+    return COMPAMS_OK;
+  }
+  const int status = workspace_status(a->workspace, a->workspace_bytes, backward_bytes(*a));
+  if (status != COMPAMS_OK) return status;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const BackwardCut cut = backward_cut(*a);
+  BackwardArgs k = {};
+  k.dm = a->dm; k.gate = a->gate; k.up = a->up; k.dgate = a->dgate; k.dup = a->dup;
+  k.ld_dm = a->ld_dm; k.ld_gate = a->ld_gate; k.ld_up = a->ld_up; k.ld_dgate = a->ld_dgate; k.ld_dup = a->ld_dup;
+  k.bias[0] = a->dgate_bias; k.bias[1] = a->dup_bias;
+  k.ld_bias[0] = a->ld_dgate_bias; k.ld_bias[1] = a->ld_dup_bias;
+  k.partial = static_cast<float*>(a->workspace);
+  k.n = static_cast<uint32_t>(a->n);
+  k.rows = static_cast<uint32_t>(a->rows);
+  k.hidden = static_cast<uint32_t>(a->hidden);
+  k.wide = cut.wide; k.across = cut.across; k.parts = cut.parts; k.part_rows = cut.part_rows;
+  k.accumulate = static_cast<uint32_t>(a->accumulate);
+  const uint32_t blocks = k.across * k.n * k.parts;
+  if (a->type == COMPAMS_F32) launch_backward<float>(k, a->activation, blocks, stream);
+  else if (a->type == COMPAMS_F16) launch_backward<half_t>(k, a->activation, blocks, stream);
+  else launch_backward<bfloat_t>(k, a->activation, blocks, stream);
+  if (cut.parts > 1 && (k.bias[0] || k.bias[1]))
+    hipLaunchKernelGGL(k_gated_bias, dim3((k.hidden + 31) / 32, k.n < 16384 ? k.n : 16384, 2), dim3(kThreads), 0, stream, k);
+  return hipGetLastError() == hipSuccess ? COMPAMS_OK : COMPAMS_HIP_ERROR;
+}
+
+}  // extern "C"

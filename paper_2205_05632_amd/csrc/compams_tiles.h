@@ -1,0 +1,396 @@
+// Products of matrices on the matrix cores, one tile of the result to a workgroup: D(m, n) = sum over k of A(m, k) B(n, k), with
+// fp32 sums.  The kernels that use it differ in what they do with the tile.  (wave64 only)
+//
+// A step takes 128 bytes of k: 64 entries of the 16-bit types, 32 of fp32.  Both operands' tiles of a step go from memory into
+// LDS without passing through registers, 16 bytes a lane, while the step before is multiplied (two buffers, one barrier a step).
+// Reads beyond a matrix give zeros (the buffer descriptors' own bounds), so no length has to be a multiple of anything but 16 bytes.
+#pragma once
+
+#include "compams_rows.h"
+
+namespace compams {
+
+// How an operand lies in memory: its rows go along k (entries of a row follow one another in k), or across it (a row has
+// one k, and all m or n).
+enum Form { kAlong, kAcross };
+
+constexpr uint32_t kStepBytes = 128;
+template <typename T>
+constexpr uint32_t kStep = kStepBytes / sizeof(T);
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+// A lane's 16 bytes of an operand, as one instruction (four of fp32) takes them: row or column l % 16 of sixteen, and of k
+// eight entries from 8 (l / 16) on (fp32: four from 4 (l / 16) on, one to an instruction).
+template <typename T>
+struct Fragment {
+  typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
+};
+
+// d(n, m) += sum of b(n, k) a(m, k).  The rows of the instruction are n: a lane gets m = l % 16 and the four neighbouring
+// n from 4 (l / 16) on, which lie next to one another in a row of the result.
+__device__ __forceinline__ void multiply(f32x4& d, Fragment<half_t>::type a, Fragment<half_t>::type b) {
+  d = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, a, d, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply(f32x4& d, Fragment<bfloat_t>::type a, Fragment<bfloat_t>::type b) {
+  d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, d, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply(f32x4& d, Fragment<float>::type a, Fragment<float>::type b) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x4f32(b[i], a[i], d, 0, 0, 0);
+}
+
+// Places in LDS.  An operand's tile has EXTENT rows (or columns) of m or n.
+//
+// kAlong: EXTENT rows of 128 bytes.  The 16 bytes c of row r are kept at place c ^ (r % 8) of the row: the sixteen rows that a
+// fragment is read from then begin in eight different places of the 128 bytes that LDS gives at once.
+//
+// kAcross: a row of EXTENT entries for every k of the step.  16-bit types are read with the transposing read: sixteen lanes read
+// four k of sixteen columns (32 bytes a row), and get four k of one column each.  The pairs of 16 bytes are moved by k so that
+// the rows of a read do not meet.  fp32 is read entry by entry, 64 bytes a row.
+template <typename T, uint32_t EXTENT>
+__device__ __forceinline__ uint32_t moved(uint32_t k) {
+  if constexpr (sizeof(T) == 2) return 2 * ((k & 3u) | (EXTENT >= 128 ? (k >> 1) & 4u : 0u));
+  else return (k >> 2 & 3u) * 4;
+}
+
+template <typename T, Form F, uint32_t EXTENT>
+struct Place {
+  static constexpr uint32_t kRowBytes = F == kAlong ? kStepBytes : EXTENT * sizeof(T);
+  static constexpr uint32_t kPerRow = kRowBytes / 16;  // 16-byte pieces
+  static constexpr uint32_t kBytes = EXTENT * kStepBytes;
+
+  // The row and the piece of it that is kept at 16-byte place p.
+  __device__ static __forceinline__ void of(uint32_t p, uint32_t& row, uint32_t& piece) {
+    row = p / kPerRow;
+    piece = p % kPerRow ^ (F == kAlong ? row & 7u : moved<T, EXTENT>(row));
+  }
+
+  // The fragment of rows (columns) first .. first + 15 and the sub-th half of the step's k.
+  __device__ static __forceinline__ typename Fragment<T>::type read(const lds_char* tile, uint32_t first, uint32_t sub) {
+    const uint32_t lane = threadIdx.x & 63u, l = lane & 15u, g = lane >> 4;
+    typename Fragment<T>::type v;
+    if constexpr (F == kAlong) {
+      const uint32_t row = first + l, piece = (sub * 4 + g) ^ (row & 7u);
+      v = *reinterpret_cast<const __attribute__((address_space(3))) typename Fragment<T>::type*>(tile + row * kRowBytes + piece * 16);
+    } else if constexpr (sizeof(T) == 2) {
+      const uint32_t k = sub * 32 + g * 8 + (l >> 2);
+      const uint32_t piece = first / 8 + (l >> 1 & 1u), in = (l & 1u) * 8;
+      s16x4 part[2];
+#pragma unroll
+      for (uint32_t h = 0; h < 2; ++h)  // (k and k + 4 are moved alike)
+        part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(
+            tile + (k + 4 * h) * kRowBytes + (piece ^ moved<T, EXTENT>(k)) * 16 + in));
+      __builtin_memcpy(&v, part, sizeof(v));
+    } else {
+      const uint32_t column = first + l;
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t k = sub * 16 + g * 4 + i;
+        v[i] = *reinterpret_cast<const __attribute__((address_space(3))) float*>(
+            tile + k * kRowBytes + (column / 4 ^ moved<T, EXTENT>(k)) * 16 + column % 4 * 4);
+      }
+    }
+    return v;
+  }
+};
+
+// An operand, from the tile's first row or column on: its bytes' bounds go with it.
+struct Side {
+  const char* p;
+  uint32_t ld;      // bytes from row to row
+  uint32_t extent;  // kAlong: rows from the tile's first on; kAcross: bytes of a row from the tile's first column on
+  uint32_t k;       // entries of k
+};
+template <typename T, Form F>
+__device__ __forceinline__ Side side(const void* p, int64_t ld, uint32_t total, uint32_t first, uint32_t k) {
+  const char* const at = static_cast<const char*>(p);
+  if (F == kAlong) return {at + static_cast<int64_t>(first) * ld, static_cast<uint32_t>(ld), total - first, k};
+  return {at + static_cast<int64_t>(first) * sizeof(T), static_cast<uint32_t>(ld), (total - first) * static_cast<uint32_t>(sizeof(T)), k};
+}
+
+template <typename T, Form F, uint32_t EXTENT, uint32_t WAVES>
+struct Loader {
+  using At = Place<T, F, EXTENT>;
+  static constexpr uint32_t kLoads = At::kBytes / (WAVES * 1024);
+  static_assert(kLoads * WAVES * 1024 == At::kBytes, "a tile is loaded in whole instructions of every wave");
+  uint32_t row[kLoads], piece[kLoads];
+
+  __device__ __forceinline__ void init(uint32_t wave) {
+    const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) At::of((i * WAVES + wave) * 64 + lane, row[i], piece[i]);
+  }
+  // TWO: the tile's rows are those of two operands in turns of sixteen.
+  template <bool TWO>
+  __device__ __forceinline__ void load(const Side& one, const Side& two, uint32_t k0, lds_char* tile, uint32_t wave) const {
+    const __amdgpu_buffer_rsrc_t of_one = bounds(one, k0, TWO);
+    const __amdgpu_buffer_rsrc_t of_two = TWO ? bounds(two, k0, TWO) : of_one;
+    const uint32_t left = (one.k - k0) * static_cast<uint32_t>(sizeof(T));
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+      uint32_t r = row[i], ld = one.ld;
+      bool second = false;
+      if constexpr (TWO) {
+        second = ((i * WAVES + wave) * 8 / 16) & 1u;  // (the same for the wave: an instruction has eight rows)
+        r = r / 32 * 16 + r % 16;
+        ld = second ? two.ld : one.ld;
+      }
+      uint32_t at = r * ld + piece[i] * 16;
+      if constexpr (F == kAlong) at = piece[i] * 16 < left ? at : 0xfffffff0u;  // (the entries behind a row's end are another's)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? of_two : of_one, (__attribute__((address_space(3))) void*)(tile + (i * WAVES + wave) * 1024),
+                                               16, at, 0, 0, 0);
+    }
+  }
+  // Up to the end of the last row's last 16 bytes, which belong to the row: an entry of 16 bits that ends it in the middle of a word
+  // would be cut off with the word.
+  __device__ static __forceinline__ uint32_t whole(uint32_t bytes) { return (bytes + 15) / 16 * 16; }
+  __device__ static __forceinline__ __amdgpu_buffer_rsrc_t bounds(const Side& s, uint32_t k0, bool two) {
+    const char* p;
+    uint32_t bytes;
+    if constexpr (F == kAlong) {
+      const uint32_t rows = min(s.extent, two ? EXTENT / 2 : EXTENT);
+      p = s.p + k0 * sizeof(T);
+      bytes = (rows - 1) * s.ld + whole((s.k - k0) * static_cast<uint32_t>(sizeof(T)));
+    } else {
+      const uint32_t rows = min(s.k - k0, kStep<T>);
+      p = s.p + static_cast<int64_t>(k0) * s.ld;
+      bytes = (rows - 1) * s.ld + whole(s.extent);
+    }
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, static_cast<int>(bytes), 0x00020000);
+  }
+};
+
+// A workgroup of WM x WN wavefronts, each with FM x FN tiles of 16 x 16.
+template <typename T_, Form FA_, Form FB_, uint32_t WM_, uint32_t WN_, uint32_t FM_, uint32_t FN_, bool TWO_ = false>
+struct Tiles {
+  using T = T_;
+  static constexpr Form FA = FA_, FB = FB_;
+  static constexpr uint32_t WM = WM_, WN = WN_, FM = FM_, FN = FN_;
+  static constexpr bool kTwo = TWO_;  // B is two matrices, in turns of sixteen columns of the result
+  static constexpr uint32_t kWaves = WM * WN, kThreads = kWaves * 64, kM = WM * FM * 16, kN = WN * FN * 16;
+  using PlaceA = Place<T, FA, kM>;
+  using PlaceB = Place<T, FB, kN>;
+  static constexpr uint32_t kBytesA = PlaceA::kBytes, kBytesB = PlaceB::kBytes;
+  f32x4 sum[FM][FN];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+      for (uint32_t j = 0; j < FN; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  __device__ static __forceinline__ uint32_t wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+  // The first row and column, in the tile, of a wavefront's part, and of a lane's entries in a tile of 16 x 16.
+  __device__ static __forceinline__ uint32_t first_m() { return wave() / WN * (FM * 16); }
+  __device__ static __forceinline__ uint32_t first_n() { return wave() % WN * (FN * 16); }
+  __device__ static __forceinline__ uint32_t lane_m() { return threadIdx.x & 15u; }
+  __device__ static __forceinline__ uint32_t lane_n() { return (threadIdx.x >> 4 & 3u) * 4; }
+
+  __device__ __forceinline__ void step(const lds_char* a, const lds_char* b) {
+    const uint32_t m = first_m(), n = first_n();
+#pragma unroll
+    for (uint32_t sub = 0; sub < 2; ++sub) {
+      typename Fragment<T>::type fa[FM], fb[FN];
+#pragma unroll
+      for (uint32_t j = 0; j < FN; ++j) fb[j] = PlaceB::read(b, n + j * 16, sub);
+#pragma unroll
+      for (uint32_t i = 0; i < FM; ++i) fa[i] = PlaceA::read(a, m + i * 16, sub);
+#pragma unroll
+      for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < FN; ++j) multiply(sum[i][j], fa[i], fb[j]);
+      __builtin_amdgcn_sched_barrier(0);  // (else the fragments of both halves are read at once, and registers spilled)
+    }
+  }
+
+  // sum += the products of `count` pairs of operands, all with the same k.  pair(i, a, b, b2) gives the i-th.
+  // (LDS as four arrays of their own: the compiler then knows that what is read is not what is being loaded.)
+  template <typename Pair>
+  __device__ __forceinline__ void run(Pair pair, uint32_t count, uint32_t k, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+    const uint32_t w = wave();
+    Loader<T, FA, kM, kWaves> la;
+    Loader<T, FB, kN, kWaves> lb;
+    la.init(w);
+    lb.init(w);
+    const uint32_t steps = (k + kStep<T> - 1) / kStep<T> * count;
+    if (steps == 0) return;
+    uint32_t at = 0, k0 = 0;
+    Side a, b, b2;
+    pair(0u, a, b, b2);
+    const auto load = [&](lds_char* ta, lds_char* tb) {
+      la.template load<false>(a, a, k0, ta, w);
+      lb.template load<kTwo>(b, b2, k0, tb, w);
+      k0 += kStep<T>;
+      if (k0 >= k) {
+        k0 = 0;
+        if (++at < count) pair(at, a, b, b2);
+      }
+    };
+    load(a0, b0);
+    for (uint32_t s = 2; s <= steps; s += 2) {
+      arrived();
+      load(a1, b1);
+      step(a0, b0);
+      arrived();
+      if (s < steps) load(a0, b0);
+      step(a1, b1);
+    }
+    if (steps & 1u) {
+      arrived();
+      step(a0, b0);
+    }
+  }
+  // What this wavefront loaded is in LDS, and so is everybody's; everybody is done with the step before.
+  __device__ static __forceinline__ void arrived() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+  template <typename Visit>
+  __device__ __forceinline__ void each(Visit visit) {
+    const uint32_t m = first_m() + lane_m(), n = first_n() + lane_n();
+#pragma unroll
+    for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+      for (uint32_t j = 0; j < FN; ++j) visit(m + i * 16, n + j * 16, sum[i][j]);
+  }
+};
+
+#define COMPAMS_TILE_LDS(TILES)                                                                                              \
+  __shared__ __attribute__((aligned(1024))) char lds_a0[TILES::kBytesA], lds_b0[TILES::kBytesB], lds_a1[TILES::kBytesA],       \
+      lds_b1[TILES::kBytesB]
+#define COMPAMS_TILE_LDS_ARGS                                                                                                 \
+  (compams::lds_char*)lds_a0, (compams::lds_char*)lds_b0, (compams::lds_char*)lds_a1, (compams::lds_char*)lds_b1
+
+// Workgroups go to the eight dies in turn, each with a cache of its own: a die gets workgroups that follow one another.
+__device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total) {
+  const uint32_t die = id % 8, in = id / 8, each = total / 8, more = total % 8;
+  return die * each + min(die, more) + in;
+}
+
+// Four neighbouring entries of a row, each rounded to T once; `left` entries of the row from the first on are there, and the
+// row is aligned to four of them where `wide`.
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const f32x4& v, int64_t left, bool wide) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 t;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t[i] = static_cast<T>(v[i]);
+  if (wide && left >= 4) {
+    *reinterpret_cast<T4*>(p) = t;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) p[i] = t[i];
+  }
+}
+
+// The same of a weight's gradient: written, or added to what is there.
+__device__ __forceinline__ void add4(float* p, const f32x4& v, int64_t left, bool wide, bool accumulate) {
+  if (!accumulate) {
+    store4(p, v, left, wide);
+  } else if (wide && left >= 4) {
+    *reinterpret_cast<f32x4*>(p) += v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) p[i] += v[i];
+  }
+}
+
+// ---- Host side -----------------------------------------------------------------------------------------------
+
+// Longest row of a product's operand, in entries: offsets within a tile of 256 rows are 31 bits.
+constexpr int64_t kMostEntries = 1 << 20;
+constexpr int64_t kMostRowBytes = 1 << 23;
+
+// A matrix as a caller has it, and as the product kernels read it: rows of whole 16-byte pieces that start on 16 bytes.  What
+// is not like that is copied into the workspace first, with zeros behind the rows (`packed`).
+struct Matrix {
+  const void* p;
+  int64_t ld;  // entries
+  int64_t rows, cols;
+  size_t size;  // bytes of an entry
+  bool as_is() const {
+    return aligned_to(p, 16) && (rows <= 1 || ld * size % 16 == 0) && cols * size % 16 == 0 &&
+           (rows <= 1 || ld * static_cast<int64_t>(size) <= kMostRowBytes);
+  }
+  int64_t packed_row_bytes() const { return (cols * static_cast<int64_t>(size) + 15) / 16 * 16; }
+  size_t packed_bytes() const { return as_is() ? 0 : (static_cast<size_t>(rows) * packed_row_bytes() + 255) / 256 * 256; }
+};
+struct Read {  // what a kernel gets
+  const void* p;
+  int64_t ld;  // bytes
+};
+constexpr uint32_t kMostPacked = 4;
+struct Packing {
+  uint32_t count = 0;
+  struct Job {
+    const void* from;
+    void* to;
+    int64_t ld;  // entries
+    uint64_t pieces;
+    uint32_t per_row, cols;
+  } job[kMostPacked];
+  // How the kernels are to read `m`; moves `workspace` on by what it takes of it.
+  Read add(const Matrix& m, char*& workspace) {
+    if (m.as_is()) return {m.p, m.rows <= 1 ? m.packed_row_bytes() : m.ld * static_cast<int64_t>(m.size)};
+    const Read r = {workspace, m.packed_row_bytes()};
+    const uint32_t per_row = static_cast<uint32_t>(m.packed_row_bytes() / 16);
+    job[count++] = {m.p, workspace, m.ld, static_cast<uint64_t>(m.rows) * per_row, per_row, static_cast<uint32_t>(m.cols)};
+    workspace += m.packed_bytes();
+    return r;
+  }
+};
+// Enqueues the copies (one launch, or none).
+void run_packing(const Packing& p, size_t size, hipStream_t stream);
+
+// Tiles as workgroups: a dimension has room for 2^32 threads.
+constexpr uint32_t kGridX = 1u << 21;
+inline dim3 tile_grid(uint64_t tiles) {
+  return dim3(static_cast<uint32_t>(tiles < kGridX ? tiles : kGridX), static_cast<uint32_t>((tiles + kGridX - 1) / kGridX));
+}
+__device__ __forceinline__ uint32_t tile_id() { return blockIdx.y * kGridX + blockIdx.x; }
+
+// Tile number `id` of a result of tall x wide tiles: strips of eight tiles down, within them column after column, so that the
+// workgroups of a die share rows of both operands in its cache.
+__device__ __forceinline__ void tile_at(uint32_t id, uint32_t tall, uint32_t wide, uint32_t& down, uint32_t& across) {
+  const uint32_t strip = id / (8 * wide), in = id - strip * 8 * wide, height = min(8u, tall - strip * 8);
+  down = strip * 8 + in % height;
+  across = in / height;
+}
+
+// Which size of tile a result of rows x cols is made with, `many` of them at once: the largest leaves compute units idle where
+// there are few.  A compute unit's tiles cost what they hold, divided by the rate that a size reaches (8192 x 8192 x 8192
+// bfloat16: 256 x 256 1270 TFLOP/s, 128 x 128 1030, 64 x 64 680; 8192 x 4096 x 768: 759, 718, 586); less where there are too few
+// for one to be loaded while another is multiplied.
+enum TileSize { kTile256, kTile128, kTile64 };
+inline TileSize tile_size(uint64_t rows, uint64_t cols, uint64_t many) {
+  const auto cost = [&](uint64_t edge, double rate1, double rate2, double rate3) {
+    const uint64_t tiles = (rows + edge - 1) / edge * ((cols + edge - 1) / edge) * many, each = (tiles + 255) / 256;
+    return static_cast<double>(each * edge * edge) / (each <= 1 ? rate1 : each <= 2 ? rate2 : rate3);
+  };
+  const double large = cost(256, 1.0, 1.0, 1.0), middle = cost(128, 0.6, 0.85, 0.85), small = cost(64, 0.3, 0.45, 0.6);
+  if (large <= middle && large <= small) return kTile256;
+  return middle <= small ? kTile128 : kTile64;
+}
+// A weight's gradients, a matrix for each of n workers.
+inline bool gradient_valid(int32_t n, int64_t rows, int64_t cols, int64_t ld, int64_t stride) {
+  constexpr int64_t kMost = static_cast<int64_t>(1) << 40;
+  return (rows <= 1 || (ld >= cols && ld < kMost)) && (n <= 1 || (stride >= 0 && stride < kMost && stride >= cols));
+}
+// Whether the tiles of a result can be numbered, `many` results of 64 x 64 tiles.
+inline bool tiles_fit(int64_t rows, int64_t cols, int64_t many) {
+  return static_cast<double>((rows + 63) / 64) * static_cast<double>((cols + 63) / 64) * static_cast<double>(many) < 2147483648.0;
+}
+inline int workspace_status(const void* p, size_t bytes, size_t need) {
+  if (need == 0) return COMPAMS_OK;
+  if (!p) return COMPAMS_INVALID_ARG;
+  if (!aligned_to(p, 256)) return COMPAMS_BAD_ALIGNMENT;
+  return bytes < need ? COMPAMS_WORKSPACE_TOO_SMALL : COMPAMS_OK;
+}
+inline uint64_t tiles_of(uint64_t count, uint32_t edge) { return (count + edge - 1) / edge; }
+
+}  // namespace compams

@@ -2,8 +2,10 @@
 
 Layer norm, dropout from a counter-based generator, the join between two branches of a transformer block (bias, dropout,
 residual add and layer norm in one pass) and the softmax cross-entropy, each with its gradient: what the forward and
-backward pass that fills the rows of `Compams.compams_step`'s g needs around its matrix products.  Same names as the C ABI
-(include/compams.h, where every formula stands).
+backward pass that fills the rows of `Compams.compams_step`'s g needs around its matrix products.  With products of their own:
+a gated feed-forward block, the gradients behind its projections, and the cross-entropy of an output layer whose logits are
+never stored.  And the norm of every worker's gradient, cut to a largest one.  Same names as the C ABI (include/compams.h,
+where every formula stands).
 
 Activations are matrices (2-D tensors, rows contiguous, any distance between them) of n * rows rows: n workers, one
 after another.  Weights are float32 vectors, such as views of theta; their gradients are n x cols float32 tensors whose
@@ -56,11 +58,66 @@ class compams_loss(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class compams_gated(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("hidden", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("activation", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("gate_weight", ctypes.c_void_p), ("ld_gate_weight", ctypes.c_int64),
+                ("up_weight", ctypes.c_void_p), ("ld_up_weight", ctypes.c_int64),
+                ("gate_bias", ctypes.c_void_p), ("up_bias", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("ld_m", ctypes.c_int64), ("gate", ctypes.c_void_p), ("ld_gate", ctypes.c_int64),
+                ("up", ctypes.c_void_p), ("ld_up", ctypes.c_int64), ("dm", ctypes.c_void_p), ("ld_dm", ctypes.c_int64),
+                ("dgate", ctypes.c_void_p), ("ld_dgate", ctypes.c_int64), ("dup", ctypes.c_void_p), ("ld_dup", ctypes.c_int64),
+                ("dgate_bias", ctypes.c_void_p), ("ld_dgate_bias", ctypes.c_int64),
+                ("dup_bias", ctypes.c_void_p), ("ld_dup_bias", ctypes.c_int64), ("accumulate", ctypes.c_int32),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class compams_projections(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("hidden", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("dgate", ctypes.c_void_p), ("ld_dgate", ctypes.c_int64),
+                ("dup", ctypes.c_void_p), ("ld_dup", ctypes.c_int64), ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("gate_weight", ctypes.c_void_p), ("ld_gate_weight", ctypes.c_int64),
+                ("up_weight", ctypes.c_void_p), ("ld_up_weight", ctypes.c_int64),
+                ("dx", ctypes.c_void_p), ("ld_dx", ctypes.c_int64),
+                ("dgate_weight", ctypes.c_void_p), ("ld_dgate_weight", ctypes.c_int64), ("stride_dgate_weight", ctypes.c_int64),
+                ("dup_weight", ctypes.c_void_p), ("ld_dup_weight", ctypes.c_int64), ("stride_dup_weight", ctypes.c_int64),
+                ("accumulate", ctypes.c_int32), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class compams_linear_loss(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("target_type", ctypes.c_int32), ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("ld_weight", ctypes.c_int64), ("targets", ctypes.c_void_p),
+                ("ignore_index", ctypes.c_int64), ("grad_scale", ctypes.c_float),
+                ("mean_loss", ctypes.c_void_p), ("losses", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("ld_dx", ctypes.c_int64),
+                ("dweight", ctypes.c_void_p), ("ld_dweight", ctypes.c_int64), ("stride_dweight", ctypes.c_int64),
+                ("accumulate", ctypes.c_int32), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class compams_clip_tensor(ctypes.Structure):
+    _fields_ = [("from", ctypes.c_void_p), ("ld_from", ctypes.c_int64), ("to", ctypes.c_void_p), ("ld_to", ctypes.c_int64),
+                ("count", ctypes.c_int64), ("from_type", ctypes.c_int32), ("to_type", ctypes.c_int32)]
+
+
+class compams_clip(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("tensors", ctypes.c_int32), ("tensor", ctypes.c_void_p),
+                ("max_norm", ctypes.c_float), ("scale", ctypes.c_float),
+                ("norms", ctypes.c_void_p), ("factors", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 # The calls below lay the structures out with one pack each: a ctypes structure takes 50 ns for every field, and the
 # smallest calls are as long as their marshalling.  (The C compiler's own padding; a null pointer is 0.)
 _DROP = struct.Struct("@dQQP")
 _NORM = struct.Struct("@iqqiif dQQP PPP PqPqPqPq PP PqPqPqPq PqPqPqi PN")
 _LOSS = struct.Struct("@iqqii Pq Pqf PP Pq PN")
+_GATED = struct.Struct("@iqqqii PqPqPq PP PqPqPq Pq PqPq PqPq i PN")
+_PROJECTIONS = struct.Struct("@iqqqi PqPq Pq PqPq Pq PqqPqq i PN")
+_LINEAR_LOSS = struct.Struct("@iqqqii PqPq Pqf PP Pq Pqq i PN")
+_CLIP_TENSOR = struct.Struct("@PqPqqii")
+_CLIP = struct.Struct("@iiPffPPPN")
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 _NO_DROP = (0.0, 0, 0, 0)
 _LOW64 = (1 << 64) - 1
 
@@ -287,3 +344,204 @@ def compams_cross_entropy(logits: torch.Tensor, targets: torch.Tensor, n: int = 
     workspace, at, size = _workspace(workspace, need, dev)
     _check(_on_stream(dev, lib().compams_cross_entropy, _LOSS.pack(*a, at, size)), "compams_cross_entropy")
     return mean_loss, losses, dlogits
+
+
+def _activation(name: str) -> int:
+    a = ACTIVATIONS.get(name)
+    if a is None:
+        raise ValueError(f"unknown activation {name!r}: one of {', '.join(ACTIVATIONS)}")
+    return a
+
+
+def _weight_gradient(t: Optional[torch.Tensor], what: str, shape, device: torch.device):
+    """(pointer, row stride, worker stride) of a weight's gradients, a matrix for every worker; (0, 0, 0) for None."""
+    if t is None:
+        return 0, 0, 0
+    if t.dtype is torch.float32 and t.shape == shape and t.device == device:
+        n, outputs, cols = shape
+        worker, row, beside = t.stride()
+        if beside == 1 or cols == 1:
+            return t.data_ptr(), row if outputs > 1 else cols, worker if n > 1 else 0
+        raise ValueError(f"the entries of a row of {what} must be contiguous, got strides {t.stride()}")
+    raise ValueError(f"{what} must be {torch.float32} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _room(size, pack, a, workspace, device):
+    """The structure with the workspace that its call asks for, and what has to live until the call is made."""
+    need = size(pack(*a, 0, 0))
+    workspace, at, given = _workspace(workspace, need, device)
+    return pack(*a, at, given), workspace
+
+
+def compams_gated_forward(x: torch.Tensor, gate_weight: torch.Tensor, up_weight: torch.Tensor, activation: str = "silu", *,
+                          gate_bias: Optional[torch.Tensor] = None, up_bias: Optional[torch.Tensor] = None,
+                          m: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                          up: Optional[torch.Tensor] = None, keep: bool = True, workspace: Optional[torch.Tensor] = None):
+    """(m, gate, up) with gate = x gate_weight' + gate_bias, up = x up_weight' + up_bias and m = act(gate) up, formed before
+    the two are rounded.  keep=False: m alone (gate and up are None), for answers without a backward pass."""
+    total, _, cols = _shape(x, "x")
+    dev, dtype = x.device, x.dtype
+    hidden = _shape(gate_weight, "gate_weight")[0]
+    shape, of_weight, of_bias = (total, hidden), (hidden, cols), (hidden,)
+    if m is None:
+        m = torch.empty(shape, dtype=dtype, device=dev)
+    if not keep:
+        if gate is not None or up is not None:
+            raise ValueError("gate or up is given, but not to be kept")
+    else:
+        if gate is None:
+            gate = torch.empty(shape, dtype=dtype, device=dev)
+        if up is None:
+            up = torch.empty(shape, dtype=dtype, device=dev)
+    a = (1, total, cols, hidden, _type(dtype, "x"), _activation(activation), *_matrix(x, "x", x.shape, dtype, dev),
+         *_matrix(gate_weight, "gate_weight", of_weight, dtype, dev), *_matrix(up_weight, "up_weight", of_weight, dtype, dev),
+         _vector(gate_bias, "gate_bias", of_bias, dev), _vector(up_bias, "up_bias", of_bias, dev),
+         *_matrix(m, "m", shape, dtype, dev), *_matrix(gate, "gate", shape, dtype, dev), *_matrix(up, "up", shape, dtype, dev),
+         0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    a, workspace = _room(lib().compams_gated_forward_workspace_size, _GATED.pack, a, workspace, dev)
+    _check(_on_stream(dev, lib().compams_gated_forward, a), "compams_gated_forward")
+    return m, gate, up
+
+
+def compams_gated_backward(dm: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, n: int = 1, activation: str = "silu", *,
+                           dgate: Optional[torch.Tensor] = None, dup: Optional[torch.Tensor] = None,
+                           dgate_bias: Optional[torch.Tensor] = None, dup_bias: Optional[torch.Tensor] = None,
+                           bias: bool = True, accumulate: bool = False, workspace: Optional[torch.Tensor] = None):
+    """(dgate, dup, dgate_bias, dup_bias): the gradients of the two projections (dgate and dup may be written over dm, gate or
+    up) and of the two biases for each of the n workers (None with bias=False).  accumulate: the biases' gradients are added
+    to what is there (they have to be given then)."""
+    total, rows, hidden = _shape(dm, "dm", n)
+    dev, dtype, shape, of_bias = dm.device, dm.dtype, dm.shape, (n, hidden)
+    if dgate is None:
+        dgate = torch.empty((total, hidden), dtype=dtype, device=dev)
+    if dup is None:
+        dup = torch.empty((total, hidden), dtype=dtype, device=dev)
+    if bias:
+        dgate_bias, dup_bias = _gradients(accumulate, n, hidden, dev, dgate_bias, dup_bias)
+    elif dgate_bias is not None or dup_bias is not None:
+        raise ValueError("a bias's gradient is given, but not asked for")
+    a = (n, rows, 0, hidden, _type(dtype, "dm"), _activation(activation), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0,
+         *_matrix(gate, "gate", shape, dtype, dev), *_matrix(up, "up", shape, dtype, dev), *_matrix(dm, "dm", shape, dtype, dev),
+         *_matrix(dgate, "dgate", shape, dtype, dev), *_matrix(dup, "dup", shape, dtype, dev),
+         *_matrix(dgate_bias, "dgate_bias", of_bias, torch.float32, dev),
+         *_matrix(dup_bias, "dup_bias", of_bias, torch.float32, dev), 1 if accumulate else 0)
+    a, workspace = _room(lib().compams_gated_backward_workspace_size, _GATED.pack, a, workspace, dev)
+    _check(_on_stream(dev, lib().compams_gated_backward, a), "compams_gated_backward")
+    return dgate, dup, dgate_bias, dup_bias
+
+
+def compams_projections_backward(dgate: torch.Tensor, dup: Optional[torch.Tensor], x: Optional[torch.Tensor],
+                                 gate_weight: Optional[torch.Tensor], up_weight: Optional[torch.Tensor], n: int = 1, *,
+                                 dx: Optional[torch.Tensor] = None, dgate_weight: Optional[torch.Tensor] = None,
+                                 dup_weight: Optional[torch.Tensor] = None, accumulate: bool = False,
+                                 workspace: Optional[torch.Tensor] = None):
+    """(dx, dgate_weight, dup_weight): the gradient of what two projections read, and of their weights for each of the n
+    workers.  One projection: dup and up_weight None (and dup_weight, which is None then too).  Without x no weight's gradient
+    is formed, without gate_weight no dx.  accumulate: the weights' gradients are added to what is there (they have to be
+    given then)."""
+    total, rows, hidden = _shape(dgate, "dgate", n)
+    dev, dtype, shape = dgate.device, dgate.dtype, dgate.shape
+    if x is None and gate_weight is None:
+        raise ValueError("neither x nor gate_weight is given: there is no gradient to form")
+    cols = _shape(x, "x")[2] if x is not None else _shape(gate_weight, "gate_weight")[2]
+    if dup is None and (up_weight is not None or dup_weight is not None):
+        raise ValueError("up_weight or dup_weight is given, but no dup")
+    if gate_weight is None:
+        if dx is not None or up_weight is not None:
+            raise ValueError("dx or up_weight is given, but no gate_weight")
+    elif dx is None:
+        dx = torch.empty((total, cols), dtype=dtype, device=dev)
+    if x is None:
+        if dgate_weight is not None or dup_weight is not None:
+            raise ValueError("a weight's gradient is given, but no x")
+    elif accumulate and (dgate_weight is None or (dup is not None and dup_weight is None)):
+        raise ValueError("accumulate needs the gradients that are added to")
+    else:
+        if dgate_weight is None:
+            dgate_weight = torch.empty((n, hidden, cols), dtype=torch.float32, device=dev)
+        if dup is not None and dup_weight is None:
+            dup_weight = torch.empty((n, hidden, cols), dtype=torch.float32, device=dev)
+    of_x, of_weight, of_gradient = (total, cols), (hidden, cols), (n, hidden, cols)
+    a = (n, rows, cols, hidden, _type(dtype, "dgate"), *_matrix(dgate, "dgate", shape, dtype, dev),
+         *_matrix(dup, "dup", shape, dtype, dev), *_matrix(x, "x", of_x, dtype, dev),
+         *_matrix(gate_weight, "gate_weight", of_weight, dtype, dev), *_matrix(up_weight, "up_weight", of_weight, dtype, dev),
+         *_matrix(dx, "dx", of_x, dtype, dev), *_weight_gradient(dgate_weight, "dgate_weight", of_gradient, dev),
+         *_weight_gradient(dup_weight, "dup_weight", of_gradient, dev), 1 if accumulate else 0)
+    a, workspace = _room(lib().compams_projections_workspace_size, _PROJECTIONS.pack, a, workspace, dev)
+    _check(_on_stream(dev, lib().compams_projections_backward, a), "compams_projections_backward")
+    return dx, dgate_weight, dup_weight
+
+
+def compams_linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, n: int = 1,
+                                 ignore_index: int = -100, grad_scale: float = 1.0, *,
+                                 mean_loss: Optional[torch.Tensor] = None, losses: Optional[torch.Tensor] = None,
+                                 dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None,
+                                 gradient: bool = True, accumulate: bool = False, workspace: Optional[torch.Tensor] = None):
+    """(mean_loss, losses, dx, dweight) of the logits x weight', which are never stored: every worker's mean loss, every
+    row's, and grad_scale times the gradients of the workers' mean losses (None with gradient=False), of the weight for
+    each of the n workers.  accumulate: dweight is added to what is there (it has to be given then)."""
+    total, rows, cols = _shape(x, "x", n)
+    dev, dtype = x.device, x.dtype
+    vocab = _shape(weight, "weight")[0]
+    if mean_loss is None:
+        mean_loss = torch.empty(n, dtype=torch.float32, device=dev)
+    if losses is None:
+        losses = torch.empty(total, dtype=torch.float32, device=dev)
+    if not gradient:
+        if dx is not None or dweight is not None:
+            raise ValueError("dx or dweight is given, but no gradient asked for")
+    else:
+        if accumulate and dweight is None:
+            raise ValueError("accumulate needs the gradients that are added to")
+        if dx is None:
+            dx = torch.empty((total, cols), dtype=dtype, device=dev)
+        if dweight is None:
+            dweight = torch.empty((n, vocab, cols), dtype=torch.float32, device=dev)
+    target_type = _TARGET_TYPE.get(targets.dtype)
+    if target_type is None:
+        raise ValueError(f"targets must be int32 or int64, got {targets.dtype}")
+    a = (n, rows, cols, vocab, _type(dtype, "x"), target_type, *_matrix(x, "x", x.shape, dtype, dev),
+         *_matrix(weight, "weight", (vocab, cols), dtype, dev), _vector(targets, "targets", (total,), dev, targets.dtype),
+         ignore_index, grad_scale, _vector(mean_loss, "mean_loss", (n,), dev), _vector(losses, "losses", (total,), dev),
+         *_matrix(dx, "dx", x.shape, dtype, dev), *_weight_gradient(dweight, "dweight", (n, vocab, cols), dev),
+         1 if accumulate else 0)
+    a, workspace = _room(lib().compams_linear_loss_workspace_size, _LINEAR_LOSS.pack, a, workspace, dev)
+    _check(_on_stream(dev, lib().compams_linear_cross_entropy, a), "compams_linear_cross_entropy")
+    return mean_loss, losses, dx, dweight
+
+
+def compams_clip_gradients(gradients, max_norm: float, n: int = 1, *, scale: float = 1.0, out=None,
+                           norms: Optional[torch.Tensor] = None, factors: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None):
+    """(out, norms, factors): scale times the norm of each worker's gradient, and factors[i] = scale min(1, max_norm /
+    norms[i]) times it (0 and zeros where it is not finite: the worker takes no part).
+    gradients: a matrix of n rows, or a list of them (a tensor's gradients of all workers each), in any mixture of types.
+    out: the same shapes, each float32 or of its gradient's type, such as views of the step's g; None: in place.
+    max_norm: math.inf cuts nothing.  scale: takes a loss's scale back."""
+    alone = isinstance(gradients, torch.Tensor)
+    given = [gradients] if alone else list(gradients)
+    to = given if out is None else [out] if isinstance(out, torch.Tensor) else list(out)
+    if len(to) != len(given):
+        raise ValueError(f"out has {len(to)} tensors for {len(given)} gradients")
+    if not given:
+        raise ValueError("no gradients are given")
+    dev = given[0].device
+    if norms is None:
+        norms = torch.empty(n, dtype=torch.float32, device=dev)
+    if factors is None:
+        factors = torch.empty(n, dtype=torch.float32, device=dev)
+    table = bytearray(_CLIP_TENSOR.size * len(given))
+    for i, (t, o) in enumerate(zip(given, to)):
+        if t.dim() != 2 or t.shape[0] != n:
+            raise ValueError(f"a gradient must be a matrix of {n} rows, got shape {tuple(t.shape)}")
+        count = t.shape[1]
+        p, lp = _matrix(t, "a gradient", t.shape, t.dtype, dev)
+        q, lq = (p, lp) if o is t else _matrix(o, "out", t.shape, o.dtype, dev)
+        _CLIP_TENSOR.pack_into(table, i * _CLIP_TENSOR.size, p, lp, q, lq, count, _type(t.dtype, "a gradient"),
+                               _type(o.dtype, "out"))
+    keep = (ctypes.c_char * len(table)).from_buffer(table)
+    a = (n, len(given), ctypes.addressof(keep), max_norm, scale, _vector(norms, "norms", (n,), dev),
+         _vector(factors, "factors", (n,), dev))
+    a, workspace = _room(lib().compams_clip_workspace_size, _CLIP.pack, a, workspace, dev)
+    _check(_on_stream(dev, lib().compams_clip_gradients, a), "compams_clip_gradients")
+    return gradients if out is None else out, norms, factors
