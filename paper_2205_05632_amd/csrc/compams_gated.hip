@@ -69,32 +69,40 @@ __global__ __launch_bounds__(TL::kThreads) void k_gated_forward(ForwardArgs a) {
     g = side<T, kAlong>(a.gate_weight.p, a.gate_weight.ld, a.hidden, h0, a.cols);
     u = side<T, kAlong>(a.up_weight.p, a.up_weight.ld, a.hidden, h0, a.cols);
   }, 1, a.cols, COMPAMS_TILE_LDS_ARGS);
-  const uint32_t m1 = m0 + TL::first_m() + TL::lane_m(), h1 = h0 + TL::first_n() / 2 + TL::lane_n();
+  // The biases, then the product in the place of the first projection's sums.
+  const uint32_t h1 = h0 + TL::first_n() / 2;
 #pragma unroll
   for (uint32_t j = 0; j < TL::FN; j += 2) {
-    const uint32_t h = h1 + j * 8;
-    if (h >= a.hidden) continue;
-    const int64_t left = a.hidden - h;
+    const uint32_t h = h1 + TL::lane_n() + j * 8;
     f32x4 bg = {}, bu = {};
 #pragma unroll
     for (uint32_t q = 0; q < 4; ++q) {
-      if (a.gate_bias && q < left) bg[q] = a.gate_bias[h + q];
-      if (a.up_bias && q < left) bu[q] = a.up_bias[h + q];
+      if (a.gate_bias && h + q < a.hidden) bg[q] = a.gate_bias[h + q];
+      if (a.up_bias && h + q < a.hidden) bu[q] = a.up_bias[h + q];
     }
 #pragma unroll
     for (uint32_t i = 0; i < TL::FM; ++i) {
-      const uint32_t r = m1 + i * 16;
-      if (r >= a.total) continue;
-      const f32x4 g = t.sum[i][j] + bg, u = t.sum[i][j + 1] + bu;
-      f32x4 m;
-      float none;
-#pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) m[q] = activate<ACT, false>(g[q], none) * u[q];
-      store4(static_cast<T*>(a.m) + static_cast<int64_t>(r) * a.ld_m + h, m, left, a.aligned & 1u);
-      if (a.gate) store4(static_cast<T*>(a.gate) + static_cast<int64_t>(r) * a.ld_gate + h, g, left, a.aligned & 2u);
-      if (a.up) store4(static_cast<T*>(a.up) + static_cast<int64_t>(r) * a.ld_up + h, u, left, a.aligned & 4u);
+      t.sum[i][j] += bg;
+      t.sum[i][j + 1] += bu;
     }
   }
+  constexpr uint32_t kPieces = TL::FN * 2;
+  __syncthreads();  // (others may still read what they multiply)
+  const auto store = [&](void* to, int64_t ld, bool wide, auto of) {
+    t.template rows_of<kPieces>((lds_char*)lds_a0, of, [&](uint32_t m, uint32_t c, const f32x4& v) {
+      const uint32_t r = m0 + m, h = h1 + c;
+      if (r < a.total) store4(static_cast<T*>(to) + static_cast<int64_t>(r) * ld + h, v, static_cast<int64_t>(a.hidden) - h, wide);
+    });
+  };
+  if (a.gate) store(a.gate, a.ld_gate, a.aligned & 2u, [&](uint32_t i, uint32_t j) { return t.sum[i][2 * j]; });
+  if (a.up) store(a.up, a.ld_up, a.aligned & 4u, [&](uint32_t i, uint32_t j) { return t.sum[i][2 * j + 1]; });
+  store(a.m, a.ld_m, a.aligned & 1u, [&](uint32_t i, uint32_t j) {
+    f32x4 m;
+    float none;
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q) m[q] = activate<ACT, false>(t.sum[i][2 * j][q], none) * t.sum[i][2 * j + 1][q];
+    return m;
+  });
 }
 
 template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
@@ -114,7 +122,7 @@ void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
 template <typename T>
 void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
   switch (tile_size(a.total, 2 * static_cast<uint64_t>(a.hidden), 1)) {
-    case kTile256: launch_forward<T, 2, 4, 8, 4>(a, act, stream); break;
+    case kTile256: launch_forward<T, 4, 2, 4, 8>(a, act, stream); break;  // (64 columns of a projection to a wavefront)
     case kTile128: launch_forward<T, 2, 2, 4, 4>(a, act, stream); break;
     default: launch_forward<T, 2, 2, 2, 2>(a, act, stream); break;
   }

@@ -281,7 +281,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_input(LossArgs a) 
     d = side<T, kAlong>(a.d, a.ld_d, a.total, m0, a.width);
     w = side<T, kAcross>(static_cast<const char*>(a.weight.p) + static_cast<int64_t>(a.first) * a.weight.ld, a.weight.ld, a.cols, n0, a.width);
   }, 1, a.width, COMPAMS_TILE_LDS_ARGS);
-  t.each([&](uint32_t m, uint32_t n, f32x4 v) {
+  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, f32x4 v) {
     const uint32_t r = m0 + m;
     if (r >= a.total || n0 + n >= a.cols) return;
     if (!a.end) {
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_weight(LossArgs a)
   }, kParts<T>, a.rows, COMPAMS_TILE_LDS_ARGS);
   const float f = a.factor[w] / kHeld<T>;
   float* const to = a.dweight + w * a.stride_dweight + static_cast<int64_t>(a.first) * a.ld_dweight;
-  t.each([&](uint32_t m, uint32_t n, const f32x4& v) {
+  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m < a.width)
       add4(to + static_cast<int64_t>(m0 + m) * a.ld_dweight + n0 + n, v * f, static_cast<int64_t>(a.cols) - n0 - n, a.aligned >> 1 & 1u,
            a.accumulate);

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_projection_input(InputArgs a) 
     d = side<T, kAlong>(a.d[i].p, a.d[i].ld, a.total, m0, a.hidden);
     w = side<T, kAcross>(a.weight[i].p, a.weight[i].ld, a.cols, n0, a.hidden);
   }, a.count, a.hidden, COMPAMS_TILE_LDS_ARGS);
-  t.each([&](uint32_t m, uint32_t n, const f32x4& v) {
+  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m < a.total)
       store4(static_cast<T*>(a.dx) + static_cast<int64_t>(m0 + m) * a.ld_dx + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.aligned);
   });
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_projection_weight(WeightArgs a
     x = side<T, kAcross>(static_cast<const char*>(a.x.p) + first * a.x.ld, a.x.ld, a.cols, n0, a.rows);
   }, 1, a.rows, COMPAMS_TILE_LDS_ARGS);
   float* const to = a.dweight[which] + w * a.stride[which];
-  t.each([&](uint32_t m, uint32_t n, const f32x4& v) {
+  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m >= a.hidden) return;
     add4(to + static_cast<int64_t>(m0 + m) * a.ld[which] + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.aligned >> which & 1u,
          a.accumulate);

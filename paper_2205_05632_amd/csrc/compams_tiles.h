@@ -1,7 +1,7 @@
 // Products of matrices on the matrix cores, one tile of the result to a workgroup: D(m, n) = sum over k of A(m, k) B(n, k), with
 // fp32 sums.  The kernels that use it differ in what they do with the tile.  (wave64 only)
 //
-// A step takes 128 bytes of k: 64 entries of the 16-bit types, 32 of fp32.  Both operands' tiles of a step go from memory into
+// A step takes 128 bytes of k, 64 entries of the 16-bit types, 32 of fp32 (or half as many).  Both operands' tiles of a step go from memory into
 // LDS without passing through registers, 16 bytes a lane, while the step before is multiplied (two buffers, one barrier a step).
 // Reads beyond a matrix give zeros (the buffer descriptors' own bounds), so no length has to be a multiple of anything but 16 bytes.
 #pragma once
@@ -14,9 +14,6 @@ namespace compams {
 // one k, and all m or n).
 enum Form { kAlong, kAcross };
 
-constexpr uint32_t kStepBytes = 128;
-template <typename T>
-constexpr uint32_t kStep = kStepBytes / sizeof(T);
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -44,7 +41,7 @@ __device__ __forceinline__ void multiply(f32x4& d, Fragment<float>::type a, Frag
 
 // Places in LDS.  An operand's tile has EXTENT rows (or columns) of m or n.
 //
-// kAlong: EXTENT rows of 128 bytes.  The 16 bytes c of row r are kept at place c ^ (r % 8) of the row: the sixteen rows that a
+// kAlong: EXTENT rows of STEP bytes.  The 16 bytes c of row r are kept at place c ^ (r % 8) of the row: the sixteen rows that a
 // fragment is read from then begin in eight different places of the 128 bytes that LDS gives at once.
 //
 // kAcross: a row of EXTENT entries for every k of the step.  16-bit types are read with the transposing read: sixteen lanes read
@@ -56,24 +53,27 @@ __device__ __forceinline__ uint32_t moved(uint32_t k) {
   else return (k >> 2 & 3u) * 4;
 }
 
-template <typename T, Form F, uint32_t EXTENT>
+template <typename T, Form F, uint32_t EXTENT, uint32_t STEP>
 struct Place {
-  static constexpr uint32_t kRowBytes = F == kAlong ? kStepBytes : EXTENT * sizeof(T);
+  static constexpr uint32_t kRowBytes = F == kAlong ? STEP : EXTENT * sizeof(T);
   static constexpr uint32_t kPerRow = kRowBytes / 16;  // 16-byte pieces
-  static constexpr uint32_t kBytes = EXTENT * kStepBytes;
+  static constexpr uint32_t kBytes = EXTENT * STEP;
+
+  // kAlong: what a piece's number is changed by in row `row`.
+  __device__ static __forceinline__ uint32_t turned(uint32_t row) { return STEP == 128 ? row & 7u : row >> 1 & 3u; }
 
   // The row and the piece of it that is kept at 16-byte place p.
   __device__ static __forceinline__ void of(uint32_t p, uint32_t& row, uint32_t& piece) {
     row = p / kPerRow;
-    piece = p % kPerRow ^ (F == kAlong ? row & 7u : moved<T, EXTENT>(row));
+    piece = p % kPerRow ^ (F == kAlong ? turned(row) : moved<T, EXTENT>(row));
   }
 
-  // The fragment of rows (columns) first .. first + 15 and the sub-th half of the step's k.
+  // The fragment of rows (columns) first .. first + 15 and the sub-th 64 bytes of the step's k.
   __device__ static __forceinline__ typename Fragment<T>::type read(const lds_char* tile, uint32_t first, uint32_t sub) {
     const uint32_t lane = threadIdx.x & 63u, l = lane & 15u, g = lane >> 4;
     typename Fragment<T>::type v;
     if constexpr (F == kAlong) {
-      const uint32_t row = first + l, piece = (sub * 4 + g) ^ (row & 7u);
+      const uint32_t row = first + l, piece = (sub * 4 + g) ^ turned(row);
       v = *reinterpret_cast<const __attribute__((address_space(3))) typename Fragment<T>::type*>(tile + row * kRowBytes + piece * 16);
     } else if constexpr (sizeof(T) == 2) {
       const uint32_t k = sub * 32 + g * 8 + (l >> 2);
@@ -111,9 +111,10 @@ __device__ __forceinline__ Side side(const void* p, int64_t ld, uint32_t total, 
   return {at + static_cast<int64_t>(first) * sizeof(T), static_cast<uint32_t>(ld), (total - first) * static_cast<uint32_t>(sizeof(T)), k};
 }
 
-template <typename T, Form F, uint32_t EXTENT, uint32_t WAVES>
+template <typename T, Form F, uint32_t EXTENT, uint32_t WAVES, uint32_t STEP>
 struct Loader {
-  using At = Place<T, F, EXTENT>;
+  using At = Place<T, F, EXTENT, STEP>;
+  static constexpr uint32_t kRows = 1024 / STEP;  // kAlong: rows of an instruction
   static constexpr uint32_t kLoads = At::kBytes / (WAVES * 1024);
   static_assert(kLoads * WAVES * 1024 == At::kBytes, "a tile is loaded in whole instructions of every wave");
   uint32_t row[kLoads], piece[kLoads];
@@ -134,7 +135,7 @@ struct Loader {
       uint32_t r = row[i], ld = one.ld;
       bool second = false;
       if constexpr (TWO) {
-        second = ((i * WAVES + wave) * 8 / 16) & 1u;  // (the same for the wave: an instruction has eight rows)
+        second = ((i * WAVES + wave) * kRows / 16) & 1u;  // (the same for the wave: an instruction has eight or sixteen rows)
         r = r / 32 * 16 + r % 16;
         ld = second ? two.ld : one.ld;
       }
@@ -155,7 +156,7 @@ struct Loader {
       p = s.p + k0 * sizeof(T);
       bytes = (rows - 1) * s.ld + whole((s.k - k0) * static_cast<uint32_t>(sizeof(T)));
     } else {
-      const uint32_t rows = min(s.k - k0, kStep<T>);
+      const uint32_t rows = min(s.k - k0, STEP / static_cast<uint32_t>(sizeof(T)));
       p = s.p + static_cast<int64_t>(k0) * s.ld;
       bytes = (rows - 1) * s.ld + whole(s.extent);
     }
@@ -164,15 +165,16 @@ struct Loader {
 };
 
 // A workgroup of WM x WN wavefronts, each with FM x FN tiles of 16 x 16.
-template <typename T_, Form FA_, Form FB_, uint32_t WM_, uint32_t WN_, uint32_t FM_, uint32_t FN_, bool TWO_ = false>
+template <typename T_, Form FA_, Form FB_, uint32_t WM_, uint32_t WN_, uint32_t FM_, uint32_t FN_, bool TWO_ = false, uint32_t STEP_ = 128>
 struct Tiles {
+  static constexpr uint32_t STEP = STEP_, kStep = STEP_ / sizeof(T_);  // of k, in bytes and in entries
   using T = T_;
   static constexpr Form FA = FA_, FB = FB_;
   static constexpr uint32_t WM = WM_, WN = WN_, FM = FM_, FN = FN_;
   static constexpr bool kTwo = TWO_;  // B is two matrices, in turns of sixteen columns of the result
   static constexpr uint32_t kWaves = WM * WN, kThreads = kWaves * 64, kM = WM * FM * 16, kN = WN * FN * 16;
-  using PlaceA = Place<T, FA, kM>;
-  using PlaceB = Place<T, FB, kN>;
+  using PlaceA = Place<T, FA, kM, STEP>;
+  using PlaceB = Place<T, FB, kN, STEP>;
   static constexpr uint32_t kBytesA = PlaceA::kBytes, kBytesB = PlaceB::kBytes;
   f32x4 sum[FM][FN];
 
@@ -192,7 +194,7 @@ struct Tiles {
   __device__ __forceinline__ void step(const lds_char* a, const lds_char* b) {
     const uint32_t m = first_m(), n = first_n();
 #pragma unroll
-    for (uint32_t sub = 0; sub < 2; ++sub) {
+    for (uint32_t sub = 0; sub < STEP / 64; ++sub) {
       typename Fragment<T>::type fa[FM], fb[FN];
 #pragma unroll
       for (uint32_t j = 0; j < FN; ++j) fb[j] = PlaceB::read(b, n + j * 16, sub);
@@ -211,11 +213,11 @@ struct Tiles {
   template <typename Pair>
   __device__ __forceinline__ void run(Pair pair, uint32_t count, uint32_t k, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
     const uint32_t w = wave();
-    Loader<T, FA, kM, kWaves> la;
-    Loader<T, FB, kN, kWaves> lb;
+    Loader<T, FA, kM, kWaves, STEP> la;
+    Loader<T, FB, kN, kWaves, STEP> lb;
     la.init(w);
     lb.init(w);
-    const uint32_t steps = (k + kStep<T> - 1) / kStep<T> * count;
+    const uint32_t steps = (k + kStep - 1) / kStep * count;
     if (steps == 0) return;
     uint32_t at = 0, k0 = 0;
     Side a, b, b2;
@@ -223,7 +225,7 @@ struct Tiles {
     const auto load = [&](lds_char* ta, lds_char* tb) {
       la.template load<false>(a, a, k0, ta, w);
       lb.template load<kTwo>(b, b2, k0, tb, w);
-      k0 += kStep<T>;
+      k0 += kStep;
       if (k0 >= k) {
         k0 = 0;
         if (++at < count) pair(at, a, b, b2);
@@ -248,6 +250,8 @@ struct Tiles {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
+  // visit(row, column, four neighbouring entries) of the tile, as the matrix cores leave them: 64 bytes of each of sixteen rows at a
+  // time.
   template <typename Visit>
   __device__ __forceinline__ void each(Visit visit) {
     const uint32_t m = first_m() + lane_m(), n = first_n() + lane_n();
@@ -255,6 +259,43 @@ struct Tiles {
     for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
       for (uint32_t j = 0; j < FN; ++j) visit(m + i * 16, n + j * 16, sum[i][j]);
+  }
+
+  // The same by way of LDS, a row's entries in neighbouring lanes, for what is stored: a wavefront's part of a row goes to memory at
+  // once (8192 x 8192 fp32 stored and nothing else: 54 us, in pieces of 64 bytes 69).  Each wavefront has room for sixteen of its
+  // rows in `lds`; piece c of row r is at place c ^ r.  of(i, j): what is to be stored of the i, j-th tile of 16 x 16, PIECES / 4
+  // of them side by side.
+  template <uint32_t PIECES, typename Of, typename Visit>
+  __device__ __forceinline__ void rows_of(lds_char* lds, Of of, Visit visit) {
+    static_assert(16 * PIECES * 16 * kWaves <= kBytesA, "sixteen rows of every wavefront");
+    const uint32_t lane = threadIdx.x & 63u, m = lane_m();
+    lds_char* const mine = lds + wave() * (16 * PIECES * 16);
+    const uint32_t c = lane % PIECES;
+#pragma unroll
+    for (uint32_t i = 0; i < FM; ++i) {
+      settled();
+#pragma unroll
+      for (uint32_t j = 0; j < PIECES / 4; ++j)
+        *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(mine + (m * PIECES + ((j * 4 + lane / 16) ^ (m & (PIECES - 1)))) * 16) = of(i, j);
+      settled();
+#pragma unroll
+      for (uint32_t q = 0; q < 16 * PIECES / 64; ++q) {
+        const uint32_t r = q * (64 / PIECES) + lane / PIECES;
+        const f32x4 v = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(mine + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
+        visit(first_m() + i * 16 + r, c * 4, v);
+      }
+    }
+  }
+  template <typename Visit>
+  __device__ __forceinline__ void rows(lds_char* lds, Visit visit) {
+    __syncthreads();  // (others may still read what they multiply)
+    const uint32_t n = first_n();
+    rows_of<FN * 4>(lds, [&](uint32_t i, uint32_t j) { return sum[i][j]; }, [&](uint32_t r, uint32_t c, const f32x4& v) { visit(r, n + c, v); });
+  }
+  // A wavefront's accesses of LDS before this come before those after it.
+  __device__ static __forceinline__ void settled() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 };
 
