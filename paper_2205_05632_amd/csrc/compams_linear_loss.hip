@@ -6,9 +6,12 @@
 // from piece to piece) and by x (dweight, of which a piece holds whole rows).  Five products of the logits' size instead of three, more
 // for the digits of d, and no matrix of rows x vocabulary.
 //
-// d is held in T, in PARTS: d = first + second (+ third), each the rounded rest of those before, for dweight is fp32 and needs
-// fp32's digits of it: fp32 one part, fp16 two (d times 2^14: the second is off by 2^-39 of the largest d), bfloat16 three (2^-25 of
-// each d).  dx, of type T, takes the first part alone: one more rounding of half a step.
+// d times 2^14 is held in float16 where the operands have 16 bits, in two parts: the second is the rounded rest of the first, so that
+// both together are off by 2^-23 of an entry or 2^-39 of the largest possible one.  dweight is fp32 and takes both; dx, which is rounded
+// to 16 bits, takes the first alone, one more rounding of half a step of float16.  (In bfloat16 three parts would be needed, and
+// half as many products again: 8192 x 50257 x 768 4.9 ms.)  bfloat16 operands of these two products are therefore turned into
+// float16, each column times the power of two that brings its largest entry just below 2^15, and the results' columns are scaled
+// back: what 2^-39 of the largest entry of its own column does not reach is lost, as it is next to it in an fp32 sum.
 #include "compams_tiles.h"
 
 namespace compams {
@@ -16,25 +19,38 @@ namespace {
 
 constexpr uint32_t kThreads = 256;
 
+// What d and the operands of its products are held in, in how many parts, and how often d.
 template <typename T>
-constexpr uint32_t kParts = sizeof(T) == 4 ? 1 : __is_same(T, half_t) ? 2 : 3;
-// d as it is held is this often d.
+struct HeldAs { typedef half_t type; };
+template <>
+struct HeldAs<float> { typedef float type; };
 template <typename T>
-constexpr float kHeld = __is_same(T, half_t) ? 16384.0f : 1.0f;
+using Held = typename HeldAs<T>::type;
+template <typename T>
+constexpr uint32_t kParts = sizeof(T) == 4 ? 1 : 2;
+template <typename T>
+constexpr float kHeld = sizeof(T) == 4 ? 1.0f : 16384.0f;
+template <typename T>
+constexpr bool kScaled = __is_same(T, bfloat_t);  // columns are scaled
 
 // What the gradient needs of a row: d_c = e^(l_c - top) over - [c = target].
 struct RowStat {
   float top, over;  // over: 1 / sum of e^(l - top); 0 for an ignored row, NaN for one without a softmax or a loss
+  int32_t target;   // -1 for such rows
+  uint32_t none;
 };
 
 struct LossArgs {
   Read x, weight;     // x: as the caller has it (ignored rows too)
-  Read x_learnt;      // x with zeros in ignored rows
+  Read x_held;        // x with zeros in ignored rows, and the weight, as the second pass's products read them
+  Read weight_held;
+  uint32_t* tops;     // bits of the largest entry of every column: of each worker's x, then of the weight
   const void* targets;
   int64_t ignore;
   uint32_t wide_targets;
   uint32_t n, rows, total, cols, vocab;
   uint32_t tall, wide;       // tiles of the launch
+  uint32_t tall_weight;      // of dweight, beside those of dx
   float2* partial;           // [span of columns][row]: maximum, sum
   float* of_target;          // the target's logit of every row
   RowStat* stat;
@@ -59,28 +75,107 @@ __device__ __forceinline__ int64_t target_of(const LossArgs& a, uint32_t r) {
   return a.wide_targets ? static_cast<const int64_t*>(a.targets)[r] : static_cast<const int32_t*>(a.targets)[r];
 }
 
-// x with zeros in the rows that nothing is learnt from: whatever they hold, they add nothing to a weight's gradient.  (A NaN there
-// would, times the zero that d is.)
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_linear_loss_rows(LossArgs a, const T* x, int64_t ld_x) {
-  constexpr uint32_t kEach = 16 / sizeof(T);
-  typedef typename Fragment<T>::type Piece;
-  const uint32_t per_row = (a.cols + kEach - 1) / kEach;
-  const uint64_t pieces = static_cast<uint64_t>(a.total) * per_row;
-  for (uint64_t i = blockIdx.x * kThreads + threadIdx.x; i < pieces; i += static_cast<uint64_t>(gridDim.x) * kThreads) {
-    const uint32_t row = static_cast<uint32_t>(i / per_row), c = static_cast<uint32_t>(i - static_cast<uint64_t>(row) * per_row) * kEach;
-    Piece v = {};
-    if (target_of(a, row) != a.ignore) {
-      const T* const from = x + static_cast<int64_t>(row) * ld_x + c;
-      if (c + kEach <= a.cols) {
-        __builtin_memcpy(&v, from, sizeof(v));
-      } else {
+// The power of two that a column is multiplied by, from the bits of its largest entry.
+__device__ __forceinline__ int shift_of(uint32_t top) {
+  const int exponent = static_cast<int>(top >> 7) - 127;  // (bfloat16: eight bits of exponent over seven)
+  return exponent == 128 ? 0 : min(14 - exponent, 126);   // (infinities and NaNs stay what they are)
+}
+
+// A workgroup's share of a matrix that is gone over by columns: `wide` lanes side by side with eight columns each, for kRowsEach rows of
+// the matrix a lane.  Matrices are the workers' x, and the weight as number n.
+struct ColumnsArgs {
+  const void *x, *weight;
+  int64_t ld_x, ld_weight;        // entries
+  uint32_t wide, across, parts_x, parts_weight;
+};
+constexpr uint32_t kRowsEach = 16;
+struct Share {
+  uint32_t matrix, first, last, column, step;  // rows first, first + step, ... before `last`
+};
+__device__ __forceinline__ bool share_of(const LossArgs& a, const ColumnsArgs& c, Share& s) {
+  const uint32_t strip = blockIdx.x % c.across, tall = kThreads / c.wide;
+  uint32_t part = blockIdx.x / c.across;
+  const uint32_t of_x = c.parts_x * a.n;
+  s.matrix = part < of_x ? part / c.parts_x : a.n;
+  part = part < of_x ? part - s.matrix * c.parts_x : part - of_x;
+  const uint32_t rows = s.matrix < a.n ? a.rows : a.vocab;
+  s.step = tall;
+  s.last = static_cast<uint32_t>(min(static_cast<uint64_t>(rows), static_cast<uint64_t>(part + 1) * tall * kRowsEach));
+  s.first = part * tall * kRowsEach + threadIdx.x / c.wide;
+  s.column = (strip * c.wide + threadIdx.x % c.wide) * kGroup;
+  return s.column < a.cols;
+}
+
+// The largest entry of every column.  (Whichever comes first: a maximum.)
+__global__ __launch_bounds__(kThreads) void k_linear_loss_tops(LossArgs a, ColumnsArgs c) {
+  __shared__ uint32_t joined[kThreads][kGroup + 1];
+  Share s;
+  const bool mine = share_of(a, c, s);
+  uint32_t top[kGroup] = {};
+  if (mine) {
+    const bool of_x = s.matrix < a.n;
+    const uint32_t row0 = of_x ? s.matrix * a.rows : 0;
+    const bfloat_t* const p = static_cast<const bfloat_t*>(of_x ? c.x : c.weight);
+    const int64_t ld = of_x ? c.ld_x : c.ld_weight;
+#pragma unroll 4
+    for (uint32_t r = s.first; r < s.last; r += s.step) {
+      if (of_x && target_of(a, row0 + r) == a.ignore) continue;
+      const typename Group<bfloat_t>::type raw = load_raw(p + static_cast<int64_t>(row0 + r) * ld, s.column, a.cols);
 #pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k)
-          if (c + k < a.cols) v[k] = from[k];
+      for (uint32_t j = 0; j < kGroup; ++j) {
+        uint16_t bits;
+        __builtin_memcpy(&bits, reinterpret_cast<const char*>(&raw) + 2 * j, 2);
+        top[j] = max(top[j], static_cast<uint32_t>(bits & 0x7fffu));
       }
     }
-    static_cast<Piece*>(const_cast<void*>(a.x_learnt.p))[i] = v;
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < kGroup; ++j) joined[threadIdx.x][j] = top[j];
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < c.wide * kGroup; i += kThreads) {
+    uint32_t most = 0;
+    for (uint32_t k = i / kGroup; k < kThreads; k += c.wide) most = max(most, joined[k][i % kGroup]);
+    const uint32_t column = blockIdx.x % c.across * c.wide * kGroup + i;
+    if (column < a.cols && most) atomicMax(a.tops + static_cast<uint64_t>(s.matrix) * a.cols + column, most);
+  }
+}
+
+// x with zeros in the rows that nothing is learnt from - whatever they hold, they add nothing to a weight's gradient (a NaN there would,
+// times the zero that d is) - and, of bfloat16, both matrices in float16 with their columns scaled.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_linear_loss_hold(LossArgs a, ColumnsArgs c) {
+  typedef typename Group<Held<T>>::type Out;
+  Share s;
+  if (!share_of(a, c, s)) return;
+  const bool of_x = s.matrix < a.n;
+  const uint32_t row0 = of_x ? s.matrix * a.rows : 0;
+  const T* const p = static_cast<const T*>(of_x ? c.x : c.weight);
+  const int64_t ld = of_x ? c.ld_x : c.ld_weight;
+  char* const to = static_cast<char*>(const_cast<void*>(of_x ? a.x_held.p : a.weight_held.p));
+  const int64_t ld_to = of_x ? a.x_held.ld : a.weight_held.ld;
+  int shift[kGroup] = {};
+  if constexpr (kScaled<T>) {
+#pragma unroll
+    for (uint32_t j = 0; j < kGroup; ++j)
+      shift[j] = s.column + j < a.cols ? shift_of(a.tops[static_cast<uint64_t>(s.matrix) * a.cols + s.column + j]) : 0;
+  }
+#pragma unroll 4
+  for (uint32_t r = s.first; r < s.last; r += s.step) {
+    Out out = {};
+    if (!of_x || target_of(a, row0 + r) != a.ignore) {
+      const typename Group<T>::type raw = load_raw(p + static_cast<int64_t>(row0 + r) * ld, s.column, a.cols);
+#pragma unroll
+      for (uint32_t j = 0; j < kGroup; ++j) {
+        if constexpr (kScaled<T>) out[j] = static_cast<half_t>(ldexpf(to_float(raw[j]), shift[j]));
+        else out[j] = raw[j];
+      }
+    }
+    char* const at = to + static_cast<int64_t>(row0 + r) * ld_to + s.column * sizeof(Held<T>);
+    if (sizeof(Held<T>) == 2 || s.column + kGroup <= a.cols + 3) {
+      __builtin_memcpy(__builtin_assume_aligned(at, 16), &out, sizeof(out));
+    } else {  // (fp32: a row is padded to four entries)
+      __builtin_memcpy(__builtin_assume_aligned(at, 16), &out, sizeof(out) / 2);
+    }
   }
 }
 
@@ -112,7 +207,9 @@ __device__ __forceinline__ float over_row(float v, Op op) {
 struct Max {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
-// e^(l - top), and 0 where nothing has come yet that is more than minus infinity (a NaN stays one, an infinity gives one).
+// e^z by the processor's 2^x.
+__device__ __forceinline__ float exp_of(float z) { return __builtin_amdgcn_exp2f(z * 1.44269504088896341f); }
+// What a row's logits are compared with: their maximum, or 0 where that is minus infinity (e^(l - top) is 0 then, and not a NaN).
 __device__ __forceinline__ float base_of(float top) { return top == -INFINITY ? 0.0f : top; }
 
 // First pass.  A wavefront has 64 columns of its rows in every size of tile, so that a row's sums are added up in the same order
@@ -127,6 +224,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) 
   if (!logits(t, a, m0, n0, COMPAMS_TILE_LDS_ARGS)) return;
   const uint32_t span = n0 + TL::first_n(), n1 = span + TL::lane_n();
   if (span >= a.vocab) return;
+  const bool last = span + kSpan > a.vocab;  // (the same for the wavefront)
 #pragma unroll
   for (uint32_t i = 0; i < TL::FM; ++i) {
     const uint32_t r = m0 + TL::first_m() + TL::lane_m() + i * 16;
@@ -135,7 +233,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) 
     for (uint32_t j = 0; j < TL::FN; ++j)
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q) {
-        if (n1 + j * 16 + q >= a.vocab) t.sum[i][j][q] = -INFINITY;
+        if (last && n1 + j * 16 + q >= a.vocab) t.sum[i][j][q] = -INFINITY;
         top = fmaxf(top, t.sum[i][j][q]);
       }
     top = over_row(top, Max());
@@ -144,17 +242,18 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) 
 #pragma unroll
     for (uint32_t j = 0; j < TL::FN; ++j)
 #pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) s += __expf(t.sum[i][j][q] - base);
+      for (uint32_t q = 0; q < 4; ++q) s += exp_of(t.sum[i][j][q] - base);
     s = over_row(s, Add());
     if (r >= a.total) continue;
     if (threadIdx.x % 64 < 16) a.partial[static_cast<uint64_t>(span / kSpan) * a.total + r] = make_float2(top, s);
-    const int64_t at = target_of(a, r) - n1;
-    if (at >= 0 && at < kSpan) {
+    const int64_t target = target_of(a, r);
+    if (target >= span && target < span + kSpan && target < a.vocab) {
+      const uint32_t at = static_cast<uint32_t>(target) - n1;
 #pragma unroll
       for (uint32_t j = 0; j < TL::FN; ++j)
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q)
-          if (at == j * 16 + q && n1 + at < a.vocab) a.of_target[r] = t.sum[i][j][q];
+          if (at == j * 16 + q) a.of_target[r] = t.sum[i][j][q];
     }
   }
 }
@@ -163,6 +262,9 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) 
 __global__ __launch_bounds__(kThreads) void k_linear_loss_join(LossArgs a) {
   __shared__ float2 part[16][17];
   const uint32_t l = threadIdx.x % 16, turn = threadIdx.x / 16, spans = (a.vocab - 1) / kSpan + 1;
+  if (a.tops)  // (cleared for the kernels that follow)
+    for (uint64_t i = blockIdx.x * kThreads + threadIdx.x; i < static_cast<uint64_t>(a.n + 1) * a.cols; i += static_cast<uint64_t>(gridDim.x) * kThreads)
+      a.tops[i] = 0;
   for (uint64_t first = blockIdx.x * 16u; first < a.total; first += static_cast<uint64_t>(gridDim.x) * 16) {
     const uint64_t r = first + l;
     float top = -INFINITY, s = 0.0f;
@@ -170,7 +272,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_loss_join(LossArgs a) {
       for (uint32_t k = turn; k < spans; k += 16) {
         const float2 one = a.partial[static_cast<uint64_t>(k) * a.total + r];
         const float more = fmaxf(top, one.x), base = base_of(more);
-        s = s * __expf(top - base) + one.y * __expf(one.x - base);
+        s = s * exp_of(top - base) + one.y * exp_of(one.x - base);
         top = more;
       }
     part[turn][l] = make_float2(top, s);
@@ -181,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_loss_join(LossArgs a) {
       for (uint32_t k = 1; k < 16; ++k) most = fmaxf(most, part[k][l].x);
       float sum = 0.0f;  // (a row without a finite logit: e^(NaN))
 #pragma unroll
-      for (uint32_t k = 0; k < 16; ++k) sum += part[k][l].y * (part[k][l].x == most && most != -INFINITY ? 1.0f : __expf(part[k][l].x - most));
+      for (uint32_t k = 0; k < 16; ++k) sum += part[k][l].y * (part[k][l].x == most && most != -INFINITY ? 1.0f : exp_of(part[k][l].x - most));
       const int64_t t = target_of(a, static_cast<uint32_t>(r));
       const bool learnt = t != a.ignore, inside = t >= 0 && t < a.vocab;
       const float loss = inside ? (most - a.of_target[r]) + logf(sum) : NAN;
@@ -189,7 +291,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_loss_join(LossArgs a) {
       float over = 1.0f / sum;
       if (!inside || !(most < INFINITY)) over = NAN;
       if (a.losses) a.losses[r] = learnt ? (over == over ? loss : NAN) : 0.0f;
-      a.stat[r] = {most, learnt ? over : 0.0f};
+      a.stat[r] = {most, learnt ? over : 0.0f, learnt && inside ? static_cast<int32_t>(t) : -1, 0u};
     }
     __syncthreads();
   }
@@ -226,50 +328,58 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_gradient(LossArgs 
   uint32_t m0, n0;
   if (!logits(t, a, m0, n0, COMPAMS_TILE_LDS_ARGS)) return;
   const uint32_t n1 = n0 + TL::first_n() + TL::lane_n();
+  const bool last = n0 + TL::kN > a.width;
 #pragma unroll
   for (uint32_t i = 0; i < TL::FM; ++i) {
     const uint32_t r = m0 + TL::first_m() + TL::lane_m() + i * 16;
-    if (r >= a.total) continue;
-    const RowStat s = a.stat[r];
-    const int64_t at = target_of(a, r) - a.first;
-    char* const to = static_cast<char*>(a.d) + static_cast<int64_t>(r) * a.ld_d;
+    const RowStat s = a.stat[min(r, a.total - 1)];
+    const float over = s.over * kHeld<T>;
+    const uint32_t at = static_cast<uint32_t>(s.target) - a.first - n1;
 #pragma unroll
-    for (uint32_t j = 0; j < TL::FN; ++j) {
-      const uint32_t n = n1 + j * 16;
-      if (n >= a.width + 16 / sizeof(T)) continue;
-      f32x4 d;
+    for (uint32_t j = 0; j < TL::FN; ++j)
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q) {
-        d[q] = __expf(t.sum[i][j][q] - s.top) * s.over;
-        if (at == n + q) d[q] -= 1.0f;
-        d[q] = s.over == 0.0f || n + q >= a.width ? 0.0f : d[q] * kHeld<T>;
+        // (the minimum: an ignored row's logits may be anything, and none is above its row's maximum in any other)
+        float d = exp_of(fminf(t.sum[i][j][q] - s.top, 0.0f)) * over;
+        d -= at == j * 16 + q ? kHeld<T> : 0.0f;
+        t.sum[i][j][q] = last && n1 + j * 16 + q >= a.width ? 0.0f : d;
       }
-      typedef T T4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-      for (uint32_t p = 0; p < kParts<T>; ++p) {
-        T4 part;
-#pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-          part[q] = static_cast<T>(d[q]);
-          d[q] -= to_float(part[q]);
-        }
-        *reinterpret_cast<T4*>(to + p * a.part_bytes + n * sizeof(T)) = part;
-      }
-    }
   }
+  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
+    if (m0 + m >= a.total || n0 + n >= a.width + 16 / sizeof(T)) return;
+    typedef Held<T> H4 __attribute__((ext_vector_type(4)));
+    char* const to = static_cast<char*>(a.d) + static_cast<int64_t>(m0 + m) * a.ld_d + (n0 + n) * sizeof(Held<T>);
+    H4 part;
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q) part[q] = static_cast<Held<T>>(v[q]);
+    *reinterpret_cast<H4*>(to) = part;
+    if constexpr (kParts<T> == 2) {
+      H4 rest;
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) rest[q] = static_cast<Held<T>>(v[q] - to_float(part[q]));
+      *reinterpret_cast<H4*>(to + a.part_bytes) = rest;
+    }
+  });
 }
 
-// dx of all rows.  The sums go on from those of the pieces before, so that they do not depend on where pieces end.
-template <typename TL>
-__global__ __launch_bounds__(TL::kThreads) void k_linear_loss_input(LossArgs a) {
-  using T = typename TL::T;
-  COMPAMS_TILE_LDS(TL);
-  const uint32_t tiles = a.tall * a.wide, id = tile_id();
-  if (id >= tiles) return;
+// 2^-shift of four columns.
+template <typename T>
+__device__ __forceinline__ f32x4 scales(const LossArgs& a, uint32_t matrix, uint32_t n) {
+  f32x4 v = {1.0f, 1.0f, 1.0f, 1.0f};
+  if constexpr (kScaled<T>) {
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q)
+      if (a.tops && n + q < a.cols) v[q] = ldexpf(1.0f, -shift_of(a.tops[static_cast<uint64_t>(matrix) * a.cols + n + q]));
+  }
+  return v;
+}
+
+// A tile of dx.  The sums go on from those of the pieces before, so that they do not depend on where pieces end.
+template <typename TL, typename T>
+__device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
   uint32_t down, across;
-  tile_at(by_die(id, tiles), a.tall, a.wide, down, across);
-  const uint32_t m0 = down * TL::kM, n0 = across * TL::kN;
-  const uint32_t padded = (a.cols + 3) / 4 * 4;
+  tile_at(by_die(id, a.tall * a.wide), a.tall, a.wide, down, across);
+  const uint32_t m0 = down * TL::kM, n0 = across * TL::kN, padded = (a.cols + 3) / 4 * 4;
   const auto sums = [&](uint32_t r, uint32_t n) { return reinterpret_cast<f32x4*>(a.dx_sum + static_cast<uint64_t>(r) * padded + n); };
   TL t;
   t.clear();
@@ -278,10 +388,12 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_input(LossArgs a) 
       if (m0 + m < a.total && n0 + n < a.cols) v = *sums(m0 + m, n0 + n);
     });
   t.run([&](uint32_t, Side& d, Side& w, Side&) {
-    d = side<T, kAlong>(a.d, a.ld_d, a.total, m0, a.width);
-    w = side<T, kAcross>(static_cast<const char*>(a.weight.p) + static_cast<int64_t>(a.first) * a.weight.ld, a.weight.ld, a.cols, n0, a.width);
-  }, 1, a.width, COMPAMS_TILE_LDS_ARGS);
-  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, f32x4 v) {
+    d = side<typename TL::T, kAlong>(a.d, a.ld_d, a.total, m0, a.width);
+    w = side<typename TL::T, kAcross>(static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.first) * a.weight_held.ld,
+                                      a.weight_held.ld, a.cols, n0, a.width);
+  }, 1, a.width, a0, b0, a1, b1);
+  const f32x4 of_column = a.end ? scales<T>(a, a.n, n0 + TL::row_n()) : f32x4{};
+  t.rows(a0, [&](uint32_t m, uint32_t n, f32x4 v) {
     const uint32_t r = m0 + m;
     if (r >= a.total || n0 + n >= a.cols) return;
     if (!a.end) {
@@ -291,70 +403,87 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_input(LossArgs a) 
     const bool learnt = a.stat[r].over != 0.0f;
     const float f = a.factor[r / a.rows] / kHeld<T>;
 #pragma unroll
-    for (uint32_t q = 0; q < 4; ++q) v[q] = learnt ? v[q] * f : 0.0f;
+    for (uint32_t q = 0; q < 4; ++q) v[q] = learnt ? v[q] * of_column[q] * f : 0.0f;
     store4(static_cast<T*>(a.dx) + static_cast<int64_t>(r) * a.ld_dx + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.aligned & 1u);
   });
 }
 
-// dweight's rows of this piece, for every worker: k is the worker's rows, once for each part of d, the least first.
-template <typename TL>
-__global__ __launch_bounds__(TL::kThreads) void k_linear_loss_weight(LossArgs a) {
-  using T = typename TL::T;
-  COMPAMS_TILE_LDS(TL);
-  const uint32_t each = a.tall * a.wide, tiles = each * a.n, id = tile_id();
-  if (id >= tiles) return;
-  const uint32_t mine = by_die(id, tiles), w = mine / each;
+// A tile of dweight's rows of this piece, of one worker: k is the worker's rows, once for each part of d, the lesser first.
+template <typename TL, typename T>
+__device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+  const uint32_t each = a.tall_weight * a.wide, mine = by_die(id, each * a.n), w = mine / each;
   uint32_t down, across;
-  tile_at(mine - w * each, a.tall, a.wide, down, across);
+  tile_at(mine - w * each, a.tall_weight, a.wide, down, across);
   const uint32_t m0 = down * TL::kM, n0 = across * TL::kN;
   TL t;
   t.clear();
   const int64_t row = static_cast<int64_t>(w) * a.rows;
   t.run([&](uint32_t i, Side& d, Side& x, Side&) {
     const char* const part = static_cast<const char*>(a.d) + (kParts<T> - 1 - i) * a.part_bytes;
-    d = side<T, kAcross>(part + row * a.ld_d, a.ld_d, a.width, m0, a.rows);  // (entries behind `width` meet no stored sum)
-    x = side<T, kAcross>(static_cast<const char*>(a.x_learnt.p) + row * a.x_learnt.ld, a.x_learnt.ld, a.cols, n0, a.rows);
-  }, kParts<T>, a.rows, COMPAMS_TILE_LDS_ARGS);
-  const float f = a.factor[w] / kHeld<T>;
+    d = side<typename TL::T, kAcross>(part + row * a.ld_d, a.ld_d, static_cast<uint32_t>(a.ld_d / sizeof(typename TL::T)), m0, a.rows);
+    x = side<typename TL::T, kAcross>(static_cast<const char*>(a.x_held.p) + row * a.x_held.ld, a.x_held.ld, a.cols, n0, a.rows);
+  }, kParts<T>, a.rows, a0, b0, a1, b1);  // (what d has behind `width` meets no sum that is stored)
+  const f32x4 f = scales<T>(a, w, n0 + TL::row_n());
+  const float factor = a.factor[w] / kHeld<T>;
   float* const to = a.dweight + w * a.stride_dweight + static_cast<int64_t>(a.first) * a.ld_dweight;
-  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
+  t.rows(a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m < a.width)
-      add4(to + static_cast<int64_t>(m0 + m) * a.ld_dweight + n0 + n, v * f, static_cast<int64_t>(a.cols) - n0 - n, a.aligned >> 1 & 1u,
-           a.accumulate);
+      add4(to + static_cast<int64_t>(m0 + m) * a.ld_dweight + n0 + n, v * f * factor, static_cast<int64_t>(a.cols) - n0 - n,
+           a.aligned >> 1 & 1u, a.accumulate);
   });
 }
 
+// Both products of a piece in one launch: dx has few tiles of many steps (the piece's columns are its k), dweight many of few, and
+// together they fill the card (apart, 96 and 384 tiles of 8192 x 4096 x 768 left a third of it idle).  dx's tiles come first.
+template <typename X, typename W, typename T>
+__global__ __launch_bounds__(X::kThreads) void k_linear_loss_products(LossArgs a) {
+  static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
+  COMPAMS_TILE_LDS(X);
+  const uint32_t of_dx = a.dx ? a.tall * a.wide : 0, of_weight = a.dweight ? a.tall_weight * a.wide * a.n : 0, id = tile_id();
+  if (id < of_dx) input_tile<X, T>(a, id, COMPAMS_TILE_LDS_ARGS);
+  else if (id < of_dx + of_weight) weight_tile<W, T>(a, id - of_dx, COMPAMS_TILE_LDS_ARGS);
+}
+
 // ---- Launches ------------------------------------------------------------------------------------------------
-enum Pass { kStats, kGradient, kInput, kWeight };
+enum Pass { kStats, kGradient };
 
 template <Pass PASS, typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
 void launch_pass(LossArgs& a, hipStream_t stream) {
-  constexpr Form A = PASS == kWeight ? kAcross : kAlong, B = PASS == kInput || PASS == kWeight ? kAcross : kAlong;
-  using TL = Tiles<T, A, B, WM, WN, FM, FN>;
-  a.tall = static_cast<uint32_t>(tiles_of(PASS == kWeight ? a.width : a.total, TL::kM));
-  a.wide = static_cast<uint32_t>(tiles_of(PASS == kStats ? a.vocab : PASS == kGradient ? a.width : a.cols, TL::kN));
-  const dim3 grid = tile_grid(static_cast<uint64_t>(a.tall) * a.wide * (PASS == kWeight ? a.n : 1)), block(TL::kThreads);
+  using TL = Tiles<T, kAlong, kAlong, WM, WN, FM, FN>;
+  a.tall = static_cast<uint32_t>(tiles_of(a.total, TL::kM));
+  a.wide = static_cast<uint32_t>(tiles_of(PASS == kStats ? a.vocab : a.width, TL::kN));
+  const dim3 grid = tile_grid(static_cast<uint64_t>(a.tall) * a.wide), block(TL::kThreads);
   if constexpr (PASS == kStats) hipLaunchKernelGGL(k_linear_loss_stats<TL>, grid, block, 0, stream, a);
-  else if constexpr (PASS == kGradient) hipLaunchKernelGGL(k_linear_loss_gradient<TL>, grid, block, 0, stream, a);
-  else if constexpr (PASS == kInput) hipLaunchKernelGGL(k_linear_loss_input<TL>, grid, block, 0, stream, a);
-  else hipLaunchKernelGGL(k_linear_loss_weight<TL>, grid, block, 0, stream, a);
-}
-template <Pass PASS>
-TileSize pass_size(const LossArgs& a) {
-  if (PASS == kStats) return tile_size(a.total, a.vocab, 1);
-  if (PASS == kGradient) return tile_size(a.total, a.width, 1);
-  if (PASS == kInput) return tile_size(a.total, a.cols, 1);
-  return tile_size(a.width, a.cols, a.n);
+  else hipLaunchKernelGGL(k_linear_loss_gradient<TL>, grid, block, 0, stream, a);
 }
 template <Pass PASS, typename T>
 void launch_pass(LossArgs& a, hipStream_t stream) {
-  switch (pass_size<PASS>(a)) {
+  switch (tile_size(a.total, PASS == kStats ? a.vocab : a.width, 1)) {
     case kTile256: launch_pass<PASS, T, 2, 4, 8, 4>(a, stream); break;
     case kTile128: launch_pass<PASS, T, 2, 2, 4, 4>(a, stream); break;
     default:
       if constexpr (PASS == kStats) launch_pass<PASS, T, 4, 1, 1, 4>(a, stream);
       else launch_pass<PASS, T, 2, 2, 2, 2>(a, stream);
       break;
+  }
+}
+template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
+void launch_products(LossArgs& a, hipStream_t stream) {
+  using X = Tiles<Held<T>, kAlong, kAcross, WM, WN, FM, FN>;
+  using W = Tiles<Held<T>, kAcross, kAcross, WM, WN, FM, FN>;
+  a.tall = static_cast<uint32_t>(tiles_of(a.total, X::kM));
+  a.tall_weight = static_cast<uint32_t>(tiles_of(a.width, X::kM));
+  a.wide = static_cast<uint32_t>(tiles_of(a.cols, X::kN));
+  const uint64_t tiles = static_cast<uint64_t>(a.wide) * ((a.dx ? a.tall : 0) + (a.dweight ? static_cast<uint64_t>(a.tall_weight) * a.n : 0));
+  if (tiles) hipLaunchKernelGGL((k_linear_loss_products<X, W, T>), tile_grid(tiles), dim3(X::kThreads), 0, stream, a);
+}
+template <typename T>
+void launch_products(LossArgs& a, hipStream_t stream) {
+  const uint64_t rows = (a.dx ? a.total : 0) + (a.dweight ? static_cast<uint64_t>(a.width) * a.n : 0);
+  switch (tile_size(rows, a.cols, 1)) {
+    case kTile256: launch_products<T, 2, 4, 8, 4>(a, stream); break;
+    case kTile128: launch_products<T, 2, 2, 4, 4>(a, stream); break;
+    default: launch_products<T, 2, 2, 2, 2>(a, stream); break;
   }
 }
 
@@ -366,16 +495,17 @@ bool linear_loss_valid(const compams_linear_loss* a) {
          tiles_fit(a->n * a->rows, a->vocab, 1) && tiles_fit(a->n * a->rows, a->cols, 1) && tiles_fit(a->vocab, a->cols, a->n);
 }
 struct Room {
-  size_t x = 0, weight = 0, x_learnt = 0, partial = 0, of_target = 0, stat = 0, losses = 0, factor = 0, d = 0, dx_sum = 0;
+  size_t x = 0, weight = 0, x_held = 0, weight_held = 0, tops = 0, partial = 0, of_target = 0, stat = 0, losses = 0, factor = 0, d = 0,
+         dx_sum = 0;
   uint32_t piece = 0, pieces = 0;
-  size_t all() const { return x + weight + x_learnt + partial + of_target + stat + losses + factor + d + dx_sum; }
+  size_t all() const { return x + weight + x_held + weight_held + tops + partial + of_target + stat + losses + factor + d + dx_sum; }
 };
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-inline uint32_t parts_of(int32_t type) { return type == COMPAMS_F32 ? kParts<float> : type == COMPAMS_F16 ? kParts<half_t> : kParts<bfloat_t>; }
+inline uint32_t parts_of(int32_t type) { return type == COMPAMS_F32 ? kParts<float> : kParts<half_t>; }
 
-// A piece's d is to stay in the memory-side cache between the products that make and read it, and to be wide enough for them to
-// fill the card.
-constexpr size_t kPieceBytes = 192u << 20;
+// A piece's d: wide enough for the products that read it to fill the card, and for dx's sums, which are read and written with every
+// piece, to be little beside it.
+constexpr size_t kPieceBytes = 288u << 20;
 constexpr uint32_t kLeastPiece = 1024;
 
 struct Operands {
@@ -399,7 +529,11 @@ Room room_of(const compams_linear_loss& a) {
   r.stat = up256(total * sizeof(RowStat));
   r.losses = a.losses ? 0 : up256(total * sizeof(float));
   if (!gradient) return r;
-  if (a.dweight) r.x_learnt = up256(total * o.x.packed_row_bytes());
+  if (a.dweight) r.x_held = up256(total * o.x.packed_row_bytes());
+  if (a.type == COMPAMS_BF16) {
+    if (a.dx) r.weight_held = up256(static_cast<size_t>(a.vocab) * o.weight.packed_row_bytes());
+    r.tops = up256((static_cast<size_t>(a.n) + 1) * a.cols * sizeof(uint32_t));
+  }
   const size_t column = total * size * parts_of(a.type);
   uint64_t piece = kPieceBytes / column / 256 * 256;
   if (piece < kLeastPiece) piece = kLeastPiece;
@@ -411,15 +545,26 @@ Room room_of(const compams_linear_loss& a) {
   return r;
 }
 
+// The kernels that go over x and the weight by columns.
+template <typename T>
+void run_hold(const LossArgs& k, const compams_linear_loss& a, hipStream_t stream) {
+  ColumnsArgs c = {a.x, a.weight, a.ld_x, a.ld_weight, 1, 1, 0, 0};
+  const uint32_t groups = (k.cols + kGroup - 1) / kGroup;
+  while (c.wide < groups && c.wide < kThreads) c.wide *= 2;
+  c.across = (groups + c.wide - 1) / c.wide;
+  const uint64_t each = static_cast<uint64_t>(kThreads / c.wide) * kRowsEach;
+  if (k.x_held.p) c.parts_x = static_cast<uint32_t>(tiles_of(k.rows, static_cast<uint32_t>(each)));
+  if (kScaled<T> && a.dx) c.parts_weight = static_cast<uint32_t>(tiles_of(k.vocab, static_cast<uint32_t>(each)));
+  const uint64_t blocks = (static_cast<uint64_t>(c.parts_x) * k.n + c.parts_weight) * c.across;
+  if (blocks == 0) return;
+  if constexpr (kScaled<T>) hipLaunchKernelGGL(k_linear_loss_tops, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, stream, k, c);
+  hipLaunchKernelGGL(k_linear_loss_hold<T>, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, stream, k, c);
+}
+
 template <typename T>
 void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room, hipStream_t stream) {
   const bool gradient = a.dx || a.dweight;
   if (k.total) {
-    if (k.x_learnt.p) {
-      const uint64_t pieces = static_cast<uint64_t>(k.total) * (k.x_learnt.ld / 16), blocks = (pieces + kThreads - 1) / kThreads;
-      hipLaunchKernelGGL(k_linear_loss_rows<T>, dim3(static_cast<uint32_t>(blocks < 16384 ? blocks : 16384)), dim3(kThreads), 0, stream, k,
-                         static_cast<const T*>(a.x), a.ld_x);
-    }
     launch_pass<kStats, T>(k, stream);
     const uint32_t blocks = (k.total + 15) / 16;
     hipLaunchKernelGGL(k_linear_loss_join, dim3(blocks < 65536 ? blocks : 65536), dim3(kThreads), 0, stream, k);
@@ -429,18 +574,19 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
   if (!k.total) {
     if (a.dweight && !a.accumulate) {  // the sums of no rows
       k.width = k.vocab;
-      launch_pass<kWeight, T>(k, stream);
+      k.tops = nullptr;
+      launch_products<T>(k, stream);
     }
     return;
   }
+  run_hold<T>(k, a, stream);
   for (uint32_t p = 0; p < room.pieces; ++p) {
     k.first = p * room.piece;
     k.width = k.vocab - k.first < room.piece ? k.vocab - k.first : room.piece;
     k.begin = p == 0;
     k.end = p + 1 == room.pieces;
     launch_pass<kGradient, T>(k, stream);
-    if (a.dx) launch_pass<kInput, T>(k, stream);
-    if (a.dweight) launch_pass<kWeight, T>(k, stream);
+    launch_products<T>(k, stream);
   }
 }
 
@@ -479,14 +625,17 @@ int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream)
     k.x = packing.add(o.x, at);
     k.weight = packing.add(o.weight, at);
     run_packing(packing, size, stream);
-    if (room.x_learnt) k.x_learnt = {at, o.x.packed_row_bytes()};
+    if (room.x_held) k.x_held = {at, o.x.packed_row_bytes()};
+    k.weight_held = room.weight_held ? Read{at + room.x_held, o.weight.packed_row_bytes()} : k.weight;
   }
   const auto take = [&](size_t bytes) {
     char* const p = at;
     at += bytes;
     return p;
   };
-  take(room.x_learnt);
+  take(room.x_held);
+  take(room.weight_held);
+  k.tops = room.tops ? reinterpret_cast<uint32_t*>(take(room.tops)) : nullptr;
   k.partial = reinterpret_cast<float2*>(take(room.partial));
   k.of_target = reinterpret_cast<float*>(take(room.of_target));
   k.stat = reinterpret_cast<RowStat*>(take(room.stat));

@@ -292,6 +292,8 @@ struct Tiles {
     const uint32_t n = first_n();
     rows_of<FN * 4>(lds, [&](uint32_t i, uint32_t j) { return sum[i][j]; }, [&](uint32_t r, uint32_t c, const f32x4& v) { visit(r, n + c, v); });
   }
+  // The first of a lane's columns there, which are the same in every row.
+  __device__ static __forceinline__ uint32_t row_n() { return first_n() + (threadIdx.x & 63u) % (FN * 4) * 4; }
   // A wavefront's accesses of LDS before this come before those after it.
   __device__ static __forceinline__ void settled() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
