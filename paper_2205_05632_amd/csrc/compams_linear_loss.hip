@@ -179,21 +179,25 @@ __global__ __launch_bounds__(kThreads) void k_linear_loss_hold(LossArgs a, Colum
   }
 }
 
+// The tile of a workgroup.
 template <typename TL>
-__device__ __forceinline__ bool logits(TL& t, const LossArgs& a, uint32_t& m0, uint32_t& n0, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
-  using T = typename TL::T;
+__device__ __forceinline__ bool logits_at(const LossArgs& a, uint32_t& m0, uint32_t& n0) {
   const uint32_t tiles = a.tall * a.wide, id = tile_id();
   if (id >= tiles) return false;
   uint32_t down, across;
   tile_at(by_die(id, tiles), a.tall, a.wide, down, across);
   m0 = down * TL::kM;
   n0 = across * TL::kN;
+  return true;
+}
+template <typename TL>
+__device__ __forceinline__ void logits(TL& t, const LossArgs& a, uint32_t m0, uint32_t n0, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+  using T = typename TL::T;
   t.clear();
   t.run([&](uint32_t, Side& x, Side& w, Side&) {
     x = side<T, kAlong>(a.x.p, a.x.ld, a.total, m0, a.cols);
     w = side<T, kAlong>(a.weight.p, a.weight.ld, a.vocab, a.first + n0, a.cols);
   }, 1, a.cols, a0, b0, a1, b1);
-  return true;
 }
 
 // op over the four lanes (l, l + 16, l + 32, l + 48) that share a row of a tile.
@@ -219,36 +223,63 @@ template <typename TL>
 __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) {
   static_assert(TL::FN * 16 == kSpan, "a wavefront's columns");
   COMPAMS_TILE_LDS(TL);
-  TL t;
   uint32_t m0, n0;
-  if (!logits(t, a, m0, n0, COMPAMS_TILE_LDS_ARGS)) return;
-  const uint32_t span = n0 + TL::first_n(), n1 = span + TL::lane_n();
-  if (span >= a.vocab) return;
-  const bool last = span + kSpan > a.vocab;  // (the same for the wavefront)
+  if (!logits_at<TL>(a, m0, n0)) return;
+  // (the targets before the products: after them, each of a lane's rows would wait for its own)
+  const uint32_t r0 = m0 + TL::first_m() + TL::lane_m();
+  int32_t target[TL::FM];
 #pragma unroll
   for (uint32_t i = 0; i < TL::FM; ++i) {
-    const uint32_t r = m0 + TL::first_m() + TL::lane_m() + i * 16;
-    float top = -INFINITY;
+    const int64_t of_row = target_of(a, min(r0 + i * 16, a.total - 1));
+    target[i] = of_row >= 0 && of_row < a.vocab ? static_cast<int32_t>(of_row) : -1;
+  }
+  TL t;
+  logits(t, a, m0, n0, COMPAMS_TILE_LDS_ARGS);
+  const uint32_t span = n0 + TL::first_n(), n1 = span + TL::lane_n();
+  if (span >= a.vocab) return;
+  if (span + kSpan > a.vocab) {  // (the same for the wavefront)
+#pragma unroll
+    for (uint32_t i = 0; i < TL::FM; ++i)
+#pragma unroll
+      for (uint32_t j = 0; j < TL::FN; ++j)
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q)
+          if (n1 + j * 16 + q >= a.vocab) t.sum[i][j][q] = -INFINITY;
+  }
+  // (rows beside one another and sums in fours: what one waits for is filled with the others)
+  float top[TL::FM], sum[TL::FM];
+#pragma unroll
+  for (uint32_t i = 0; i < TL::FM; ++i) {
+    f32x4 most = t.sum[i][0];
+#pragma unroll
+    for (uint32_t j = 1; j < TL::FN; ++j)
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) most[q] = fmaxf(most[q], t.sum[i][j][q]);
+    top[i] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < TL::FM; ++i) top[i] = over_row(top[i], Max());
+#pragma unroll
+  for (uint32_t i = 0; i < TL::FM; ++i) {
+    const float base = base_of(top[i]);
+    f32x4 s;
 #pragma unroll
     for (uint32_t j = 0; j < TL::FN; ++j)
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q) {
-        if (last && n1 + j * 16 + q >= a.vocab) t.sum[i][j][q] = -INFINITY;
-        top = fmaxf(top, t.sum[i][j][q]);
+        const float e = exp_of(t.sum[i][j][q] - base);
+        s[q] = j == 0 ? e : s[q] + e;
       }
-    top = over_row(top, Max());
-    const float base = base_of(top);
-    float s = 0.0f;
+    sum[i] = (s[0] + s[1]) + (s[2] + s[3]);
+  }
 #pragma unroll
-    for (uint32_t j = 0; j < TL::FN; ++j)
+  for (uint32_t i = 0; i < TL::FM; ++i) sum[i] = over_row(sum[i], Add());
 #pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) s += exp_of(t.sum[i][j][q] - base);
-    s = over_row(s, Add());
+  for (uint32_t i = 0; i < TL::FM; ++i) {
+    const uint32_t r = r0 + i * 16, at = static_cast<uint32_t>(target[i]) - n1;
     if (r >= a.total) continue;
-    if (threadIdx.x % 64 < 16) a.partial[static_cast<uint64_t>(span / kSpan) * a.total + r] = make_float2(top, s);
-    const int64_t target = target_of(a, r);
-    if (target >= span && target < span + kSpan && target < a.vocab) {
-      const uint32_t at = static_cast<uint32_t>(target) - n1;
+    if (threadIdx.x % 64 < 16) a.partial[static_cast<uint64_t>(span / kSpan) * a.total + r] = make_float2(top[i], sum[i]);
+    if (at < kSpan) {
 #pragma unroll
       for (uint32_t j = 0; j < TL::FN; ++j)
 #pragma unroll
@@ -324,9 +355,10 @@ template <typename TL>
 __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_gradient(LossArgs a) {
   using T = typename TL::T;
   COMPAMS_TILE_LDS(TL);
-  TL t;
   uint32_t m0, n0;
-  if (!logits(t, a, m0, n0, COMPAMS_TILE_LDS_ARGS)) return;
+  if (!logits_at<TL>(a, m0, n0)) return;
+  TL t;
+  logits(t, a, m0, n0, COMPAMS_TILE_LDS_ARGS);
   const uint32_t n1 = n0 + TL::first_n() + TL::lane_n();
   const bool last = n0 + TL::kN > a.width;
 #pragma unroll
