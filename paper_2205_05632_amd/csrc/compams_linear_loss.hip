@@ -40,6 +40,11 @@ struct RowStat {
   uint32_t none;
 };
 
+struct Piece {
+  uint32_t first, width;  // its first entry and how many
+  char* d;                // [part][row][entry]
+};
+
 struct LossArgs {
   Read x, weight;     // x: as the caller has it (ignored rows too)
   Read x_held;        // x with zeros in ignored rows, and the weight, as the second pass's products read them
@@ -51,16 +56,16 @@ struct LossArgs {
   uint32_t n, rows, total, cols, vocab;
   uint32_t tall, wide;       // tiles of the launch
   uint32_t tall_weight;      // of dweight, beside those of dx
+  uint32_t wide_next;        // of the next piece's d
   float2* partial;           // [span of columns][row]: maximum, sum
   float* of_target;          // the target's logit of every row
   RowStat* stat;
   float* factor;             // grad_scale / count of every worker
   float grad_scale;
   float *mean_loss, *losses;
-  // a piece of the vocabulary
-  uint32_t first, width;     // its first entry and how many
-  void* d;                   // [part][row][piece]
-  int64_t ld_d;              // bytes
+  // a piece of the vocabulary that is multiplied, and the one after it, whose d is made meanwhile
+  Piece now, next;
+  int64_t ld_d;              // bytes from row to row of d
   int64_t part_bytes;
   float* dx_sum;             // fp32 sums of dx
   void* dx;
@@ -179,24 +184,13 @@ __global__ __launch_bounds__(kThreads) void k_linear_loss_hold(LossArgs a, Colum
   }
 }
 
-// The tile of a workgroup.
 template <typename TL>
-__device__ __forceinline__ bool logits_at(const LossArgs& a, uint32_t& m0, uint32_t& n0) {
-  const uint32_t tiles = a.tall * a.wide, id = tile_id();
-  if (id >= tiles) return false;
-  uint32_t down, across;
-  tile_at(by_die(id, tiles), a.tall, a.wide, down, across);
-  m0 = down * TL::kM;
-  n0 = across * TL::kN;
-  return true;
-}
-template <typename TL>
-__device__ __forceinline__ void logits(TL& t, const LossArgs& a, uint32_t m0, uint32_t n0, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+__device__ __forceinline__ void logits(TL& t, const LossArgs& a, uint32_t m0, uint32_t v0, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
   using T = typename TL::T;
   t.clear();
   t.run([&](uint32_t, Side& x, Side& w, Side&) {
     x = side<T, kAlong>(a.x.p, a.x.ld, a.total, m0, a.cols);
-    w = side<T, kAlong>(a.weight.p, a.weight.ld, a.vocab, a.first + n0, a.cols);
+    w = side<T, kAlong>(a.weight.p, a.weight.ld, a.vocab, v0, a.cols);
   }, 1, a.cols, a0, b0, a1, b1);
 }
 
@@ -223,8 +217,11 @@ template <typename TL>
 __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) {
   static_assert(TL::FN * 16 == kSpan, "a wavefront's columns");
   COMPAMS_TILE_LDS(TL);
-  uint32_t m0, n0;
-  if (!logits_at<TL>(a, m0, n0)) return;
+  const uint32_t tiles = a.tall * a.wide, id = tile_id();
+  if (id >= tiles) return;
+  uint32_t down, across;
+  tile_at(by_die(id, tiles), a.tall, a.wide, down, across);
+  const uint32_t m0 = down * TL::kM, n0 = across * TL::kN;
   // (the targets before the products: after them, each of a lane's rows would wait for its own)
   const uint32_t r0 = m0 + TL::first_m() + TL::lane_m();
   int32_t target[TL::FM];
@@ -350,23 +347,25 @@ __global__ __launch_bounds__(1024) void k_linear_loss_mean(LossArgs a) {
   }
 }
 
-// Second pass, a piece's d.  Entries behind the vocabulary's last are written too, as 0: they are read as a part of the last 16 bytes.
+// Second pass, a tile of the next piece's d.  Entries behind the vocabulary's last are written too, as 0: they are read as a part of the
+// last 16 bytes.
 template <typename TL>
-__global__ __launch_bounds__(TL::kThreads) void k_linear_loss_gradient(LossArgs a) {
+__device__ __forceinline__ void gradient_tile(const LossArgs& a, uint32_t id, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
   using T = typename TL::T;
-  COMPAMS_TILE_LDS(TL);
-  uint32_t m0, n0;
-  if (!logits_at<TL>(a, m0, n0)) return;
+  const Piece p = a.next;
+  uint32_t down, across;
+  tile_at(by_die(id, a.tall * a.wide_next), a.tall, a.wide_next, down, across);
+  const uint32_t m0 = down * TL::kM, n0 = across * TL::kN;
   TL t;
-  logits(t, a, m0, n0, COMPAMS_TILE_LDS_ARGS);
+  logits(t, a, m0, p.first + n0, a0, b0, a1, b1);
   const uint32_t n1 = n0 + TL::first_n() + TL::lane_n();
-  const bool last = n0 + TL::kN > a.width;
+  const bool last = n0 + TL::kN > p.width;
 #pragma unroll
   for (uint32_t i = 0; i < TL::FM; ++i) {
     const uint32_t r = m0 + TL::first_m() + TL::lane_m() + i * 16;
     const RowStat s = a.stat[min(r, a.total - 1)];
     const float over = s.over * kHeld<T>;
-    const uint32_t at = static_cast<uint32_t>(s.target) - a.first - n1;
+    const uint32_t at = static_cast<uint32_t>(s.target) - p.first - n1;
 #pragma unroll
     for (uint32_t j = 0; j < TL::FN; ++j)
 #pragma unroll
@@ -374,13 +373,13 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_gradient(LossArgs 
         // (the minimum: an ignored row's logits may be anything, and none is above its row's maximum in any other)
         float d = exp_of(fminf(t.sum[i][j][q] - s.top, 0.0f)) * over;
         d -= at == j * 16 + q ? kHeld<T> : 0.0f;
-        t.sum[i][j][q] = last && n1 + j * 16 + q >= a.width ? 0.0f : d;
+        t.sum[i][j][q] = last && n1 + j * 16 + q >= p.width ? 0.0f : d;
       }
   }
-  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
-    if (m0 + m >= a.total || n0 + n >= a.width + 16 / sizeof(T)) return;
+  t.rows(a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
+    if (m0 + m >= a.total || n0 + n >= p.width + 16 / sizeof(T)) return;
     typedef Held<T> H4 __attribute__((ext_vector_type(4)));
-    char* const to = static_cast<char*>(a.d) + static_cast<int64_t>(m0 + m) * a.ld_d + (n0 + n) * sizeof(Held<T>);
+    char* const to = p.d + static_cast<int64_t>(m0 + m) * a.ld_d + (n0 + n) * sizeof(Held<T>);
     H4 part;
 #pragma unroll
     for (uint32_t q = 0; q < 4; ++q) part[q] = static_cast<Held<T>>(v[q]);
@@ -420,10 +419,10 @@ __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, lds_c
       if (m0 + m < a.total && n0 + n < a.cols) v = *sums(m0 + m, n0 + n);
     });
   t.run([&](uint32_t, Side& d, Side& w, Side&) {
-    d = side<typename TL::T, kAlong>(a.d, a.ld_d, a.total, m0, a.width);
-    w = side<typename TL::T, kAcross>(static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.first) * a.weight_held.ld,
-                                      a.weight_held.ld, a.cols, n0, a.width);
-  }, 1, a.width, a0, b0, a1, b1);
+    d = side<typename TL::T, kAlong>(a.now.d, a.ld_d, a.total, m0, a.now.width);
+    w = side<typename TL::T, kAcross>(static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.now.first) * a.weight_held.ld,
+                                      a.weight_held.ld, a.cols, n0, a.now.width);
+  }, 1, a.now.width, a0, b0, a1, b1);
   const f32x4 of_column = a.end ? scales<T>(a, a.n, n0 + TL::row_n()) : f32x4{};
   t.rows(a0, [&](uint32_t m, uint32_t n, f32x4 v) {
     const uint32_t r = m0 + m;
@@ -451,71 +450,76 @@ __device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, lds_
   t.clear();
   const int64_t row = static_cast<int64_t>(w) * a.rows;
   t.run([&](uint32_t i, Side& d, Side& x, Side&) {
-    const char* const part = static_cast<const char*>(a.d) + (kParts<T> - 1 - i) * a.part_bytes;
+    const char* const part = a.now.d + (kParts<T> - 1 - i) * a.part_bytes;
     d = side<typename TL::T, kAcross>(part + row * a.ld_d, a.ld_d, static_cast<uint32_t>(a.ld_d / sizeof(typename TL::T)), m0, a.rows);
     x = side<typename TL::T, kAcross>(static_cast<const char*>(a.x_held.p) + row * a.x_held.ld, a.x_held.ld, a.cols, n0, a.rows);
   }, kParts<T>, a.rows, a0, b0, a1, b1);  // (what d has behind `width` meets no sum that is stored)
   const f32x4 f = scales<T>(a, w, n0 + TL::row_n());
   const float factor = a.factor[w] / kHeld<T>;
-  float* const to = a.dweight + w * a.stride_dweight + static_cast<int64_t>(a.first) * a.ld_dweight;
+  float* const to = a.dweight + w * a.stride_dweight + static_cast<int64_t>(a.now.first) * a.ld_dweight;
   t.rows(a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
-    if (m0 + m < a.width)
+    if (m0 + m < a.now.width)
       add4(to + static_cast<int64_t>(m0 + m) * a.ld_dweight + n0 + n, v * f * factor, static_cast<int64_t>(a.cols) - n0 - n,
            a.aligned >> 1 & 1u, a.accumulate);
   });
 }
 
-// Both products of a piece in one launch: dx has few tiles of many steps (the piece's columns are its k), dweight many of few, and
-// together they fill the card (apart, 96 and 384 tiles of 8192 x 4096 x 768 left a third of it idle).  dx's tiles come first.
-template <typename X, typename W, typename T>
-__global__ __launch_bounds__(X::kThreads) void k_linear_loss_products(LossArgs a) {
+// A piece's products, and the d of the piece after it, in one launch: dx has few tiles of many steps (the piece's columns are its k),
+// dweight many of few, d's tiles store more than they multiply, and together they fill the card.  (8192 x 50257 x 768 bfloat16, in one
+// launch each 96 tiles of dx and 384 of dweight left a third of it idle; d apart 165 us, the products 375 for 8448 columns.)
+// dx's tiles come first, the shortest last.
+template <typename D, typename X, typename W, typename T>
+__global__ __launch_bounds__(X::kThreads) void k_linear_loss_piece(LossArgs a) {
   static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
+  static_assert(X::kBytesA == D::kBytesA && X::kBytesB == D::kBytesB && X::kThreads == D::kThreads, "one kind of tile");
   COMPAMS_TILE_LDS(X);
-  const uint32_t of_dx = a.dx ? a.tall * a.wide : 0, of_weight = a.dweight ? a.tall_weight * a.wide * a.n : 0, id = tile_id();
-  if (id < of_dx) input_tile<X, T>(a, id, COMPAMS_TILE_LDS_ARGS);
-  else if (id < of_dx + of_weight) weight_tile<W, T>(a, id - of_dx, COMPAMS_TILE_LDS_ARGS);
+  const bool any = a.now.width != 0;
+  const uint32_t of_dx = any && a.dx ? a.tall * a.wide : 0, of_weight = any && a.dweight ? a.tall_weight * a.wide * a.n : 0;
+  const uint32_t of_d = a.next.width ? a.tall * a.wide_next : 0;
+  uint32_t id = tile_id();
+  if (id < of_dx) return input_tile<X, T>(a, id, COMPAMS_TILE_LDS_ARGS);
+  id -= of_dx;
+  if (id < of_weight) return weight_tile<W, T>(a, id, COMPAMS_TILE_LDS_ARGS);
+  id -= of_weight;
+  if (id < of_d) gradient_tile<D>(a, id, COMPAMS_TILE_LDS_ARGS);
 }
 
 // ---- Launches ------------------------------------------------------------------------------------------------
-enum Pass { kStats, kGradient };
-
-template <Pass PASS, typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
-void launch_pass(LossArgs& a, hipStream_t stream) {
+template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
+void launch_stats(LossArgs& a, hipStream_t stream) {
   using TL = Tiles<T, kAlong, kAlong, WM, WN, FM, FN>;
   a.tall = static_cast<uint32_t>(tiles_of(a.total, TL::kM));
-  a.wide = static_cast<uint32_t>(tiles_of(PASS == kStats ? a.vocab : a.width, TL::kN));
-  const dim3 grid = tile_grid(static_cast<uint64_t>(a.tall) * a.wide), block(TL::kThreads);
-  if constexpr (PASS == kStats) hipLaunchKernelGGL(k_linear_loss_stats<TL>, grid, block, 0, stream, a);
-  else hipLaunchKernelGGL(k_linear_loss_gradient<TL>, grid, block, 0, stream, a);
+  a.wide = static_cast<uint32_t>(tiles_of(a.vocab, TL::kN));
+  hipLaunchKernelGGL(k_linear_loss_stats<TL>, tile_grid(static_cast<uint64_t>(a.tall) * a.wide), dim3(TL::kThreads), 0, stream, a);
 }
-template <Pass PASS, typename T>
-void launch_pass(LossArgs& a, hipStream_t stream) {
-  switch (tile_size(a.total, PASS == kStats ? a.vocab : a.width, 1)) {
-    case kTile256: launch_pass<PASS, T, 2, 4, 8, 4>(a, stream); break;
-    case kTile128: launch_pass<PASS, T, 2, 2, 4, 4>(a, stream); break;
-    default:
-      if constexpr (PASS == kStats) launch_pass<PASS, T, 4, 1, 1, 4>(a, stream);
-      else launch_pass<PASS, T, 2, 2, 2, 2>(a, stream);
-      break;
+template <typename T>
+void launch_stats(LossArgs& a, hipStream_t stream) {
+  switch (tile_size(a.total, a.vocab, 1)) {
+    case kTile256: launch_stats<T, 2, 4, 8, 4>(a, stream); break;
+    case kTile128: launch_stats<T, 2, 2, 4, 4>(a, stream); break;
+    default: launch_stats<T, 4, 1, 1, 4>(a, stream); break;
   }
 }
 template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
-void launch_products(LossArgs& a, hipStream_t stream) {
+void launch_piece(LossArgs& a, hipStream_t stream) {
+  using D = Tiles<T, kAlong, kAlong, WM, WN, FM, FN>;
   using X = Tiles<Held<T>, kAlong, kAcross, WM, WN, FM, FN>;
   using W = Tiles<Held<T>, kAcross, kAcross, WM, WN, FM, FN>;
   a.tall = static_cast<uint32_t>(tiles_of(a.total, X::kM));
-  a.tall_weight = static_cast<uint32_t>(tiles_of(a.width, X::kM));
+  a.tall_weight = static_cast<uint32_t>(tiles_of(a.now.width, X::kM));
   a.wide = static_cast<uint32_t>(tiles_of(a.cols, X::kN));
-  const uint64_t tiles = static_cast<uint64_t>(a.wide) * ((a.dx ? a.tall : 0) + (a.dweight ? static_cast<uint64_t>(a.tall_weight) * a.n : 0));
-  if (tiles) hipLaunchKernelGGL((k_linear_loss_products<X, W, T>), tile_grid(tiles), dim3(X::kThreads), 0, stream, a);
+  a.wide_next = static_cast<uint32_t>(tiles_of(a.next.width, X::kN));
+  uint64_t tiles = static_cast<uint64_t>(a.tall) * a.wide_next;
+  if (a.now.width)
+    tiles += static_cast<uint64_t>(a.wide) * ((a.dx ? a.tall : 0) + (a.dweight ? static_cast<uint64_t>(a.tall_weight) * a.n : 0));
+  if (tiles) hipLaunchKernelGGL((k_linear_loss_piece<D, X, W, T>), tile_grid(tiles), dim3(X::kThreads), 0, stream, a);
 }
 template <typename T>
-void launch_products(LossArgs& a, hipStream_t stream) {
-  const uint64_t rows = (a.dx ? a.total : 0) + (a.dweight ? static_cast<uint64_t>(a.width) * a.n : 0);
-  switch (tile_size(rows, a.cols, 1)) {
-    case kTile256: launch_products<T, 2, 4, 8, 4>(a, stream); break;
-    case kTile128: launch_products<T, 2, 2, 4, 4>(a, stream); break;
-    default: launch_products<T, 2, 2, 2, 2>(a, stream); break;
+void launch_piece(LossArgs& a, TileSize size, hipStream_t stream) {
+  switch (size) {
+    case kTile256: launch_piece<T, 2, 4, 8, 4>(a, stream); break;
+    case kTile128: launch_piece<T, 2, 2, 4, 4>(a, stream); break;
+    default: launch_piece<T, 2, 2, 2, 2>(a, stream); break;
   }
 }
 
@@ -530,14 +534,14 @@ struct Room {
   size_t x = 0, weight = 0, x_held = 0, weight_held = 0, tops = 0, partial = 0, of_target = 0, stat = 0, losses = 0, factor = 0, d = 0,
          dx_sum = 0;
   uint32_t piece = 0, pieces = 0;
-  size_t all() const { return x + weight + x_held + weight_held + tops + partial + of_target + stat + losses + factor + d + dx_sum; }
+  size_t all() const { return x + weight + x_held + weight_held + tops + partial + of_target + stat + losses + factor + (pieces > 1 ? 2 : 1) * d + dx_sum; }
 };
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 inline uint32_t parts_of(int32_t type) { return type == COMPAMS_F32 ? kParts<float> : kParts<half_t>; }
 
 // A piece's d: wide enough for the products that read it to fill the card, and for dx's sums, which are read and written with every
 // piece, to be little beside it.
-constexpr size_t kPieceBytes = 288u << 20;
+constexpr size_t kPieceBytes = 288u << 20;  // (two of them)
 constexpr uint32_t kLeastPiece = 1024;
 
 struct Operands {
@@ -572,7 +576,7 @@ Room room_of(const compams_linear_loss& a) {
   r.pieces = static_cast<uint32_t>(tiles_of(a.vocab, piece));
   r.piece = static_cast<uint32_t>((tiles_of(a.vocab, r.pieces) + 255) / 256 * 256);
   r.pieces = static_cast<uint32_t>(tiles_of(a.vocab, r.piece));
-  r.d = up256(column * r.piece);
+  r.d = up256(column * r.piece);  // (of one)
   if (a.dx && r.pieces > 1) r.dx_sum = up256(total * ((a.cols + 3) / 4 * 4) * sizeof(float));
   return r;
 }
@@ -597,7 +601,7 @@ template <typename T>
 void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room, hipStream_t stream) {
   const bool gradient = a.dx || a.dweight;
   if (k.total) {
-    launch_pass<kStats, T>(k, stream);
+    launch_stats<T>(k, stream);
     const uint32_t blocks = (k.total + 15) / 16;
     hipLaunchKernelGGL(k_linear_loss_join, dim3(blocks < 65536 ? blocks : 65536), dim3(kThreads), 0, stream, k);
   }
@@ -605,20 +609,33 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
   if (!gradient) return;
   if (!k.total) {
     if (a.dweight && !a.accumulate) {  // the sums of no rows
-      k.width = k.vocab;
+      k.now.width = k.vocab;
       k.tops = nullptr;
-      launch_products<T>(k, stream);
+      launch_piece<T>(k, tile_size(static_cast<uint64_t>(k.vocab) * k.n, k.cols, 1), stream);
     }
     return;
   }
   run_hold<T>(k, a, stream);
+  const auto piece = [&](uint32_t p) {
+    if (p >= room.pieces) return Piece{0, 0, nullptr};
+    const uint32_t first = p * room.piece, left = k.vocab - first;
+    return Piece{first, left < room.piece ? left : room.piece, k.now.d + (p & 1u ? room.d : 0)};
+  };
+  char* const d = k.now.d;
+  const uint64_t rows = (a.dx ? k.total : 0) + (a.dweight ? static_cast<uint64_t>(room.piece) * k.n : 0);
+  const uint64_t large = tiles_of(rows, 256) * tiles_of(k.cols, 256) + tiles_of(k.total, 256) * tiles_of(room.piece, 256);
+  const TileSize products = large >= 512 ? kTile256 : tile_size(rows, k.cols, 1);
+  k.next = piece(0);
+  k.now = {0, 0, d};
+  launch_piece<T>(k, tile_size(k.total, k.next.width, 1), stream);
   for (uint32_t p = 0; p < room.pieces; ++p) {
-    k.first = p * room.piece;
-    k.width = k.vocab - k.first < room.piece ? k.vocab - k.first : room.piece;
+    k.now.d = d;
+    const Piece now = piece(p), next = piece(p + 1);
+    k.now = now;
+    k.next = next;
     k.begin = p == 0;
     k.end = p + 1 == room.pieces;
-    launch_pass<kGradient, T>(k, stream);
-    launch_products<T>(k, stream);
+    launch_piece<T>(k, products, stream);
   }
 }
 
@@ -674,7 +691,7 @@ int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream)
   float* const losses = reinterpret_cast<float*>(take(room.losses));
   k.losses = a->losses ? a->losses : losses;
   k.factor = reinterpret_cast<float*>(take(room.factor));
-  k.d = take(room.d);
+  k.now.d = take((room.pieces > 1 ? 2 : 1) * room.d);
   k.dx_sum = reinterpret_cast<float*>(take(room.dx_sum));
   k.targets = a->targets;
   k.ignore = a->ignore_index;
