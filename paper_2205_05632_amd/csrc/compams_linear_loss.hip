@@ -469,7 +469,7 @@ __device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, lds_
 // launch each 96 tiles of dx and 384 of dweight left a third of it idle; d apart 165 us, the products 375 for 8448 columns.)
 // dx's tiles come first, the shortest last.
 template <typename D, typename X, typename W, typename T>
-__global__ __launch_bounds__(X::kThreads) void k_linear_loss_piece(LossArgs a) {
+__global__ __launch_bounds__(X::kThreads, 2) void k_linear_loss_piece(LossArgs a) {
   static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
   static_assert(X::kBytesA == D::kBytesA && X::kBytesB == D::kBytesB && X::kThreads == D::kThreads, "one kind of tile");
   COMPAMS_TILE_LDS(X);
@@ -500,11 +500,11 @@ void launch_stats(LossArgs& a, hipStream_t stream) {
     default: launch_stats<T, 4, 1, 1, 4>(a, stream); break;
   }
 }
-template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
+template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN, uint32_t STEP = 128>
 void launch_piece(LossArgs& a, hipStream_t stream) {
-  using D = Tiles<T, kAlong, kAlong, WM, WN, FM, FN>;
-  using X = Tiles<Held<T>, kAlong, kAcross, WM, WN, FM, FN>;
-  using W = Tiles<Held<T>, kAcross, kAcross, WM, WN, FM, FN>;
+  using D = Tiles<T, kAlong, kAlong, WM, WN, FM, FN, false, STEP>;
+  using X = Tiles<Held<T>, kAlong, kAcross, WM, WN, FM, FN, false, STEP>;
+  using W = Tiles<Held<T>, kAcross, kAcross, WM, WN, FM, FN, false, STEP>;
   a.tall = static_cast<uint32_t>(tiles_of(a.total, X::kM));
   a.tall_weight = static_cast<uint32_t>(tiles_of(a.now.width, X::kM));
   a.wide = static_cast<uint32_t>(tiles_of(a.cols, X::kN));
@@ -517,7 +517,7 @@ void launch_piece(LossArgs& a, hipStream_t stream) {
 template <typename T>
 void launch_piece(LossArgs& a, TileSize size, hipStream_t stream) {
   switch (size) {
-    case kTile256: launch_piece<T, 2, 4, 8, 4>(a, stream); break;
+    case kTile256: launch_piece<T, 2, 2, 8, 4, 64>(a, stream); break;
     case kTile128: launch_piece<T, 2, 2, 4, 4>(a, stream); break;
     default: launch_piece<T, 2, 2, 2, 2>(a, stream); break;
   }
