@@ -48,7 +48,6 @@ struct ForwardArgs {
   void *m, *gate, *up;
   int64_t ld_m, ld_gate, ld_up;
   uint32_t total, cols, hidden, tall, wide;
-  uint32_t aligned;  // whether four entries of an output's row can be stored at once
 };
 
 // A tile of 256 x 256 is 256 rows of x and 128 columns of each projection, which take turns of sixteen: what belongs together
@@ -56,7 +55,7 @@ struct ForwardArgs {
 template <typename TL, int ACT>
 __global__ __launch_bounds__(TL::kThreads) void k_gated_forward(ForwardArgs a) {
   using T = typename TL::T;
-  COMPAMS_TILE_LDS(TL);
+  COMPAMS_TILE_LDS(TL, lds);
   const uint32_t tiles = a.tall * a.wide, id = tile_id();
   if (id >= tiles) return;
   uint32_t down, across;
@@ -68,7 +67,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_gated_forward(ForwardArgs a) {
     x = side<T, kAlong>(a.x.p, a.x.ld, a.total, m0, a.cols);
     g = side<T, kAlong>(a.gate_weight.p, a.gate_weight.ld, a.hidden, h0, a.cols);
     u = side<T, kAlong>(a.up_weight.p, a.up_weight.ld, a.hidden, h0, a.cols);
-  }, 1, a.cols, COMPAMS_TILE_LDS_ARGS);
+  }, 1, a.cols, lds);
   // The biases, then the product in the place of the first projection's sums.
   const uint32_t h1 = h0 + TL::first_n() / 2;
 #pragma unroll
@@ -88,15 +87,15 @@ __global__ __launch_bounds__(TL::kThreads) void k_gated_forward(ForwardArgs a) {
   }
   constexpr uint32_t kPieces = TL::FN * 2;
   __syncthreads();  // (others may still read what they multiply)
-  const auto store = [&](void* to, int64_t ld, bool wide, auto of) {
-    t.template rows_of<kPieces>((lds_char*)lds_a0, of, [&](uint32_t m, uint32_t c, const f32x4& v) {
+  const auto store = [&](void* to, int64_t ld, auto of) {
+    t.template rows_of<kPieces>(lds.a[0], of, [&](uint32_t m, uint32_t c, const f32x4& v) {
       const uint32_t r = m0 + m, h = h1 + c;
-      if (r < a.total) store4(static_cast<T*>(to) + static_cast<int64_t>(r) * ld + h, v, static_cast<int64_t>(a.hidden) - h, wide);
+      if (r < a.total) store4(static_cast<T*>(to) + static_cast<int64_t>(r) * ld + h, v, static_cast<int64_t>(a.hidden) - h);
     });
   };
-  if (a.gate) store(a.gate, a.ld_gate, a.aligned & 2u, [&](uint32_t i, uint32_t j) { return t.sum[i][2 * j]; });
-  if (a.up) store(a.up, a.ld_up, a.aligned & 4u, [&](uint32_t i, uint32_t j) { return t.sum[i][2 * j + 1]; });
-  store(a.m, a.ld_m, a.aligned & 1u, [&](uint32_t i, uint32_t j) {
+  if (a.gate) store(a.gate, a.ld_gate, [&](uint32_t i, uint32_t j) { return t.sum[i][2 * j]; });
+  if (a.up) store(a.up, a.ld_up, [&](uint32_t i, uint32_t j) { return t.sum[i][2 * j + 1]; });
+  store(a.m, a.ld_m, [&](uint32_t i, uint32_t j) {
     f32x4 m;
     float none;
 #pragma unroll
@@ -326,8 +325,6 @@ int compams_gated_forward(const compams_gated* a, void* hip_stream) {
   k.gate_bias = a->gate_bias; k.up_bias = a->up_bias;
   k.m = a->m; k.gate = a->gate; k.up = a->up;
   k.ld_m = a->ld_m; k.ld_gate = a->ld_gate; k.ld_up = a->ld_up;
-  const auto four = [&](const void* p, int64_t ld) { return aligned_to(p, 4 * size) && ld % 4 == 0; };
-  k.aligned = four(k.m, k.ld_m) | four(k.gate, k.ld_gate) << 1 | four(k.up, k.ld_up) << 2;
   k.total = static_cast<uint32_t>(a->n * a->rows);
   k.cols = static_cast<uint32_t>(a->cols);
   k.hidden = static_cast<uint32_t>(a->hidden);

@@ -72,7 +72,6 @@ struct LossArgs {
   int64_t ld_dx;
   float* dweight;
   int64_t ld_dweight, stride_dweight;
-  uint32_t aligned;          // 1: four of dx at once, 2: of dweight
   uint32_t accumulate, begin, end;  // begin, end: the first and the last piece
 };
 
@@ -185,13 +184,13 @@ __global__ __launch_bounds__(kThreads) void k_linear_loss_hold(LossArgs a, Colum
 }
 
 template <typename TL>
-__device__ __forceinline__ void logits(TL& t, const LossArgs& a, uint32_t m0, uint32_t v0, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+__device__ __forceinline__ void logits(TL& t, const LossArgs& a, uint32_t m0, uint32_t v0, const TileLds& lds) {
   using T = typename TL::T;
   t.clear();
   t.run([&](uint32_t, Side& x, Side& w, Side&) {
     x = side<T, kAlong>(a.x.p, a.x.ld, a.total, m0, a.cols);
     w = side<T, kAlong>(a.weight.p, a.weight.ld, a.vocab, v0, a.cols);
-  }, 1, a.cols, a0, b0, a1, b1);
+  }, 1, a.cols, lds);
 }
 
 // op over the four lanes (l, l + 16, l + 32, l + 48) that share a row of a tile.
@@ -216,7 +215,7 @@ constexpr uint32_t kSpan = 64;
 template <typename TL>
 __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) {
   static_assert(TL::FN * 16 == kSpan, "a wavefront's columns");
-  COMPAMS_TILE_LDS(TL);
+  COMPAMS_TILE_LDS(TL, lds);
   const uint32_t tiles = a.tall * a.wide, id = tile_id();
   if (id >= tiles) return;
   uint32_t down, across;
@@ -231,7 +230,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) 
     target[i] = of_row >= 0 && of_row < a.vocab ? static_cast<int32_t>(of_row) : -1;
   }
   TL t;
-  logits(t, a, m0, n0, COMPAMS_TILE_LDS_ARGS);
+  logits(t, a, m0, n0, lds);
   const uint32_t span = n0 + TL::first_n(), n1 = span + TL::lane_n();
   if (span >= a.vocab) return;
   if (span + kSpan > a.vocab) {  // (the same for the wavefront)
@@ -350,14 +349,14 @@ __global__ __launch_bounds__(1024) void k_linear_loss_mean(LossArgs a) {
 // Second pass, a tile of the next piece's d.  Entries behind the vocabulary's last are written too, as 0: they are read as a part of the
 // last 16 bytes.
 template <typename TL>
-__device__ __forceinline__ void gradient_tile(const LossArgs& a, uint32_t id, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+__device__ __forceinline__ void gradient_tile(const LossArgs& a, uint32_t id, const TileLds& lds) {
   using T = typename TL::T;
   const Piece p = a.next;
   uint32_t down, across;
   tile_at(by_die(id, a.tall * a.wide_next), a.tall, a.wide_next, down, across);
   const uint32_t m0 = down * TL::kM, n0 = across * TL::kN;
   TL t;
-  logits(t, a, m0, p.first + n0, a0, b0, a1, b1);
+  logits(t, a, m0, p.first + n0, lds);
   const uint32_t n1 = n0 + TL::first_n() + TL::lane_n();
   const bool last = n0 + TL::kN > p.width;
 #pragma unroll
@@ -376,7 +375,7 @@ __device__ __forceinline__ void gradient_tile(const LossArgs& a, uint32_t id, ld
         t.sum[i][j][q] = last && n1 + j * 16 + q >= p.width ? 0.0f : d;
       }
   }
-  t.rows(a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
+  t.rows(lds.a[0], [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m >= a.total || n0 + n >= p.width + 16 / sizeof(T)) return;
     typedef Held<T> H4 __attribute__((ext_vector_type(4)));
     char* const to = p.d + static_cast<int64_t>(m0 + m) * a.ld_d + (n0 + n) * sizeof(Held<T>);
@@ -407,7 +406,7 @@ __device__ __forceinline__ f32x4 scales(const LossArgs& a, uint32_t matrix, uint
 
 // A tile of dx.  The sums go on from those of the pieces before, so that they do not depend on where pieces end.
 template <typename TL, typename T>
-__device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+__device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, const TileLds& lds) {
   uint32_t down, across;
   tile_at(by_die(id, a.tall * a.wide), a.tall, a.wide, down, across);
   const uint32_t m0 = down * TL::kM, n0 = across * TL::kN, padded = (a.cols + 3) / 4 * 4;
@@ -422,9 +421,9 @@ __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, lds_c
     d = side<typename TL::T, kAlong>(a.now.d, a.ld_d, a.total, m0, a.now.width);
     w = side<typename TL::T, kAcross>(static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.now.first) * a.weight_held.ld,
                                       a.weight_held.ld, a.cols, n0, a.now.width);
-  }, 1, a.now.width, a0, b0, a1, b1);
+  }, 1, a.now.width, lds);
   const f32x4 of_column = a.end ? scales<T>(a, a.n, n0 + TL::row_n()) : f32x4{};
-  t.rows(a0, [&](uint32_t m, uint32_t n, f32x4 v) {
+  t.rows(lds.a[0], [&](uint32_t m, uint32_t n, f32x4 v) {
     const uint32_t r = m0 + m;
     if (r >= a.total || n0 + n >= a.cols) return;
     if (!a.end) {
@@ -435,13 +434,13 @@ __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, lds_c
     const float f = a.factor[r / a.rows] / kHeld<T>;
 #pragma unroll
     for (uint32_t q = 0; q < 4; ++q) v[q] = learnt ? v[q] * of_column[q] * f : 0.0f;
-    store4(static_cast<T*>(a.dx) + static_cast<int64_t>(r) * a.ld_dx + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.aligned & 1u);
+    store4(static_cast<T*>(a.dx) + static_cast<int64_t>(r) * a.ld_dx + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n);
   });
 }
 
 // A tile of dweight's rows of this piece, of one worker: k is the worker's rows, once for each part of d, the lesser first.
 template <typename TL, typename T>
-__device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+__device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, const TileLds& lds) {
   const uint32_t each = a.tall_weight * a.wide, mine = by_die(id, each * a.n), w = mine / each;
   uint32_t down, across;
   tile_at(mine - w * each, a.tall_weight, a.wide, down, across);
@@ -453,14 +452,13 @@ __device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, lds_
     const char* const part = a.now.d + (kParts<T> - 1 - i) * a.part_bytes;
     d = side<typename TL::T, kAcross>(part + row * a.ld_d, a.ld_d, static_cast<uint32_t>(a.ld_d / sizeof(typename TL::T)), m0, a.rows);
     x = side<typename TL::T, kAcross>(static_cast<const char*>(a.x_held.p) + row * a.x_held.ld, a.x_held.ld, a.cols, n0, a.rows);
-  }, kParts<T>, a.rows, a0, b0, a1, b1);  // (what d has behind `width` meets no sum that is stored)
+  }, kParts<T>, a.rows, lds);  // (what d has behind `width` meets no sum that is stored)
   const f32x4 f = scales<T>(a, w, n0 + TL::row_n());
   const float factor = a.factor[w] / kHeld<T>;
   float* const to = a.dweight + w * a.stride_dweight + static_cast<int64_t>(a.now.first) * a.ld_dweight;
-  t.rows(a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
+  t.rows(lds.a[0], [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m < a.now.width)
-      add4(to + static_cast<int64_t>(m0 + m) * a.ld_dweight + n0 + n, v * f * factor, static_cast<int64_t>(a.cols) - n0 - n,
-           a.aligned >> 1 & 1u, a.accumulate);
+      add4(to + static_cast<int64_t>(m0 + m) * a.ld_dweight + n0 + n, v * f * factor, static_cast<int64_t>(a.cols) - n0 - n, a.accumulate);
   });
 }
 
@@ -472,16 +470,16 @@ template <typename D, typename X, typename W, typename T>
 __global__ __launch_bounds__(X::kThreads, 2) void k_linear_loss_piece(LossArgs a) {
   static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
   static_assert(X::kBytesA == D::kBytesA && X::kBytesB == D::kBytesB && X::kThreads == D::kThreads, "one kind of tile");
-  COMPAMS_TILE_LDS(X);
+  COMPAMS_TILE_LDS(X, lds);
   const bool any = a.now.width != 0;
   const uint32_t of_dx = any && a.dx ? a.tall * a.wide : 0, of_weight = any && a.dweight ? a.tall_weight * a.wide * a.n : 0;
   const uint32_t of_d = a.next.width ? a.tall * a.wide_next : 0;
   uint32_t id = tile_id();
-  if (id < of_dx) return input_tile<X, T>(a, id, COMPAMS_TILE_LDS_ARGS);
+  if (id < of_dx) return input_tile<X, T>(a, id, lds);
   id -= of_dx;
-  if (id < of_weight) return weight_tile<W, T>(a, id, COMPAMS_TILE_LDS_ARGS);
+  if (id < of_weight) return weight_tile<W, T>(a, id, lds);
   id -= of_weight;
-  if (id < of_d) gradient_tile<D>(a, id, COMPAMS_TILE_LDS_ARGS);
+  if (id < of_d) gradient_tile<D>(a, id, lds);
 }
 
 // ---- Launches ------------------------------------------------------------------------------------------------
@@ -707,8 +705,6 @@ int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream)
   k.part_bytes = k.ld_d * k.total;
   k.dx = a->dx; k.ld_dx = a->ld_dx;
   k.dweight = a->dweight; k.ld_dweight = a->ld_dweight; k.stride_dweight = a->stride_dweight;
-  k.aligned = (aligned_to(a->dx, 4 * size) && a->ld_dx % 4 == 0) |
-              (aligned_to(a->dweight, 16) && a->ld_dweight % 4 == 0 && a->stride_dweight % 4 == 0) << 1;
   k.accumulate = static_cast<uint32_t>(a->accumulate);
   if (a->type == COMPAMS_F32) run_linear_loss<float>(k, *a, room, stream);
   else if (a->type == COMPAMS_F16) run_linear_loss<half_t>(k, *a, room, stream);

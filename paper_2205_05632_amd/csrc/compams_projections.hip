@@ -8,7 +8,7 @@ struct InputArgs {  // dx = dgate Wg + dup Wu
   Read d[2], weight[2];
   void* dx;
   int64_t ld_dx;
-  uint32_t count, total, cols, hidden, tall, wide, aligned;
+  uint32_t count, total, cols, hidden, tall, wide;
 };
 
 // k goes through the one projection's outputs and then the other's, so that dx is rounded once.  The weights' rows go across k:
@@ -16,7 +16,7 @@ struct InputArgs {  // dx = dgate Wg + dup Wu
 template <typename TL>
 __global__ __launch_bounds__(TL::kThreads) void k_projection_input(InputArgs a) {
   using T = typename TL::T;
-  COMPAMS_TILE_LDS(TL);
+  COMPAMS_TILE_LDS(TL, lds);
   const uint32_t tiles = a.tall * a.wide, id = tile_id();
   if (id >= tiles) return;
   uint32_t down, across;
@@ -27,10 +27,10 @@ __global__ __launch_bounds__(TL::kThreads) void k_projection_input(InputArgs a) 
   t.run([&](uint32_t i, Side& d, Side& w, Side&) {
     d = side<T, kAlong>(a.d[i].p, a.d[i].ld, a.total, m0, a.hidden);
     w = side<T, kAcross>(a.weight[i].p, a.weight[i].ld, a.cols, n0, a.hidden);
-  }, a.count, a.hidden, COMPAMS_TILE_LDS_ARGS);
-  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
+  }, a.count, a.hidden, lds);
+  t.rows(lds.a[0], [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m < a.total)
-      store4(static_cast<T*>(a.dx) + static_cast<int64_t>(m0 + m) * a.ld_dx + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.aligned);
+      store4(static_cast<T*>(a.dx) + static_cast<int64_t>(m0 + m) * a.ld_dx + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n);
   });
 }
 
@@ -38,14 +38,14 @@ struct WeightArgs {  // dW of worker i = d_i' x_i
   Read d[2], x;
   float* dweight[2];
   int64_t ld[2], stride[2];
-  uint32_t n, rows, cols, hidden, tall, wide, count, aligned, accumulate;
+  uint32_t n, rows, cols, hidden, tall, wide, count, accumulate;
 };
 
 // A worker's rows are k, so both operands go across it.  fp32 sums go straight to where the step reads them.
 template <typename TL>
 __global__ __launch_bounds__(TL::kThreads) void k_projection_weight(WeightArgs a) {
   using T = typename TL::T;
-  COMPAMS_TILE_LDS(TL);
+  COMPAMS_TILE_LDS(TL, lds);
   const uint32_t each = a.tall * a.wide, tiles = each * a.count * a.n, id = tile_id();
   if (id >= tiles) return;
   const uint32_t mine = by_die(id, tiles), which = mine / each % a.count, w = mine / each / a.count;
@@ -58,12 +58,11 @@ __global__ __launch_bounds__(TL::kThreads) void k_projection_weight(WeightArgs a
     const int64_t first = static_cast<int64_t>(w) * a.rows;
     d = side<T, kAcross>(static_cast<const char*>(a.d[which].p) + first * a.d[which].ld, a.d[which].ld, a.hidden, m0, a.rows);
     x = side<T, kAcross>(static_cast<const char*>(a.x.p) + first * a.x.ld, a.x.ld, a.cols, n0, a.rows);
-  }, 1, a.rows, COMPAMS_TILE_LDS_ARGS);
+  }, 1, a.rows, lds);
   float* const to = a.dweight[which] + w * a.stride[which];
-  t.rows((lds_char*)lds_a0, [&](uint32_t m, uint32_t n, const f32x4& v) {
+  t.rows(lds.a[0], [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m >= a.hidden) return;
-    add4(to + static_cast<int64_t>(m0 + m) * a.ld[which] + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.aligned >> which & 1u,
-         a.accumulate);
+    add4(to + static_cast<int64_t>(m0 + m) * a.ld[which] + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.accumulate);
   });
 }
 
@@ -183,7 +182,6 @@ int compams_projections_backward(const compams_projections* a, void* hip_stream)
   in.total = static_cast<uint32_t>(a->n * a->rows);
   in.cols = of.cols = static_cast<uint32_t>(a->cols);
   in.hidden = of.hidden = static_cast<uint32_t>(a->hidden);
-  in.aligned = aligned_to(a->dx, 4 * size) && a->ld_dx % 4 == 0;
   of.n = static_cast<uint32_t>(a->n);
   of.rows = static_cast<uint32_t>(a->rows);
   of.accumulate = static_cast<uint32_t>(a->accumulate);
@@ -193,7 +191,6 @@ int compams_projections_backward(const compams_projections* a, void* hip_stream)
     of.dweight[of.count] = dweight[i];
     of.ld[of.count] = ld[i];
     of.stride[of.count] = stride[i];
-    of.aligned |= (aligned_to(dweight[i], 16) && ld[i] % 4 == 0 && stride[i] % 4 == 0) << of.count;
     ++of.count;
   }
   if (a->type == COMPAMS_F32) launch_both<float>(in, of, stream);

@@ -164,6 +164,11 @@ struct Loader {
   }
 };
 
+// The two buffers of a workgroup's tiles.
+struct TileLds {
+  lds_char *a[2], *b[2];
+};
+
 // A workgroup of WM x WN wavefronts, each with FM x FN tiles of 16 x 16.
 template <typename T_, Form FA_, Form FB_, uint32_t WM_, uint32_t WN_, uint32_t FM_, uint32_t FN_, bool TWO_ = false, uint32_t STEP_ = 128>
 struct Tiles {
@@ -209,9 +214,8 @@ struct Tiles {
   }
 
   // sum += the products of `count` pairs of operands, all with the same k.  pair(i, a, b, b2) gives the i-th.
-  // (LDS as four arrays of their own: the compiler then knows that what is read is not what is being loaded.)
   template <typename Pair>
-  __device__ __forceinline__ void run(Pair pair, uint32_t count, uint32_t k, lds_char* a0, lds_char* b0, lds_char* a1, lds_char* b1) {
+  __device__ __forceinline__ void run(Pair pair, uint32_t count, uint32_t k, const TileLds& lds) {
     const uint32_t w = wave();
     Loader<T, FA, kM, kWaves, STEP> la;
     Loader<T, FB, kN, kWaves, STEP> lb;
@@ -231,18 +235,18 @@ struct Tiles {
         if (++at < count) pair(at, a, b, b2);
       }
     };
-    load(a0, b0);
+    load(lds.a[0], lds.b[0]);
     for (uint32_t s = 2; s <= steps; s += 2) {
       arrived();
-      load(a1, b1);
-      step(a0, b0);
+      load(lds.a[1], lds.b[1]);
+      step(lds.a[0], lds.b[0]);
       arrived();
-      if (s < steps) load(a0, b0);
-      step(a1, b1);
+      if (s < steps) load(lds.a[0], lds.b[0]);
+      step(lds.a[1], lds.b[1]);
     }
     if (steps & 1u) {
       arrived();
-      step(a0, b0);
+      step(lds.a[0], lds.b[0]);
     }
   }
   // What this wavefront loaded is in LDS, and so is everybody's; everybody is done with the step before.
@@ -301,11 +305,12 @@ struct Tiles {
   }
 };
 
-#define COMPAMS_TILE_LDS(TILES)                                                                                              \
+// (Four arrays of their own: the compiler then knows that what is read is not what is being loaded.)
+#define COMPAMS_TILE_LDS(TILES, NAME)                                                                                         \
   __shared__ __attribute__((aligned(1024))) char lds_a0[TILES::kBytesA], lds_b0[TILES::kBytesB], lds_a1[TILES::kBytesA],       \
-      lds_b1[TILES::kBytesB]
-#define COMPAMS_TILE_LDS_ARGS                                                                                                 \
-  (compams::lds_char*)lds_a0, (compams::lds_char*)lds_b0, (compams::lds_char*)lds_a1, (compams::lds_char*)lds_b1
+      lds_b1[TILES::kBytesB];                                                                                                \
+  const compams::TileLds NAME = {{(compams::lds_char*)lds_a0, (compams::lds_char*)lds_a1},                                     \
+                                 {(compams::lds_char*)lds_b0, (compams::lds_char*)lds_b1}}
 
 // Workgroups go to the eight dies in turn, each with a cache of its own: a die gets workgroups that follow one another.
 __device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total) {
@@ -313,34 +318,36 @@ __device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total) {
   return die * each + min(die, more) + in;
 }
 
-// Four neighbouring entries of a row, each rounded to T once; `left` entries of the row from the first on are there, and the
-// row is aligned to four of them where `wide`.
+// Four neighbouring entries of a row, each rounded to T once; `left` entries of the row from the first on are there.  (Rows may start at
+// any multiple of an entry's size: unaligned accesses are the processor's.)
 template <typename T>
-__device__ __forceinline__ void store4(T* p, const f32x4& v, int64_t left, bool wide) {
+__device__ __forceinline__ void store4(T* p, const f32x4& v, int64_t left) {
   typedef T T4 __attribute__((ext_vector_type(4)));
   T4 t;
 #pragma unroll
   for (int i = 0; i < 4; ++i) t[i] = static_cast<T>(v[i]);
-  if (wide && left >= 4) {
-    *reinterpret_cast<T4*>(p) = t;
+  if (left >= 4) {
+    __builtin_memcpy(p, &t, sizeof(t));
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 3; ++i)
       if (i < left) p[i] = t[i];
   }
 }
-
 // The same of a weight's gradient: written, or added to what is there.
-__device__ __forceinline__ void add4(float* p, const f32x4& v, int64_t left, bool wide, bool accumulate) {
-  if (!accumulate) {
-    store4(p, v, left, wide);
-  } else if (wide && left >= 4) {
-    *reinterpret_cast<f32x4*>(p) += v;
-  } else {
+__device__ __forceinline__ void add4(float* p, f32x4 v, int64_t left, bool accumulate) {
+  if (accumulate) {
+    f32x4 before = {};
+    if (left >= 4) {
+      __builtin_memcpy(&before, p, sizeof(before));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < left) p[i] += v[i];
+      for (int i = 0; i < 3; ++i)
+        if (i < left) before[i] = p[i];
+    }
+    v += before;
   }
+  store4(p, v, left);
 }
 
 // ---- Host side -----------------------------------------------------------------------------------------------
