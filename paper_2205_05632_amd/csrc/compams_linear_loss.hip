@@ -492,7 +492,7 @@ void launch_stats(LossArgs& a, hipStream_t stream) {
 }
 template <typename T>
 void launch_stats(LossArgs& a, hipStream_t stream) {
-  switch (tile_size(a.total, a.vocab, 1)) {
+  switch (tile_size({{a.total, a.vocab, 1, a.cols}}, sizeof(T) == 4)) {
     case kTile256: launch_stats<T, 2, 4, 8, 4>(a, stream); break;
     case kTile128: launch_stats<T, 2, 2, 4, 4>(a, stream); break;
     default: launch_stats<T, 4, 1, 1, 4>(a, stream); break;
@@ -609,7 +609,7 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
     if (a.dweight && !a.accumulate) {  // the sums of no rows
       k.now.width = k.vocab;
       k.tops = nullptr;
-      launch_piece<T>(k, tile_size(static_cast<uint64_t>(k.vocab) * k.n, k.cols, 1), stream);
+      launch_piece<T>(k, kTile64, stream);
     }
     return;
   }
@@ -620,12 +620,14 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
     return Piece{first, left < room.piece ? left : room.piece, k.now.d + (p & 1u ? room.d : 0)};
   };
   char* const d = k.now.d;
-  const uint64_t rows = (a.dx ? k.total : 0) + (a.dweight ? static_cast<uint64_t>(room.piece) * k.n : 0);
-  const uint64_t large = tiles_of(rows, 256) * tiles_of(k.cols, 256) + tiles_of(k.total, 256) * tiles_of(room.piece, 256);
-  const TileSize products = large >= 512 ? kTile256 : tile_size(rows, k.cols, 1);
+  const auto size = [&] {
+    return tile_size({{a.dx ? k.total : 0, k.cols, 1, k.now.width},
+                      {a.dweight ? k.now.width : 0, k.cols, k.n, static_cast<uint64_t>(k.rows) * kParts<T>},
+                      {k.total, k.next.width, 1, k.cols}}, sizeof(T) == 4);
+  };
   k.next = piece(0);
   k.now = {0, 0, d};
-  launch_piece<T>(k, tile_size(k.total, k.next.width, 1), stream);
+  launch_piece<T>(k, size(), stream);
   for (uint32_t p = 0; p < room.pieces; ++p) {
     k.now.d = d;
     const Piece now = piece(p), next = piece(p + 1);
@@ -633,7 +635,7 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
     k.next = next;
     k.begin = p == 0;
     k.end = p + 1 == room.pieces;
-    launch_piece<T>(k, products, stream);
+    launch_piece<T>(k, size(), stream);
   }
 }
 

@@ -4,23 +4,28 @@
 namespace compams {
 namespace {
 
-struct InputArgs {  // dx = dgate Wg + dup Wu
-  Read d[2], weight[2];
+struct ProjectionArgs {
+  Read d[2], weight[2], x;
   void* dx;
   int64_t ld_dx;
-  uint32_t count, total, cols, hidden, tall, wide;
+  float* dweight[2];
+  int64_t ld[2], stride[2];
+  uint32_t n, rows, total, cols, hidden;
+  uint32_t count;         // projections
+  uint32_t weights;       // of their weights' gradients, how many are asked for
+  uint32_t of[2];         // which
+  uint32_t accumulate;
+  uint32_t tall, wide;    // tiles of dx
+  uint32_t tall_weight;   // of a weight's gradient, beside those
 };
 
-// k goes through the one projection's outputs and then the other's, so that dx is rounded once.  The weights' rows go across k:
-// they are read as they lie and transposed on the way out of LDS.
+// dx = dgate Wg + dup Wu: k goes through the one projection's outputs and then the other's, so that dx is rounded once.  The weights' rows go
+// across k: they are read as they lie and transposed on the way out of LDS.
 template <typename TL>
-__global__ __launch_bounds__(TL::kThreads) void k_projection_input(InputArgs a) {
+__device__ __forceinline__ void input_tile(const ProjectionArgs& a, uint32_t id, const TileLds& lds) {
   using T = typename TL::T;
-  COMPAMS_TILE_LDS(TL, lds);
-  const uint32_t tiles = a.tall * a.wide, id = tile_id();
-  if (id >= tiles) return;
   uint32_t down, across;
-  tile_at(by_die(id, tiles), a.tall, a.wide, down, across);
+  tile_at(by_die(id, a.tall * a.wide), a.tall, a.wide, down, across);
   const uint32_t m0 = down * TL::kM, n0 = across * TL::kN;
   TL t;
   t.clear();
@@ -34,23 +39,14 @@ __global__ __launch_bounds__(TL::kThreads) void k_projection_input(InputArgs a) 
   });
 }
 
-struct WeightArgs {  // dW of worker i = d_i' x_i
-  Read d[2], x;
-  float* dweight[2];
-  int64_t ld[2], stride[2];
-  uint32_t n, rows, cols, hidden, tall, wide, count, accumulate;
-};
-
-// A worker's rows are k, so both operands go across it.  fp32 sums go straight to where the step reads them.
+// dW of worker i = d_i' x_i: a worker's rows are k, so both operands go across it.  fp32 sums go straight to where the step reads them.
 template <typename TL>
-__global__ __launch_bounds__(TL::kThreads) void k_projection_weight(WeightArgs a) {
+__device__ __forceinline__ void weight_tile(const ProjectionArgs& a, uint32_t id, const TileLds& lds) {
   using T = typename TL::T;
-  COMPAMS_TILE_LDS(TL, lds);
-  const uint32_t each = a.tall * a.wide, tiles = each * a.count * a.n, id = tile_id();
-  if (id >= tiles) return;
-  const uint32_t mine = by_die(id, tiles), which = mine / each % a.count, w = mine / each / a.count;
+  const uint32_t each = a.tall_weight * a.wide, mine = by_die(id, each * a.weights * a.n), matrix = mine / each;
+  const uint32_t which = a.of[matrix % a.weights], w = matrix / a.weights;
   uint32_t down, across;
-  tile_at(mine % each, a.tall, a.wide, down, across);
+  tile_at(mine - matrix * each, a.tall_weight, a.wide, down, across);
   const uint32_t m0 = down * TL::kM, n0 = across * TL::kN;
   TL t;
   t.clear();
@@ -61,41 +57,39 @@ __global__ __launch_bounds__(TL::kThreads) void k_projection_weight(WeightArgs a
   }, 1, a.rows, lds);
   float* const to = a.dweight[which] + w * a.stride[which];
   t.rows(lds.a[0], [&](uint32_t m, uint32_t n, const f32x4& v) {
-    if (m0 + m >= a.hidden) return;
-    add4(to + static_cast<int64_t>(m0 + m) * a.ld[which] + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.accumulate);
+    if (m0 + m < a.hidden)
+      add4(to + static_cast<int64_t>(m0 + m) * a.ld[which] + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n, a.accumulate);
   });
 }
 
-template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
-void launch_input(InputArgs& a, hipStream_t stream) {
-  using TL = Tiles<T, kAlong, kAcross, WM, WN, FM, FN>;
-  a.tall = static_cast<uint32_t>(tiles_of(a.total, TL::kM));
-  a.wide = static_cast<uint32_t>(tiles_of(a.cols, TL::kN));
-  hipLaunchKernelGGL(k_projection_input<TL>, tile_grid(static_cast<uint64_t>(a.tall) * a.wide), dim3(TL::kThreads), 0, stream, a);
+// All of it in one launch: dx has few tiles with many terms to a sum, the weights' gradients many with few, and together they fill the card
+// (8 x 1024 x 768 x 2048 bfloat16: 64.5 + 66.7 us apart).  dx's tiles come first.
+template <typename X, typename W>
+__global__ __launch_bounds__(X::kThreads, 2) void k_projections(ProjectionArgs a) {
+  static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
+  COMPAMS_TILE_LDS(X, lds);
+  const uint32_t of_dx = a.dx ? a.tall * a.wide : 0, of_weights = a.tall_weight * a.wide * a.weights * a.n, id = tile_id();
+  if (id < of_dx) input_tile<X>(a, id, lds);
+  else if (id < of_dx + of_weights) weight_tile<W>(a, id - of_dx, lds);
 }
-template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN>
-void launch_weight(WeightArgs& a, hipStream_t stream) {
-  using TL = Tiles<T, kAcross, kAcross, WM, WN, FM, FN>;
-  a.tall = static_cast<uint32_t>(tiles_of(a.hidden, TL::kM));
-  a.wide = static_cast<uint32_t>(tiles_of(a.cols, TL::kN));
-  hipLaunchKernelGGL(k_projection_weight<TL>, tile_grid(static_cast<uint64_t>(a.tall) * a.wide * a.count * a.n), dim3(TL::kThreads), 0,
-                     stream, a);
+
+template <typename T, uint32_t WM, uint32_t WN, uint32_t FM, uint32_t FN, uint32_t STEP = 128>
+void launch(ProjectionArgs& a, hipStream_t stream) {
+  using X = Tiles<T, kAlong, kAcross, WM, WN, FM, FN, false, STEP>;
+  using W = Tiles<T, kAcross, kAcross, WM, WN, FM, FN, false, STEP>;
+  a.tall = static_cast<uint32_t>(tiles_of(a.total, X::kM));
+  a.tall_weight = static_cast<uint32_t>(tiles_of(a.hidden, X::kM));
+  a.wide = static_cast<uint32_t>(tiles_of(a.cols, X::kN));
+  const uint64_t tiles = static_cast<uint64_t>(a.wide) * ((a.dx ? a.tall : 0) + static_cast<uint64_t>(a.tall_weight) * a.weights * a.n);
+  if (tiles) hipLaunchKernelGGL((k_projections<X, W>), tile_grid(tiles), dim3(X::kThreads), 0, stream, a);
 }
 template <typename T>
-void launch_both(InputArgs& in, WeightArgs& of, hipStream_t stream) {
-  if (in.dx && in.total) {
-    switch (tile_size(in.total, in.cols, 1)) {
-      case kTile256: launch_input<T, 2, 4, 8, 4>(in, stream); break;
-      case kTile128: launch_input<T, 2, 2, 4, 4>(in, stream); break;
-      default: launch_input<T, 2, 2, 2, 2>(in, stream); break;
-    }
-  }
-  if (of.count) {
-    switch (tile_size(of.hidden, of.cols, static_cast<uint64_t>(of.count) * of.n)) {
-      case kTile256: launch_weight<T, 2, 4, 8, 4>(of, stream); break;
-      case kTile128: launch_weight<T, 2, 2, 4, 4>(of, stream); break;
-      default: launch_weight<T, 2, 2, 2, 2>(of, stream); break;
-    }
+void launch(ProjectionArgs& a, hipStream_t stream) {
+  switch (tile_size({{a.dx ? a.total : 0, a.cols, 1, static_cast<uint64_t>(a.hidden) * a.count},
+                     {a.weights ? a.hidden : 0, a.cols, static_cast<uint64_t>(a.weights) * a.n, a.rows}}, sizeof(T) == 4)) {
+    case kTile256: launch<T, 2, 2, 8, 4, 64>(a, stream); break;  // (256 x 128, two workgroups to a compute unit)
+    case kTile128: launch<T, 2, 2, 4, 4>(a, stream); break;
+    default: launch<T, 2, 2, 2, 2>(a, stream); break;
   }
 }
 
@@ -162,40 +156,37 @@ int compams_projections_backward(const compams_projections* a, void* hip_stream)
   const int status = workspace_status(a->workspace, a->workspace_bytes, projections_bytes(*a));
   if (status != COMPAMS_OK) return status;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  InputArgs in = {};
-  WeightArgs of = {};
+  ProjectionArgs k = {};
   if (a->rows > 0) {
     // (two launches at most: a launch has room for four matrices)
     Packing one, two;
     char* room = static_cast<char*>(a->workspace);
     for (int i = 0; i < 2; ++i) {
-      if (o.d[i].p) in.d[i] = one.add(o.d[i], room);
-      if (a->dx && o.weight[i].p) in.weight[i] = one.add(o.weight[i], room);
+      if (o.d[i].p) k.d[i] = one.add(o.d[i], room);
+      if (a->dx && o.weight[i].p) k.weight[i] = one.add(o.weight[i], room);
     }
-    if (o.x.p && (dweight[0] || dweight[1])) of.x = two.add(o.x, room);
+    if (o.x.p && (dweight[0] || dweight[1])) k.x = two.add(o.x, room);
     run_packing(one, size, stream);
     run_packing(two, size, stream);
+    k.dx = a->dx;
   }
-  in.dx = a->dx;
-  in.ld_dx = a->ld_dx;
-  in.count = a->dup ? 2 : 1;
-  in.total = static_cast<uint32_t>(a->n * a->rows);
-  in.cols = of.cols = static_cast<uint32_t>(a->cols);
-  in.hidden = of.hidden = static_cast<uint32_t>(a->hidden);
-  of.n = static_cast<uint32_t>(a->n);
-  of.rows = static_cast<uint32_t>(a->rows);
-  of.accumulate = static_cast<uint32_t>(a->accumulate);
+  k.ld_dx = a->ld_dx;
+  k.count = a->dup ? 2 : 1;
+  k.n = static_cast<uint32_t>(a->n);
+  k.rows = static_cast<uint32_t>(a->rows);
+  k.total = k.n * k.rows;
+  k.cols = static_cast<uint32_t>(a->cols);
+  k.hidden = static_cast<uint32_t>(a->hidden);
+  k.accumulate = static_cast<uint32_t>(a->accumulate);
   for (int i = 0; i < 2; ++i) {
-    if (!dweight[i]) continue;
-    of.d[of.count] = in.d[i];
-    of.dweight[of.count] = dweight[i];
-    of.ld[of.count] = ld[i];
-    of.stride[of.count] = stride[i];
-    ++of.count;
+    k.dweight[i] = dweight[i];
+    k.ld[i] = ld[i];
+    k.stride[i] = stride[i];
+    if (dweight[i]) k.of[k.weights++] = static_cast<uint32_t>(i);
   }
-  if (a->type == COMPAMS_F32) launch_both<float>(in, of, stream);
-  else if (a->type == COMPAMS_F16) launch_both<half_t>(in, of, stream);
-  else launch_both<bfloat_t>(in, of, stream);
+  if (a->type == COMPAMS_F32) launch<float>(k, stream);
+  else if (a->type == COMPAMS_F16) launch<half_t>(k, stream);
+  else launch<bfloat_t>(k, stream);
   return hipGetLastError() == hipSuccess ? COMPAMS_OK : COMPAMS_HIP_ERROR;
 }
 

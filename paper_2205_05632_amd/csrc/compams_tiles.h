@@ -6,6 +6,8 @@
 // Reads beyond a matrix give zeros (the buffer descriptors' own bounds), so no length has to be a multiple of anything but 16 bytes.
 #pragma once
 
+#include <initializer_list>
+
 #include "compams_rows.h"
 
 namespace compams {
@@ -412,20 +414,39 @@ __device__ __forceinline__ void tile_at(uint32_t id, uint32_t tall, uint32_t wid
   across = in / height;
 }
 
-// Which size of tile a result of rows x cols is made with, `many` of them at once: the largest leaves compute units idle where
-// there are few.  A compute unit's tiles cost what they hold, divided by the rate that a size reaches (8192 x 8192 x 8192
-// bfloat16: 256 x 256 1270 TFLOP/s, 128 x 128 1030, 64 x 64 680; 8192 x 4096 x 768: 759, 718, 586); less where there are too few
-// for one to be loaded while another is multiplied.
+// Which size of tile the results of a launch are made with, each of them `many` matrices of rows x cols with `k` terms in a sum.
+// The larger a tile, the higher its rate; but the compute units' shares of few large tiles are uneven, and a tile alone on a compute unit
+// has nothing beside it while it loads.  Rates of a full card, and of one tile to a compute unit, relative to the first (8192 x 8192 x
+// 768 bfloat16, TFLOP/s: 256 x 256 1340, 128 x 128 1130, 64 x 64 770; alone, 1024 x 1024 x 2048 and the like: 1100, 800, 375.  fp32, where
+// the matrix cores bound every size: 133, 133, 130; alone 64 x 64 100).
 enum TileSize { kTile256, kTile128, kTile64 };
-inline TileSize tile_size(uint64_t rows, uint64_t cols, uint64_t many) {
-  const auto cost = [&](uint64_t edge, double rate1, double rate2, double rate3) {
-    const uint64_t tiles = (rows + edge - 1) / edge * ((cols + edge - 1) / edge) * many, each = (tiles + 255) / 256;
-    return static_cast<double>(each * edge * edge) / (each <= 1 ? rate1 : each <= 2 ? rate2 : rate3);
+struct Work {
+  uint64_t rows, cols, many, k;
+};
+inline TileSize tile_size(std::initializer_list<Work> all, bool wide_type) {
+  const auto cost = [&](uint64_t edge, double full, double alone) {
+    double sum = 0.0, longest = 0.0;
+    uint64_t tiles = 0;
+    for (const Work& w : all) {
+      const uint64_t count = (w.rows + edge - 1) / edge * ((w.cols + edge - 1) / edge) * w.many;
+      if (count == 0 || w.k == 0) continue;
+      const double one = static_cast<double>(edge * edge) * static_cast<double>(w.k);
+      tiles += count;
+      sum += static_cast<double>(count) * one;
+      longest = one > longest ? one : longest;
+    }
+    // whole tiles to a compute unit
+    const double share = tiles ? sum / static_cast<double>(tiles) * static_cast<double>((tiles + 255) / 256) : 0.0;
+    return (share / full > longest / alone) ? share / full : longest / alone;
   };
-  const double large = cost(256, 1.0, 1.0, 1.0), middle = cost(128, 0.6, 0.85, 0.85), small = cost(64, 0.3, 0.45, 0.6);
+  const double large = wide_type ? cost(256, 1.0, 0.95) : cost(256, 1.0, 0.82);
+  const double middle = wide_type ? cost(128, 1.0, 0.9) : cost(128, 0.84, 0.6);
+  const double small = wide_type ? cost(64, 0.97, 0.75) : cost(64, 0.57, 0.28);
   if (large <= middle && large <= small) return kTile256;
   return middle <= small ? kTile128 : kTile64;
 }
+inline uint64_t tiles_of(uint64_t count, uint32_t edge) { return (count + edge - 1) / edge; }
+
 // A weight's gradients, a matrix for each of n workers.
 inline bool gradient_valid(int32_t n, int64_t rows, int64_t cols, int64_t ld, int64_t stride) {
   constexpr int64_t kMost = static_cast<int64_t>(1) << 40;
@@ -441,6 +462,5 @@ inline int workspace_status(const void* p, size_t bytes, size_t need) {
   if (!aligned_to(p, 256)) return COMPAMS_BAD_ALIGNMENT;
   return bytes < need ? COMPAMS_WORKSPACE_TOO_SMALL : COMPAMS_OK;
 }
-inline uint64_t tiles_of(uint64_t count, uint32_t edge) { return (count + edge - 1) / edge; }
 
 }  // namespace compams
