@@ -85,14 +85,13 @@ __device__ __forceinline__ int shift_of(uint32_t top) {
   return exponent == 128 ? 0 : min(14 - exponent, 126);   // (infinities and NaNs stay what they are)
 }
 
-// A workgroup's share of a matrix that is gone over by columns: `wide` lanes side by side with eight columns each, for kRowsEach rows of
+// A workgroup's share of a matrix that is gone over by columns: `wide` lanes side by side with eight columns each, for `each` rows of
 // the matrix a lane.  Matrices are the workers' x, and the weight as number n.
 struct ColumnsArgs {
   const void *x, *weight;
   int64_t ld_x, ld_weight;        // entries
-  uint32_t wide, across, parts_x, parts_weight;
+  uint32_t wide, across, each, parts_x, parts_weight;
 };
-constexpr uint32_t kRowsEach = 16;
 struct Share {
   uint32_t matrix, first, last, column, step;  // rows first, first + step, ... before `last`
 };
@@ -104,8 +103,8 @@ __device__ __forceinline__ bool share_of(const LossArgs& a, const ColumnsArgs& c
   part = part < of_x ? part - s.matrix * c.parts_x : part - of_x;
   const uint32_t rows = s.matrix < a.n ? a.rows : a.vocab;
   s.step = tall;
-  s.last = static_cast<uint32_t>(min(static_cast<uint64_t>(rows), static_cast<uint64_t>(part + 1) * tall * kRowsEach));
-  s.first = part * tall * kRowsEach + threadIdx.x / c.wide;
+  s.last = static_cast<uint32_t>(min(static_cast<uint64_t>(rows), static_cast<uint64_t>(part + 1) * tall * c.each));
+  s.first = part * tall * c.each + threadIdx.x / c.wide;
   s.column = (strip * c.wide + threadIdx.x % c.wide) * kGroup;
   return s.column < a.cols;
 }
@@ -582,11 +581,14 @@ Room room_of(const compams_linear_loss& a) {
 // The kernels that go over x and the weight by columns.
 template <typename T>
 void run_hold(const LossArgs& k, const compams_linear_loss& a, hipStream_t stream) {
-  ColumnsArgs c = {a.x, a.weight, a.ld_x, a.ld_weight, 1, 1, 0, 0};
+  ColumnsArgs c = {a.x, a.weight, a.ld_x, a.ld_weight, 1, 1, 16, 0, 0};
   const uint32_t groups = (k.cols + kGroup - 1) / kGroup;
   while (c.wide < groups && c.wide < kThreads) c.wide *= 2;
   c.across = (groups + c.wide - 1) / c.wide;
-  const uint64_t each = static_cast<uint64_t>(kThreads / c.wide) * kRowsEach;
+  // (fewer rows a lane where that leaves compute units idle: 2048 x 256 fp32 9.7 us with sixteen)
+  const uint64_t tall = kThreads / c.wide, rows = (k.x_held.p ? k.total : 0) + (kScaled<T> && a.dx ? k.vocab : 0);
+  while (c.each > 2 && rows * c.across < 512 * tall * c.each) c.each /= 2;
+  const uint64_t each = tall * c.each;
   if (k.x_held.p) c.parts_x = static_cast<uint32_t>(tiles_of(k.rows, static_cast<uint32_t>(each)));
   if (kScaled<T> && a.dx) c.parts_weight = static_cast<uint32_t>(tiles_of(k.vocab, static_cast<uint32_t>(each)));
   const uint64_t blocks = (static_cast<uint64_t>(c.parts_x) * k.n + c.parts_weight) * c.across;

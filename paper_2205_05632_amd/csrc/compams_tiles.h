@@ -419,18 +419,20 @@ __device__ __forceinline__ void tile_at(uint32_t id, uint32_t tall, uint32_t wid
 // has nothing beside it while it loads.  Rates of a full card, and of one tile to a compute unit, relative to the first (8192 x 8192 x
 // 768 bfloat16, TFLOP/s: 256 x 256 1340, 128 x 128 1130, 64 x 64 770; alone, 1024 x 1024 x 2048 and the like: 1100, 800, 375.  fp32, where
 // the matrix cores bound every size: 133, 133, 130; alone 64 x 64 100).
+// Launches of more than one kind of result take 256 x 128 in steps of 64 bytes for the largest, of which two and three workgroups share a
+// compute unit: one stores while another multiplies (8 x 1024 x 768 x 2048 projections' gradients 115 us, with 128 x 128 123).
 enum TileSize { kTile256, kTile128, kTile64 };
 struct Work {
   uint64_t rows, cols, many, k;
 };
 inline TileSize tile_size(std::initializer_list<Work> all, bool wide_type) {
-  const auto cost = [&](uint64_t edge, double full, double alone) {
+  const auto cost = [&](uint64_t edge, uint64_t across, double full, double alone) {
     double sum = 0.0, longest = 0.0;
     uint64_t tiles = 0;
     for (const Work& w : all) {
-      const uint64_t count = (w.rows + edge - 1) / edge * ((w.cols + edge - 1) / edge) * w.many;
+      const uint64_t count = (w.rows + edge - 1) / edge * ((w.cols + across - 1) / across) * w.many;
       if (count == 0 || w.k == 0) continue;
-      const double one = static_cast<double>(edge * edge) * static_cast<double>(w.k);
+      const double one = static_cast<double>(edge * across) * static_cast<double>(w.k);
       tiles += count;
       sum += static_cast<double>(count) * one;
       longest = one > longest ? one : longest;
@@ -439,9 +441,9 @@ inline TileSize tile_size(std::initializer_list<Work> all, bool wide_type) {
     const double share = tiles ? sum / static_cast<double>(tiles) * static_cast<double>((tiles + 255) / 256) : 0.0;
     return (share / full > longest / alone) ? share / full : longest / alone;
   };
-  const double large = wide_type ? cost(256, 1.0, 0.95) : cost(256, 1.0, 0.82);
-  const double middle = wide_type ? cost(128, 1.0, 0.9) : cost(128, 0.84, 0.6);
-  const double small = wide_type ? cost(64, 0.97, 0.75) : cost(64, 0.57, 0.28);
+  const double large = all.size() > 1 ? cost(256, 128, 0.97, wide_type ? 0.9 : 0.6) : cost(256, 256, 1.0, 0.97);
+  const double middle = wide_type ? cost(128, 128, 1.0, 0.9) : cost(128, 128, 0.84, 0.6);
+  const double small = wide_type ? cost(64, 64, 0.97, 0.75) : cost(64, 64, 0.57, 0.28);
   if (large <= middle && large <= small) return kTile256;
   return middle <= small ? kTile128 : kTile64;
 }
