@@ -538,7 +538,7 @@ inline uint32_t parts_of(int32_t type) { return type == COMPAMS_F32 ? kParts<flo
 
 // A piece's d: wide enough for the products that read it to fill the card, and for dx's sums, which are read and written with every
 // piece, to be little beside it.
-constexpr size_t kPieceBytes = 288u << 20;  // (two of them)
+constexpr size_t kPieceBytes = 96u << 20;  // (two of them)
 constexpr uint32_t kLeastPiece = 1024;
 
 struct Operands {

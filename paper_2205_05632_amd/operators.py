@@ -15,6 +15,7 @@ Every output may be given by name, and is then written in place and returned; wh
 is recorded for autograd.  Work is enqueued on the current stream of the tensors' device.
 """
 import ctypes
+import functools
 import struct
 from typing import Optional
 
@@ -510,6 +511,11 @@ def compams_linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets:
     return mean_loss, losses, dx, dweight
 
 
+@functools.lru_cache(maxsize=64)
+def _clip_table(count: int):
+    return struct.Struct("@" + _CLIP_TENSOR.format[1:] * count)
+
+
 def compams_clip_gradients(gradients, max_norm: float, n: int = 1, *, scale: float = 1.0, out=None,
                            norms: Optional[torch.Tensor] = None, factors: Optional[torch.Tensor] = None,
                            workspace: Optional[torch.Tensor] = None):
@@ -530,17 +536,29 @@ def compams_clip_gradients(gradients, max_norm: float, n: int = 1, *, scale: flo
         norms = torch.empty(n, dtype=torch.float32, device=dev)
     if factors is None:
         factors = torch.empty(n, dtype=torch.float32, device=dev)
-    table = bytearray(_CLIP_TENSOR.size * len(given))
-    for i, (t, o) in enumerate(zip(given, to)):
-        if t.dim() != 2 or t.shape[0] != n:
-            raise ValueError(f"a gradient must be a matrix of {n} rows, got shape {tuple(t.shape)}")
-        count = t.shape[1]
-        p, lp = _matrix(t, "a gradient", t.shape, t.dtype, dev)
-        q, lq = (p, lp) if o is t else _matrix(o, "out", t.shape, o.dtype, dev)
-        _CLIP_TENSOR.pack_into(table, i * _CLIP_TENSOR.size, p, lp, q, lq, count, _type(t.dtype, "a gradient"),
-                               _type(o.dtype, "out"))
-    keep = (ctypes.c_char * len(table)).from_buffer(table)
-    a = (n, len(given), ctypes.addressof(keep), max_norm, scale, _vector(norms, "norms", (n,), dev),
+    table, where = [], norms.get_device()
+    for t, o in zip(given, to):    # (an answer of many tensors waits for this loop: a microsecond a tensor)
+        shape, kind = t.shape, _TYPE.get(t.dtype)
+        if len(shape) != 2 or shape[0] != n:
+            raise ValueError(f"a gradient must be a matrix of {n} rows, got shape {tuple(shape)}")
+        apart, beside = t.stride()
+        count = shape[1]
+        if kind is None or t.get_device() != where or (beside != 1 and count > 1):
+            _matrix(t, "a gradient", shape, t.dtype, dev)
+            _type(t.dtype, "a gradient")
+        p = t.data_ptr()
+        if o is t:
+            table += (p, apart, p, apart, count, kind, kind)
+            continue
+        kind_to = _TYPE.get(o.dtype)
+        apart_to, beside = o.stride() if o.dim() == 2 else (0, 0)
+        if kind_to is None or o.shape != shape or o.get_device() != where or (beside != 1 and count > 1):
+            _matrix(o, "out", shape, o.dtype, dev)
+            _type(o.dtype, "out")
+        table += (p, apart, o.data_ptr(), apart_to, count, kind, kind_to)
+    table = _clip_table(len(given)).pack(*table)
+    keep = ctypes.c_char_p(table)
+    a = (n, len(given), ctypes.cast(keep, ctypes.c_void_p).value, max_norm, scale, _vector(norms, "norms", (n,), dev),
          _vector(factors, "factors", (n,), dev))
     a, workspace = _room(lib().compams_clip_workspace_size, _CLIP.pack, a, workspace, dev)
     _check(_on_stream(dev, lib().compams_clip_gradients, a), "compams_clip_gradients")
