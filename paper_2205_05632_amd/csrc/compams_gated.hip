@@ -269,8 +269,9 @@ struct BackwardCut {
 BackwardCut backward_cut(const compams_gated& a) {
   BackwardCut c;
   const uint64_t groups = (static_cast<uint64_t>(a.hidden) + kGroup - 1) / kGroup;
+  // (a wavefront's width at most: several rows of a workgroup are added up in it, and fewer parts are written)
   c.wide = 1;
-  while (c.wide < groups && c.wide < kThreads) c.wide *= 2;
+  while (c.wide < groups && c.wide < 64) c.wide *= 2;
   c.across = static_cast<uint32_t>((groups + c.wide - 1) / c.wide);
   const uint64_t tall = kThreads / c.wide;
   uint64_t rows = tall * 8;  // of a part
