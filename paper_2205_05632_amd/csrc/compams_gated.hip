@@ -140,6 +140,7 @@ struct BackwardArgs {
   uint32_t accumulate;
 };
 constexpr uint32_t kThreads = 256;
+constexpr uint32_t kTogether = 4;  // rows of a lane
 
 // A workgroup takes a part of a worker's rows and wide * 8 columns of them, a lane eight columns of every (256 / wide)-th row.
 // Bound by memory: three matrices read, two written.
@@ -154,25 +155,38 @@ __global__ __launch_bounds__(kThreads) void k_gated_backward(BackwardArgs a) {
   const uint32_t first = part * a.part_rows, last = min(first + a.part_rows, a.rows);
   float sg[kGroup] = {}, su[kGroup] = {};
   if (c < a.hidden) {
-    for (uint32_t in = first + down; in < last; in += tall) {
-      const int64_t r = static_cast<int64_t>(w) * a.rows + in;
-      float dm[kGroup], g[kGroup], u[kGroup], dg[kGroup], du[kGroup];
-      load_group(dm, static_cast<const T*>(a.dm) + r * a.ld_dm, c, a.hidden);
-      load_group(g, static_cast<const T*>(a.gate) + r * a.ld_gate, c, a.hidden);
-      load_group(u, static_cast<const T*>(a.up) + r * a.ld_up, c, a.hidden);
+    // (kTogether rows' loads under way at once: outputs may lie over inputs, so the compiler keeps the order of accesses)
+    for (uint32_t in = first + down; in < last; in += tall * kTogether) {
+      typename Group<T>::type dm_raw[kTogether], g_raw[kTogether], u_raw[kTogether];
 #pragma unroll
-      for (uint32_t j = 0; j < kGroup; ++j) {
-        float slope;
-        const float v = activate<ACT, true>(g[j], slope);
-        dg[j] = dm[j] * u[j] * slope;
-        du[j] = dm[j] * v;
-        if constexpr (BIAS) {
-          sg[j] += dg[j];
-          su[j] += du[j];
-        }
+      for (uint32_t q = 0; q < kTogether; ++q) {
+        const int64_t r = static_cast<int64_t>(w) * a.rows + min(in + q * tall, last - 1);
+        dm_raw[q] = load_raw(static_cast<const T*>(a.dm) + r * a.ld_dm, c, a.hidden);
+        g_raw[q] = load_raw(static_cast<const T*>(a.gate) + r * a.ld_gate, c, a.hidden);
+        u_raw[q] = load_raw(static_cast<const T*>(a.up) + r * a.ld_up, c, a.hidden);
       }
-      store_group<T>(static_cast<T*>(a.dgate) + r * a.ld_dgate, c, a.hidden, dg);
-      store_group<T>(static_cast<T*>(a.dup) + r * a.ld_dup, c, a.hidden, du);
+#pragma unroll
+      for (uint32_t q = 0; q < kTogether; ++q) {
+        if (in + q * tall >= last) break;
+        const int64_t r = static_cast<int64_t>(w) * a.rows + in + q * tall;
+        float dm[kGroup], g[kGroup], u[kGroup], dg[kGroup], du[kGroup];
+        unpack(dm, dm_raw[q]);
+        unpack(g, g_raw[q]);
+        unpack(u, u_raw[q]);
+#pragma unroll
+        for (uint32_t j = 0; j < kGroup; ++j) {
+          float slope;
+          const float v = activate<ACT, true>(g[j], slope);
+          dg[j] = dm[j] * u[j] * slope;
+          du[j] = dm[j] * v;
+          if constexpr (BIAS) {
+            sg[j] += dg[j];
+            su[j] += du[j];
+          }
+        }
+        store_group<T>(static_cast<T*>(a.dgate) + r * a.ld_dgate, c, a.hidden, dg);
+        store_group<T>(static_cast<T*>(a.dup) + r * a.ld_dup, c, a.hidden, du);
+      }
     }
   }
   if constexpr (BIAS) {
