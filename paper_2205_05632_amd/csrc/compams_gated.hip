@@ -118,8 +118,121 @@ void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
     default: hipLaunchKernelGGL((k_gated_forward<TL, COMPAMS_SIGMOID>), grid, block, 0, stream, a); break;
   }
 }
+// Few rows: the weights are read once and there is little to do with them.  A workgroup takes sixteen columns of both projections, its
+// wavefronts 128 bytes of k in turn, straight from memory into registers (no row has to be aligned), and their sums are joined in LDS.
+// A lane's two pieces of 16 bytes lie side by side, so that a read's neighbours fill whole lines: k may be taken in any order
+// that is the same for both operands.  Bound by memory (16 x 4096 x 8192 bfloat16, 134 MB: 64 x 64 tiles 50 us).
+template <typename T>
+__device__ __forceinline__ typename Fragment<T>::type load_piece(const char* row, uint32_t at, uint32_t cols) {
+  constexpr uint32_t kEach = 16 / sizeof(T);
+  typename Fragment<T>::type v = {};
+  if (at + kEach <= cols) {
+    __builtin_memcpy(&v, row + at * sizeof(T), sizeof(v));
+  } else {
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j)
+      if (at + j < cols) v[j] = reinterpret_cast<const T*>(row)[at + j];
+  }
+  return v;
+}
+constexpr uint32_t kFewRows = 32;
+
+template <typename T, int ACT, uint32_t FM, uint32_t WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_gated_few(ForwardArgs a) {
+  constexpr uint32_t kEach = 16 / sizeof(T), kDeep = 8 * kEach;  // k of a step
+  constexpr uint32_t kAhead = 2;                                 // steps whose loads are under way at once
+  __shared__ f32x4 joined[WAVES][2 * FM][64];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63u, l = lane & 15u, g = lane >> 4;
+  const uint32_t h0 = blockIdx.x * 16, h = min(h0 + l, a.hidden - 1);
+  const char* const of_gate = static_cast<const char*>(a.gate_weight.p) + h * a.gate_weight.ld;
+  const char* const of_up = static_cast<const char*>(a.up_weight.p) + h * a.up_weight.ld;
+  const char* of_x[FM];
+#pragma unroll
+  for (uint32_t i = 0; i < FM; ++i) of_x[i] = static_cast<const char*>(a.x.p) + min(i * 16 + l, a.total - 1) * a.x.ld;
+  f32x4 sum[2 * FM];
+#pragma unroll
+  for (uint32_t i = 0; i < 2 * FM; ++i) sum[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  typedef typename Fragment<T>::type Piece;
+  const auto take = [&](uint32_t s, Piece (&gate)[2], Piece (&up)[2], Piece (&x)[FM][2], bool whole) {
+#pragma unroll
+    for (uint32_t q = 0; q < 2; ++q) {
+      const uint32_t at = s * kDeep + (2 * g + q) * kEach, cols = whole ? ~0u : a.cols;
+      gate[q] = load_piece<T>(of_gate, at, cols);
+      up[q] = load_piece<T>(of_up, at, cols);
+#pragma unroll
+      for (uint32_t i = 0; i < FM; ++i) x[i][q] = load_piece<T>(of_x[i], at, cols);
+    }
+  };
+  const auto add = [&](const Piece (&gate)[2], const Piece (&up)[2], const Piece (&x)[FM][2]) {
+#pragma unroll
+    for (uint32_t q = 0; q < 2; ++q)
+#pragma unroll
+      for (uint32_t i = 0; i < FM; ++i) {
+        multiply(sum[2 * i], x[i][q], gate[q]);
+        multiply(sum[2 * i + 1], x[i][q], up[q]);
+      }
+  };
+  const uint32_t full = a.cols / kDeep;
+  uint32_t s = wave;
+  for (; s + (kAhead - 1) * WAVES < full; s += kAhead * WAVES) {
+    Piece gate[kAhead][2], up[kAhead][2], x[kAhead][FM][2];
+#pragma unroll
+    for (uint32_t u = 0; u < kAhead; ++u) take(s + u * WAVES, gate[u], up[u], x[u], true);
+#pragma unroll
+    for (uint32_t u = 0; u < kAhead; ++u) add(gate[u], up[u], x[u]);
+  }
+  for (; s <= full; s += WAVES) {  // (the last step may be a part of one, or nothing)
+    Piece gate[2], up[2], x[FM][2];
+    take(s, gate, up, x, false);
+    add(gate, up, x);
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < 2 * FM; ++i) joined[wave][i][lane] = sum[i];
+  __syncthreads();
+  for (uint32_t e = threadIdx.x; e < FM * 256; e += WAVES * 64) {
+    // entry (m, c) of a tile is number c % 4 of lane m + 16 (c / 4)
+    const uint32_t i = e / 256, m = e / 16 % 16, c = e % 16, r = i * 16 + m, to = h0 + c;
+    if (r >= a.total || to >= a.hidden) continue;
+    float ga = a.gate_bias ? a.gate_bias[to] : 0.0f, ub = a.up_bias ? a.up_bias[to] : 0.0f;
+    float sg = 0.0f, su = 0.0f;
+#pragma unroll
+    for (uint32_t k = 0; k < WAVES; ++k) {
+      sg += joined[k][2 * i][m + 16 * (c / 4)][c % 4];
+      su += joined[k][2 * i + 1][m + 16 * (c / 4)][c % 4];
+    }
+    ga += sg;
+    ub += su;
+    float none;
+    if (a.gate) static_cast<T*>(a.gate)[r * a.ld_gate + to] = static_cast<T>(ga);
+    if (a.up) static_cast<T*>(a.up)[r * a.ld_up + to] = static_cast<T>(ub);
+    static_cast<T*>(a.m)[r * a.ld_m + to] = static_cast<T>(activate<ACT, false>(ga, none) * ub);
+  }
+}
+
+template <typename T, int ACT>
+void launch_few(const ForwardArgs& a, hipStream_t stream) {
+  const dim3 grid((a.hidden + 15) / 16);
+  // (eight wavefronts where each has two steps or more)
+  const bool many = a.cols * sizeof(T) >= 16 * 128;
+  if (a.total <= 16 && many) hipLaunchKernelGGL((k_gated_few<T, ACT, 1, 8>), grid, dim3(512), 0, stream, a);
+  else if (a.total <= 16) hipLaunchKernelGGL((k_gated_few<T, ACT, 1, 4>), grid, dim3(256), 0, stream, a);
+  else if (many) hipLaunchKernelGGL((k_gated_few<T, ACT, 2, 8>), grid, dim3(512), 0, stream, a);
+  else hipLaunchKernelGGL((k_gated_few<T, ACT, 2, 4>), grid, dim3(256), 0, stream, a);
+}
+
+template <typename T>
+void launch_few(const ForwardArgs& a, int act, hipStream_t stream) {
+  switch (act) {
+    case COMPAMS_SILU: launch_few<T, COMPAMS_SILU>(a, stream); break;
+    case COMPAMS_GELU: launch_few<T, COMPAMS_GELU>(a, stream); break;
+    case COMPAMS_GELU_TANH: launch_few<T, COMPAMS_GELU_TANH>(a, stream); break;
+    case COMPAMS_RELU: launch_few<T, COMPAMS_RELU>(a, stream); break;
+    default: launch_few<T, COMPAMS_SIGMOID>(a, stream); break;
+  }
+}
 template <typename T>
 void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
+  if (a.total <= kFewRows) return launch_few<T>(a, act, stream);
   switch (tile_size({{a.total, 2 * static_cast<uint64_t>(a.hidden), 1, a.cols}}, sizeof(T) == 4)) {
     case kTile256: launch_forward<T, 4, 2, 4, 8>(a, act, stream); break;  // (64 columns of a projection to a wavefront)
     case kTile128: launch_forward<T, 2, 2, 4, 4>(a, act, stream); break;
@@ -271,7 +384,7 @@ Operands operands(const compams_gated& a) {
           {a.up_weight, a.ld_up_weight, a.hidden, a.cols, size}};
 }
 size_t forward_bytes(const compams_gated& a) {
-  if (a.rows == 0) return 0;
+  if (a.n * a.rows <= kFewRows) return 0;
   const Operands o = operands(a);
   return o.x.packed_bytes() + o.gate.packed_bytes() + o.up.packed_bytes();
 }
@@ -331,12 +444,19 @@ int compams_gated_forward(const compams_gated* a, void* hip_stream) {
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   ForwardArgs k = {};
   const Operands o = operands(*a);
-  Packing packing;
-  char* room = static_cast<char*>(a->workspace);
-  k.x = packing.add(o.x, room);
-  k.gate_weight = packing.add(o.gate, room);
-  k.up_weight = packing.add(o.up, room);
-  run_packing(packing, size, stream);
+  const auto as_is = [&](const Matrix& m) { return Read{m.p, m.ld * static_cast<int64_t>(size)}; };
+  if (a->n * a->rows <= kFewRows) {
+    k.x = as_is(o.x);
+    k.gate_weight = as_is(o.gate);
+    k.up_weight = as_is(o.up);
+  } else {
+    Packing packing;
+    char* room = static_cast<char*>(a->workspace);
+    k.x = packing.add(o.x, room);
+    k.gate_weight = packing.add(o.gate, room);
+    k.up_weight = packing.add(o.up, room);
+    run_packing(packing, size, stream);
+  }
   k.gate_bias = a->gate_bias; k.up_bias = a->up_bias;
   k.m = a->m; k.gate = a->gate; k.up = a->up;
   k.ld_m = a->ld_m; k.ld_gate = a->ld_gate; k.ld_up = a->ld_up;
