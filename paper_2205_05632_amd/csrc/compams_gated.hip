@@ -135,7 +135,7 @@ __device__ __forceinline__ typename Fragment<T>::type load_piece(const char* row
   }
   return v;
 }
-constexpr uint32_t kFewRows = 32;
+constexpr uint32_t kFewRows = 64;
 
 template <typename T, int ACT, uint32_t FM, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * 64) void k_gated_few(ForwardArgs a) {
@@ -178,6 +178,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_gated_few(ForwardArgs a) {
     Piece gate[kAhead][2], up[kAhead][2], x[kAhead][FM][2];
 #pragma unroll
     for (uint32_t u = 0; u < kAhead; ++u) take(s + u * WAVES, gate[u], up[u], x[u], true);
+    __builtin_amdgcn_sched_barrier(0);  // (all on their way before the first is waited for)
 #pragma unroll
     for (uint32_t u = 0; u < kAhead; ++u) add(gate[u], up[u], x[u]);
   }
@@ -216,6 +217,7 @@ void launch_few(const ForwardArgs& a, hipStream_t stream) {
   const bool many = a.cols * sizeof(T) >= 16 * 128;
   if (a.total <= 16 && many) hipLaunchKernelGGL((k_gated_few<T, ACT, 1, 8>), grid, dim3(512), 0, stream, a);
   else if (a.total <= 16) hipLaunchKernelGGL((k_gated_few<T, ACT, 1, 4>), grid, dim3(256), 0, stream, a);
+  else if (a.total > 32) hipLaunchKernelGGL((k_gated_few<T, ACT, 4, 4>), grid, dim3(256), 0, stream, a);
   else if (many) hipLaunchKernelGGL((k_gated_few<T, ACT, 2, 8>), grid, dim3(512), 0, stream, a);
   else hipLaunchKernelGGL((k_gated_few<T, ACT, 2, 4>), grid, dim3(256), 0, stream, a);
 }
