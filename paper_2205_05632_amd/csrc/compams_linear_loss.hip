@@ -284,24 +284,38 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) 
   }
 }
 
-// A row's loss and softmax from its spans' maxima and sums: sixteen rows to a workgroup, sixteen lanes to a row.
-__global__ __launch_bounds__(kThreads) void k_linear_loss_join(LossArgs a) {
-  __shared__ float2 part[16][17];
+// A row's loss and softmax from its spans' maxima and sums: sixteen rows to a workgroup, 64 lanes to a row.
+constexpr uint32_t kJoinLanes = 64;
+__global__ __launch_bounds__(16 * kJoinLanes) void k_linear_loss_join(LossArgs a) {
+  __shared__ float2 part[kJoinLanes][17];
   const uint32_t l = threadIdx.x % 16, turn = threadIdx.x / 16, spans = (a.vocab - 1) / kSpan + 1;
   if (a.tops)  // (cleared for the kernels that follow)
-    for (uint64_t i = blockIdx.x * kThreads + threadIdx.x; i < static_cast<uint64_t>(a.n + 1) * a.cols; i += static_cast<uint64_t>(gridDim.x) * kThreads)
+    for (uint64_t i = blockIdx.x * blockDim.x + threadIdx.x; i < static_cast<uint64_t>(a.n + 1) * a.cols; i += static_cast<uint64_t>(gridDim.x) * blockDim.x)
       a.tops[i] = 0;
   for (uint64_t first = blockIdx.x * 16u; first < a.total; first += static_cast<uint64_t>(gridDim.x) * 16) {
     const uint64_t r = first + l;
     float top = -INFINITY, s = 0.0f;
     if (r < a.total)
-      for (uint32_t k = turn; k < spans; k += 16) {
+#pragma unroll 4
+      for (uint32_t k = turn; k < spans; k += kJoinLanes) {
         const float2 one = a.partial[static_cast<uint64_t>(k) * a.total + r];
         const float more = fmaxf(top, one.x), base = base_of(more);
         s = s * exp_of(top - base) + one.y * exp_of(one.x - base);
         top = more;
       }
-    part[turn][l] = make_float2(top, s);
+    // (the lanes of a row in a tree, every half in the other's place)
+    for (uint32_t half = kJoinLanes / 2; half >= 16; half /= 2) {
+      part[turn][l] = make_float2(top, s);
+      __syncthreads();
+      if (turn < half) {
+        const float2 one = part[turn + half][l];
+        const float more = fmaxf(top, one.x), base = base_of(more);
+        s = s * exp_of(top - base) + one.y * exp_of(one.x - base);
+        top = more;
+      }
+      __syncthreads();
+    }
+    if (turn < 16) part[turn][l] = make_float2(top, s);
     __syncthreads();
     if (turn == 0 && r < a.total) {
       float most = part[0][l].x;
@@ -603,7 +617,7 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
   if (k.total) {
     launch_stats<T>(k, stream);
     const uint32_t blocks = (k.total + 15) / 16;
-    hipLaunchKernelGGL(k_linear_loss_join, dim3(blocks < 65536 ? blocks : 65536), dim3(kThreads), 0, stream, k);
+    hipLaunchKernelGGL(k_linear_loss_join, dim3(blocks < 65536 ? blocks : 65536), dim3(16 * kJoinLanes), 0, stream, k);
   }
   if (a.mean_loss || gradient) hipLaunchKernelGGL(k_linear_loss_mean, dim3(k.n), dim3(1024), 0, stream, k);
   if (!gradient) return;

@@ -383,15 +383,15 @@ struct Packing {
     const void* from;
     void* to;
     int64_t ld;  // entries
-    uint64_t pieces;
-    uint32_t per_row, cols;
+    int64_t rows;
+    uint32_t per_row, cols;  // pieces of 16 bytes, entries
   } job[kMostPacked];
   // How the kernels are to read `m`; moves `workspace` on by what it takes of it.
   Read add(const Matrix& m, char*& workspace) {
     if (m.as_is()) return {m.p, m.rows <= 1 ? m.packed_row_bytes() : m.ld * static_cast<int64_t>(m.size)};
     const Read r = {workspace, m.packed_row_bytes()};
     const uint32_t per_row = static_cast<uint32_t>(m.packed_row_bytes() / 16);
-    job[count++] = {m.p, workspace, m.ld, static_cast<uint64_t>(m.rows) * per_row, per_row, static_cast<uint32_t>(m.cols)};
+    job[count++] = {m.p, workspace, m.ld, m.rows, per_row, static_cast<uint32_t>(m.cols)};
     workspace += m.packed_bytes();
     return r;
   }

@@ -4,25 +4,43 @@
 namespace compams {
 namespace {
 
-// One lane to a piece of 16 bytes; bound by memory.  (Rows that start on 16 bytes and have whole pieces are not copied.)
+// A workgroup takes whole rows, a lane a piece of 16 bytes of each of four at a time, as many lanes side by side as a row has pieces.  (Rows
+// that start on 16 bytes and have whole pieces are not copied.)
+template <typename T>
+__device__ __forceinline__ typename Fragment<T>::type piece_of(const T* from, uint32_t c, uint32_t cols) {
+  constexpr uint32_t kEach = 16 / sizeof(T);
+  typename Fragment<T>::type v = {};
+  if (c + kEach <= cols) {
+    __builtin_memcpy(&v, from + c, sizeof(v));  // (wherever it starts)
+  } else {
+#pragma unroll
+    for (uint32_t k = 0; k < kEach; ++k)
+      if (c + k < cols) v[k] = from[c + k];
+  }
+  return v;
+}
+constexpr uint32_t kAtOnce = 4;
 template <typename T>
 __global__ __launch_bounds__(256) void k_pack(Packing p) {
-  constexpr uint32_t kEach = 16 / sizeof(T);
   typedef typename Fragment<T>::type Piece;
   const Packing::Job& j = p.job[blockIdx.y];
-  for (uint64_t i = blockIdx.x * 256u + threadIdx.x; i < j.pieces; i += gridDim.x * 256u) {
-    const uint64_t row = i / j.per_row;
-    const uint32_t c = static_cast<uint32_t>(i - row * j.per_row) * kEach;
-    const T* const from = static_cast<const T*>(j.from) + static_cast<int64_t>(row) * j.ld + c;
-    Piece v;
-    if (c + kEach <= j.cols) {
-      __builtin_memcpy(&v, from, sizeof(v));  // (wherever it starts)
-    } else {
+  const uint32_t side = j.per_row < 256 ? 256 / j.per_row : 1;  // rows side by side
+  const uint32_t in = j.per_row < 256 ? threadIdx.x / j.per_row : 0;
+  if (in >= side) return;
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * side * kAtOnce + in; first < j.rows; first += static_cast<int64_t>(gridDim.x) * side * kAtOnce)
+    for (uint32_t c = threadIdx.x - in * j.per_row; c < j.per_row; c += 256) {
+      Piece v[kAtOnce];
 #pragma unroll
-      for (uint32_t k = 0; k < kEach; ++k) v[k] = c + k < j.cols ? from[k] : static_cast<T>(0.0f);
+      for (uint32_t q = 0; q < kAtOnce; ++q) {
+        const int64_t r = first + q * side;
+        v[q] = piece_of(static_cast<const T*>(j.from) + (r < j.rows ? r : j.rows - 1) * j.ld, c * (16 / sizeof(T)), j.cols);
+      }
+#pragma unroll
+      for (uint32_t q = 0; q < kAtOnce; ++q) {
+        const int64_t r = first + q * side;
+        if (r < j.rows) static_cast<Piece*>(j.to)[r * j.per_row + c] = v[q];
+      }
     }
-    static_cast<Piece*>(j.to)[i] = v;
-  }
 }
 
 }  // namespace
@@ -30,9 +48,12 @@ __global__ __launch_bounds__(256) void k_pack(Packing p) {
 void run_packing(const Packing& p, size_t size, hipStream_t stream) {
   if (p.count == 0) return;
   uint64_t most = 1;
-  for (uint32_t i = 0; i < p.count; ++i) most = p.job[i].pieces > most ? p.job[i].pieces : most;
-  const uint64_t blocks = (most + 255) / 256;
-  const dim3 grid(static_cast<uint32_t>(blocks < 16384 ? blocks : 16384), p.count);
+  for (uint32_t i = 0; i < p.count; ++i) {
+    const Packing::Job& j = p.job[i];
+    const uint64_t each = (j.per_row < 256 ? 256 / j.per_row : 1) * kAtOnce, blocks = (static_cast<uint64_t>(j.rows) + each - 1) / each;
+    most = blocks > most ? blocks : most;
+  }
+  const dim3 grid(static_cast<uint32_t>(most < 16384 ? most : 16384), p.count);
   if (size == 4) hipLaunchKernelGGL(k_pack<float>, grid, dim3(256), 0, stream, p);
   else hipLaunchKernelGGL(k_pack<half_t>, grid, dim3(256), 0, stream, p);  // (bits)
 }
