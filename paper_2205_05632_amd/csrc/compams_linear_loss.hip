@@ -67,7 +67,8 @@ struct LossArgs {
   Piece now, next;
   int64_t ld_d;              // bytes from row to row of d
   int64_t part_bytes;
-  float* dx_sum;             // fp32 sums of dx
+  float* dx_sum;             // fp32 sums of dx, of every split
+  uint32_t splits;           // parts of a piece's columns whose sums of dx are formed apart
   void* dx;
   int64_t ld_dx;
   float* dweight;
@@ -417,13 +418,27 @@ __device__ __forceinline__ f32x4 scales(const LossArgs& a, uint32_t matrix, uint
   return v;
 }
 
+template <typename T>
+__device__ __forceinline__ void store_dx(const LossArgs& a, uint32_t r, uint32_t n, f32x4 v, const f32x4& of_column) {
+  const bool learnt = a.stat[r].over != 0.0f;
+  const float f = a.factor[r / a.rows] / kHeld<T>;
+#pragma unroll
+  for (uint32_t q = 0; q < 4; ++q) v[q] = learnt ? v[q] * of_column[q] * f : 0.0f;
+  store4(static_cast<T*>(a.dx) + static_cast<int64_t>(r) * a.ld_dx + n, v, static_cast<int64_t>(a.cols) - n);
+}
+
 // A tile of dx.  The sums go on from those of the pieces before, so that they do not depend on where pieces end.
 template <typename TL, typename T>
 __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, const TileLds& lds) {
+  const uint32_t each = a.tall * a.wide, mine = by_die(id, each * a.splits), split = mine / each;
   uint32_t down, across;
-  tile_at(by_die(id, a.tall * a.wide), a.tall, a.wide, down, across);
+  tile_at(mine - split * each, a.tall, a.wide, down, across);
   const uint32_t m0 = down * TL::kM, n0 = across * TL::kN, padded = (a.cols + 3) / 4 * 4;
-  const auto sums = [&](uint32_t r, uint32_t n) { return reinterpret_cast<f32x4*>(a.dx_sum + static_cast<uint64_t>(r) * padded + n); };
+  const uint32_t share = ((a.now.width + a.splits - 1) / a.splits + 63) / 64 * 64;
+  const uint32_t k0 = min(split * share, a.now.width), width = min(share, a.now.width - k0);
+  const auto sums = [&](uint32_t r, uint32_t n) {
+    return reinterpret_cast<f32x4*>(a.dx_sum + (static_cast<uint64_t>(split) * a.total + r) * padded + n);
+  };
   TL t;
   t.clear();
   if (!a.begin)
@@ -431,23 +446,17 @@ __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, const
       if (m0 + m < a.total && n0 + n < a.cols) v = *sums(m0 + m, n0 + n);
     });
   t.run([&](uint32_t, Side& d, Side& w, Side&) {
-    d = side<typename TL::T, kAlong>(a.now.d, a.ld_d, a.total, m0, a.now.width);
-    w = side<typename TL::T, kAcross>(static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.now.first) * a.weight_held.ld,
-                                      a.weight_held.ld, a.cols, n0, a.now.width);
-  }, 1, a.now.width, lds);
-  const f32x4 of_column = a.end ? scales<T>(a, a.n, n0 + TL::row_n()) : f32x4{};
+    d = side<typename TL::T, kAlong>(a.now.d + k0 * sizeof(typename TL::T), a.ld_d, a.total, m0, width);
+    w = side<typename TL::T, kAcross>(static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.now.first + k0) * a.weight_held.ld,
+                                      a.weight_held.ld, a.cols, n0, width);
+  }, 1, width, lds);
+  const bool end = a.end && a.splits == 1;
+  const f32x4 of_column = end ? scales<T>(a, a.n, n0 + TL::row_n()) : f32x4{};
   t.rows(lds.a[0], [&](uint32_t m, uint32_t n, f32x4 v) {
     const uint32_t r = m0 + m;
     if (r >= a.total || n0 + n >= a.cols) return;
-    if (!a.end) {
-      *sums(r, n0 + n) = v;
-      return;
-    }
-    const bool learnt = a.stat[r].over != 0.0f;
-    const float f = a.factor[r / a.rows] / kHeld<T>;
-#pragma unroll
-    for (uint32_t q = 0; q < 4; ++q) v[q] = learnt ? v[q] * of_column[q] * f : 0.0f;
-    store4(static_cast<T*>(a.dx) + static_cast<int64_t>(r) * a.ld_dx + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n);
+    if (end) store_dx<T>(a, r, n0 + n, v, of_column);
+    else *sums(r, n0 + n) = v;
   });
 }
 
@@ -480,12 +489,12 @@ __device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, cons
 // launch each 96 tiles of dx and 384 of dweight left a third of it idle; d apart 165 us, the products 375 for 8448 columns.)
 // dx's tiles come first, the shortest last.
 template <typename D, typename X, typename W, typename T>
-__global__ __launch_bounds__(X::kThreads, 2) void k_linear_loss_piece(LossArgs a) {
+__global__ __launch_bounds__(X::kThreads, X::STEP == 64 && sizeof(T) == 2 ? 3 : 2) void k_linear_loss_piece(LossArgs a) {
   static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
   static_assert(X::kBytesA == D::kBytesA && X::kBytesB == D::kBytesB && X::kThreads == D::kThreads, "one kind of tile");
   COMPAMS_TILE_LDS(X, lds);
   const bool any = a.now.width != 0;
-  const uint32_t of_dx = any && a.dx ? a.tall * a.wide : 0, of_weight = any && a.dweight ? a.tall_weight * a.wide * a.n : 0;
+  const uint32_t of_dx = any && a.dx ? a.tall * a.wide * a.splits : 0, of_weight = any && a.dweight ? a.tall_weight * a.wide * a.n : 0;
   const uint32_t of_d = a.next.width ? a.tall * a.wide_next : 0;
   uint32_t id = tile_id();
   if (id < of_dx) return input_tile<X, T>(a, id, lds);
@@ -493,6 +502,19 @@ __global__ __launch_bounds__(X::kThreads, 2) void k_linear_loss_piece(LossArgs a
   if (id < of_weight) return weight_tile<W, T>(a, id, lds);
   id -= of_weight;
   if (id < of_d) gradient_tile<D>(a, id, lds);
+}
+
+// dx from the sums of its splits, four entries to a lane.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_linear_loss_input(LossArgs a) {
+  const uint32_t per_row = (a.cols + 3) / 4;
+  const uint64_t all = static_cast<uint64_t>(a.total) * per_row;
+  for (uint64_t i = blockIdx.x * kThreads + threadIdx.x; i < all; i += static_cast<uint64_t>(gridDim.x) * kThreads) {
+    const uint32_t r = static_cast<uint32_t>(i / per_row), n = static_cast<uint32_t>(i - static_cast<uint64_t>(r) * per_row) * 4;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t s = 0; s < a.splits; ++s) v += reinterpret_cast<const f32x4*>(a.dx_sum)[s * all + i];
+    store_dx<T>(a, r, n, v, scales<T>(a, a.n, n));
+  }
 }
 
 // ---- Launches ------------------------------------------------------------------------------------------------
@@ -522,7 +544,7 @@ void launch_piece(LossArgs& a, hipStream_t stream) {
   a.wide_next = static_cast<uint32_t>(tiles_of(a.next.width, X::kN));
   uint64_t tiles = static_cast<uint64_t>(a.tall) * a.wide_next;
   if (a.now.width)
-    tiles += static_cast<uint64_t>(a.wide) * ((a.dx ? a.tall : 0) + (a.dweight ? static_cast<uint64_t>(a.tall_weight) * a.n : 0));
+    tiles += static_cast<uint64_t>(a.wide) * ((a.dx ? static_cast<uint64_t>(a.tall) * a.splits : 0) + (a.dweight ? static_cast<uint64_t>(a.tall_weight) * a.n : 0));
   if (tiles) hipLaunchKernelGGL((k_linear_loss_piece<D, X, W, T>), tile_grid(tiles), dim3(X::kThreads), 0, stream, a);
 }
 template <typename T>
@@ -544,7 +566,7 @@ bool linear_loss_valid(const compams_linear_loss* a) {
 struct Room {
   size_t x = 0, weight = 0, x_held = 0, weight_held = 0, tops = 0, partial = 0, of_target = 0, stat = 0, losses = 0, factor = 0, d = 0,
          dx_sum = 0;
-  uint32_t piece = 0, pieces = 0;
+  uint32_t piece = 0, pieces = 0, splits = 1;
   size_t all() const { return x + weight + x_held + weight_held + tops + partial + of_target + stat + losses + factor + (pieces > 1 ? 2 : 1) * d + dx_sum; }
 };
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -588,7 +610,8 @@ Room room_of(const compams_linear_loss& a) {
   r.piece = static_cast<uint32_t>((tiles_of(a.vocab, r.pieces) + 255) / 256 * 256);
   r.pieces = static_cast<uint32_t>(tiles_of(a.vocab, r.piece));
   r.d = up256(column * r.piece);  // (of one)
-  if (a.dx && r.pieces > 1) r.dx_sum = up256(total * ((a.cols + 3) / 4 * 4) * sizeof(float));
+  if (a.dx) r.splits = splits_of(total, a.cols, a.vocab < r.piece ? a.vocab : r.piece);
+  if (a.dx && (r.pieces > 1 || r.splits > 1)) r.dx_sum = up256(r.splits * total * ((a.cols + 3) / 4 * 4) * sizeof(float));
   return r;
 }
 
@@ -637,7 +660,7 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
   };
   char* const d = k.now.d;
   const auto size = [&] {
-    return tile_size({{a.dx ? k.total : 0, k.cols, 1, k.now.width},
+    return tile_size({{a.dx ? k.total : 0, k.cols, k.splits, k.now.width / k.splits},
                       {a.dweight ? k.now.width : 0, k.cols, k.n, static_cast<uint64_t>(k.rows) * kParts<T>},
                       {k.total, k.next.width, 1, k.cols}}, sizeof(T) == 4);
   };
@@ -652,6 +675,10 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
     k.begin = p == 0;
     k.end = p + 1 == room.pieces;
     launch_piece<T>(k, size(), stream);
+  }
+  if (a.dx && k.splits > 1) {
+    const uint64_t blocks = (static_cast<uint64_t>(k.total) * ((k.cols + 3) / 4) + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL(k_linear_loss_input<T>, dim3(static_cast<uint32_t>(blocks < 16384 ? blocks : 16384)), dim3(kThreads), 0, stream, k);
   }
 }
 
@@ -709,6 +736,7 @@ int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream)
   k.factor = reinterpret_cast<float*>(take(room.factor));
   k.now.d = take((room.pieces > 1 ? 2 : 1) * room.d);
   k.dx_sum = reinterpret_cast<float*>(take(room.dx_sum));
+  k.splits = room.splits;
   k.targets = a->targets;
   k.ignore = a->ignore_index;
   k.wide_targets = a->target_type == COMPAMS_I64;

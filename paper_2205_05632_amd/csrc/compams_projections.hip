@@ -15,6 +15,8 @@ struct ProjectionArgs {
   uint32_t weights;       // of their weights' gradients, how many are asked for
   uint32_t of[2];         // which
   uint32_t accumulate;
+  uint32_t splits;        // parts of the projections' outputs whose sums of dx are formed apart,
+  float* sums;            // and these: [split][row][cols]
   uint32_t tall, wide;    // tiles of dx
   uint32_t tall_weight;   // of a weight's gradient, beside those
 };
@@ -24,19 +26,37 @@ struct ProjectionArgs {
 template <typename TL>
 __device__ __forceinline__ void input_tile(const ProjectionArgs& a, uint32_t id, const TileLds& lds) {
   using T = typename TL::T;
+  const uint32_t each = a.tall * a.wide, mine = by_die(id, each * a.splits), split = mine / each;
   uint32_t down, across;
-  tile_at(by_die(id, a.tall * a.wide), a.tall, a.wide, down, across);
+  tile_at(mine - split * each, a.tall, a.wide, down, across);
   const uint32_t m0 = down * TL::kM, n0 = across * TL::kN;
+  const uint32_t share = ((a.hidden + a.splits - 1) / a.splits + 63) / 64 * 64;
+  const uint32_t k0 = min(split * share, a.hidden), k = min(share, a.hidden - k0);
   TL t;
   t.clear();
   t.run([&](uint32_t i, Side& d, Side& w, Side&) {
-    d = side<T, kAlong>(a.d[i].p, a.d[i].ld, a.total, m0, a.hidden);
-    w = side<T, kAcross>(a.weight[i].p, a.weight[i].ld, a.cols, n0, a.hidden);
-  }, a.count, a.hidden, lds);
+    d = side<T, kAlong>(static_cast<const char*>(a.d[i].p) + k0 * sizeof(T), a.d[i].ld, a.total, m0, k);
+    w = side<T, kAcross>(static_cast<const char*>(a.weight[i].p) + static_cast<int64_t>(k0) * a.weight[i].ld, a.weight[i].ld, a.cols, n0, k);
+  }, a.count, k, lds);
   t.rows(lds.a[0], [&](uint32_t m, uint32_t n, const f32x4& v) {
-    if (m0 + m < a.total)
-      store4(static_cast<T*>(a.dx) + static_cast<int64_t>(m0 + m) * a.ld_dx + n0 + n, v, static_cast<int64_t>(a.cols) - n0 - n);
+    const uint32_t r = m0 + m;
+    const int64_t left = static_cast<int64_t>(a.cols) - n0 - n;
+    if (r >= a.total) return;
+    if (a.splits == 1) store4(static_cast<T*>(a.dx) + static_cast<int64_t>(r) * a.ld_dx + n0 + n, v, left);
+    else store4(a.sums + (static_cast<int64_t>(split) * a.total + r) * a.cols + n0 + n, v, left);
   });
+}
+
+// dx from the sums of its splits.
+template <typename T>
+__global__ __launch_bounds__(256) void k_projection_input(ProjectionArgs a) {
+  const uint64_t all = static_cast<uint64_t>(a.total) * a.cols;
+  for (uint64_t i = blockIdx.x * 256u + threadIdx.x; i < all; i += static_cast<uint64_t>(gridDim.x) * 256) {
+    float v = 0.0f;
+    for (uint32_t s = 0; s < a.splits; ++s) v += a.sums[s * all + i];
+    const uint64_t r = i / a.cols;
+    static_cast<T*>(a.dx)[static_cast<int64_t>(r) * a.ld_dx + static_cast<int64_t>(i - r * a.cols)] = static_cast<T>(v);
+  }
 }
 
 // dW of worker i = d_i' x_i: a worker's rows are k, so both operands go across it.  fp32 sums go straight to where the step reads them.
@@ -68,7 +88,7 @@ template <typename X, typename W>
 __global__ __launch_bounds__(X::kThreads, 2) void k_projections(ProjectionArgs a) {
   static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
   COMPAMS_TILE_LDS(X, lds);
-  const uint32_t of_dx = a.dx ? a.tall * a.wide : 0, of_weights = a.tall_weight * a.wide * a.weights * a.n, id = tile_id();
+  const uint32_t of_dx = a.dx ? a.tall * a.wide * a.splits : 0, of_weights = a.tall_weight * a.wide * a.weights * a.n, id = tile_id();
   if (id < of_dx) input_tile<X>(a, id, lds);
   else if (id < of_dx + of_weights) weight_tile<W>(a, id - of_dx, lds);
 }
@@ -80,16 +100,20 @@ void launch(ProjectionArgs& a, hipStream_t stream) {
   a.tall = static_cast<uint32_t>(tiles_of(a.total, X::kM));
   a.tall_weight = static_cast<uint32_t>(tiles_of(a.hidden, X::kM));
   a.wide = static_cast<uint32_t>(tiles_of(a.cols, X::kN));
-  const uint64_t tiles = static_cast<uint64_t>(a.wide) * ((a.dx ? a.tall : 0) + static_cast<uint64_t>(a.tall_weight) * a.weights * a.n);
+  const uint64_t tiles = static_cast<uint64_t>(a.wide) * ((a.dx ? static_cast<uint64_t>(a.tall) * a.splits : 0) + static_cast<uint64_t>(a.tall_weight) * a.weights * a.n);
   if (tiles) hipLaunchKernelGGL((k_projections<X, W>), tile_grid(tiles), dim3(X::kThreads), 0, stream, a);
 }
 template <typename T>
 void launch(ProjectionArgs& a, hipStream_t stream) {
-  switch (tile_size({{a.dx ? a.total : 0, a.cols, 1, static_cast<uint64_t>(a.hidden) * a.count},
+  switch (tile_size({{a.dx ? a.total : 0, a.cols, a.splits, static_cast<uint64_t>(a.hidden) * a.count / a.splits},
                      {a.weights ? a.hidden : 0, a.cols, static_cast<uint64_t>(a.weights) * a.n, a.rows}}, sizeof(T) == 4)) {
     case kTile256: launch<T, 2, 2, 8, 4, 64>(a, stream); break;
     case kTile128: launch<T, 2, 2, 4, 4>(a, stream); break;
     default: launch<T, 2, 2, 2, 2>(a, stream); break;
+  }
+  if (a.dx && a.splits > 1) {
+    const uint64_t blocks = (static_cast<uint64_t>(a.total) * a.cols + 255) / 256;
+    hipLaunchKernelGGL(k_projection_input<T>, dim3(static_cast<uint32_t>(blocks < 16384 ? blocks : 16384)), dim3(256), 0, stream, a);
   }
 }
 
@@ -109,6 +133,13 @@ Operands operands(const compams_projections& a) {
           {a.x, a.ld_x, total, a.cols, size},
           {{a.gate_weight, a.ld_gate_weight, a.hidden, a.cols, size}, {a.up_weight, a.ld_up_weight, a.hidden, a.cols, size}}};
 }
+uint32_t dx_splits(const compams_projections& a) {
+  return splits_of(static_cast<uint64_t>(a.n) * a.rows, a.cols, static_cast<uint64_t>(a.hidden) * (a.dup ? 2 : 1));
+}
+size_t sums_bytes(const compams_projections& a) {
+  const size_t splits = dx_splits(a);
+  return a.dx && splits > 1 ? (splits * a.n * a.rows * a.cols * sizeof(float) + 255) / 256 * 256 : 0;
+}
 size_t projections_bytes(const compams_projections& a) {
   if (a.rows == 0) return 0;
   const Operands o = operands(a);
@@ -117,7 +148,7 @@ size_t projections_bytes(const compams_projections& a) {
     if (o.d[i].p) bytes += o.d[i].packed_bytes();
     if (a.dx && o.weight[i].p) bytes += o.weight[i].packed_bytes();
   }
-  return bytes + (o.x.p && (a.dgate_weight || a.dup_weight) ? o.x.packed_bytes() : 0);
+  return bytes + (o.x.p && (a.dgate_weight || a.dup_weight) ? o.x.packed_bytes() : 0) + sums_bytes(a);
 }
 
 }  // namespace
@@ -169,8 +200,10 @@ int compams_projections_backward(const compams_projections* a, void* hip_stream)
     run_packing(one, size, stream);
     run_packing(two, size, stream);
     k.dx = a->dx;
+    k.sums = reinterpret_cast<float*>(room);
   }
   k.ld_dx = a->ld_dx;
+  k.splits = dx_splits(*a);
   k.count = a->dup ? 2 : 1;
   k.n = static_cast<uint32_t>(a->n);
   k.rows = static_cast<uint32_t>(a->rows);

@@ -426,13 +426,13 @@ struct Work {
   uint64_t rows, cols, many, k;
 };
 inline TileSize tile_size(std::initializer_list<Work> all, bool wide_type) {
-  const auto cost = [&](uint64_t edge, uint64_t across, double full, double alone) {
+  const auto cost = [&](uint64_t edge, uint64_t across, double full, double alone, double apiece) {
     double sum = 0.0, longest = 0.0;
     uint64_t tiles = 0;
     for (const Work& w : all) {
       const uint64_t count = (w.rows + edge - 1) / edge * ((w.cols + across - 1) / across) * w.many;
       if (count == 0 || w.k == 0) continue;
-      const double one = static_cast<double>(edge * across) * static_cast<double>(w.k);
+      const double one = static_cast<double>(edge * across) * static_cast<double>(w.k) + apiece;
       tiles += count;
       sum += static_cast<double>(count) * one;
       longest = one > longest ? one : longest;
@@ -441,11 +441,21 @@ inline TileSize tile_size(std::initializer_list<Work> all, bool wide_type) {
     const double share = tiles ? sum / static_cast<double>(tiles) * static_cast<double>((tiles + 255) / 256) : 0.0;
     return (share / full > longest / alone) ? share / full : longest / alone;
   };
-  const double large = all.size() > 1 ? cost(256, 128, 0.97, wide_type ? 0.9 : 0.6) : cost(256, 256, 1.0, 0.97);
-  const double middle = wide_type ? cost(128, 128, 1.0, 0.9) : cost(128, 128, 0.84, 0.6);
-  const double small = wide_type ? cost(64, 64, 0.97, 0.75) : cost(64, 64, 0.57, 0.28);
+  // (the last: what a tile takes besides its products, some 2 us to load the first step and to store, as far as the others on its
+  // compute unit do not hide it: 180 x 3818 x 29084 bfloat16, sums of 90 terms in 54000 tiles of 64 x 64, 564 us)
+  const double large = all.size() > 1 ? cost(256, 128, 0.97, wide_type ? 0.9 : 0.6, 2.6e6) : cost(256, 256, 1.0, 0.97, 6e6);
+  const double middle = wide_type ? cost(128, 128, 1.0, 0.9, 0.4e6) : cost(128, 128, 0.84, 0.6, 2.6e6);
+  const double small = wide_type ? cost(64, 64, 0.97, 0.75, 0.15e6) : cost(64, 64, 0.57, 0.28, 1e6);
   if (large <= middle && large <= small) return kTile256;
   return middle <= small ? kTile128 : kTile64;
+}
+// Into how many parts the k of a result is cut whose tiles are too few for the card, each part with a thousand terms and more: their sums are
+// joined afterwards.
+inline uint32_t splits_of(uint64_t rows, uint64_t cols, uint64_t k) {
+  const uint64_t tiles = (rows + 63) / 64 * ((cols + 63) / 64);
+  uint64_t splits = tiles ? 1024 / tiles : 1;
+  if (splits > k / 1024) splits = k / 1024;
+  return static_cast<uint32_t>(splits > 16 ? 16 : splits > 1 ? splits : 1);
 }
 inline uint64_t tiles_of(uint64_t count, uint32_t edge) { return (count + edge - 1) / edge; }
 

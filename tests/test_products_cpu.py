@@ -43,7 +43,7 @@ FAKE = 0x1000    # never dereferenced: validation fails first
 
 
 def gated(**kw):
-    a = ops.compams_gated(n=2, rows=3, cols=16, hidden=8, type=ops.F32, activation=0, x=FAKE, ld_x=16, gate_weight=FAKE, ld_gate_weight=16,
+    a = ops.compams_gated(n=2, rows=300, cols=16, hidden=8, type=ops.F32, activation=0, x=FAKE, ld_x=16, gate_weight=FAKE, ld_gate_weight=16,
                           up_weight=FAKE, ld_up_weight=16, m=FAKE, ld_m=8, gate=FAKE, ld_gate=8, up=FAKE, ld_up=8, dm=FAKE, ld_dm=8,
                           dgate=FAKE, ld_dgate=8, dup=FAKE, ld_dup=8)
     for k, v in kw.items():
@@ -60,8 +60,8 @@ BOTH = [(dict(n=0), -1), (dict(n=65536), -1), (dict(rows=-1), -1), (dict(rows=1 
     (dict(cols=0), -1), (dict(cols=(1 << 20) + 1), -1), (dict(x=None), -1), (dict(gate_weight=None), -1), (dict(up_weight=None), -1), (dict(m=None), -1),
     (dict(ld_x=15), -1), (dict(ld_gate_weight=15), -1), (dict(ld_up_weight=1), -1), (dict(ld_m=7), -1), (dict(x=FAKE + 2), -2),
     (dict(gate_weight=FAKE + 1), -2), (dict(up_weight=FAKE + 3), -2), (dict(m=FAKE + 2), -2), (dict(gate_bias=FAKE + 2), -2), (dict(up_bias=FAKE + 1), -2),
-    (dict(x=FAKE + 4), -1), (dict(x=FAKE + 4, workspace=FAKE, workspace_bytes=100), -3), (dict(x=FAKE + 4, workspace=FAKE + 16, workspace_bytes=4096), -2),
-    (dict(cols=15), -1), (dict(ld_up_weight=17), -1), (dict(rows=0), 0),
+    (dict(x=FAKE + 4), -1), (dict(x=FAKE + 4, workspace=FAKE, workspace_bytes=100), -3),
+    (dict(x=FAKE + 4, workspace=FAKE + 16, workspace_bytes=4096), -2), (dict(cols=15), -1), (dict(ld_up_weight=17), -1), (dict(rows=0), 0),
 ])
 def test_gated_forward_refuses(kw, code):
     assert B.lib().compams_gated_forward(gated(**kw), None) == code
@@ -157,6 +157,7 @@ def test_null_and_workspace_sizes():
         assert size(None) == 0
     # nothing is copied where rows start on 16 bytes and have whole pieces of them
     assert L.compams_gated_forward_workspace_size(gated()) == 0
+    assert L.compams_gated_forward_workspace_size(gated(n=1, rows=3, x=FAKE + 4)) == 0     # (nor is it for few rows)
     assert L.compams_gated_forward_workspace_size(gated(x=FAKE + 4)) > 0 and L.compams_gated_forward_workspace_size(gated(ld_gate_weight=17)) > 0
     assert L.compams_projections_workspace_size(projections()) == 0
     assert L.compams_projections_workspace_size(projections(cols=15)) > 0
