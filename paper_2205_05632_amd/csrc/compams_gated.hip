@@ -262,8 +262,9 @@ constexpr uint32_t kTogether = 4;  // rows of a lane
 template <typename T, int ACT, bool BIAS>
 __global__ __launch_bounds__(kThreads) void k_gated_backward(BackwardArgs a) {
   __shared__ float sums[BIAS ? 2 * kThreads * kGroup : 1];
-  const uint32_t tall = kThreads / a.wide;
-  const uint32_t strip = blockIdx.x % a.across, piece = blockIdx.x / a.across;
+  const uint32_t tall = kThreads / a.wide, id = tile_id();
+  const uint32_t strip = id % a.across, piece = id / a.across;
+  if (piece >= a.n * a.parts) return;
   const uint32_t w = piece / a.parts, part = piece - w * a.parts;
   const uint32_t lane = threadIdx.x & (a.wide - 1), down = threadIdx.x / a.wide;
   const uint32_t c = (strip * a.wide + lane) * kGroup;
@@ -352,12 +353,12 @@ __global__ __launch_bounds__(kThreads) void k_gated_bias(BackwardArgs a) {
 }
 
 template <typename T, int ACT>
-void launch_backward(const BackwardArgs& a, uint32_t blocks, hipStream_t stream) {
-  if (a.bias[0] || a.bias[1]) hipLaunchKernelGGL((k_gated_backward<T, ACT, true>), dim3(blocks), dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((k_gated_backward<T, ACT, false>), dim3(blocks), dim3(kThreads), 0, stream, a);
+void launch_backward(const BackwardArgs& a, uint64_t blocks, hipStream_t stream) {
+  if (a.bias[0] || a.bias[1]) hipLaunchKernelGGL((k_gated_backward<T, ACT, true>), tile_grid(blocks), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((k_gated_backward<T, ACT, false>), tile_grid(blocks), dim3(kThreads), 0, stream, a);
 }
 template <typename T>
-void launch_backward(const BackwardArgs& a, int act, uint32_t blocks, hipStream_t stream) {
+void launch_backward(const BackwardArgs& a, int act, uint64_t blocks, hipStream_t stream) {
   switch (act) {
     case COMPAMS_SILU: launch_backward<T, COMPAMS_SILU>(a, blocks, stream); break;
     case COMPAMS_GELU: launch_backward<T, COMPAMS_GELU>(a, blocks, stream); break;
@@ -404,8 +405,8 @@ BackwardCut backward_cut(const compams_gated& a) {
   c.across = static_cast<uint32_t>((groups + c.wide - 1) / c.wide);
   const uint64_t tall = kThreads / c.wide;
   uint64_t rows = tall * 8;  // of a part
-  // (workgroups are 2^23 at most: a grid has room for 2^32 threads)
-  const uint64_t most = (1u << 23) / c.across / static_cast<uint64_t>(a.n) + 1;
+  // (so that the workgroups can be numbered)
+  const uint64_t most = (1u << 30) / c.across / static_cast<uint64_t>(a.n) + 1;
   if ((static_cast<uint64_t>(a.rows) + rows - 1) / rows > most) rows = (static_cast<uint64_t>(a.rows) + most - 1) / most;
   c.part_rows = static_cast<uint32_t>(rows);
   c.parts = static_cast<uint32_t>((static_cast<uint64_t>(a.rows) + rows - 1) / rows);
@@ -506,7 +507,7 @@ int compams_gated_backward(const compams_gated* a, void* hip_stream) {
   k.hidden = static_cast<uint32_t>(a->hidden);
   k.wide = cut.wide; k.across = cut.across; k.parts = cut.parts; k.part_rows = cut.part_rows;
   k.accumulate = static_cast<uint32_t>(a->accumulate);
-  const uint32_t blocks = k.across * k.n * k.parts;
+  const uint64_t blocks = static_cast<uint64_t>(k.across) * k.n * k.parts;
   if (a->type == COMPAMS_F32) launch_backward<float>(k, a->activation, blocks, stream);
   else if (a->type == COMPAMS_F16) launch_backward<half_t>(k, a->activation, blocks, stream);
   else launch_backward<bfloat_t>(k, a->activation, blocks, stream);

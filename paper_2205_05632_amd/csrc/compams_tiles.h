@@ -142,7 +142,7 @@ struct Loader {
         ld = second ? two.ld : one.ld;
       }
       uint32_t at = r * ld + piece[i] * 16;
-      if constexpr (F == kAlong) at = piece[i] * 16 < left ? at : 0xfffffff0u;  // (the entries behind a row's end are another's)
+      if constexpr (F == kAlong) at = piece[i] * 16 < left ? at : 0x80000000u;  // (the entries behind a row's end are another's)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? of_two : of_one, (__attribute__((address_space(3))) void*)(tile + (i * WAVES + wave) * 1024),
                                                16, at, 0, 0, 0);
     }

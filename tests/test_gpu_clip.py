@@ -148,3 +148,22 @@ def test_captured_and_on_another_stream():
         torch.cuda.synchronize()
         for a, b in zip(eager, (rows, norms, factors)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,out_type", [(F32, F32), (BF16, F32), (F16, F16)])
+def test_more_than_the_caches_hold(dtype, out_type):
+    """Gradients of more than 192 MB, in three tensors that start anywhere."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    n, sizes = 2, [27_000_001, 4097, 25_000_000]
+    base = torch.randn((n, sum(sizes) + 3), generator=g, device="cuda").to(dtype)
+    tensors = [base[:, 1 + sum(sizes[:i]):1 + sum(sizes[:i + 1])] for i in range(3)]
+    room = torch.full((n, sum(sizes) + 2), 7.0, dtype=out_type, device="cuda")
+    out = list(room[:, 1:1 + sum(sizes)].split(sizes, 1))
+    _, norms, factors = ops.compams_clip_gradients(tensors, 100.0, n, scale=0.5, out=out)
+    want = base[:, 1:1 + sum(sizes)].double().square().sum(1).sqrt() * 0.5
+    close(norms, want.cpu(), 1.01 * U * want.cpu(), "norms")
+    factor = 0.5 * 100.0 / want
+    close(factors, factor.cpu(), 1.01 * U * factor.cpu(), "factors")
+    got, exact = room[:, 1:1 + sum(sizes)].double(), base[:, 1:1 + sum(sizes)].double() * factor[:, None]
+    assert bool(((got - exact).abs() <= (UNIT[out_type] + 2.1 * U) * exact.abs() + LEAST[out_type]).all())
+    assert bool((room[:, 0] == 7).all()) and bool((room[:, -1] == 7).all())

@@ -423,3 +423,68 @@ def test_captured_calls():
         torch.cuda.synchronize()
         for i, (a, b) in enumerate(zip(eager, outs)):
             assert torch.equal(a, b), (turn, i)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("rows,cols,hidden", [(1, 4096, 64), (5, 1031, 40), (16, 520, 17), (17, 2056, 33), (32, 96, 130), (33, 640, 24), (48, 1000, 16),
+                                              (64, 129, 300), (65, 64, 16)])
+def test_gated_forward_of_few_rows(rows, cols, hidden, dtype):
+    """One token to a few: the form that answers take, up to the number of rows from which on tiles are used."""
+    test_gated_forward(rows, cols, hidden, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,rows,cols,hidden", [(1, 3, 40, 5000), (2, 30, 100, 2303), (1, 100, 72, 1030), (16, 8, 369, 2303)])
+def test_projections_with_long_sums(n, rows, cols, hidden, dtype):
+    """Few tiles of dx, whose sums are formed in parts."""
+    test_projections_backward(n, rows, cols, hidden, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,rows,cols,vocab", [(8, 3, 78, 11718), (1, 1, 40, 5000), (2, 14, 133, 4099)])
+def test_linear_cross_entropy_with_long_sums(n, rows, cols, vocab, dtype):
+    test_linear_cross_entropy(n, rows, cols, vocab, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_linear_cross_entropy_keeps_the_digits_of_every_column(dtype):
+    """Columns of x and of the weight that differ in size by many powers of two: each column's gradients have its own digits.  (A column's
+    largest entry is 2^15 in float16, and an entry of a 2^16th of it still has its eight bits.)"""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    n, rows, cols, vocab = 2, 200, 64, 700
+    size = 2.0 ** torch.linspace(-12, 3, cols, device="cuda").round()
+    if dtype == F16:
+        size = size.clamp(min=2.0 ** -4)
+    x = (torch.randn((n * rows, cols), generator=g, device="cuda") * size).to(dtype)
+    w = (torch.randn((vocab, cols), generator=g, device="cuda") * size.flip(0) * 0.05).to(dtype)
+    t = torch.randint(0, vocab, (n * rows,), generator=g, device="cuda")
+    _, _, dx, dw = ops.compams_linear_cross_entropy(x, w, t, n)
+    d = torch.softmax(x.double() @ w.double().t(), 1)
+    d[torch.arange(n * rows), t] -= 1
+    d /= rows
+    want_x = d @ w.double()
+    want_w = torch.stack([p.t() @ q for p, q in zip(d.split(rows), x.double().split(rows))])
+    # as in the test of ordinary sizes, column by column; logits of size 4.  dx's entries are below 2^-14 in some columns, where float16
+    # rounds to multiples of 2^-24 whatever their size: each is off by up to 2^-25, and a column's 2-norm by sqrt(rows) times that
+    off = 4 * U * 8 * 4 + 200 * U
+    for k in range(cols):
+        denormal = 2.0 ** -25 * math.sqrt(n * rows) / float(want_x[:, k].norm()) if dtype == F16 else 0.0
+        assert relative(dx[:, k], want_x[:, k]) < 2 * UNIT.get(dtype, 0.0) + off + 4 * U * math.sqrt(vocab) + denormal
+        assert relative(dw[:, :, k], want_w[:, :, k]) < off + 4 * U * math.sqrt(rows)
+
+
+def test_calls_on_two_streams():
+    """Two calls under way at once, each with its own workspace, against the same calls one after the other."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    make = lambda r, c, s=1.0: (torch.randn((r, c), generator=g, device="cuda") * s).to(BF16)  # noqa: E731
+    sets = [(make(600, 120), make(3000, 120, 0.2), torch.randint(0, 3000, (600,), generator=g, device="cuda")) for _ in range(2)]
+    one = [ops.compams_linear_cross_entropy(x, w, t, 3) for x, w, t in sets]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in sets], []
+    for _ in range(3):
+        for s, (x, w, t) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                got.append(ops.compams_linear_cross_entropy(x, w, t, 3))
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(out, one[i % 2]))
