@@ -65,8 +65,8 @@ __device__ __forceinline__ double sum_doubles(double v, double* slots, uint32_t 
   return s;
 }
 
-// STREAM: past the caches.  (A template parameter: between two accesses that differ in nothing else the compiler drops the hint.)
-// What is beyond the row's last entry is 0.
+// STREAM: past the caches.  (A template parameter: between two accesses that differ in nothing else the compiler drops the
+// hint.) What is beyond the row's last entry is 0.
 template <bool STREAM, typename F>
 __device__ __forceinline__ void load_chunk(float (&v)[kTurns<F>][kPiece<F>], const F* row, int64_t first, int64_t count) {
   typedef Few<F, kPiece<F>> Load;
@@ -126,7 +126,8 @@ __device__ __forceinline__ void store_chunk(T* row, int64_t first, int64_t count
 template <bool STREAM, typename F>
 __device__ __forceinline__ double squares(const Tensor& t, uint32_t w, uint32_t chunk) {
   float v[kTurns<F>][kPiece<F>];
-  load_chunk<STREAM>(v, static_cast<const F*>(t.from) + static_cast<int64_t>(w) * t.ld_from, static_cast<int64_t>(chunk) * kChunk, t.count);
+  const F* const row = static_cast<const F*>(t.from) + static_cast<int64_t>(w) * t.ld_from;
+  load_chunk<STREAM>(v, row, static_cast<int64_t>(chunk) * kChunk, t.count);
   double s = 0.0;
 #pragma unroll
   for (uint32_t k = 0; k < kTurns<F>; ++k)
@@ -135,8 +136,8 @@ __device__ __forceinline__ double squares(const Tensor& t, uint32_t w, uint32_t 
   return s;
 }
 
-// Sums of squares of a worker's parts.  Bound by memory (712 MB fp32 read and nothing else: 120 us, past the caches 108).  A square of an
-// fp32 number is exact in fp64 up to its last five bits, and no sum of them leaves its range.
+// Sums of squares of a worker's parts.  Bound by memory (712 MB fp32 read and nothing else: 120 us, past the caches 108).  A
+// square of an fp32 number is exact in fp64 up to its last five bits, and no sum of them leaves its range.
 template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_clip_norm(ClipArgs a) {
   __shared__ double slots[kThreads / 64];
@@ -152,7 +153,8 @@ __global__ __launch_bounds__(kThreads) void k_clip_norm(ClipArgs a) {
   if (threadIdx.x == 0) a.partial[static_cast<uint64_t>(w) * a.all + a.before + blockIdx.x] = s;
 }
 
-// A worker's factor, from its parts, added up in the same order by everybody.  It is 0 where zeros are to be written whatever is there.
+// A worker's factor, from its parts, added up in the same order by everybody.  It is 0 where zeros are to be written whatever
+// is there.
 __device__ __forceinline__ float factor_of(const ClipArgs& a, uint32_t w, double* slots, bool tell) {
   double s = 0.0;
   for (uint32_t i = threadIdx.x; i < a.all; i += kThreads) s += a.partial[static_cast<uint64_t>(w) * a.all + i];
@@ -173,8 +175,8 @@ __global__ __launch_bounds__(kThreads) void k_clip_factor(ClipArgs a) {
   if (threadIdx.x == 0) a.known[blockIdx.x] = factor;
 }
 
-// Entries of a row in front of the first one on 32 bytes: a chunk's pieces start there, the entries before are the first chunk's besides.
-// (Not where squares are added up: their order would be the address's.)
+// Entries of a row in front of the first one on 32 bytes: a chunk's pieces start there, the entries before are the first
+// chunk's besides.  (Not where squares are added up: their order would be the address's.)
 template <typename T>
 __device__ __forceinline__ uint32_t before_whole(const T* row, int64_t count) {
   const uint32_t n = (32u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row) & 31u)) % 32u / sizeof(T);
@@ -200,9 +202,9 @@ __device__ __forceinline__ void scaled(const ClipArgs& a, const Tensor& t, uint3
   if (mine) to[threadIdx.x] = static_cast<T>(factor == 0.0f ? 0.0f : one * factor);
 }
 
-// From the last chunk to the first: what was read last for the norms is what the caches still have.  A chunk that is multiplied by one where
-// it stands is left alone.  Bound by memory: 16 x 11.2 million fp32 read and written take 238 us in this shape (16 bytes a lane, four
-// times, past the caches), 260 to 275 in others.
+// From the last chunk to the first: what was read last for the norms is what the caches still have.  A chunk that is
+// multiplied by one where it stands is left alone.  Bound by memory: 16 x 11.2 million fp32 read and written take 238 us in
+// this shape (16 bytes a lane, four times, past the caches), 260 to 275 in others.
 template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_clip_scale(ClipArgs a) {
   __shared__ double slots[kThreads / 64];
@@ -287,7 +289,9 @@ Cut cut_of(const compams_clip& a) {
   return c;
 }
 size_t known_bytes(const compams_clip& a) { return up256(static_cast<size_t>(a.n) * sizeof(float)); }
-size_t bytes_of(const compams_clip& a) { return known_bytes(a) + up256(static_cast<size_t>(a.n) * cut_of(a).parts * sizeof(double)); }
+size_t bytes_of(const compams_clip& a) {
+  return known_bytes(a) + up256(static_cast<size_t>(a.n) * cut_of(a).parts * sizeof(double));
+}
 
 // launch(k) for every kMostTensors tensors.
 template <typename Launch>

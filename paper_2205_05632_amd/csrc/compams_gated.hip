@@ -118,10 +118,11 @@ void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
     default: hipLaunchKernelGGL((k_gated_forward<TL, COMPAMS_SIGMOID>), grid, block, 0, stream, a); break;
   }
 }
-// Few rows: the weights are read once and there is little to do with them.  A workgroup takes sixteen columns of both projections, its
-// wavefronts 128 bytes of k in turn, straight from memory into registers (no row has to be aligned), and their sums are joined in LDS.
-// A lane's two pieces of 16 bytes lie side by side, so that a read's neighbours fill whole lines: k may be taken in any order
-// that is the same for both operands.  Bound by memory (16 x 4096 x 8192 bfloat16, 134 MB: 64 x 64 tiles 50 us).
+// Few rows: the weights are read once and there is little to do with them.  A workgroup takes sixteen columns of both
+// projections, its wavefronts 128 bytes of k in turn, straight from memory into registers (no row has to be aligned), and
+// their sums are joined in LDS.  A lane's two pieces of 16 bytes lie side by side, so that a read's neighbours fill whole
+// lines: k may be taken in any order that is the same for both operands.  Bound by memory (16 x 4096 x 8192 bfloat16, 134 MB:
+// 64 x 64 tiles 50 us).
 template <typename T>
 __device__ __forceinline__ typename Fragment<T>::type load_piece(const char* row, uint32_t at, uint32_t cols) {
   constexpr uint32_t kEach = 16 / sizeof(T);
@@ -338,7 +339,8 @@ __global__ __launch_bounds__(kThreads) void k_gated_bias(BackwardArgs a) {
   for (uint32_t w = blockIdx.y; w < a.n; w += gridDim.y) {
     float s = 0.0f;
     if (column < a.hidden)
-      for (uint32_t p = turn; p < a.parts; p += 8) s += a.partial[((static_cast<uint64_t>(w) * a.parts + p) * 2 + which) * a.hidden + column];
+      for (uint32_t p = turn; p < a.parts; p += 8)
+        s += a.partial[((static_cast<uint64_t>(w) * a.parts + p) * 2 + which) * a.hidden + column];
     sums[turn][l] = s;
     __syncthreads();
     if (turn == 0 && column < a.hidden) {

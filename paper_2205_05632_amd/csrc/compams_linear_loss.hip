@@ -1,17 +1,18 @@
 // Softmax cross-entropy of an output layer, with logits l = weight x that are never stored, and its gradients.
 //
-// The vocabulary is gone over twice.  First every tile of the logits leaves a maximum and a sum of exponentials for each of its
-// rows, from which a row's loss and its softmax's denominator follow.  Then, piece by piece of the vocabulary, the logits are formed
-// again, turned into d = softmax - [target], and multiplied by the piece's weights (dx, whose fp32 sums wait in the workspace
-// from piece to piece) and by x (dweight, of which a piece holds whole rows).  Five products of the logits' size instead of three, more
-// for the digits of d, and no matrix of rows x vocabulary.
+// The vocabulary is gone over twice.  First every tile of the logits leaves a maximum and a sum of exponentials for each of
+// its rows, from which a row's loss and its softmax's denominator follow.  Then, piece by piece of the vocabulary, the logits
+// are formed again, turned into d = softmax - [target], and multiplied by the piece's weights (dx, whose fp32 sums wait in the
+// workspace from piece to piece) and by x (dweight, of which a piece holds whole rows).  Five products of the logits' size
+// instead of three, more for the digits of d, and no matrix of rows x vocabulary.
 //
-// d times 2^14 is held in float16 where the operands have 16 bits, in two parts: the second is the rounded rest of the first, so that
-// both together are off by 2^-23 of an entry or 2^-39 of the largest possible one.  dweight is fp32 and takes both; dx, which is rounded
-// to 16 bits, takes the first alone, one more rounding of half a step of float16.  (In bfloat16 three parts would be needed, and
-// half as many products again: 8192 x 50257 x 768 4.9 ms.)  bfloat16 operands of these two products are therefore turned into
-// float16, each column times the power of two that brings its largest entry just below 2^15, and the results' columns are scaled
-// back: what 2^-39 of the largest entry of its own column does not reach is lost, as it is next to it in an fp32 sum.
+// d times 2^14 is held in float16 where the operands have 16 bits, in two parts: the second is the rounded rest of the first,
+// so that both together are off by 2^-23 of an entry or 2^-39 of the largest possible one. dweight is fp32 and takes both; dx,
+// which is rounded to 16 bits, takes the first alone, one more rounding of half a step of float16.  (In bfloat16 three parts
+// would be needed, and half as many products again: 8192 x 50257 x 768 4.9 ms.) bfloat16 operands of these two products are
+// therefore turned into float16, each column times the power of two that brings its largest entry just below 2^15, and the
+// results' columns are scaled back: what 2^-39 of the largest entry of its own column does not reach is lost, as it is next to
+// it in an fp32 sum.
 #include "compams_tiles.h"
 
 namespace compams {
@@ -86,8 +87,8 @@ __device__ __forceinline__ int shift_of(uint32_t top) {
   return exponent == 128 ? 0 : min(14 - exponent, 126);   // (infinities and NaNs stay what they are)
 }
 
-// A workgroup's share of a matrix that is gone over by columns: `wide` lanes side by side with eight columns each, for `each` rows of
-// the matrix a lane.  Matrices are the workers' x, and the weight as number n.
+// A workgroup's share of a matrix that is gone over by columns: `wide` lanes side by side with eight columns each, for `each`
+// rows of the matrix a lane.  Matrices are the workers' x, and the weight as number n.
 struct ColumnsArgs {
   const void *x, *weight;
   int64_t ld_x, ld_weight;        // entries
@@ -144,8 +145,8 @@ __global__ __launch_bounds__(kThreads) void k_linear_loss_tops(LossArgs a, Colum
   }
 }
 
-// x with zeros in the rows that nothing is learnt from - whatever they hold, they add nothing to a weight's gradient (a NaN there would,
-// times the zero that d is) - and, of bfloat16, both matrices in float16 with their columns scaled.
+// x with zeros in the rows that nothing is learnt from - whatever they hold, they add nothing to a weight's gradient (a NaN
+// there would, times the zero that d is) - and, of bfloat16, both matrices in float16 with their columns scaled.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_linear_loss_hold(LossArgs a, ColumnsArgs c) {
   typedef typename Group<Held<T>>::type Out;
@@ -206,11 +207,12 @@ struct Max {
 };
 // e^z by the processor's 2^x.
 __device__ __forceinline__ float exp_of(float z) { return __builtin_amdgcn_exp2f(z * 1.44269504088896341f); }
-// What a row's logits are compared with: their maximum, or 0 where that is minus infinity (e^(l - top) is 0 then, and not a NaN).
+// What a row's logits are compared with: their maximum, or 0 where that is minus infinity (e^(l - top) is 0 then, and not a
+// NaN).
 __device__ __forceinline__ float base_of(float top) { return top == -INFINITY ? 0.0f : top; }
 
-// First pass.  A wavefront has 64 columns of its rows in every size of tile, so that a row's sums are added up in the same order
-// beside however many others.
+// First pass.  A wavefront has 64 columns of its rows in every size of tile, so that a row's sums are added up in the same
+// order beside however many others.
 constexpr uint32_t kSpan = 64;
 template <typename TL>
 __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) {
@@ -291,7 +293,8 @@ __global__ __launch_bounds__(16 * kJoinLanes) void k_linear_loss_join(LossArgs a
   __shared__ float2 part[kJoinLanes][17];
   const uint32_t l = threadIdx.x % 16, turn = threadIdx.x / 16, spans = (a.vocab - 1) / kSpan + 1;
   if (a.tops)  // (cleared for the kernels that follow)
-    for (uint64_t i = blockIdx.x * blockDim.x + threadIdx.x; i < static_cast<uint64_t>(a.n + 1) * a.cols; i += static_cast<uint64_t>(gridDim.x) * blockDim.x)
+    for (uint64_t i = blockIdx.x * blockDim.x + threadIdx.x; i < static_cast<uint64_t>(a.n + 1) * a.cols;
+         i += static_cast<uint64_t>(gridDim.x) * blockDim.x)
       a.tops[i] = 0;
   for (uint64_t first = blockIdx.x * 16u; first < a.total; first += static_cast<uint64_t>(gridDim.x) * 16) {
     const uint64_t r = first + l;
@@ -324,7 +327,7 @@ __global__ __launch_bounds__(16 * kJoinLanes) void k_linear_loss_join(LossArgs a
       for (uint32_t k = 1; k < 16; ++k) most = fmaxf(most, part[k][l].x);
       float sum = 0.0f;  // (a row without a finite logit: e^(NaN))
 #pragma unroll
-      for (uint32_t k = 0; k < 16; ++k) sum += part[k][l].y * (part[k][l].x == most && most != -INFINITY ? 1.0f : exp_of(part[k][l].x - most));
+      for (uint32_t k = 0; k < 16; ++k) sum += part[k][l].y * exp_of(part[k][l].x - most);
       const int64_t t = target_of(a, static_cast<uint32_t>(r));
       const bool learnt = t != a.ignore, inside = t >= 0 && t < a.vocab;
       const float loss = inside ? (most - a.of_target[r]) + logf(sum) : NAN;
@@ -360,8 +363,8 @@ __global__ __launch_bounds__(1024) void k_linear_loss_mean(LossArgs a) {
   }
 }
 
-// Second pass, a tile of the next piece's d.  Entries behind the vocabulary's last are written too, as 0: they are read as a part of the
-// last 16 bytes.
+// Second pass, a tile of the next piece's d.  Entries behind the vocabulary's last are written too, as 0: they are read as a
+// part of the last 16 bytes.
 template <typename TL>
 __device__ __forceinline__ void gradient_tile(const LossArgs& a, uint32_t id, const TileLds& lds) {
   using T = typename TL::T;
@@ -447,8 +450,8 @@ __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, const
     });
   t.run([&](uint32_t, Side& d, Side& w, Side&) {
     d = side<typename TL::T, kAlong>(a.now.d + k0 * sizeof(typename TL::T), a.ld_d, a.total, m0, width);
-    w = side<typename TL::T, kAcross>(static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.now.first + k0) * a.weight_held.ld,
-                                      a.weight_held.ld, a.cols, n0, width);
+    const char* const rows = static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.now.first + k0) * a.weight_held.ld;
+    w = side<typename TL::T, kAcross>(rows, a.weight_held.ld, a.cols, n0, width);
   }, 1, width, lds);
   const bool end = a.end && a.splits == 1;
   const f32x4 of_column = end ? scales<T>(a, a.n, n0 + TL::row_n()) : f32x4{};
@@ -472,7 +475,8 @@ __device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, cons
   const int64_t row = static_cast<int64_t>(w) * a.rows;
   t.run([&](uint32_t i, Side& d, Side& x, Side&) {
     const char* const part = a.now.d + (kParts<T> - 1 - i) * a.part_bytes;
-    d = side<typename TL::T, kAcross>(part + row * a.ld_d, a.ld_d, static_cast<uint32_t>(a.ld_d / sizeof(typename TL::T)), m0, a.rows);
+    const uint32_t columns = static_cast<uint32_t>(a.ld_d / sizeof(typename TL::T));
+    d = side<typename TL::T, kAcross>(part + row * a.ld_d, a.ld_d, columns, m0, a.rows);
     x = side<typename TL::T, kAcross>(static_cast<const char*>(a.x_held.p) + row * a.x_held.ld, a.x_held.ld, a.cols, n0, a.rows);
   }, kParts<T>, a.rows, lds);  // (what d has behind `width` meets no sum that is stored)
   const f32x4 f = scales<T>(a, w, n0 + TL::row_n());
@@ -480,21 +484,23 @@ __device__ __forceinline__ void weight_tile(const LossArgs& a, uint32_t id, cons
   float* const to = a.dweight + w * a.stride_dweight + static_cast<int64_t>(a.now.first) * a.ld_dweight;
   t.rows(lds.a[0], [&](uint32_t m, uint32_t n, const f32x4& v) {
     if (m0 + m < a.now.width)
-      add4(to + static_cast<int64_t>(m0 + m) * a.ld_dweight + n0 + n, v * f * factor, static_cast<int64_t>(a.cols) - n0 - n, a.accumulate);
+      add4(to + static_cast<int64_t>(m0 + m) * a.ld_dweight + n0 + n, v * f * factor, static_cast<int64_t>(a.cols) - n0 - n,
+           a.accumulate);
   });
 }
 
-// A piece's products, and the d of the piece after it, in one launch: dx has few tiles of many steps (the piece's columns are its k),
-// dweight many of few, d's tiles store more than they multiply, and together they fill the card.  (8192 x 50257 x 768 bfloat16, in one
-// launch each 96 tiles of dx and 384 of dweight left a third of it idle; d apart 165 us, the products 375 for 8448 columns.)
-// dx's tiles come first, the shortest last.
+// A piece's products, and the d of the piece after it, in one launch: dx has few tiles of many steps (the piece's columns are
+// its k), dweight many of few, d's tiles store more than they multiply, and together they fill the card.  (8192 x 50257 x 768
+// bfloat16, in one launch each 96 tiles of dx and 384 of dweight left a third of it idle; d apart 165 us, the products 375 for
+// 8448 columns.) dx's tiles come first, the shortest last.
 template <typename D, typename X, typename W, typename T>
 __global__ __launch_bounds__(X::kThreads, X::STEP == 64 && sizeof(T) == 2 ? 3 : 2) void k_linear_loss_piece(LossArgs a) {
   static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
   static_assert(X::kBytesA == D::kBytesA && X::kBytesB == D::kBytesB && X::kThreads == D::kThreads, "one kind of tile");
   COMPAMS_TILE_LDS(X, lds);
   const bool any = a.now.width != 0;
-  const uint32_t of_dx = any && a.dx ? a.tall * a.wide * a.splits : 0, of_weight = any && a.dweight ? a.tall_weight * a.wide * a.n : 0;
+  const uint32_t of_dx = any && a.dx ? a.tall * a.wide * a.splits : 0;
+  const uint32_t of_weight = any && a.dweight ? a.tall_weight * a.wide * a.n : 0;
   const uint32_t of_d = a.next.width ? a.tall * a.wide_next : 0;
   uint32_t id = tile_id();
   if (id < of_dx) return input_tile<X, T>(a, id, lds);
@@ -544,7 +550,8 @@ void launch_piece(LossArgs& a, hipStream_t stream) {
   a.wide_next = static_cast<uint32_t>(tiles_of(a.next.width, X::kN));
   uint64_t tiles = static_cast<uint64_t>(a.tall) * a.wide_next;
   if (a.now.width)
-    tiles += static_cast<uint64_t>(a.wide) * ((a.dx ? static_cast<uint64_t>(a.tall) * a.splits : 0) + (a.dweight ? static_cast<uint64_t>(a.tall_weight) * a.n : 0));
+    tiles += static_cast<uint64_t>(a.wide) * ((a.dx ? static_cast<uint64_t>(a.tall) * a.splits : 0) +
+                                              (a.dweight ? static_cast<uint64_t>(a.tall_weight) * a.n : 0));
   if (tiles) hipLaunchKernelGGL((k_linear_loss_piece<D, X, W, T>), tile_grid(tiles), dim3(X::kThreads), 0, stream, a);
 }
 template <typename T>
@@ -561,19 +568,21 @@ bool linear_loss_valid(const compams_linear_loss* a) {
   return a && rows_valid(a->n, a->rows, a->cols) && a->cols <= kMostEntries && a->vocab >= 1 &&
          a->vocab < (static_cast<int64_t>(1) << 31) && float_type(a->type) &&
          (a->target_type == COMPAMS_I32 || a->target_type == COMPAMS_I64) && (a->accumulate == 0 || a->accumulate == 1) &&
-         tiles_fit(a->n * a->rows, a->vocab, 1) && tiles_fit(a->n * a->rows, a->cols, 1) && tiles_fit(a->vocab, a->cols, a->n);
+         tiles_fit(a->n * a->rows, a->vocab, 1) && tiles_fit(a->n * a->rows, a->cols, 16) && tiles_fit(a->vocab, a->cols, a->n);
 }
 struct Room {
-  size_t x = 0, weight = 0, x_held = 0, weight_held = 0, tops = 0, partial = 0, of_target = 0, stat = 0, losses = 0, factor = 0, d = 0,
-         dx_sum = 0;
+  size_t x = 0, weight = 0, x_held = 0, weight_held = 0, tops = 0, partial = 0, of_target = 0, stat = 0, losses = 0, factor = 0;
+  size_t d = 0, dx_sum = 0;
   uint32_t piece = 0, pieces = 0, splits = 1;
-  size_t all() const { return x + weight + x_held + weight_held + tops + partial + of_target + stat + losses + factor + (pieces > 1 ? 2 : 1) * d + dx_sum; }
+  size_t all() const {
+    return x + weight + x_held + weight_held + tops + partial + of_target + stat + losses + factor + (pieces > 1 ? 2 : 1) * d + dx_sum;
+  }
 };
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 inline uint32_t parts_of(int32_t type) { return type == COMPAMS_F32 ? kParts<float> : kParts<half_t>; }
 
-// A piece's d: wide enough for the products that read it to fill the card, and for dx's sums, which are read and written with every
-// piece, to be little beside it.
+// A piece's d: wide enough for the products that read it to fill the card, and for dx's sums, which are read and written with
+// every piece, to be little beside it.
 constexpr size_t kPieceBytes = 96u << 20;  // (two of them)
 constexpr uint32_t kLeastPiece = 1024;
 
@@ -610,7 +619,7 @@ Room room_of(const compams_linear_loss& a) {
   r.piece = static_cast<uint32_t>((tiles_of(a.vocab, r.pieces) + 255) / 256 * 256);
   r.pieces = static_cast<uint32_t>(tiles_of(a.vocab, r.piece));
   r.d = up256(column * r.piece);  // (of one)
-  if (a.dx) r.splits = splits_of(total, a.cols, a.vocab < r.piece ? a.vocab : r.piece);
+  if (a.dx) r.splits = splits_of(total, a.cols, a.vocab < r.piece ? a.vocab : r.piece, size == 4);
   if (a.dx && (r.pieces > 1 || r.splits > 1)) r.dx_sum = up256(r.splits * total * ((a.cols + 3) / 4 * 4) * sizeof(float));
   return r;
 }
@@ -630,8 +639,9 @@ void run_hold(const LossArgs& k, const compams_linear_loss& a, hipStream_t strea
   if (kScaled<T> && a.dx) c.parts_weight = static_cast<uint32_t>(tiles_of(k.vocab, static_cast<uint32_t>(each)));
   const uint64_t blocks = (static_cast<uint64_t>(c.parts_x) * k.n + c.parts_weight) * c.across;
   if (blocks == 0) return;
-  if constexpr (kScaled<T>) hipLaunchKernelGGL(k_linear_loss_tops, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, stream, k, c);
-  hipLaunchKernelGGL(k_linear_loss_hold<T>, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, stream, k, c);
+  const dim3 grid(static_cast<uint32_t>(blocks));
+  if constexpr (kScaled<T>) hipLaunchKernelGGL(k_linear_loss_tops, grid, dim3(kThreads), 0, stream, k, c);
+  hipLaunchKernelGGL(k_linear_loss_hold<T>, grid, dim3(kThreads), 0, stream, k, c);
 }
 
 template <typename T>
@@ -678,7 +688,8 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
   }
   if (a.dx && k.splits > 1) {
     const uint64_t blocks = (static_cast<uint64_t>(k.total) * ((k.cols + 3) / 4) + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL(k_linear_loss_input<T>, dim3(static_cast<uint32_t>(blocks < 16384 ? blocks : 16384)), dim3(kThreads), 0, stream, k);
+    const dim3 grid(static_cast<uint32_t>(blocks < 16384 ? blocks : 16384));
+    hipLaunchKernelGGL(k_linear_loss_input<T>, grid, dim3(kThreads), 0, stream, k);
   }
 }
 

@@ -21,8 +21,8 @@ struct ProjectionArgs {
   uint32_t tall_weight;   // of a weight's gradient, beside those
 };
 
-// dx = dgate Wg + dup Wu: k goes through the one projection's outputs and then the other's, so that dx is rounded once.  The weights' rows go
-// across k: they are read as they lie and transposed on the way out of LDS.
+// dx = dgate Wg + dup Wu: k goes through the one projection's outputs and then the other's, so that dx is rounded once.  The
+// weights' rows go across k: they are read as they lie and transposed on the way out of LDS.
 template <typename TL>
 __device__ __forceinline__ void input_tile(const ProjectionArgs& a, uint32_t id, const TileLds& lds) {
   using T = typename TL::T;
@@ -36,7 +36,8 @@ __device__ __forceinline__ void input_tile(const ProjectionArgs& a, uint32_t id,
   t.clear();
   t.run([&](uint32_t i, Side& d, Side& w, Side&) {
     d = side<T, kAlong>(static_cast<const char*>(a.d[i].p) + k0 * sizeof(T), a.d[i].ld, a.total, m0, k);
-    w = side<T, kAcross>(static_cast<const char*>(a.weight[i].p) + static_cast<int64_t>(k0) * a.weight[i].ld, a.weight[i].ld, a.cols, n0, k);
+    w = side<T, kAcross>(static_cast<const char*>(a.weight[i].p) + static_cast<int64_t>(k0) * a.weight[i].ld, a.weight[i].ld,
+                         a.cols, n0, k);
   }, a.count, k, lds);
   t.rows(lds.a[0], [&](uint32_t m, uint32_t n, const f32x4& v) {
     const uint32_t r = m0 + m;
@@ -59,7 +60,8 @@ __global__ __launch_bounds__(256) void k_projection_input(ProjectionArgs a) {
   }
 }
 
-// dW of worker i = d_i' x_i: a worker's rows are k, so both operands go across it.  fp32 sums go straight to where the step reads them.
+// dW of worker i = d_i' x_i: a worker's rows are k, so both operands go across it. fp32 sums go straight to where the step
+// reads them.
 template <typename TL>
 __device__ __forceinline__ void weight_tile(const ProjectionArgs& a, uint32_t id, const TileLds& lds) {
   using T = typename TL::T;
@@ -82,13 +84,14 @@ __device__ __forceinline__ void weight_tile(const ProjectionArgs& a, uint32_t id
   });
 }
 
-// All of it in one launch: dx has few tiles with many terms to a sum, the weights' gradients many with few, and together they fill the card
-// (8 x 1024 x 768 x 2048 bfloat16: 64.5 + 66.7 us apart).  dx's tiles come first.
+// All of it in one launch: dx has few tiles with many terms to a sum, the weights' gradients many with few, and together they
+// fill the card (8 x 1024 x 768 x 2048 bfloat16: 64.5 + 66.7 us apart). dx's tiles come first.
 template <typename X, typename W>
 __global__ __launch_bounds__(X::kThreads, 2) void k_projections(ProjectionArgs a) {
   static_assert(X::kBytesA == W::kBytesA && X::kBytesB == W::kBytesB && X::kThreads == W::kThreads, "one kind of tile");
   COMPAMS_TILE_LDS(X, lds);
-  const uint32_t of_dx = a.dx ? a.tall * a.wide * a.splits : 0, of_weights = a.tall_weight * a.wide * a.weights * a.n, id = tile_id();
+  const uint32_t of_dx = a.dx ? a.tall * a.wide * a.splits : 0, of_weights = a.tall_weight * a.wide * a.weights * a.n;
+  const uint32_t id = tile_id();
   if (id < of_dx) input_tile<X>(a, id, lds);
   else if (id < of_dx + of_weights) weight_tile<W>(a, id - of_dx, lds);
 }
@@ -100,7 +103,8 @@ void launch(ProjectionArgs& a, hipStream_t stream) {
   a.tall = static_cast<uint32_t>(tiles_of(a.total, X::kM));
   a.tall_weight = static_cast<uint32_t>(tiles_of(a.hidden, X::kM));
   a.wide = static_cast<uint32_t>(tiles_of(a.cols, X::kN));
-  const uint64_t tiles = static_cast<uint64_t>(a.wide) * ((a.dx ? static_cast<uint64_t>(a.tall) * a.splits : 0) + static_cast<uint64_t>(a.tall_weight) * a.weights * a.n);
+  const uint64_t tiles = static_cast<uint64_t>(a.wide) * ((a.dx ? static_cast<uint64_t>(a.tall) * a.splits : 0) +
+                                                          static_cast<uint64_t>(a.tall_weight) * a.weights * a.n);
   if (tiles) hipLaunchKernelGGL((k_projections<X, W>), tile_grid(tiles), dim3(X::kThreads), 0, stream, a);
 }
 template <typename T>
@@ -113,7 +117,8 @@ void launch(ProjectionArgs& a, hipStream_t stream) {
   }
   if (a.dx && a.splits > 1) {
     const uint64_t blocks = (static_cast<uint64_t>(a.total) * a.cols + 255) / 256;
-    hipLaunchKernelGGL(k_projection_input<T>, dim3(static_cast<uint32_t>(blocks < 16384 ? blocks : 16384)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(k_projection_input<T>, dim3(static_cast<uint32_t>(blocks < 16384 ? blocks : 16384)), dim3(256), 0, stream,
+                       a);
   }
 }
 
@@ -121,7 +126,8 @@ void launch(ProjectionArgs& a, hipStream_t stream) {
 bool projections_valid(const compams_projections* a) {
   return a && rows_valid(a->n, a->rows, a->hidden) && a->hidden <= kMostEntries && a->cols >= 1 && a->cols <= kMostEntries &&
          float_type(a->type) && (a->dup || (!a->up_weight && !a->dup_weight) || a->rows == 0) &&
-         (a->accumulate == 0 || a->accumulate == 1) && tiles_fit(a->n * a->rows, a->cols, 1) && tiles_fit(a->hidden, a->cols, 2 * a->n);
+         (a->accumulate == 0 || a->accumulate == 1) && tiles_fit(a->n * a->rows, a->cols, 16) &&
+         tiles_fit(a->hidden, a->cols, 2 * a->n);
 }
 struct Operands {
   Matrix d[2], x, weight[2];
@@ -134,7 +140,8 @@ Operands operands(const compams_projections& a) {
           {{a.gate_weight, a.ld_gate_weight, a.hidden, a.cols, size}, {a.up_weight, a.ld_up_weight, a.hidden, a.cols, size}}};
 }
 uint32_t dx_splits(const compams_projections& a) {
-  return splits_of(static_cast<uint64_t>(a.n) * a.rows, a.cols, static_cast<uint64_t>(a.hidden) * (a.dup ? 2 : 1));
+  return splits_of(static_cast<uint64_t>(a.n) * a.rows, a.cols, static_cast<uint64_t>(a.hidden) * (a.dup ? 2 : 1),
+                   a.type == COMPAMS_F32);
 }
 size_t sums_bytes(const compams_projections& a) {
   const size_t splits = dx_splits(a);

@@ -1,9 +1,10 @@
-// Products of matrices on the matrix cores, one tile of the result to a workgroup: D(m, n) = sum over k of A(m, k) B(n, k), with
-// fp32 sums.  The kernels that use it differ in what they do with the tile.  (wave64 only)
+// Products of matrices on the matrix cores, one tile of the result to a workgroup: D(m, n) = sum over k of A(m, k) B(n, k),
+// with fp32 sums.  The kernels that use it differ in what they do with the tile.  (wave64 only)
 //
-// A step takes 128 bytes of k, 64 entries of the 16-bit types, 32 of fp32 (or half as many).  Both operands' tiles of a step go from memory into
-// LDS without passing through registers, 16 bytes a lane, while the step before is multiplied (two buffers, one barrier a step).
-// Reads beyond a matrix give zeros (the buffer descriptors' own bounds), so no length has to be a multiple of anything but 16 bytes.
+// A step takes 128 bytes of k, 64 entries of the 16-bit types, 32 of fp32 (or half as many).  Both operands' tiles of a step
+// go from memory into LDS without passing through registers, 16 bytes a lane, while the step before is multiplied (two
+// buffers, one barrier a step).  Reads beyond a matrix give zeros (the buffer descriptors' own bounds), so no length has to be
+// a multiple of anything but 16 bytes.
 #pragma once
 
 #include <initializer_list>
@@ -46,9 +47,9 @@ __device__ __forceinline__ void multiply(f32x4& d, Fragment<float>::type a, Frag
 // kAlong: EXTENT rows of STEP bytes.  The 16 bytes c of row r are kept at place c ^ (r % 8) of the row: the sixteen rows that a
 // fragment is read from then begin in eight different places of the 128 bytes that LDS gives at once.
 //
-// kAcross: a row of EXTENT entries for every k of the step.  16-bit types are read with the transposing read: sixteen lanes read
-// four k of sixteen columns (32 bytes a row), and get four k of one column each.  The pairs of 16 bytes are moved by k so that
-// the rows of a read do not meet.  fp32 is read entry by entry, 64 bytes a row.
+// kAcross: a row of EXTENT entries for every k of the step. 16-bit types are read with the transposing read: sixteen lanes
+// read four k of sixteen columns (32 bytes a row), and get four k of one column each.  The pairs of 16 bytes are moved by k so
+// that the rows of a read do not meet. fp32 is read entry by entry, 64 bytes a row.
 template <typename T, uint32_t EXTENT>
 __device__ __forceinline__ uint32_t moved(uint32_t k) {
   if constexpr (sizeof(T) == 2) return 2 * ((k & 3u) | (EXTENT >= 128 ? (k >> 1) & 4u : 0u));
@@ -76,7 +77,8 @@ struct Place {
     typename Fragment<T>::type v;
     if constexpr (F == kAlong) {
       const uint32_t row = first + l, piece = (sub * 4 + g) ^ turned(row);
-      v = *reinterpret_cast<const __attribute__((address_space(3))) typename Fragment<T>::type*>(tile + row * kRowBytes + piece * 16);
+      v = *reinterpret_cast<const __attribute__((address_space(3))) typename Fragment<T>::type*>(tile + row * kRowBytes +
+                                                                                                 piece * 16);
     } else if constexpr (sizeof(T) == 2) {
       const uint32_t k = sub * 32 + g * 8 + (l >> 2);
       const uint32_t piece = first / 8 + (l >> 1 & 1u), in = (l & 1u) * 8;
@@ -110,7 +112,8 @@ template <typename T, Form F>
 __device__ __forceinline__ Side side(const void* p, int64_t ld, uint32_t total, uint32_t first, uint32_t k) {
   const char* const at = static_cast<const char*>(p);
   if (F == kAlong) return {at + static_cast<int64_t>(first) * ld, static_cast<uint32_t>(ld), total - first, k};
-  return {at + static_cast<int64_t>(first) * sizeof(T), static_cast<uint32_t>(ld), (total - first) * static_cast<uint32_t>(sizeof(T)), k};
+  return {at + static_cast<int64_t>(first) * sizeof(T), static_cast<uint32_t>(ld),
+          (total - first) * static_cast<uint32_t>(sizeof(T)), k};
 }
 
 template <typename T, Form F, uint32_t EXTENT, uint32_t WAVES, uint32_t STEP>
@@ -143,12 +146,12 @@ struct Loader {
       }
       uint32_t at = r * ld + piece[i] * 16;
       if constexpr (F == kAlong) at = piece[i] * 16 < left ? at : 0x80000000u;  // (the entries behind a row's end are another's)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? of_two : of_one, (__attribute__((address_space(3))) void*)(tile + (i * WAVES + wave) * 1024),
-                                               16, at, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          second ? of_two : of_one, (__attribute__((address_space(3))) void*)(tile + (i * WAVES + wave) * 1024), 16, at, 0, 0, 0);
     }
   }
-  // Up to the end of the last row's last 16 bytes, which belong to the row: an entry of 16 bits that ends it in the middle of a word
-  // would be cut off with the word.
+  // Up to the end of the last row's last 16 bytes, which belong to the row: an entry of 16 bits that ends it in the middle of
+  // a word would be cut off with the word.
   __device__ static __forceinline__ uint32_t whole(uint32_t bytes) { return (bytes + 15) / 16 * 16; }
   __device__ static __forceinline__ __amdgpu_buffer_rsrc_t bounds(const Side& s, uint32_t k0, bool two) {
     const char* p;
@@ -172,7 +175,8 @@ struct TileLds {
 };
 
 // A workgroup of WM x WN wavefronts, each with FM x FN tiles of 16 x 16.
-template <typename T_, Form FA_, Form FB_, uint32_t WM_, uint32_t WN_, uint32_t FM_, uint32_t FN_, bool TWO_ = false, uint32_t STEP_ = 128>
+template <typename T_, Form FA_, Form FB_, uint32_t WM_, uint32_t WN_, uint32_t FM_, uint32_t FN_, bool TWO_ = false,
+          uint32_t STEP_ = 128>
 struct Tiles {
   static constexpr uint32_t STEP = STEP_, kStep = STEP_ / sizeof(T_);  // of k, in bytes and in entries
   using T = T_;
@@ -256,8 +260,8 @@ struct Tiles {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
-  // visit(row, column, four neighbouring entries) of the tile, as the matrix cores leave them: 64 bytes of each of sixteen rows at a
-  // time.
+  // visit(row, column, four neighbouring entries) of the tile, as the matrix cores leave them: 64 bytes of each of sixteen
+  // rows at a time.
   template <typename Visit>
   __device__ __forceinline__ void each(Visit visit) {
     const uint32_t m = first_m() + lane_m(), n = first_n() + lane_n();
@@ -267,27 +271,30 @@ struct Tiles {
       for (uint32_t j = 0; j < FN; ++j) visit(m + i * 16, n + j * 16, sum[i][j]);
   }
 
-  // The same by way of LDS, a row's entries in neighbouring lanes, for what is stored: a wavefront's part of a row goes to memory at
-  // once (8192 x 8192 fp32 stored and nothing else: 54 us, in pieces of 64 bytes 69).  Each wavefront has room for sixteen of its
-  // rows in `lds`; piece c of row r is at place c ^ r.  of(i, j): what is to be stored of the i, j-th tile of 16 x 16, PIECES / 4
-  // of them side by side.
+  // The same by way of LDS, a row's entries in neighbouring lanes, for what is stored: a wavefront's part of a row goes to
+  // memory at once (8192 x 8192 fp32 stored and nothing else: 54 us, in pieces of 64 bytes 69).  Each wavefront has room for
+  // sixteen of its rows in `lds`; piece c of row r is at place c ^ r. of(i, j): what is to be stored of the i, j-th tile of 16
+  // x 16, PIECES / 4 of them side by side.
   template <uint32_t PIECES, typename Of, typename Visit>
   __device__ __forceinline__ void rows_of(lds_char* lds, Of of, Visit visit) {
     static_assert(16 * PIECES * 16 * kWaves <= kBytesA, "sixteen rows of every wavefront");
     const uint32_t lane = threadIdx.x & 63u, m = lane_m();
     lds_char* const mine = lds + wave() * (16 * PIECES * 16);
     const uint32_t c = lane % PIECES;
+    const auto at = [](lds_char* from, uint32_t row, uint32_t piece) {
+      return reinterpret_cast<__attribute__((address_space(3))) f32x4*>(from + (row * PIECES + (piece ^ (row & (PIECES - 1)))) * 16);
+    };
 #pragma unroll
     for (uint32_t i = 0; i < FM; ++i) {
       settled();
 #pragma unroll
       for (uint32_t j = 0; j < PIECES / 4; ++j)
-        *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(mine + (m * PIECES + ((j * 4 + lane / 16) ^ (m & (PIECES - 1)))) * 16) = of(i, j);
+        *at(mine, m, j * 4 + lane / 16) = of(i, j);
       settled();
 #pragma unroll
       for (uint32_t q = 0; q < 16 * PIECES / 64; ++q) {
         const uint32_t r = q * (64 / PIECES) + lane / PIECES;
-        const f32x4 v = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>(mine + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
+        const f32x4 v = *at(mine, r, c);
         visit(first_m() + i * 16 + r, c * 4, v);
       }
     }
@@ -296,7 +303,8 @@ struct Tiles {
   __device__ __forceinline__ void rows(lds_char* lds, Visit visit) {
     __syncthreads();  // (others may still read what they multiply)
     const uint32_t n = first_n();
-    rows_of<FN * 4>(lds, [&](uint32_t i, uint32_t j) { return sum[i][j]; }, [&](uint32_t r, uint32_t c, const f32x4& v) { visit(r, n + c, v); });
+    rows_of<FN * 4>(lds, [&](uint32_t i, uint32_t j) { return sum[i][j]; },
+                    [&](uint32_t r, uint32_t c, const f32x4& v) { visit(r, n + c, v); });
   }
   // The first of a lane's columns there, which are the same in every row.
   __device__ static __forceinline__ uint32_t row_n() { return first_n() + (threadIdx.x & 63u) % (FN * 4) * 4; }
@@ -320,8 +328,8 @@ __device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total) {
   return die * each + min(die, more) + in;
 }
 
-// Four neighbouring entries of a row, each rounded to T once; `left` entries of the row from the first on are there.  (Rows may start at
-// any multiple of an entry's size: unaligned accesses are the processor's.)
+// Four neighbouring entries of a row, each rounded to T once; `left` entries of the row from the first on are there.  (Rows
+// may start at any multiple of an entry's size: unaligned accesses are the processor's.)
 template <typename T>
 __device__ __forceinline__ void store4(T* p, const f32x4& v, int64_t left) {
   typedef T T4 __attribute__((ext_vector_type(4)));
@@ -414,12 +422,12 @@ __device__ __forceinline__ void tile_at(uint32_t id, uint32_t tall, uint32_t wid
   across = in / height;
 }
 
-// Which size of tile the results of a launch are made with, each of them `many` matrices of rows x cols with `k` terms in a sum.
-// The larger a tile, the higher its rate; but the compute units' shares of few large tiles are uneven, and a tile alone on a compute unit
-// has nothing beside it while it loads.  Rates of a full card, and of one tile to a compute unit, relative to the first (8192 x 8192 x
-// 768 bfloat16, TFLOP/s: 256 x 256 1340, 128 x 128 1130, 64 x 64 770; alone, 1024 x 1024 x 2048 and the like: 1100, 800, 375.  fp32, where
-// the matrix cores bound every size: 133, 133, 130; alone 64 x 64 100).
-// Launches of more than one kind of result take 256 x 128 in steps of 64 bytes for the largest, of which two and three workgroups share a
+// Which size of tile the results of a launch are made with, each of them `many` matrices of rows x cols with `k` terms in a
+// sum.  The larger a tile, the higher its rate; but the compute units' shares of few large tiles are uneven, and a tile alone
+// on a compute unit has nothing beside it while it loads.  Rates of a full card, and of one tile to a compute unit, relative
+// to the first (8192 x 8192 x 768 bfloat16, TFLOP/s: 256 x 256 1340, 128 x 128 1130, 64 x 64 770; alone, 1024 x 1024 x 2048
+// and the like: 1100, 800, 375. fp32, where the matrix cores bound every size: 133, 133, 130; alone 64 x 64 100).  Launches of
+// more than one kind of result take 256 x 128 in steps of 64 bytes for the largest, of which two and three workgroups share a
 // compute unit: one stores while another multiplies (8 x 1024 x 768 x 2048 projections' gradients 115 us, with 128 x 128 123).
 enum TileSize { kTile256, kTile128, kTile64 };
 struct Work {
@@ -441,20 +449,20 @@ inline TileSize tile_size(std::initializer_list<Work> all, bool wide_type) {
     const double share = tiles ? sum / static_cast<double>(tiles) * static_cast<double>((tiles + 255) / 256) : 0.0;
     return (share / full > longest / alone) ? share / full : longest / alone;
   };
-  // (the last: what a tile takes besides its products, some 2 us to load the first step and to store, as far as the others on its
-  // compute unit do not hide it: 180 x 3818 x 29084 bfloat16, sums of 90 terms in 54000 tiles of 64 x 64, 564 us)
+  // (the last: what a tile takes besides its products, some 2 us to load the first step and to store, as far as the others on
+  // its compute unit do not hide it: 180 x 3818 x 29084 bfloat16, sums of 90 terms in 54000 tiles of 64 x 64, 564 us)
   const double large = all.size() > 1 ? cost(256, 128, 0.97, wide_type ? 0.9 : 0.6, 2.6e6) : cost(256, 256, 1.0, 0.97, 6e6);
   const double middle = wide_type ? cost(128, 128, 1.0, 0.9, 0.4e6) : cost(128, 128, 0.84, 0.6, 2.6e6);
   const double small = wide_type ? cost(64, 64, 0.97, 0.75, 0.15e6) : cost(64, 64, 0.57, 0.28, 1e6);
   if (large <= middle && large <= small) return kTile256;
   return middle <= small ? kTile128 : kTile64;
 }
-// Into how many parts the k of a result is cut whose tiles are too few for the card, each part with a thousand terms and more: their sums are
-// joined afterwards.
-inline uint32_t splits_of(uint64_t rows, uint64_t cols, uint64_t k) {
-  const uint64_t tiles = (rows + 63) / 64 * ((cols + 63) / 64);
+// Into how many parts the k of a result is cut whose tiles are too few for the card, each part with 1024 terms and more (fp32, whose
+// products take longer: 512): their sums are joined afterwards.
+inline uint32_t splits_of(uint64_t rows, uint64_t cols, uint64_t k, bool wide_type) {
+  const uint64_t tiles = (rows + 63) / 64 * ((cols + 63) / 64), most = k / (wide_type ? 512 : 1024);
   uint64_t splits = tiles ? 1024 / tiles : 1;
-  if (splits > k / 1024) splits = k / 1024;
+  if (splits > most) splits = most;
   return static_cast<uint32_t>(splits > 16 ? 16 : splits > 1 ? splits : 1);
 }
 inline uint64_t tiles_of(uint64_t count, uint32_t edge) { return (count + edge - 1) / edge; }

@@ -4,8 +4,8 @@
 namespace compams {
 namespace {
 
-// A workgroup takes whole rows, a lane a piece of 16 bytes of each of AT_ONCE at a time, as many lanes side by side as a row has pieces.  (Rows
-// that start on 16 bytes and have whole pieces are not copied.)
+// A workgroup takes whole rows, a lane a piece of 16 bytes of each of AT_ONCE at a time, as many lanes side by side as a row
+// has pieces.  (Rows that start on 16 bytes and have whole pieces are not copied.)
 template <typename T>
 __device__ __forceinline__ typename Fragment<T>::type piece_of(const T* from, uint32_t c, uint32_t cols) {
   constexpr uint32_t kEach = 16 / sizeof(T);
@@ -26,7 +26,8 @@ __global__ __launch_bounds__(256) void k_pack(Packing p) {
   const uint32_t side = j.per_row < 256 ? 256 / j.per_row : 1;  // rows side by side
   const uint32_t in = j.per_row < 256 ? threadIdx.x / j.per_row : 0;
   if (in >= side) return;
-  for (int64_t first = static_cast<int64_t>(blockIdx.x) * side * AT_ONCE + in; first < j.rows; first += static_cast<int64_t>(gridDim.x) * side * AT_ONCE)
+  const int64_t step = static_cast<int64_t>(gridDim.x) * side * AT_ONCE;
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * side * AT_ONCE + in; first < j.rows; first += step)
     for (uint32_t c = threadIdx.x - in * j.per_row; c < j.per_row; c += 256) {
       Piece v[AT_ONCE];
 #pragma unroll

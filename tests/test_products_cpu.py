@@ -225,3 +225,19 @@ def test_reference_bounds_hold_for_32_bits():
     P.close(loss, want[1], bound[1], "losses")
     P.close(leaf.grad, want[2], bound[2], "dx")
     P.close(w.grad, want[3].sum(0), bound[3].sum(0), "dweight")
+
+
+def test_registers_of_the_kernels():
+    """No more than eight registers of a lane are spilled, and where three workgroups are to share a compute unit, three fit."""
+    pytest.importorskip("msgpack")
+    import re
+    import test_operator_kernels_cpu as K
+    found = {}
+    for elf in K.code_objects(open(B.LIB_PATH, "rb").read()):
+        found.update(K.kernels(elf))
+    ours = {k: v for k, v in found.items() if re.search(r"k_(gated|projection|linear_loss|clip|pack)", k)}
+    assert len(ours) > 100
+    over = {k: v[".vgpr_spill_count"] for k, v in ours.items() if v[".vgpr_spill_count"] > 8}
+    assert not over, over
+    three = {k: v[".vgpr_count"] for k, v in ours.items() if "linear_loss_piece" in k and "DF16" in k and v[".group_segment_fixed_size"] == 49152}
+    assert len(three) == 2 and max(three.values()) <= 168, three
