@@ -627,21 +627,24 @@ Room room_of(const compams_linear_loss& a) {
 // The kernels that go over x and the weight by columns.
 template <typename T>
 void run_hold(const LossArgs& k, const compams_linear_loss& a, hipStream_t stream) {
-  ColumnsArgs c = {a.x, a.weight, a.ld_x, a.ld_weight, 1, 1, 16, 0, 0};
-  const uint32_t groups = (k.cols + kGroup - 1) / kGroup;
-  while (c.wide < groups && c.wide < kThreads) c.wide *= 2;
-  c.across = (groups + c.wide - 1) / c.wide;
-  // (fewer rows a lane where that leaves compute units idle: 2048 x 256 fp32 9.7 us with sixteen)
-  const uint64_t tall = kThreads / c.wide, rows = (k.x_held.p ? k.total : 0) + (kScaled<T> && a.dx ? k.vocab : 0);
-  while (c.each > 2 && rows * c.across < 512 * tall * c.each) c.each /= 2;
-  const uint64_t each = tall * c.each;
-  if (k.x_held.p) c.parts_x = static_cast<uint32_t>(tiles_of(k.rows, static_cast<uint32_t>(each)));
-  if (kScaled<T> && a.dx) c.parts_weight = static_cast<uint32_t>(tiles_of(k.vocab, static_cast<uint32_t>(each)));
-  const uint64_t blocks = (static_cast<uint64_t>(c.parts_x) * k.n + c.parts_weight) * c.across;
-  if (blocks == 0) return;
-  const dim3 grid(static_cast<uint32_t>(blocks));
-  if constexpr (kScaled<T>) hipLaunchKernelGGL(k_linear_loss_tops, grid, dim3(kThreads), 0, stream, k, c);
-  hipLaunchKernelGGL(k_linear_loss_hold<T>, grid, dim3(kThreads), 0, stream, k, c);
+  // (fewer rows a lane where that leaves compute units idle, 2048 x 256 fp32 9.7 us with sixteen; but every workgroup's maxima are
+  // joined in memory, so not too few of those)
+  const auto launch = [&](uint32_t least, auto go) {
+    ColumnsArgs c = {a.x, a.weight, a.ld_x, a.ld_weight, 1, 1, 16, 0, 0};
+    const uint32_t groups = (k.cols + kGroup - 1) / kGroup;
+    c.wide = lanes_across(groups);
+    c.across = (groups + c.wide - 1) / c.wide;
+    const uint64_t tall = kThreads / c.wide, rows = (k.x_held.p ? k.total : 0) + (kScaled<T> && a.dx ? k.vocab : 0);
+    while (c.each > least && rows * c.across < 512 * tall * c.each) c.each /= 2;
+    const uint64_t each = tall * c.each;
+    if (k.x_held.p) c.parts_x = static_cast<uint32_t>(tiles_of(k.rows, static_cast<uint32_t>(each)));
+    if (kScaled<T> && a.dx) c.parts_weight = static_cast<uint32_t>(tiles_of(k.vocab, static_cast<uint32_t>(each)));
+    const uint64_t blocks = (static_cast<uint64_t>(c.parts_x) * k.n + c.parts_weight) * c.across;
+    if (blocks) go(dim3(static_cast<uint32_t>(blocks)), c);
+  };
+  if constexpr (kScaled<T>)
+    launch(8, [&](dim3 grid, const ColumnsArgs& c) { hipLaunchKernelGGL(k_linear_loss_tops, grid, dim3(kThreads), 0, stream, k, c); });
+  launch(2, [&](dim3 grid, const ColumnsArgs& c) { hipLaunchKernelGGL(k_linear_loss_hold<T>, grid, dim3(kThreads), 0, stream, k, c); });
 }
 
 template <typename T>
