@@ -3,8 +3,8 @@
 // The vocabulary is gone over twice.  First every tile of the logits leaves a maximum and a sum of exponentials for each of
 // its rows, from which a row's loss and its softmax's denominator follow.  Then, piece by piece of the vocabulary, the logits
 // are formed again, turned into d = softmax - [target], and multiplied by the piece's weights (dx, whose fp32 sums wait in the
-// workspace from piece to piece) and by x (dweight, of which a piece holds whole rows).  Five products of the logits' size
-// instead of three, more for the digits of d, and no matrix of rows x vocabulary.
+// workspace from piece to piece) and by x (dweight, of which a piece holds whole rows).  Four products of the logits' size
+// instead of three, a fifth for the digits of d, and no matrix of rows x vocabulary.
 //
 // d times 2^14 is held in float16 where the operands have 16 bits, in two parts: the second is the rounded rest of the first,
 // so that both together are off by 2^-23 of an entry or 2^-39 of the largest possible one. dweight is fp32 and takes both; dx,
