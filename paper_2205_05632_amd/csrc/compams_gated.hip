@@ -44,7 +44,7 @@ __device__ __forceinline__ float activate(float a, float& slope) {
     return q;
   } else if constexpr (ACT == COMPAMS_SILU) {
     const float q = logistic(a), v = a < -88.0f ? -0.0f : a * q;  // (beyond it q is 0)
-    if constexpr (SLOPE) slope = q + v * logistic(-a);
+    if constexpr (SLOPE) slope = a > 88.0f ? q : q + v * logistic(-a);  // (infinity times 0 beyond it)
     return v;
   } else if constexpr (ACT == COMPAMS_GELU) {
     const float e = exp_fast(-0.5f * a * a), cdf = normal_cdf(a, e);

@@ -98,8 +98,8 @@ struct Share {
   uint32_t matrix, first, last, column, step;  // rows first, first + step, ... before `last`
 };
 __device__ __forceinline__ bool share_of(const LossArgs& a, const ColumnsArgs& c, Share& s) {
-  const uint32_t strip = blockIdx.x % c.across, tall = kThreads / c.wide;
-  uint32_t part = blockIdx.x / c.across;
+  const uint32_t strip = tile_id() % c.across, tall = kThreads / c.wide;
+  uint32_t part = tile_id() / c.across;
   const uint32_t of_x = c.parts_x * a.n;
   s.matrix = part < of_x ? part / c.parts_x : a.n;
   part = part < of_x ? part - s.matrix * c.parts_x : part - of_x;
@@ -108,7 +108,7 @@ __device__ __forceinline__ bool share_of(const LossArgs& a, const ColumnsArgs& c
   s.last = static_cast<uint32_t>(min(static_cast<uint64_t>(rows), static_cast<uint64_t>(part + 1) * tall * c.each));
   s.first = part * tall * c.each + threadIdx.x / c.wide;
   s.column = (strip * c.wide + threadIdx.x % c.wide) * kGroup;
-  return s.column < a.cols;
+  return s.column < a.cols && part < (s.matrix < a.n ? c.parts_x : c.parts_weight);
 }
 
 // The largest entry of every column.  (Whichever comes first: a maximum.)
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void k_linear_loss_tops(LossArgs a, Colum
   for (uint32_t i = threadIdx.x; i < c.wide * kGroup; i += kThreads) {
     uint32_t most = 0;
     for (uint32_t k = i / kGroup; k < kThreads; k += c.wide) most = max(most, joined[k][i % kGroup]);
-    const uint32_t column = blockIdx.x % c.across * c.wide * kGroup + i;
+    const uint32_t column = tile_id() % c.across * c.wide * kGroup + i;
     if (column < a.cols && most) atomicMax(a.tops + static_cast<uint64_t>(s.matrix) * a.cols + column, most);
   }
 }
@@ -640,7 +640,7 @@ void run_hold(const LossArgs& k, const compams_linear_loss& a, hipStream_t strea
     if (k.x_held.p) c.parts_x = static_cast<uint32_t>(tiles_of(k.rows, static_cast<uint32_t>(each)));
     if (kScaled<T> && a.dx) c.parts_weight = static_cast<uint32_t>(tiles_of(k.vocab, static_cast<uint32_t>(each)));
     const uint64_t blocks = (static_cast<uint64_t>(c.parts_x) * k.n + c.parts_weight) * c.across;
-    if (blocks) go(dim3(static_cast<uint32_t>(blocks)), c);
+    if (blocks) go(tile_grid(blocks), c);
   };
   if constexpr (kScaled<T>)
     launch(8, [&](dim3 grid, const ColumnsArgs& c) { hipLaunchKernelGGL(k_linear_loss_tops, grid, dim3(kThreads), 0, stream, k, c); });

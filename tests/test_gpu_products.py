@@ -168,6 +168,19 @@ def test_gated_backward_of_strange_entries(act):
 
 
 @pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_gated_backward_of_infinite_gates(dtype, act):
+    """A gate that passed its type's largest value has the activation's limits; far ones beside it have them too."""
+    gates = torch.tensor([[math.inf, -math.inf, 60000.0, -60000.0, 100.0, -200.0]], dtype=dtype, device="cuda")
+    two = torch.full_like(gates, 2.0)
+    dg, du = ops.compams_gated_backward(two, gates, two, 1, act)[:2]
+    up = gates > 0
+    one = torch.zeros_like(gates) if act == "sigmoid" else up.to(dtype)
+    assert torch.equal(dg, 4 * one)
+    assert torch.equal(du, 2 * (up.to(dtype) if act == "sigmoid" else torch.where(up, gates, 0.0)))
+
+
+@pytest.mark.parametrize("act", ACTS)
 def test_gated_gradients_against_differences(act):
     """dgate and dup are the slopes of the forward call's m."""
     rng = np.random.default_rng(11)
