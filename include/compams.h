@@ -478,7 +478,7 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream);
  *     after the first (a parameter's place in a worker's row of g, with ld = cols and stride = that row's).
  *   - Products are formed from the operands as they are, with fp32 sums.
  *   - cols and hidden are at most COMPAMS_MOST_ENTRIES.
- *   - Operands whose rows do not all begin on 16 bytes and hold a multiple of 16 bytes are first copied into the workspace,
+ *   - Operands whose rows do not all begin on 16 bytes are first copied into the workspace,
  *     so the workspace's size depends on pointers and strides too: ask with the fields that the call gets. */
 #define COMPAMS_MOST_ENTRIES (1 << 20)
 enum {

@@ -448,7 +448,7 @@ __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, const
     t.each([&](uint32_t m, uint32_t n, f32x4& v) {
       if (m0 + m < a.total && n0 + n < a.cols) v = *sums(m0 + m, n0 + n);
     });
-  t.run([&](uint32_t, Side& d, Side& w, Side&) {
+  t.template run<false>([&](uint32_t, Side& d, Side& w, Side&) {
     d = side<typename TL::T, kAlong>(a.now.d + k0 * sizeof(typename TL::T), a.ld_d, a.total, m0, width);
     const char* const rows = static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.now.first + k0) * a.weight_held.ld;
     w = side<typename TL::T, kAcross>(rows, a.weight_held.ld, a.cols, n0, width);

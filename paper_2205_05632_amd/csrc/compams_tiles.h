@@ -3,8 +3,9 @@
 //
 // A step takes 128 bytes of k, 64 entries of the 16-bit types, 32 of fp32 (or half as many).  Both operands' tiles of a step
 // go from memory into LDS without passing through registers, 16 bytes a lane, while the step before is multiplied (two
-// buffers, one barrier a step).  Reads beyond a matrix give zeros (the buffer descriptors' own bounds), so no length has to be
-// a multiple of anything but 16 bytes.
+// buffers, one barrier a step).  Reads beyond a matrix give zeros (the buffer descriptors' own bounds), and what rows along k
+// have behind their last entry in the same 16 bytes is overwritten with zeros in LDS, so no length has to be a multiple of
+// anything; rows have to start on 16 bytes.
 #pragma once
 
 #include <initializer_list>
@@ -64,6 +65,19 @@ struct Place {
 
   // kAlong: what a piece's number is changed by in row `row`.
   __device__ static __forceinline__ uint32_t turned(uint32_t row) { return STEP == 128 ? row & 7u : row >> 1 & 3u; }
+
+  // kAlong: zeros behind the first `keep` of the step's entries, as far as those 16 bytes go (a multiple: nothing).
+  __device__ static __forceinline__ void cut(lds_char* tile, uint32_t keep, uint32_t threads) {
+    constexpr uint32_t kEach = 16 / sizeof(T);
+    for (uint32_t row = threadIdx.x; row < EXTENT; row += threads) {
+      typedef __attribute__((address_space(3))) typename Fragment<T>::type Kept;
+      Kept* const at = reinterpret_cast<Kept*>(tile + row * kRowBytes + (keep / kEach ^ turned(row)) * 16);
+      typename Fragment<T>::type v = *at;
+#pragma unroll
+      for (uint32_t j = 1; j < kEach; ++j) v[j] = j < keep % kEach ? v[j] : T(0);
+      *at = v;
+    }
+  }
 
   // The row and the piece of it that is kept at 16-byte place p.
   __device__ static __forceinline__ void of(uint32_t p, uint32_t& row, uint32_t& piece) {
@@ -150,9 +164,8 @@ struct Loader {
           second ? of_two : of_one, (__attribute__((address_space(3))) void*)(tile + (i * WAVES + wave) * 1024), 16, at, 0, 0, 0);
     }
   }
-  // Up to the end of the last row's last 16 bytes, which belong to the row: an entry of 16 bits that ends it in the middle of
-  // a word would be cut off with the word.
-  __device__ static __forceinline__ uint32_t whole(uint32_t bytes) { return (bytes + 15) / 16 * 16; }
+  // Up to the end of the last row's last word: an entry of 16 bits that ends it in the middle of one would be cut off with it.
+  __device__ static __forceinline__ uint32_t whole(uint32_t bytes) { return (bytes + 3) / 4 * 4; }
   __device__ static __forceinline__ __amdgpu_buffer_rsrc_t bounds(const Side& s, uint32_t k0, bool two) {
     const char* p;
     uint32_t bytes;
@@ -219,8 +232,9 @@ struct Tiles {
     }
   }
 
-  // sum += the products of `count` pairs of operands, all with the same k.  pair(i, a, b, b2) gives the i-th.
-  template <typename Pair>
+  // sum += the products of `count` pairs of operands, all with the same k.  pair(i, a, b, b2) gives the i-th; one or two. CUT: rows
+  // along k may have something other than zeros behind their last entry.
+  template <bool CUT = true, typename Pair>
   __device__ __forceinline__ void run(Pair pair, uint32_t count, uint32_t k, const TileLds& lds) {
     const uint32_t w = wave();
     Loader<T, FA, kM, kWaves, STEP> la;
@@ -242,17 +256,53 @@ struct Tiles {
       }
     };
     load(lds.a[0], lds.b[0]);
-    for (uint32_t s = 2; s <= steps; s += 2) {
+    if constexpr (CUT && (FA == kAlong || FB == kAlong)) {
+      // The last step of a pair whose rows end within 16 bytes: what follows there may be anything, a NaN too.
+      const auto cut = [&](lds_char* ta, lds_char* tb) {
+        if (k % (16 / sizeof(T)) == 0) return;
+        if constexpr (FA == kAlong) PlaceA::cut(ta, k % kStep, kThreads);
+        if constexpr (FB == kAlong) PlaceB::cut(tb, k % kStep, kThreads);
+        __syncthreads();
+      };
+      const auto first_ends = [&](uint32_t s) { return count == 2 && 2 * s == steps; };
+      // (the last step stands apart, in one place for both buffers: registers are spilled with its cut in the loop, 8192 x
+      // 50257 x 768 first pass 628 -> 725 us, and far more with a copy of the step for each buffer)
+      uint32_t s = 1;
+      for (; s + 1 < steps; s += 2) {
+        arrived();
+        load(lds.a[1], lds.b[1]);
+        if (first_ends(s)) cut(lds.a[0], lds.b[0]);
+        step(lds.a[0], lds.b[0]);
+        arrived();
+        load(lds.a[0], lds.b[0]);
+        if (first_ends(s + 1)) cut(lds.a[1], lds.b[1]);
+        step(lds.a[1], lds.b[1]);
+      }
       arrived();
-      load(lds.a[1], lds.b[1]);
-      step(lds.a[0], lds.b[0]);
-      arrived();
-      if (s < steps) load(lds.a[0], lds.b[0]);
-      step(lds.a[1], lds.b[1]);
-    }
-    if (steps & 1u) {
-      arrived();
-      step(lds.a[0], lds.b[0]);
+      lds_char *ta = lds.a[0], *tb = lds.b[0];
+      if (s < steps) {
+        load(lds.a[1], lds.b[1]);
+        if (first_ends(s)) cut(ta, tb);
+        step(ta, tb);
+        arrived();
+        ta = lds.a[1];
+        tb = lds.b[1];
+      }
+      cut(ta, tb);
+      step(ta, tb);
+    } else {
+      for (uint32_t s = 2; s <= steps; s += 2) {
+        arrived();
+        load(lds.a[1], lds.b[1]);
+        step(lds.a[0], lds.b[0]);
+        arrived();
+        if (s < steps) load(lds.a[0], lds.b[0]);
+        step(lds.a[1], lds.b[1]);
+      }
+      if (steps & 1u) {
+        arrived();
+        step(lds.a[0], lds.b[0]);
+      }
     }
   }
   // What this wavefront loaded is in LDS, and so is everybody's; everybody is done with the step before.
@@ -366,16 +416,15 @@ __device__ __forceinline__ void add4(float* p, f32x4 v, int64_t left, bool accum
 constexpr int64_t kMostEntries = 1 << 20;
 constexpr int64_t kMostRowBytes = 1 << 23;
 
-// A matrix as a caller has it, and as the product kernels read it: rows of whole 16-byte pieces that start on 16 bytes.  What
-// is not like that is copied into the workspace first, with zeros behind the rows (`packed`).
+// A matrix as a caller has it, and as the product kernels read it: rows that start on 16 bytes.  What is not like that is
+// copied into the workspace first, with zeros behind the rows (`packed`).
 struct Matrix {
   const void* p;
   int64_t ld;  // entries
   int64_t rows, cols;
   size_t size;  // bytes of an entry
   bool as_is() const {
-    return aligned_to(p, 16) && (rows <= 1 || ld * size % 16 == 0) && cols * size % 16 == 0 &&
-           (rows <= 1 || ld * static_cast<int64_t>(size) <= kMostRowBytes);
+    return aligned_to(p, 16) && (rows <= 1 || (ld * size % 16 == 0 && ld * static_cast<int64_t>(size) <= kMostRowBytes));
   }
   int64_t packed_row_bytes() const { return (cols * static_cast<int64_t>(size) + 15) / 16 * 16; }
   size_t packed_bytes() const { return as_is() ? 0 : (static_cast<size_t>(rows) * packed_row_bytes() + 255) / 256 * 256; }

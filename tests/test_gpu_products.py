@@ -501,3 +501,29 @@ def test_calls_on_two_streams():
     torch.cuda.synchronize()
     for i, out in enumerate(got):
         assert all(torch.equal(a, b) for a, b in zip(out, one[i % 2]))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,rows,cols,hidden", [(1, 70, 1, 3), (2, 40, 63, 65), (3, 100, 129, 77), (1, 256, 257, 130), (4, 300, 777, 1111), (2, 1500, 70, 301)])
+def test_rows_that_end_within_sixteen_bytes(n, rows, cols, hidden, dtype):
+    """Rows of any length that start on 16 bytes are read where they are; what lies behind them (NaN here) adds nothing."""
+    rng = np.random.default_rng(n * 1000 + rows * 10 + cols + hidden)
+    each, total = 16 // dtype.itemsize, n * rows
+    make = lambda count, wide, scale: matrix(rng, count, wide, dtype, -wide % each, 0, scale)  # noqa: E731
+    x, x64 = make(total, cols, 1.0)
+    wg, wg64 = make(hidden, cols, 1 / math.sqrt(cols))
+    wu, wu64 = make(hidden, cols, 1 / math.sqrt(cols))
+    da, da64 = make(total, hidden, 1.0)
+    db, db64 = make(total, hidden, 1.0)
+    zero = torch.zeros(hidden, dtype=torch.float64)
+    want, bound = P.gated_forward(x64, wg64, wu64, zero, zero, "silu", dtype)
+    all_close(ops.compams_gated_forward(x, wg, wu), want, bound, ("m", "gate", "up"))
+    want, bound = P.projections([da64, db64], x64, [wg64, wu64], n, dtype)
+    all_close(ops.compams_projections_backward(da, db, x, wg, wu, n), want, bound, ("dx", "dgate_weight", "dup_weight"))
+    t = tokens(rng, total, hidden, -1)
+    want, bound = P.linear_cross_entropy(x64, wg64, t, n, -1, 1.0 if dtype != F16 else 64.0, dtype)
+    got = ops.compams_linear_cross_entropy(x, wg, t.cuda(), n, -1, 1.0 if dtype != F16 else 64.0)
+    all_close(got, want, bound, ("mean_loss", "losses", "dx", "dweight"))
+    # beside the same rows without a gap, which are copied first
+    for a, b in zip(got, ops.compams_linear_cross_entropy(x.contiguous(), wg.contiguous(), t.cuda(), n, -1, 1.0 if dtype != F16 else 64.0)):
+        assert torch.equal(a, b)

@@ -61,7 +61,7 @@ BOTH = [(dict(n=0), -1), (dict(n=65536), -1), (dict(rows=-1), -1), (dict(rows=1 
     (dict(ld_x=15), -1), (dict(ld_gate_weight=15), -1), (dict(ld_up_weight=1), -1), (dict(ld_m=7), -1), (dict(x=FAKE + 2), -2),
     (dict(gate_weight=FAKE + 1), -2), (dict(up_weight=FAKE + 3), -2), (dict(m=FAKE + 2), -2), (dict(gate_bias=FAKE + 2), -2), (dict(up_bias=FAKE + 1), -2),
     (dict(x=FAKE + 4), -1), (dict(x=FAKE + 4, workspace=FAKE, workspace_bytes=100), -3),
-    (dict(x=FAKE + 4, workspace=FAKE + 16, workspace_bytes=4096), -2), (dict(cols=15), -1), (dict(ld_up_weight=17), -1), (dict(rows=0), 0),
+    (dict(x=FAKE + 4, workspace=FAKE + 16, workspace_bytes=4096), -2), (dict(cols=15, ld_x=17), -1), (dict(ld_up_weight=17), -1), (dict(rows=0), 0),
 ])
 def test_gated_forward_refuses(kw, code):
     assert B.lib().compams_gated_forward(gated(**kw), None) == code
@@ -160,7 +160,7 @@ def test_null_and_workspace_sizes():
     assert L.compams_gated_forward_workspace_size(gated(n=1, rows=3, x=FAKE + 4)) == 0     # (nor is it for few rows)
     assert L.compams_gated_forward_workspace_size(gated(x=FAKE + 4)) > 0 and L.compams_gated_forward_workspace_size(gated(ld_gate_weight=17)) > 0
     assert L.compams_projections_workspace_size(projections()) == 0
-    assert L.compams_projections_workspace_size(projections(cols=15)) > 0
+    assert L.compams_projections_workspace_size(projections(ld_x=17)) > 0
     # the pieces of a vocabulary, whatever its size, are bounded
     large = dict(n=8, rows=1024, cols=768, type=ops.BF16, ld_x=768, ld_weight=768, ld_dx=768, ld_dweight=768, stride_dweight=1 << 30)
     for vocab in (50257, 500000):
