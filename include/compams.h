@@ -478,8 +478,8 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream);
  *     after the first (a parameter's place in a worker's row of g, with ld = cols and stride = that row's).
  *   - Products are formed from the operands as they are, with fp32 sums.
  *   - cols and hidden are at most COMPAMS_MOST_ENTRIES.
- *   - Operands whose rows do not all begin on 16 bytes are first copied into the workspace,
- *     so the workspace's size depends on pointers and strides too: ask with the fields that the call gets. */
+ *   - Operands whose rows do not all begin on 16 bytes are first copied into the workspace, so the workspace's size depends on
+ *     pointers and strides too: ask with the fields that the call gets. */
 #define COMPAMS_MOST_ENTRIES (1 << 20)
 enum {
   COMPAMS_SILU = 0,      /* a / (1 + exp(-a)) */
@@ -587,7 +587,8 @@ int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream)
  *   to = factors[i] * from
  * A worker whose gradient holds a NaN or an infinity has a norm that says so, factors[i] = 0 and zeros in `to`: it takes no
  * part in the step.  Squares and their sums are fp64, so no finite gradient has a norm beyond range or below it, in
- * fp32 or narrower types, unless the norm itself is. */
+ * fp32 or narrower types, unless the norm itself is.  Rows that are written lie over no other tensor's, so none is listed
+ * twice: such calls are refused where a first row shows it. */
 typedef struct compams_clip_tensor {
   const void* from; int64_t ld_from; /* n rows of `count` entries, ld_from entries apart */
   void* to;         int64_t ld_to;   /* the same, or NULL: nothing is written; may be `from` where both have one type */

@@ -1,4 +1,7 @@
 // The norm of every worker's gradient over all its tensors, and the gradient cut to a largest norm.
+#include <algorithm>
+#include <cstdlib>
+
 #include "compams_tiles.h"
 
 namespace compams {
@@ -249,7 +252,7 @@ int check(const compams_clip* a) {
     if (!aligned_to(t.from, type_size(t.from_type))) return COMPAMS_BAD_ALIGNMENT;
     if (t.to) {
       if (!float_type(t.to_type) || (t.to_type != t.from_type && t.to_type != COMPAMS_F32) ||
-          (a->n > 1 && (t.ld_to < t.count || t.ld_to >= kMost)) || (t.to == t.from && t.to_type != t.from_type))
+          (a->n > 1 && (t.ld_to < t.count || t.ld_to >= kMost)) || (t.to == t.from && (t.to_type != t.from_type || (a->n > 1 && t.ld_to != t.ld_from))))
         return COMPAMS_INVALID_ARG;
       if (!aligned_to(t.to, type_size(t.to_type))) return COMPAMS_BAD_ALIGNMENT;
     }
@@ -257,6 +260,39 @@ int check(const compams_clip* a) {
   }
   // (a launch's workgroups of one worker: 2^24 in a dimension of 2^32 threads)
   return chunks < (1u << 24) - 1 ? COMPAMS_OK : COMPAMS_INVALID_ARG;
+}
+// Whether a worker's first rows that are written lie over others: a tensor that is listed twice would be scaled twice, or once.
+// (Rows that are only read may be the same.)
+bool apart(const compams_clip& a) {
+  struct Row {
+    const char *begin, *end;
+    bool written;
+  };
+  if (a.tensors == 0) return true;
+  Row* const rows = static_cast<Row*>(std::malloc(2 * sizeof(Row) * static_cast<size_t>(a.tensors)));
+  if (!rows) return false;
+  size_t count = 0;
+  const auto add = [&](const void* p, int64_t entries, int32_t type, bool written) {
+    const char* const at = static_cast<const char*>(p);
+    rows[count++] = {at, at + entries * static_cast<int64_t>(type_size(type)), written};
+  };
+  for (int32_t i = 0; i < a.tensors; ++i) {
+    const compams_clip_tensor& t = a.tensor[i];
+    if (t.count == 0) continue;
+    if (t.to != t.from) add(t.from, t.count, t.from_type, false);
+    if (t.to) add(t.to, t.count, t.to_type, true);
+  }
+  std::sort(rows, rows + count, [](const Row& x, const Row& y) { return x.begin < y.begin; });
+  const char *any = nullptr, *written = nullptr;  // how far the rows so far go
+  bool good = true;
+  for (size_t i = 0; i < count; ++i) {
+    const Row& r = rows[i];
+    if (r.begin < (r.written ? any : written)) good = false;
+    any = r.end > any ? r.end : any;
+    if (r.written && r.end > written) written = r.end;
+  }
+  std::free(rows);
+  return good;
 }
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -329,6 +365,7 @@ int compams_clip_gradients(const compams_clip* a, void* hip_stream) {
   const int checked = check(a);
   if (checked != COMPAMS_OK) return checked;
   if (!aligned_to(a->norms, 4) || !aligned_to(a->factors, 4)) return COMPAMS_BAD_ALIGNMENT;
+  if (!apart(*a)) return COMPAMS_INVALID_ARG;
   const int status = workspace_status(a->workspace, a->workspace_bytes, bytes_of(*a));
   if (status != COMPAMS_OK) return status;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

@@ -466,6 +466,7 @@ int compams_gated_forward(const compams_gated* a, void* hip_stream) {
   if (!aligned_to(a->x, size) || !aligned_to(a->gate_weight, size) || !aligned_to(a->up_weight, size) || !aligned_to(a->m, size) ||
       !aligned_to(a->gate, size) || !aligned_to(a->up, size) || !aligned_to(a->gate_bias, 4) || !aligned_to(a->up_bias, 4))
     return COMPAMS_BAD_ALIGNMENT;
+  if (a->m == a->gate || a->m == a->up || (a->gate && a->gate == a->up)) return COMPAMS_INVALID_ARG;
   const int status = workspace_status(a->workspace, a->workspace_bytes, forward_bytes(*a));
   if (status != COMPAMS_OK) return status;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -505,6 +506,7 @@ int compams_gated_backward(const compams_gated* a, void* hip_stream) {
     if (a->n > 1 && (ld < a->hidden || ld >= (static_cast<int64_t>(1) << 40))) return COMPAMS_INVALID_ARG;
     if (!aligned_to(p, 4)) return COMPAMS_BAD_ALIGNMENT;
   }
+  if (a->dgate_bias && a->dgate_bias == a->dup_bias) return COMPAMS_INVALID_ARG;
   if (a->rows > 0) {
     if (!a->dm || !a->gate || !a->up || !a->dgate || !a->dup || !stride_valid(a->ld_dm, a->hidden) ||
         !stride_valid(a->ld_gate, a->hidden) || !stride_valid(a->ld_up, a->hidden) || !stride_valid(a->ld_dgate, a->hidden) ||
@@ -513,6 +515,7 @@ int compams_gated_backward(const compams_gated* a, void* hip_stream) {
     if (!aligned_to(a->dm, size) || !aligned_to(a->gate, size) || !aligned_to(a->up, size) || !aligned_to(a->dgate, size) ||
         !aligned_to(a->dup, size))
       return COMPAMS_BAD_ALIGNMENT;
+    if (a->dgate == a->dup) return COMPAMS_INVALID_ARG;
   } else if (!a->dgate_bias && !a->dup_bias) {
     return COMPAMS_OK;
   }

@@ -178,6 +178,7 @@ int compams_projections_backward(const compams_projections* a, void* hip_stream)
     if (!gradient_valid(a->n, a->hidden, a->cols, ld[i], stride[i])) return COMPAMS_INVALID_ARG;
     if (!aligned_to(dweight[i], 4)) return COMPAMS_BAD_ALIGNMENT;
   }
+  if (dweight[0] && dweight[0] == dweight[1]) return COMPAMS_INVALID_ARG;
   const Operands o = operands(*a);
   if (a->rows > 0) {
     const bool weights = dweight[0] || dweight[1];

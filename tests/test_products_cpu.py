@@ -39,13 +39,13 @@ def test_packed_arguments_have_the_structures_layout(name):
     assert [getattr(got, f) for f, _ in struct._fields_] == values
 
 
-FAKE = 0x1000    # never dereferenced: validation fails first
+FAKE, MORE, LAST = 0x1000, 0x100000, 0x200000    # never dereferenced: validation fails first
 
 
 def gated(**kw):
     a = ops.compams_gated(n=2, rows=300, cols=16, hidden=8, type=ops.F32, activation=0, x=FAKE, ld_x=16, gate_weight=FAKE, ld_gate_weight=16,
-                          up_weight=FAKE, ld_up_weight=16, m=FAKE, ld_m=8, gate=FAKE, ld_gate=8, up=FAKE, ld_up=8, dm=FAKE, ld_dm=8,
-                          dgate=FAKE, ld_dgate=8, dup=FAKE, ld_dup=8)
+                          up_weight=FAKE, ld_up_weight=16, m=FAKE, ld_m=8, gate=MORE, ld_gate=8, up=LAST, ld_up=8, dm=FAKE, ld_dm=8,
+                          dgate=MORE, ld_dgate=8, dup=LAST, ld_dup=8)
     for k, v in kw.items():
         setattr(a, k, v)
     return ctypes.byref(a)
@@ -62,13 +62,14 @@ BOTH = [(dict(n=0), -1), (dict(n=65536), -1), (dict(rows=-1), -1), (dict(rows=1 
     (dict(gate_weight=FAKE + 1), -2), (dict(up_weight=FAKE + 3), -2), (dict(m=FAKE + 2), -2), (dict(gate_bias=FAKE + 2), -2), (dict(up_bias=FAKE + 1), -2),
     (dict(x=FAKE + 4), -1), (dict(x=FAKE + 4, workspace=FAKE, workspace_bytes=100), -3),
     (dict(x=FAKE + 4, workspace=FAKE + 16, workspace_bytes=4096), -2), (dict(cols=15, ld_x=17), -1), (dict(ld_up_weight=17), -1), (dict(rows=0), 0),
+    (dict(gate=FAKE), -1), (dict(up=FAKE), -1), (dict(gate=LAST), -1),
 ])
 def test_gated_forward_refuses(kw, code):
     assert B.lib().compams_gated_forward(gated(**kw), None) == code
 
 
 @pytest.mark.parametrize("kw,code", BOTH + [
-    (dict(dm=None), -1), (dict(gate=None), -1), (dict(up=None), -1), (dict(dgate=None), -1), (dict(dup=None), -1), (dict(ld_dm=7), -1),
+    (dict(dgate=LAST), -1), (dict(dgate_bias=FAKE, ld_dgate_bias=8, dup_bias=FAKE, ld_dup_bias=8), -1), (dict(dm=None), -1), (dict(gate=None), -1), (dict(up=None), -1), (dict(dgate=None), -1), (dict(dup=None), -1), (dict(ld_dm=7), -1),
     (dict(ld_dgate=7), -1), (dict(ld_dup=7), -1), (dict(dm=FAKE + 2), -2), (dict(dgate=FAKE + 2), -2), (dict(dup=FAKE + 2), -2), (dict(accumulate=2), -1),
     (dict(dgate_bias=FAKE, ld_dgate_bias=7), -1), (dict(dup_bias=FAKE + 2, ld_dup_bias=8), -2),
     (dict(rows=100000, dgate_bias=FAKE, ld_dgate_bias=8), -1),
@@ -82,7 +83,7 @@ def test_gated_backward_refuses(kw, code):
 def projections(**kw):
     a = ops.compams_projections(n=2, rows=3, cols=16, hidden=8, type=ops.F32, dgate=FAKE, ld_dgate=8, dup=FAKE, ld_dup=8, x=FAKE, ld_x=16,
                                 gate_weight=FAKE, ld_gate_weight=16, up_weight=FAKE, ld_up_weight=16, dx=FAKE, ld_dx=16,
-                                dgate_weight=FAKE, ld_dgate_weight=16, stride_dgate_weight=128, dup_weight=FAKE, ld_dup_weight=16,
+                                dgate_weight=FAKE, ld_dgate_weight=16, stride_dgate_weight=128, dup_weight=MORE, ld_dup_weight=16,
                                 stride_dup_weight=128)
     for k, v in kw.items():
         setattr(a, k, v)
@@ -92,7 +93,7 @@ def projections(**kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(n=0), -1), (dict(rows=-1), -1), (dict(cols=0), -1), (dict(hidden=0), -1), (dict(cols=(1 << 20) + 1), -1), (dict(hidden=(1 << 20) + 1), -1),
     (dict(type=4), -1), (dict(dgate=None), -1), (dict(dup=None), -1), (dict(x=None), -1), (dict(gate_weight=None), -1), (dict(up_weight=None), -1),
-    (dict(dx=None, dgate_weight=None, dup_weight=None), -1), (dict(ld_dgate=7), -1), (dict(ld_dup=7), -1), (dict(ld_x=15), -1), (dict(ld_dx=15), -1),
+    (dict(dx=None, dgate_weight=None, dup_weight=None), -1), (dict(dup_weight=FAKE), -1), (dict(ld_dgate=7), -1), (dict(ld_dup=7), -1), (dict(ld_x=15), -1), (dict(ld_dx=15), -1),
     (dict(ld_gate_weight=15), -1), (dict(ld_dgate_weight=15), -1), (dict(stride_dup_weight=15), -1), (dict(stride_dup_weight=-1), -1),
     (dict(dgate=FAKE + 2), -2), (dict(x=FAKE + 1), -2), (dict(dx=FAKE + 2), -2), (dict(up_weight=FAKE + 2), -2), (dict(dgate_weight=FAKE + 2), -2),
     (dict(accumulate=-1), -1), (dict(x=FAKE + 4), -1), (dict(x=FAKE + 4, workspace=FAKE, workspace_bytes=64), -3), (dict(n=65535, rows=1, hidden=1 << 20, cols=1 << 20), -1),
@@ -147,6 +148,19 @@ def test_clip_refuses(tensor, kw, code):
     assert B.lib().compams_clip_gradients(ctypes.byref(clip([tensor], **kw)), None) == code
 
 
+@pytest.mark.parametrize("tensors,code", [
+    ([{}, {}], -1),                                                         # the same tensor twice, in place
+    ([{}, {"from": FAKE + 16, "to": FAKE + 16}], -1),                       # rows that overlap
+    ([{"to": MORE}, {"from": LAST, "to": MORE}], -1), ([{"to": MORE}, {"from": MORE, "to": LAST}], -1), ([{"to": FAKE + 4}], -1),
+    ([{"ld_to": 16}], -1),                                                  # in place with another stride
+    ([{"to": None}, {"to": None}], -3), ([{"to": None}, {"to": MORE}], -3),  # read twice (what is refused is the workspace)
+    ([{"ld_from": 16, "ld_to": 16}, {"from": FAKE + 32, "to": FAKE + 32, "ld_from": 16, "ld_to": 16}], -3),    # beside one another in rows
+    ([{}, {"count": 0}], -3),
+])
+def test_clip_refuses_rows_that_are_written_twice(tensors, code):
+    assert B.lib().compams_clip_gradients(ctypes.byref(clip(tensors, workspace_bytes=255)), None) == code
+
+
 def test_null_and_workspace_sizes():
     L = B.lib()
     for call in (L.compams_gated_forward, L.compams_gated_backward, L.compams_projections_backward, L.compams_linear_cross_entropy,
@@ -155,7 +169,7 @@ def test_null_and_workspace_sizes():
     for size in (L.compams_gated_forward_workspace_size, L.compams_gated_backward_workspace_size, L.compams_projections_workspace_size,
                  L.compams_linear_loss_workspace_size, L.compams_clip_workspace_size):
         assert size(None) == 0
-    # nothing is copied where rows start on 16 bytes and have whole pieces of them
+    # nothing is copied where rows start on 16 bytes
     assert L.compams_gated_forward_workspace_size(gated()) == 0
     assert L.compams_gated_forward_workspace_size(gated(n=1, rows=3, x=FAKE + 4)) == 0     # (nor is it for few rows)
     assert L.compams_gated_forward_workspace_size(gated(x=FAKE + 4)) > 0 and L.compams_gated_forward_workspace_size(gated(ld_gate_weight=17)) > 0
