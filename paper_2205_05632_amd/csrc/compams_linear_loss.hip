@@ -4,15 +4,15 @@
 // its rows, from which a row's loss and its softmax's denominator follow.  Then, piece by piece of the vocabulary, the logits
 // are formed again, turned into d = softmax - [target], and multiplied by the piece's weights (dx, whose fp32 sums wait in the
 // workspace from piece to piece) and by x (dweight, of which a piece holds whole rows).  Four products of the logits' size
-// instead of three, a fifth for the digits of d, and no matrix of rows x vocabulary.
+// instead of three, two more for the digits of d where the operands have 16 bits, and no matrix of rows x vocabulary.
 //
 // d times 2^14 is held in float16 where the operands have 16 bits, in two parts: the second is the rounded rest of the first,
-// so that both together are off by 2^-23 of an entry or 2^-39 of the largest possible one. dweight is fp32 and takes both; dx,
-// which is rounded to 16 bits, takes the first alone, one more rounding of half a step of float16.  (In bfloat16 three parts
-// would be needed, and half as many products again: 8192 x 50257 x 768 4.9 ms.) bfloat16 operands of these two products are
-// therefore turned into float16, each column times the power of two that brings its largest entry just below 2^15, and the
-// results' columns are scaled back: what 2^-39 of the largest entry of its own column does not reach is lost, as it is next to
-// it in an fp32 sum.
+// so that both together are off by 2^-23 of an entry or 2^-39 of the largest possible one.  Both products take both parts. (With
+// the first alone dx would be formed from eleven bits of every probability: 8192 x 50257 x 768 bfloat16 in 3.5 instead of 4.1 ms,
+// but float16 up to 1.5 times as far from 64 bits, and few digits right where a column's terms cancel.  In bfloat16 three parts
+// would be needed, and half as many products again.) bfloat16 operands of these products are therefore turned into float16, each
+// column times the power of two that brings its largest entry just below 2^15, and the results' columns are scaled back: what
+// 2^-39 of the largest entry of its own column does not reach is lost, as it is next to it in an fp32 sum.
 #include "compams_tiles.h"
 
 namespace compams {
@@ -430,7 +430,8 @@ __device__ __forceinline__ void store_dx(const LossArgs& a, uint32_t r, uint32_t
   store4(static_cast<T*>(a.dx) + static_cast<int64_t>(r) * a.ld_dx + n, v, static_cast<int64_t>(a.cols) - n);
 }
 
-// A tile of dx.  The sums go on from those of the pieces before, so that they do not depend on where pieces end.
+// A tile of dx: k is the piece's columns, once for each part of d, the lesser first.  The sums go on from those of the pieces
+// before.
 template <typename TL, typename T>
 __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, const TileLds& lds) {
   const uint32_t each = a.tall * a.wide, mine = by_die(id, each * a.splits), split = mine / each;
@@ -448,11 +449,12 @@ __device__ __forceinline__ void input_tile(const LossArgs& a, uint32_t id, const
     t.each([&](uint32_t m, uint32_t n, f32x4& v) {
       if (m0 + m < a.total && n0 + n < a.cols) v = *sums(m0 + m, n0 + n);
     });
-  t.template run<false>([&](uint32_t, Side& d, Side& w, Side&) {
-    d = side<typename TL::T, kAlong>(a.now.d + k0 * sizeof(typename TL::T), a.ld_d, a.total, m0, width);
+  t.template run<false>([&](uint32_t i, Side& d, Side& w, Side&) {
+    const char* const part = a.now.d + (kParts<T> - 1 - i) * a.part_bytes;
+    d = side<typename TL::T, kAlong>(part + k0 * sizeof(typename TL::T), a.ld_d, a.total, m0, width);
     const char* const rows = static_cast<const char*>(a.weight_held.p) + static_cast<int64_t>(a.now.first + k0) * a.weight_held.ld;
     w = side<typename TL::T, kAcross>(rows, a.weight_held.ld, a.cols, n0, width);
-  }, 1, width, lds);
+  }, kParts<T>, width, lds);
   const bool end = a.end && a.splits == 1;
   const f32x4 of_column = end ? scales<T>(a, a.n, n0 + TL::row_n()) : f32x4{};
   t.rows(lds.a[0], [&](uint32_t m, uint32_t n, f32x4 v) {
@@ -673,7 +675,7 @@ void run_linear_loss(LossArgs& k, const compams_linear_loss& a, const Room& room
   };
   char* const d = k.now.d;
   const auto size = [&] {
-    return tile_size({{a.dx ? k.total : 0, k.cols, k.splits, k.now.width / k.splits},
+    return tile_size({{a.dx ? k.total : 0, k.cols, k.splits, static_cast<uint64_t>(k.now.width) * kParts<T> / k.splits},
                       {a.dweight ? k.now.width : 0, k.cols, k.n, static_cast<uint64_t>(k.rows) * kParts<T>},
                       {k.total, k.next.width, 1, k.cols}}, sizeof(T) == 4);
   };
