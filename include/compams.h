@@ -556,9 +556,9 @@ int compams_projections_backward(const compams_projections* a, void* hip_stream)
  * losses of these logits (in fp32), and, with its dlogits d in fp32,
  *   dx = weight' d,  dweight = the sum over the worker's rows of d x'
  * The vocabulary is gone over twice, in pieces the second time.  A piece's gradients d, before grad_scale / count, are held in the
- * workspace: in fp32 where `type` is, else as two float16 numbers, whose sum is off by 2^-23 of d or by 2^-39 (d's entries are at
- * most 1).  For these products bfloat16 x and weights become float16, every column (x: of a worker) times a power of two: entries
- * below 2^-39 of their column's largest count as 0.  Ignored rows: loss and dx are 0 and nothing is added to dweight, whatever x
+ * workspace: in fp32 where `type` is, with every probability's own digits; else as two float16 numbers, whose sum is off by 2^-23 of
+ * d or by 2^-39 (d's entries are at most 1).  For these products bfloat16 x and weights become float16, every column (x: of a worker)
+ * times a power of two: entries are off by up to 2^-39 of their column's largest.  Ignored rows: loss and dx are 0 and nothing is added to dweight, whatever x
  * holds there. */
 typedef struct compams_linear_loss {
   int32_t n;

@@ -205,8 +205,14 @@ __device__ __forceinline__ float over_row(float v, Op op) {
 struct Max {
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
-// e^z by the processor's 2^x.
-__device__ __forceinline__ float exp_of(float z) { return __builtin_amdgcn_exp2f(z * 1.44269504088896341f); }
+// e^z for z <= 0.  fp32 keeps its digits at any distance z; of 16-bit operands the product with log2(e) is rounded once, which puts
+// an entry off by 1.2 |z| units of 2^-24 (their sum by the mean distance by weight, log(vocab) at most), while the parts of d hold it
+// to 2^-39 of the largest.
+template <typename T>
+__device__ __forceinline__ float exp_of(float z) {
+  if constexpr (sizeof(T) == 4) return exp_kept(z);
+  else return __builtin_amdgcn_exp2f(z * 1.44269504088896341f);
+}
 // What a row's logits are compared with: their maximum, or 0 where that is minus infinity (e^(l - top) is 0 then, and not a
 // NaN).
 __device__ __forceinline__ float base_of(float top) { return top == -INFINITY ? 0.0f : top; }
@@ -265,7 +271,7 @@ __global__ __launch_bounds__(TL::kThreads) void k_linear_loss_stats(LossArgs a) 
     for (uint32_t j = 0; j < TL::FN; ++j)
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q) {
-        const float e = exp_of(t.sum[i][j][q] - base);
+        const float e = exp_of<typename TL::T>(t.sum[i][j][q] - base);
         s[q] = j == 0 ? e : s[q] + e;
       }
     sum[i] = (s[0] + s[1]) + (s[2] + s[3]);
@@ -304,7 +310,7 @@ __global__ __launch_bounds__(16 * kJoinLanes) void k_linear_loss_join(LossArgs a
       for (uint32_t k = turn; k < spans; k += kJoinLanes) {
         const float2 one = a.partial[static_cast<uint64_t>(k) * a.total + r];
         const float more = fmaxf(top, one.x), base = base_of(more);
-        s = s * exp_of(top - base) + one.y * exp_of(one.x - base);
+        s = s * exp_kept(top - base) + one.y * exp_kept(one.x - base);
         top = more;
       }
     // (the lanes of a row in a tree, every half in the other's place)
@@ -314,7 +320,7 @@ __global__ __launch_bounds__(16 * kJoinLanes) void k_linear_loss_join(LossArgs a
       if (turn < half) {
         const float2 one = part[turn + half][l];
         const float more = fmaxf(top, one.x), base = base_of(more);
-        s = s * exp_of(top - base) + one.y * exp_of(one.x - base);
+        s = s * exp_kept(top - base) + one.y * exp_kept(one.x - base);
         top = more;
       }
       __syncthreads();
@@ -327,7 +333,7 @@ __global__ __launch_bounds__(16 * kJoinLanes) void k_linear_loss_join(LossArgs a
       for (uint32_t k = 1; k < 16; ++k) most = fmaxf(most, part[k][l].x);
       float sum = 0.0f;  // (a row without a finite logit: e^(NaN))
 #pragma unroll
-      for (uint32_t k = 0; k < 16; ++k) sum += part[k][l].y * exp_of(part[k][l].x - most);
+      for (uint32_t k = 0; k < 16; ++k) sum += part[k][l].y * exp_kept(part[k][l].x - most);
       const int64_t t = target_of(a, static_cast<uint32_t>(r));
       const bool learnt = t != a.ignore, inside = t >= 0 && t < a.vocab;
       const float loss = inside ? (most - a.of_target[r]) + logf(sum) : NAN;
@@ -387,7 +393,7 @@ __device__ __forceinline__ void gradient_tile(const LossArgs& a, uint32_t id, co
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q) {
         // (the minimum: an ignored row's logits may be anything, and none is above its row's maximum in any other)
-        float d = exp_of(fminf(t.sum[i][j][q] - s.top, 0.0f)) * over;
+        float d = exp_of<T>(fminf(t.sum[i][j][q] - s.top, 0.0f)) * over;
         d -= at == j * 16 + q ? kHeld<T> : 0.0f;
         t.sum[i][j][q] = last && n1 + j * 16 + q >= p.width ? 0.0f : d;
       }

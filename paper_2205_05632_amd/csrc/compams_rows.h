@@ -17,6 +17,19 @@ __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(half_t v) { return static_cast<float>(v); }
 __device__ __forceinline__ float to_float(bfloat_t v) { return static_cast<float>(v); }
 
+// e^z to three units of 2^-24 at any z: the exponent of 2 as a whole number and a part in -1/2 .. 1/2, which is formed with the
+// rounding of the product and of log2(e) put right.  (Rounded once, an exponent of 60 is off by up to 2^-19: 22 such units of the
+// result.)  Beyond 200 in size z counts as that: whatever it is, 0 or infinity is left.  A NaN stays one.
+__device__ __forceinline__ float exp_kept(float z) {
+  constexpr double kExact = 1.44269504088896340736;
+  constexpr float kLog2E = static_cast<float>(kExact), kRest = static_cast<float>(kExact - static_cast<double>(kLog2E));
+  constexpr float kShift = 0x1.8p23f;  // what is added to it is rounded to a whole number, which is in the low bits then
+  const float at = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -200.0f), 200.0f);
+  const float shifted = fmaf(at, kLog2E, kShift), whole = shifted - kShift;
+  const float part = fmaf(at, kRest, fmaf(at, kLog2E, -whole));
+  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(part), static_cast<int16_t>(__float_as_uint(shifted)));
+}
+
 // A lane works on groups of eight neighbouring columns: 16 bytes of the narrow types, and one counter of the generator.
 constexpr uint32_t kGroup = 8;
 

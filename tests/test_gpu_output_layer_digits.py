@@ -71,3 +71,25 @@ def test_dx_of_several_pieces_has_the_digits_of_fp32(n, rows, cols, vocab, dtype
     off = 4 * U * math.sqrt(2 * vocab) + 4 * U * math.sqrt(cols) * 3 + 200 * U + 2.0 ** -22
     column = dx[:, 0].double()
     assert float(column.norm()) < off * math.sqrt(n * rows) and float(column.abs().max()) < 5 * off
+
+
+@pytest.mark.parametrize("n,vocab", [(3, 8), (4, 40), (2, 130), (70, 300)])
+def test_far_entries_of_fp32_keep_their_digits(n, vocab):
+    """Probabilities down to e^-80: exact to some units of fp32 however far their logits are.  (The weight is the unit matrix and the
+    logits are eighths, so that neither they nor their distances are rounded; a row to a worker.)"""
+    g = torch.Generator().manual_seed(vocab)
+    x = -torch.randint(160, 641, (n, vocab), generator=g).double() / 8
+    x[:, 3] = 0.0
+    t = torch.randint(0, vocab, (n,), generator=g)
+    t[0] = 3
+    got = ops.compams_linear_cross_entropy(x.float().cuda(), torch.eye(vocab, device="cuda"), t.cuda(), n)
+    p = torch.softmax(x, 1)
+    hot = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
+    d = p - hot
+    # an exponential 3 U, 1 / sum (1 and terms below e^-20) 3 U, products with that, the factor and x U each; next to the target's 1
+    # the difference is rounded, and a difference of 0 may have all of p's errors
+    off = 10 * U * p + 2 * U * hot
+    close(got[2], d, off, "dx")
+    close(got[3], d[:, :, None] * x[:, None, :], (off + U * d.abs())[:, :, None] * x.abs()[:, None, :], "dweight")
+    want = torch.logsumexp(x, 1) - x.gather(1, t[:, None])[:, 0]
+    close(got[1], want, 2 * U * want.abs() + 4 * U * p.sort(1).values[:, :-1].sum(1) + 2 * U * (p.sort(1).values[:, :-1].sum(1) > 0), "losses")
