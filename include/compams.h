@@ -513,7 +513,7 @@ typedef struct compams_gated {
   void* up;   int64_t ld_up;   /* the same of b */
   /* backward */
   const void* dm; int64_t ld_dm;
-  void* dgate;    int64_t ld_dgate; /* may be gate, up or dm */
+  void* dgate;    int64_t ld_dgate; /* may be gate, up or dm, with the same ld */
   void* dup;      int64_t ld_dup;   /* may be another of them */
   float* dgate_bias; int64_t ld_dgate_bias; /* per worker, or NULL */
   float* dup_bias;   int64_t ld_dup_bias;

@@ -1,0 +1,34 @@
+// What a call reads and writes, and whether two such areas share memory.  Plain host functions.
+#pragma once
+
+#include <numeric>
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace compams {
+
+// Rows of `bytes` bytes, `ld` bytes apart: what a call reads or writes.
+struct Area {
+  const void* p;
+  int64_t rows, bytes, ld;
+};
+inline Area area(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t size) {
+  return {p, rows, cols * static_cast<int64_t>(size), ld * static_cast<int64_t>(size)};
+}
+// Whether two areas share a byte: if their extents do, and the places of their rows within the distance from row to row. (Of two
+// distances, within the largest that divides both: areas that meet nowhere there are apart.)  Nothing is shared with a null pointer.
+inline bool meet(const Area& a, const Area& b) {
+  typedef __int128 Wide;
+  if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0) return false;
+  const Wide from = reinterpret_cast<intptr_t>(b.p) - static_cast<Wide>(reinterpret_cast<intptr_t>(a.p));  // b's first byte, from a's
+  if (from >= static_cast<Wide>(a.rows - 1) * a.ld + a.bytes || -from >= static_cast<Wide>(b.rows - 1) * b.ld + b.bytes) return false;
+  if (a.rows == 1 && b.rows == 1) return true;
+  const int64_t ld = a.rows == 1 ? b.ld : b.rows == 1 ? a.ld : std::gcd(a.ld, b.ld);
+  const int64_t at = static_cast<int64_t>((from % ld + ld) % ld);
+  return at < a.bytes || at + b.bytes > ld;
+}
+// The same place: what may be written over what is read there.
+inline bool same(const Area& a, const Area& b) { return a.p == b.p && (a.rows <= 1 || a.ld == b.ld); }
+
+}  // namespace compams

@@ -578,6 +578,16 @@ int compams_gated_backward(const compams_gated* a, void* hip_stream) {
   }
   const int status = workspace_status(a->workspace, a->workspace_bytes, backward_bytes(*a));
   if (status != COMPAMS_OK) return status;
+  // (what is written over an input in other places than it is read from would be read by other workgroups)
+  const int64_t total = a->n * a->rows;
+  const Area out[] = {area(a->dgate, total, a->hidden, a->ld_dgate, size), area(a->dup, total, a->hidden, a->ld_dup, size)};
+  const Area bias[] = {area(a->dgate_bias, a->n, a->hidden, a->ld_dgate_bias, 4), area(a->dup_bias, a->n, a->hidden, a->ld_dup_bias, 4)};
+  if (meet(out[0], out[1]) || meet(bias[0], bias[1])) return COMPAMS_INVALID_ARG;
+  for (const Area& in : {area(a->dm, total, a->hidden, a->ld_dm, size), area(a->gate, total, a->hidden, a->ld_gate, size),
+                         area(a->up, total, a->hidden, a->ld_up, size)})
+    for (int i = 0; i < 2; ++i)
+      if ((meet(out[i], in) && !same(out[i], in)) || meet(bias[i], in) || meet(bias[i], out[0]) || meet(bias[i], out[1]))
+        return COMPAMS_INVALID_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const BackwardCut cut = backward_cut(*a);
   BackwardArgs k = {};

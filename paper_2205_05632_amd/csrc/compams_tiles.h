@@ -10,6 +10,7 @@
 
 #include <initializer_list>
 
+#include "compams_areas.h"
 #include "compams_rows.h"
 
 namespace compams {

@@ -1,0 +1,32 @@
+"""The operators with products on matrices that lie side by side in one buffer, on the GPU against the same call on buffers of their own."""
+import pytest
+import torch
+
+from paper_2205_05632_amd import operators as ops
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+def columns(rows, widths, dtype, seed):
+    """Matrices of these widths, side by side in one buffer with a column between them, and copies of them."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    pool = torch.randn((rows, sum(widths) + len(widths)), generator=g, device="cuda").to(dtype)
+    first = [sum(widths[:i]) + i for i in range(len(widths))]
+    views = [pool[:, a:a + w] for a, w in zip(first, widths)]
+    return views, [v.contiguous() for v in views]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,rows,hidden", [(2, 40, 24), (3, 100, 33)])
+def test_gated_backward(n, rows, hidden, dtype):
+    """Inputs and outputs between one another's rows, and outputs over their inputs."""
+    views, own = columns(n * rows, [hidden] * 5, dtype, hidden)
+    bias = torch.full((n, 2 * hidden + 1), 7.0, device="cuda")
+    want = ops.compams_gated_backward(*own[:3], n)
+    got = ops.compams_gated_backward(*views[:3], n, dgate=views[3], dup=views[4], dgate_bias=bias[:, :hidden], dup_bias=bias[:, hidden + 1:])
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool((bias[:, hidden] == 7).all())
+    assert all(torch.equal(a, b) for a, b in zip(views[:3], own[:3]))
+    got = ops.compams_gated_backward(*views[:3], n, dgate=views[2], dup=views[0])
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(views[1], own[1])

@@ -1,0 +1,48 @@
+"""Host-only checks of what calls of the operators with products refuse: outputs that lie over inputs, or over one another, where a
+kernel would read what another workgroup has written.  (The pointers are never dereferenced: these calls end before anything is enqueued.)"""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from paper_2205_05632_amd import binding as B
+from paper_2205_05632_amd import operators as ops
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+MB = 1 << 20
+ROOM = dict(workspace=1 << 40, workspace_bytes=1 << 38)
+
+
+def at(place, shift=0):
+    """A buffer of its own for every place, 16 MB apart."""
+    return (16 * place + 16) * MB + shift
+
+
+def test_areas_against_their_bytes(tmp_path):
+    """Every pair of small areas: none that share a byte is missed, and of equal distances none is taken to that does not."""
+    out = str(tmp_path / "model")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", os.path.join(os.path.dirname(HERE), "paper_2205_05632_amd", "csrc"),
+                    os.path.join(HERE, "areas_model.cpp"), "-o", out], check=True)
+    r = subprocess.run([out], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, r.stdout
+
+
+def backward(**kw):
+    a = ops.compams_gated(n=2, rows=300, hidden=8, type=ops.F32, activation=0, dm=at(0), ld_dm=8, gate=at(1), ld_gate=8, up=at(2), ld_up=8,
+                          dgate=at(3), ld_dgate=8, dup=at(4), ld_dup=8, dgate_bias=at(5), ld_dgate_bias=8, dup_bias=at(6), ld_dup_bias=8, **ROOM)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return ctypes.byref(a)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dgate=at(1), ld_dgate=16),                                     # over gate with another distance from row to row
+    dict(dup=at(0), ld_dup=16), dict(dgate=at(2), ld_dgate=9),
+    dict(dgate=at(1, 32)), dict(dup=at(2, -32)), dict(dgate=at(0, 16)),  # a row further, a row before, a part of one
+    dict(dgate=at(4, 32)), dict(dup=at(3, 299 * 32)),                   # over one another
+    dict(dgate_bias=at(6, 32)), dict(dgate_bias=at(0, 64)), dict(dup_bias=at(4, 160)),
+    dict(gate=at(1), ld_gate=24, dgate=at(1, 28), ld_dgate=24),          # beside gate's columns, but for one
+])
+def test_gated_backward_refuses_outputs_over_inputs(kw):
+    assert B.lib().compams_gated_backward(backward(**kw), None) == -1
