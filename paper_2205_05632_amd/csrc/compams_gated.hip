@@ -526,6 +526,15 @@ int compams_gated_forward(const compams_gated* a, void* hip_stream) {
   if (a->m == a->gate || a->m == a->up || (a->gate && a->gate == a->up)) return COMPAMS_INVALID_ARG;
   const int status = workspace_status(a->workspace, a->workspace_bytes, forward_bytes(*a));
   if (status != COMPAMS_OK) return status;
+  // (other workgroups still read the inputs)
+  const int64_t total = a->n * a->rows;
+  const Area out[] = {area(a->m, total, a->hidden, a->ld_m, size), area(a->gate, total, a->hidden, a->ld_gate, size),
+                      area(a->up, total, a->hidden, a->ld_up, size)};
+  if (meet(out[0], out[1]) || meet(out[0], out[2]) || meet(out[1], out[2])) return COMPAMS_INVALID_ARG;
+  for (const Area& in : {area(a->x, total, a->cols, a->ld_x, size), area(a->gate_weight, a->hidden, a->cols, a->ld_gate_weight, size),
+                         area(a->up_weight, a->hidden, a->cols, a->ld_up_weight, size), area(a->gate_bias, 1, a->hidden, 0, 4),
+                         area(a->up_bias, 1, a->hidden, 0, 4)})
+    if (meet(out[0], in) || meet(out[1], in) || meet(out[2], in)) return COMPAMS_INVALID_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   ForwardArgs k = {};
   const Operands o = operands(*a);

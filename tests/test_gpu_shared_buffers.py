@@ -30,3 +30,14 @@ def test_gated_backward(n, rows, hidden, dtype):
     assert all(torch.equal(a, b) for a, b in zip(views[:3], own[:3]))
     got = ops.compams_gated_backward(*views[:3], n, dgate=views[2], dup=views[0])
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(views[1], own[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,hidden", [(1, 40, 24), (30, 56, 17), (200, 64, 48)])
+def test_gated_forward(rows, cols, hidden, dtype):
+    (x, m, gate, up), own = columns(rows, [cols, hidden, hidden, hidden], dtype, hidden)
+    (wg, wu), w = columns(hidden, [cols] * 2, dtype, rows)
+    want = ops.compams_gated_forward(own[0], *w)
+    got = ops.compams_gated_forward(x, wg, wu, m=m, gate=gate, up=up)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(x, own[0])
+    assert torch.equal(wg, w[0]) and torch.equal(wu, w[1])

@@ -46,3 +46,22 @@ def backward(**kw):
 ])
 def test_gated_backward_refuses_outputs_over_inputs(kw):
     assert B.lib().compams_gated_backward(backward(**kw), None) == -1
+
+
+def forward(**kw):
+    a = ops.compams_gated(n=2, rows=300, cols=16, hidden=8, type=ops.F32, activation=0, x=at(0), ld_x=16, gate_weight=at(1), ld_gate_weight=16,
+                          up_weight=at(2), ld_up_weight=16, gate_bias=at(3), up_bias=at(4), m=at(5), ld_m=8, gate=at(6), ld_gate=8, up=at(7),
+                          ld_up=8, **ROOM)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return ctypes.byref(a)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(m=at(0)), dict(m=at(0), ld_m=16), dict(gate=at(0), ld_gate=16), dict(up=at(0, 32), ld_up=16),     # x
+    dict(n=1, rows=1, m=at(0)), dict(n=1, rows=1, gate=at(1)),           # a token
+    dict(m=at(1)), dict(up=at(2, 7 * 64)), dict(gate=at(3, 28)), dict(m=at(4)),
+    dict(m=at(6, 32)), dict(gate=at(7, 599 * 32)), dict(up=at(5, 4)),    # one another
+])
+def test_gated_forward_refuses_outputs_over_inputs(kw):
+    assert B.lib().compams_gated_forward(forward(**kw), None) == -1
