@@ -31,4 +31,18 @@ inline bool meet(const Area& a, const Area& b) {
 // The same place: what may be written over what is read there.
 inline bool same(const Area& a, const Area& b) { return a.p == b.p && (a.rows <= 1 || a.ld == b.ld); }
 
+// A weight's gradients, for n workers a matrix of floats each: as an area, a worker's extent to a row.
+struct Gradients {
+  const float* p;
+  int64_t n, rows, cols, ld, stride;
+  Area extents() const { return area(p, n, (rows - 1) * (rows > 1 ? ld : 0) + cols, stride, sizeof(float)); }
+  Area of(int64_t worker) const { return area(p + worker * stride, rows, cols, ld, sizeof(float)); }
+};
+// Whether the gradients of two weights share memory, as far as a worker's and its neighbour's show.
+inline bool meet(const Gradients& a, const Gradients& b) {
+  if (!a.p || !b.p) return false;
+  if (meet(a.of(0), b.of(0))) return true;
+  return a.n > 1 && (meet(a.of(0), b.of(1)) || meet(a.of(1), b.of(0)));
+}
+
 }  // namespace compams

@@ -194,6 +194,18 @@ int compams_projections_backward(const compams_projections* a, void* hip_stream)
   }
   const int status = workspace_status(a->workspace, a->workspace_bytes, projections_bytes(*a));
   if (status != COMPAMS_OK) return status;
+  // (other workgroups still read the inputs)
+  const Gradients of_weight[] = {{dweight[0], a->n, a->hidden, a->cols, ld[0], stride[0]},
+                                 {dweight[1], a->n, a->hidden, a->cols, ld[1], stride[1]}};
+  if (meet(of_weight[0], of_weight[1])) return COMPAMS_INVALID_ARG;
+  const auto as_area = [&](const Matrix& m) { return area(m.p, m.rows, m.cols, m.ld, m.size); };
+  const Area dx = area(a->dx, a->n * a->rows, a->cols, a->ld_dx, size), none = {};
+  const Area extents[] = {of_weight[0].extents(), of_weight[1].extents()};
+  const bool weights = dweight[0] || dweight[1];
+  if (meet(extents[0], dx) || meet(extents[1], dx)) return COMPAMS_INVALID_ARG;
+  for (const Area& in : {as_area(o.d[0]), as_area(o.d[1]), weights ? as_area(o.x) : none, a->dx ? as_area(o.weight[0]) : none,
+                         a->dx ? as_area(o.weight[1]) : none})
+    if (meet(dx, in) || meet(extents[0], in) || meet(extents[1], in)) return COMPAMS_INVALID_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   ProjectionArgs k = {};
   if (a->rows > 0) {

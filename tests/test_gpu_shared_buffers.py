@@ -41,3 +41,18 @@ def test_gated_forward(rows, cols, hidden, dtype):
     got = ops.compams_gated_forward(x, wg, wu, m=m, gate=gate, up=up)
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(x, own[0])
     assert torch.equal(wg, w[0]) and torch.equal(wu, w[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,rows,cols,hidden", [(1, 3, 8, 5), (2, 40, 24, 16), (3, 70, 33, 24)])
+def test_projections_backward(n, rows, cols, hidden, dtype):
+    """The weights' gradients between one another's columns and between one another's workers, and a whole buffer for the rest."""
+    views, own = columns(n * rows, [hidden, hidden, cols, cols], dtype, hidden)
+    (wg, wu), w = columns(hidden, [cols] * 2, dtype, rows)
+    want = ops.compams_projections_backward(*own[:3], *w, n)
+    sides = torch.full((n, hidden, 2 * cols + 1), 7.0, device="cuda")
+    turns = torch.full((hidden, 2, n, cols), 7.0, device="cuda")
+    for dwg, dwu in ((sides[:, :, :cols], sides[:, :, cols + 1:]), (turns[:, 0].transpose(0, 1), turns[:, 1].transpose(0, 1))):
+        got = ops.compams_projections_backward(*views[:3], wg, wu, n, dx=views[3], dgate_weight=dwg, dup_weight=dwu)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(torch.equal(a, b) for a, b in zip(views[:3], own[:3]))
+    assert bool((sides[:, :, cols] == 7).all())

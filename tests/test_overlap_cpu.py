@@ -65,3 +65,24 @@ def forward(**kw):
 ])
 def test_gated_forward_refuses_outputs_over_inputs(kw):
     assert B.lib().compams_gated_forward(forward(**kw), None) == -1
+
+
+def projections(**kw):
+    a = ops.compams_projections(n=2, rows=300, cols=16, hidden=8, type=ops.F32, dgate=at(0), ld_dgate=8, dup=at(1), ld_dup=8, x=at(2), ld_x=16,
+                                gate_weight=at(3), ld_gate_weight=16, up_weight=at(4), ld_up_weight=16, dx=at(5), ld_dx=16,
+                                dgate_weight=at(6), ld_dgate_weight=16, stride_dgate_weight=1024, dup_weight=at(7), ld_dup_weight=16,
+                                stride_dup_weight=1024, **ROOM)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return ctypes.byref(a)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dx=at(0)), dict(dx=at(0), ld_dx=32), dict(dx=at(1)), dict(dx=at(2)), dict(dx=at(2, 64)), dict(dx=at(3)), dict(dx=at(4, 64)),
+    dict(dx=at(6)), dict(dx=at(7, 4096)), dict(dgate_weight=at(0)), dict(dup_weight=at(2)), dict(dgate_weight=at(4)),
+    dict(dup_weight=at(6, 7 * 64)), dict(dup_weight=at(6, 4096)), dict(dgate_weight=at(7, 4096 + 60)),      # one another's, of one worker or two
+    dict(ld_dgate_weight=32, ld_dup_weight=32, dup_weight=at(6, 60)),    # beside one another's columns, but for one
+    dict(dup=None, up_weight=None, dup_weight=None, dx=at(0)), dict(dup=None, up_weight=None, dup_weight=None, dgate_weight=at(2)),
+])
+def test_projections_refuse_outputs_over_inputs(kw):
+    assert B.lib().compams_projections_backward(projections(**kw), None) == -1
