@@ -17,10 +17,10 @@ inline Area area(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t s
   return {p, rows, cols * static_cast<int64_t>(size), ld * static_cast<int64_t>(size)};
 }
 // Whether two areas share a byte: if their extents do, and the places of their rows within the distance from row to row. (Of two
-// distances, within the largest that divides both: areas that meet nowhere there are apart.)  Nothing is shared with a null pointer.
+// distances, within the largest that divides both: areas that meet nowhere there are apart.)  Nothing is shared with what is empty, or a null pointer.
 inline bool meet(const Area& a, const Area& b) {
   typedef __int128 Wide;
-  if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0) return false;
+  if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0 || a.bytes <= 0 || b.bytes <= 0) return false;
   const Wide from = reinterpret_cast<intptr_t>(b.p) - static_cast<Wide>(reinterpret_cast<intptr_t>(a.p));  // b's first byte, from a's
   if (from >= static_cast<Wide>(a.rows - 1) * a.ld + a.bytes || -from >= static_cast<Wide>(b.rows - 1) * b.ld + b.bytes) return false;
   if (a.rows == 1 && b.rows == 1) return true;

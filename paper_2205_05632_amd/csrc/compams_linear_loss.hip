@@ -730,6 +730,19 @@ int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream)
   const Room room = room_of(*a);
   const int status = workspace_status(a->workspace, a->workspace_bytes, room.all());
   if (status != COMPAMS_OK) return status;
+  // (what is written while it is still read, here or by a later launch; x is read for the last time before the launch that writes dx)
+  const int64_t total = a->n * a->rows;
+  const Area in[] = {area(a->x, total, a->cols, a->ld_x, size), area(a->weight, a->vocab, a->cols, a->ld_weight, size),
+                     area(a->targets, 1, total, 0, type_size(a->target_type))};
+  const Area out[] = {area(a->dx, total, a->cols, a->ld_dx, size),
+                      Gradients{a->dweight, a->n, a->vocab, a->cols, a->ld_dweight, a->stride_dweight}.extents(),
+                      area(a->losses, 1, total, 0, 4), area(a->mean_loss, 1, a->n, 0, 4)};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return COMPAMS_INVALID_ARG;
+    for (int j = i == 0 ? 1 : 0; j < 3; ++j)
+      if (total && meet(out[i], in[j])) return COMPAMS_INVALID_ARG;
+  }
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   LossArgs k = {};
   char* at = static_cast<char*>(a->workspace);

@@ -11,8 +11,8 @@ int main() {
   const char* const base = reinterpret_cast<const char*>(1 << 20);
   std::vector<Area> all;
   for (int64_t rows = 0; rows <= 4; ++rows)
-    for (int64_t bytes = 1; bytes <= 4; ++bytes)
-      for (int64_t ld = rows <= 1 ? 0 : bytes; ld <= (rows <= 1 ? 0 : 7); ++ld) all.push_back({base, rows, bytes, ld});
+    for (int64_t bytes = 0; bytes <= 4; ++bytes)
+      for (int64_t ld = rows <= 1 ? 0 : bytes ? bytes : 1; ld <= (rows <= 1 ? 0 : 7); ++ld) all.push_back({base, rows, bytes, ld});
   int64_t exact = 0, wrong = 0, cautious = 0;
   for (const Area& a : all)
     for (const Area& b0 : all)
@@ -21,7 +21,7 @@ int main() {
         b.p = base + at;
         bool shared = false;
         for (int64_t i = 0; i < a.rows; ++i)
-          for (int64_t j = 0; j < b.rows; ++j) shared |= at + j * b.ld < i * a.ld + a.bytes && i * a.ld < at + j * b.ld + b.bytes;
+          for (int64_t j = 0; j < b.rows; ++j) shared |= a.bytes && b.bytes && at + j * b.ld < i * a.ld + a.bytes && i * a.ld < at + j * b.ld + b.bytes;
         const bool met = compams::meet(a, b);
         if (met == shared) ++exact;
         // only of two distances may areas be taken to meet that do not

@@ -56,3 +56,17 @@ def test_projections_backward(n, rows, cols, hidden, dtype):
         got = ops.compams_projections_backward(*views[:3], wg, wu, n, dx=views[3], dgate_weight=dwg, dup_weight=dwu)
         assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(torch.equal(a, b) for a, b in zip(views[:3], own[:3]))
     assert bool((sides[:, :, cols] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,rows,cols,vocab", [(1, 3, 8, 5), (2, 40, 24, 70), (3, 70, 33, 300)])
+def test_linear_cross_entropy(n, rows, cols, vocab, dtype):
+    """x and dx between one another's rows, the weight's gradients between something else's."""
+    (x, dx), own = columns(n * rows, [cols, cols], dtype, vocab)
+    (w, _), of_w = columns(vocab, [cols] * 2, dtype, rows)
+    t = torch.randint(0, vocab, (n * rows,), generator=torch.Generator().manual_seed(1)).cuda()
+    want = ops.compams_linear_cross_entropy(own[0], of_w[0], t, n)
+    room = torch.full((n, vocab, cols + 3), 7.0, device="cuda")
+    got = ops.compams_linear_cross_entropy(x, w, t, n, dx=dx, dweight=room[:, :, 2:2 + cols])
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(x, own[0]) and torch.equal(w, of_w[0])
+    assert bool((room[:, :, :2] == 7).all()) and bool((room[:, :, -1] == 7).all())

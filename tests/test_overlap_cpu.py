@@ -86,3 +86,21 @@ def projections(**kw):
 ])
 def test_projections_refuse_outputs_over_inputs(kw):
     assert B.lib().compams_projections_backward(projections(**kw), None) == -1
+
+
+def linear_loss(**kw):
+    a = ops.compams_linear_loss(n=2, rows=300, cols=16, vocab=50, type=ops.F32, target_type=ops.I64, x=at(0), ld_x=16, weight=at(1), ld_weight=16,
+                                targets=at(2), grad_scale=1.0, mean_loss=at(3), losses=at(4), dx=at(5), ld_dx=16, dweight=at(6), ld_dweight=16,
+                                stride_dweight=1024, **ROOM)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return ctypes.byref(a)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dx=at(1)), dict(dx=at(1, 49 * 64)), dict(dx=at(1), ld_dx=32), dict(dx=at(2)), dict(dx=at(6, 4096)), dict(dweight=at(0)),
+    dict(dweight=at(1)), dict(dweight=at(1, -64)), dict(dweight=at(2, 8)), dict(losses=at(0, 4)), dict(losses=at(2)), dict(mean_loss=at(4, 4)),
+    dict(mean_loss=at(1)), dict(losses=at(5)), dict(dx=at(4, -599 * 64)),
+])
+def test_linear_cross_entropy_refuses_outputs_over_inputs(kw):
+    assert B.lib().compams_linear_cross_entropy(linear_loss(**kw), None) == -1
