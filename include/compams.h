@@ -589,8 +589,9 @@ int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream)
  *   to = factors[i] * from
  * A worker whose gradient holds a NaN or an infinity has a norm that says so, factors[i] = 0 and zeros in `to`: it takes no
  * part in the step.  Squares and their sums are fp64, so no finite gradient has a norm beyond range or below it, in
- * fp32 or narrower types, unless the norm itself is.  Rows that are written lie over no other tensor's, so none is listed
- * twice: such calls are refused where a first row shows it. */
+ * fp32 or narrower types, unless the norm itself is.  Rows that are written lie over no
+ * other worker's and no other tensor's, so none is listed twice: such calls are refused where a tensor's own rows, or the first
+ * worker's, show it. */
 typedef struct compams_clip_tensor {
   const void* from; int64_t ld_from; /* n rows of `count` entries, ld_from entries apart */
   void* to;         int64_t ld_to;   /* the same, or NULL: nothing is written; may be `from` where both have one type */

@@ -261,9 +261,15 @@ int check(const compams_clip* a) {
   // (a launch's workgroups of one worker: 2^24 in a dimension of 2^32 threads)
   return chunks < (1u << 24) - 1 ? COMPAMS_OK : COMPAMS_INVALID_ARG;
 }
-// Whether a worker's first rows that are written lie over others: a tensor that is listed twice would be scaled twice, or once.
-// (Rows that are only read may be the same.)
+// Whether what is written lies over nothing that is read elsewhere: no worker's rows of a tensor over another worker's, which would be
+// scaled before they are read, and of the first worker no tensor's rows over another's: a tensor that is listed twice would be scaled
+// twice, or once.  (Rows that are only read may be the same.)
 bool apart(const compams_clip& a) {
+  for (int32_t i = 0; i < a.tensors; ++i) {
+    const compams_clip_tensor& t = a.tensor[i];
+    if (t.to != t.from && meet(area(t.from, a.n, t.count, t.ld_from, type_size(t.from_type)), area(t.to, a.n, t.count, t.ld_to, type_size(t.to_type))))
+      return false;
+  }
   struct Row {
     const char *begin, *end;
     bool written;

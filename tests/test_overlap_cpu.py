@@ -104,3 +104,22 @@ def linear_loss(**kw):
 ])
 def test_linear_cross_entropy_refuses_outputs_over_inputs(kw):
     assert B.lib().compams_linear_cross_entropy(linear_loss(**kw), None) == -1
+
+
+def clip(n, **kw):
+    t = ops.compams_clip_tensor(**{"from": at(0), "ld_from": 100, "to": at(1), "ld_to": 100, "count": 40, "from_type": ops.F32, "to_type": ops.F32, **kw})
+    a = ops.compams_clip(n=n, tensors=1, tensor=ctypes.addressof(t), max_norm=1.0, scale=1.0, norms=at(2), factors=at(3), workspace=at(4),
+                         workspace_bytes=255)
+    a.table = t
+    return a
+
+
+@pytest.mark.parametrize("n,kw,code", [
+    (3, {"to": at(0, 400)}, -1), (3, {"to": at(0, -800)}, -1), (3, {"to": at(0, 2 * 400 + 156)}, -1), (3, {"to": at(0, 300)}, -1),
+    (4, {"to": at(0, 800), "ld_to": 50}, -1), (2, {"from_type": ops.F16, "to": at(0, 200)}, -1),
+    # side by side, behind one another, of one worker (what is refused is the workspace)
+    (3, {"to": at(0, 160)}, -3), (3, {"to": at(0, 400 + 240)}, -3), (3, {"to": at(0, 1200)}, -3), (1, {"to": at(0, 400)}, -3),
+    (3, {"to": at(0, 160), "ld_to": 200}, -3), (3, {}, -3),
+])
+def test_clip_refuses_rows_over_another_workers(n, kw, code):
+    assert B.lib().compams_clip_gradients(ctypes.byref(clip(n, **kw)), None) == code
