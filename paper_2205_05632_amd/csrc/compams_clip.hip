@@ -41,7 +41,8 @@ struct ClipArgs {
   float max_norm, scale;
   Tensor tensor[kMostTensors];
 };
-// Parts of a worker: every workgroup that scales a chunk adds them up for itself, four to a lane.
+// Parts of a worker, and one more for each launch of kMostTensors tensors at most, whose last part may be a small one.  Every
+// workgroup that scales a chunk adds them up for itself, some four to a lane.
 constexpr uint32_t kMostParts = 1024;
 
 // The tensor that chunk number c is of.
@@ -171,7 +172,7 @@ __device__ __forceinline__ float factor_of(const ClipArgs& a, uint32_t w, double
   return factor;
 }
 
-// The factors of many chunks, once for all of them.
+// The factors of many chunks, once for all of them, or of a call that writes nothing else.
 __global__ __launch_bounds__(kThreads) void k_clip_factor(ClipArgs a) {
   __shared__ double slots[kThreads / 64];
   const float factor = factor_of(a, blockIdx.x, slots, true);
@@ -390,13 +391,15 @@ int compams_clip_gradients(const compams_clip* a, void* hip_stream) {
   if (cut.chunks == 0) {
     hipLaunchKernelGGL(k_clip_none, dim3((n + kThreads - 1) / kThreads), dim3(kThreads), 0, stream, k);
   } else {
+    bool written = false;
+    for (int32_t i = 0; i < a->tensors; ++i) written = written || (a->tensor[i].to && a->tensor[i].count);
     const bool past = cut.bytes * n > kStreamBytes;
     by_launch(*a, k, [&](const ClipArgs& l) {
       if (past) hipLaunchKernelGGL(k_clip_norm<true>, dim3(l.parts, n), dim3(kThreads), 0, stream, l);
       else hipLaunchKernelGGL(k_clip_norm<false>, dim3(l.parts, n), dim3(kThreads), 0, stream, l);
     });
-    if (past) hipLaunchKernelGGL(k_clip_factor, dim3(n), dim3(kThreads), 0, stream, k);
-    by_launch(*a, k, [&](const ClipArgs& l) {
+    if (past || !written) hipLaunchKernelGGL(k_clip_factor, dim3(n), dim3(kThreads), 0, stream, k);
+    if (written) by_launch(*a, k, [&](const ClipArgs& l) {
       if (past) hipLaunchKernelGGL(k_clip_scale<true>, dim3(l.chunks, n), dim3(kThreads), 0, stream, l);
       else hipLaunchKernelGGL(k_clip_scale<false>, dim3(l.chunks, n), dim3(kThreads), 0, stream, l);
     });
