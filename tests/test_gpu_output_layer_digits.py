@@ -16,13 +16,13 @@ TYPES = [F32, F16, BF16]
 IDS = ["f32", "f16", "bf16"]
 
 
-def gradient(x, w, t, n, grad_scale, dtype):
-    """dx and its bound where no row is ignored.  A probability p is off by its logit's error and its maximum's, by the sum of the
-    exponentials (64 of a span, the spans in chains) and by 4 U (z + 3) at a distance z; d by that and 4 U.  16 bits: two parts of
-    2^14 d hold it to 2^-22 of itself or 2^-38, and an entry of bfloat16's weight is lost below 2^-38 of its column's largest.  The
-    sum of dx goes once through the vocabulary for each part."""
+def gradients(x, w, t, n, grad_scale, dtype):
+    """(dx, dweight) and their bounds where no row is ignored.  A probability p is off by its logit's error and its maximum's, by the
+    sum of the exponentials (64 of a span, the spans in chains) and by 4 U (z + 3) at a distance z; d by that and 4 U.  16 bits: two
+    parts of 2^14 d hold it to 2^-22 of itself or 2^-38, and an entry of bfloat16's operands is off by 2^-38 of its column's largest.
+    Both sums go once through their terms for each part."""
     total, cols = x.shape
-    vocab, parts = w.shape[0], 1 if dtype == F32 else 2
+    vocab, rows, parts = w.shape[0], total // n, 1 if dtype == F32 else 2
     logits = x @ w.t()
     off_l = P.sums(x, w.t(), cols)
     away = logits.amax(1, keepdim=True) - logits
@@ -33,16 +33,21 @@ def gradient(x, w, t, n, grad_scale, dtype):
     off_d = p * (off_s + 4 * U * (away + 3) + 2 * off_l) + 4 * U * (p + hot) + 2.0 ** -140
     if parts == 2:
         off_d = off_d + 2.0 ** -22 * d.abs() + 2.0 ** -38
-    f = grad_scale / (total // n)
-    lost = 2.0 ** -38 * w.abs().amax(0) * d.abs().sum(1, keepdim=True) if dtype == BF16 else 0.0
-    off = f * (off_d @ w.abs() + P.sums(d, w, parts * vocab) + 4 * U * (d.abs() @ w.abs()) + lost)
+    f, lost = grad_scale / rows, 2.0 ** -38 if dtype == BF16 else 0.0
+
+    def product(off, a, b, terms):
+        return f * (off @ b.abs() + P.sums(a, b, parts * terms) + 4 * U * (a.abs() @ b.abs()) + lost * b.abs().amax(0) * a.abs().sum(1, keepdim=True))
+
     dx = f * (d @ w)
-    return dx, rounding(dx, dtype) + 1.01 * off + LEAST[dtype]
+    of = lambda v, i: v[i * rows:(i + 1) * rows]  # noqa: E731
+    dw = torch.stack([f * (of(d, i).t() @ of(x, i)) for i in range(n)])
+    off_w = torch.stack([product(of(off_d, i).t(), of(d, i).t(), of(x, i), rows) for i in range(n)])
+    return (dx, dw), (rounding(dx, dtype) + 1.01 * product(off_d, d, w, vocab) + LEAST[dtype], off_w + U * dw.abs() + 2.0 ** -140)
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 @pytest.mark.parametrize("n,rows,cols,vocab", [(2, 33, 8, 32), (1, 100, 16, 64), (3, 20, 40, 300), (1, 300, 24, 1100), (1, 9, 16, 5000)])
-def test_dx_has_the_digits_of_fp32(n, rows, cols, vocab, dtype):
+def test_gradients_have_the_digits_of_fp32(n, rows, cols, vocab, dtype):
     """Every entry of dx is rounded once, and what it is rounded from has fp32's error: in columns whose terms cancel it shows.  (A
     gradient's entries add up to 0, so the first column's is 0: its weights are all 1.)"""
     rng = np.random.default_rng(vocab)
@@ -51,9 +56,9 @@ def test_dx_has_the_digits_of_fp32(n, rows, cols, vocab, dtype):
     x[:, 0], w[:, 0] = 0.0, 1.0
     w[:, 1] = (1.0 + w[:, 1].float() / 64).to(dtype)
     t = torch.from_numpy(rng.integers(0, vocab, n * rows))
-    dx = ops.compams_linear_cross_entropy(x.cuda(), w.cuda(), t.cuda(), n, -100, float(rows))[2]
-    want, bound = gradient(x.double(), w.double(), t, n, float(rows), dtype)
-    close(dx, want, bound, "dx")
+    got = ops.compams_linear_cross_entropy(x.cuda(), w.cuda(), t.cuda(), n, -100, float(rows))[2:]
+    for g, want, bound, what in zip(got, *gradients(x.double(), w.double(), t, n, float(rows), dtype), ("dx", "dweight")):
+        close(g, want, bound, what)
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
