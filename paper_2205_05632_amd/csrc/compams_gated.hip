@@ -214,7 +214,10 @@ __device__ __forceinline__ typename Fragment<T>::type load_piece(const char* row
   }
   return v;
 }
-constexpr uint32_t kFewRows = 64;
+// Up to 32 rows, and up to 64 where every workgroup has a compute unit of its own.  (us, this and tiles: 32 rows of bfloat16, 4096 x 4096 17.1
+// and 29.5, 2048 x 8192 17.2 and 17.1; 64 rows 26.6 and 29.6, 768 x 2048 9.1 and 8.0, 4096 x 1024 25.6 and 19.3, 2048 x 8192 27.2 and 17.2; fp32
+// 64 rows 50 and 84, 15.3 and 18.4, 48 and 83, 79 and 44.)
+inline bool few_rows(int64_t total, int64_t hidden) { return total <= 32 || (total <= 64 && hidden <= 16 * 256); }
 
 template <typename T, int ACT, uint32_t FM, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * 64) void k_gated_few(ForwardArgs a) {
@@ -313,7 +316,7 @@ void launch_few(const ForwardArgs& a, int act, hipStream_t stream) {
 }
 template <typename T>
 void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
-  if (a.total <= kFewRows) return launch_few<T>(a, act, stream);
+  if (few_rows(a.total, a.hidden)) return launch_few<T>(a, act, stream);
   switch (tile_size({{a.total, 2 * static_cast<uint64_t>(a.hidden), 1, a.cols}}, sizeof(T) == 4)) {
     case kTile256: launch_forward<T, 4, 2, 4, 8>(a, act, stream); break;  // (64 columns of a projection to a wavefront)
     case kTile128: launch_forward<T, 2, 2, 4, 4>(a, act, stream); break;
@@ -469,7 +472,7 @@ Operands operands(const compams_gated& a) {
           {a.up_weight, a.ld_up_weight, a.hidden, a.cols, size}};
 }
 size_t forward_bytes(const compams_gated& a) {
-  if (a.n * a.rows <= kFewRows) return 0;
+  if (few_rows(a.n * a.rows, a.hidden)) return 0;
   const Operands o = operands(a);
   return o.x.packed_bytes() + o.gate.packed_bytes() + o.up.packed_bytes();
 }
@@ -539,7 +542,7 @@ int compams_gated_forward(const compams_gated* a, void* hip_stream) {
   ForwardArgs k = {};
   const Operands o = operands(*a);
   const auto as_is = [&](const Matrix& m) { return Read{m.p, m.ld * static_cast<int64_t>(size)}; };
-  if (a->n * a->rows <= kFewRows) {
+  if (few_rows(a->n * a->rows, a->hidden)) {
     k.x = as_is(o.x);
     k.gate_weight = as_is(o.gate);
     k.up_weight = as_is(o.up);
