@@ -479,7 +479,9 @@ int compams_cross_entropy(const compams_loss* a, void* hip_stream);
  *   - Products are formed from the operands as they are, with fp32 sums.
  *   - cols and hidden are at most COMPAMS_MOST_ENTRIES.
  *   - Operands whose rows do not all begin on 16 bytes are first copied into the workspace, so the workspace's size depends on
- *     pointers and strides too: ask with the fields that the call gets. */
+ *     pointers and strides too: ask with the fields that the call gets.
+ *   - Matrices may lie side by side in one buffer.  An output that shares memory with an input or another output, where no "may
+ *     be" allows it, is refused (COMPAMS_INVALID_ARG) as far as pointers and strides show it. */
 #define COMPAMS_MOST_ENTRIES (1 << 20)
 enum {
   COMPAMS_SILU = 0,      /* a / (1 + exp(-a)) */
@@ -555,11 +557,11 @@ int compams_projections_backward(const compams_projections* a, void* hip_stream)
 /* Softmax cross-entropy of an output layer, with logits weight x that are never stored: compams_cross_entropy's mean_loss and
  * losses of these logits (in fp32), and, with its dlogits d in fp32,
  *   dx = weight' d,  dweight = the sum over the worker's rows of d x'
- * The vocabulary is gone over twice, in pieces the second time.  A piece's gradients d, before grad_scale / count, are held in the
- * workspace: in fp32 where `type` is, with every probability's own digits; else as two float16 numbers, whose sum is off by 2^-23 of
- * d or by 2^-39 (d's entries are at most 1).  For these products bfloat16 x and weights become float16, every column (x: of a worker)
- * times a power of two: entries are off by up to 2^-39 of their column's largest.  Ignored rows: loss and dx are 0 and nothing is added to dweight, whatever x
- * holds there. */
+ * The vocabulary is gone over twice, in pieces the second time.  A piece's gradients d, before grad_scale / count, are held in
+ * the workspace: in fp32 where `type` is, with every probability's own digits; else as two float16 numbers, whose sum is off by
+ * 2^-23 of d or by 2^-39 (d's entries are at most 1).  For these products bfloat16 x and weights become float16, every column
+ * (x: of a worker) times a power of two: entries are off by up to 2^-39 of their column's largest.  Ignored rows: loss and dx
+ * are 0 and nothing is added to dweight, whatever x holds there. */
 typedef struct compams_linear_loss {
   int32_t n;
   int64_t rows, cols;
@@ -589,9 +591,9 @@ int compams_linear_cross_entropy(const compams_linear_loss* a, void* hip_stream)
  *   to = factors[i] * from
  * A worker whose gradient holds a NaN or an infinity has a norm that says so, factors[i] = 0 and zeros in `to`: it takes no
  * part in the step.  Squares and their sums are fp64, so no finite gradient has a norm beyond range or below it, in
- * fp32 or narrower types, unless the norm itself is.  Rows that are written lie over no
- * other worker's and no other tensor's, so none is listed twice: such calls are refused where a tensor's own rows, or the first
- * worker's, show it. */
+ * fp32 or narrower types, unless the norm itself is.  max_norm and scale are fp32 numbers; a factor is rounded to one once.  Rows
+ * that are written lie over no other worker's and no other tensor's, so none is listed twice: such calls are refused where a
+ * tensor's own rows, or the first worker's, show it. */
 typedef struct compams_clip_tensor {
   const void* from; int64_t ld_from; /* n rows of `count` entries, ld_from entries apart */
   void* to;         int64_t ld_to;   /* the same, or NULL: nothing is written; may be `from` where both have one type */

@@ -16,15 +16,19 @@ struct Area {
 inline Area area(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t size) {
   return {p, rows, cols * static_cast<int64_t>(size), ld * static_cast<int64_t>(size)};
 }
-// Whether two areas share a byte: if their extents do, and the places of their rows within the distance from row to row. (Of two
-// distances, within the largest that divides both: areas that meet nowhere there are apart.)  Nothing is shared with what is empty, or a null pointer.
+// Whether two areas share a byte: if their extents do, and the places of their rows within the distance from row to row.  (Of
+// two distances, within the largest that divides both: areas that meet nowhere there are apart.)  What is empty, and a null
+// pointer, shares nothing.
 inline bool meet(const Area& a, const Area& b) {
   typedef __int128 Wide;
   if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0 || a.bytes <= 0 || b.bytes <= 0) return false;
-  const Wide from = reinterpret_cast<intptr_t>(b.p) - static_cast<Wide>(reinterpret_cast<intptr_t>(a.p));  // b's first byte, from a's
-  if (from >= static_cast<Wide>(a.rows - 1) * a.ld + a.bytes || -from >= static_cast<Wide>(b.rows - 1) * b.ld + b.bytes) return false;
+  const auto extent = [](const Area& v) { return static_cast<Wide>(v.rows - 1) * v.ld + v.bytes; };
+  // b's first byte, from a's
+  const Wide from = reinterpret_cast<intptr_t>(b.p) - static_cast<Wide>(reinterpret_cast<intptr_t>(a.p));
+  if (from >= extent(a) || -from >= extent(b)) return false;
   if (a.rows == 1 && b.rows == 1) return true;
   const int64_t ld = a.rows == 1 ? b.ld : b.rows == 1 ? a.ld : std::gcd(a.ld, b.ld);
+  if (ld <= 0) return true;
   const int64_t at = static_cast<int64_t>((from % ld + ld) % ld);
   return at < a.bytes || at + b.bytes > ld;
 }

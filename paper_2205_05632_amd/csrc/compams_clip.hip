@@ -262,13 +262,14 @@ int check(const compams_clip* a) {
   // (a launch's workgroups of one worker: 2^24 in a dimension of 2^32 threads)
   return chunks < (1u << 24) - 1 ? COMPAMS_OK : COMPAMS_INVALID_ARG;
 }
-// Whether what is written lies over nothing that is read elsewhere: no worker's rows of a tensor over another worker's, which would be
-// scaled before they are read, and of the first worker no tensor's rows over another's: a tensor that is listed twice would be scaled
-// twice, or once.  (Rows that are only read may be the same.)
+// Whether what is written lies over nothing that is read elsewhere: no worker's rows of a tensor over another worker's, which
+// would be scaled before they are read, and of the first worker no tensor's rows over another's: a tensor that is listed twice
+// would be scaled twice, or once.  (Rows that are only read may be the same.)
 bool apart(const compams_clip& a) {
   for (int32_t i = 0; i < a.tensors; ++i) {
     const compams_clip_tensor& t = a.tensor[i];
-    if (t.to != t.from && meet(area(t.from, a.n, t.count, t.ld_from, type_size(t.from_type)), area(t.to, a.n, t.count, t.ld_to, type_size(t.to_type))))
+    if (t.to != t.from && meet(area(t.from, a.n, t.count, t.ld_from, type_size(t.from_type)),
+                               area(t.to, a.n, t.count, t.ld_to, type_size(t.to_type))))
       return false;
   }
   struct Row {
@@ -355,7 +356,9 @@ void by_launch(const compams_clip& a, ClipArgs& k, Launch launch) {
   }
 }
 
-// Gradients that no cache holds until they are read again.
+// Gradients that no cache holds until they are read again.  (us by size, through the caches and past them: into other rows
+// 128 MB 66 and 68, 160 84 and 84, 192 104 and 99, 224 126 and 115; in place 128 65 and 70, 192 91 and 101, 256 122 and 133, 384
+// 206 and 195.)
 constexpr uint64_t kStreamBytes = 192u << 20;
 
 }  // namespace

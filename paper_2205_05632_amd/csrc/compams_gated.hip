@@ -64,8 +64,8 @@ __device__ __forceinline__ float activate_fast(float a, float& slope) {
 
 // The same for fp32 results, which keep their digits at any a (rounded once, an exponential's argument z costs it |z| units): one
 // exponential E = e^-|z|, of which logistic(z) and logistic(-z) are 1 / (1 + E) and E / (1 + E), and what the roundings of z leave
-// over.  (2048 x 8192 backward, bound by memory: gelu 73.5 us, tanh's 75.2, silu 70.8; with a unit for every one of z 72.9, 70.6, 71.6.
-// 8192 x 768 x 2048 forward: 2 to 3 % more.)
+// over.  (2048 x 8192 backward, bound by memory: gelu 73.5 us, tanh's 75.2, silu 70.8; with a unit for every one of z 72.9, 70.6,
+// 71.6.  8192 x 768 x 2048 forward: 2 to 3 % more.)
 struct Both {
   float of, of_minus;  // logistic(z), logistic(-z)
 };
@@ -214,9 +214,9 @@ __device__ __forceinline__ typename Fragment<T>::type load_piece(const char* row
   }
   return v;
 }
-// Up to 32 rows, and up to 64 where every workgroup has a compute unit of its own.  (us, this and tiles: 32 rows of bfloat16, 4096 x 4096 17.1
-// and 29.5, 2048 x 8192 17.2 and 17.1; 64 rows 26.6 and 29.6, 768 x 2048 9.1 and 8.0, 4096 x 1024 25.6 and 19.3, 2048 x 8192 27.2 and 17.2; fp32
-// 64 rows 50 and 84, 15.3 and 18.4, 48 and 83, 79 and 44.)
+// Up to 32 rows, and up to 64 where every workgroup has a compute unit of its own.  (us, this and tiles: 32 rows of bfloat16,
+// 4096 x 4096 17.1 and 29.5, 2048 x 8192 17.2 and 17.1; 64 rows 26.6 and 29.6, 27.2 and 17.2, 768 x 2048 9.1 and 8.0, 4096 x 1024
+// 25.6 and 19.3; fp32 64 rows 50 and 84, 79 and 44, 15.3 and 18.4, 48 and 83.)
 inline bool few_rows(int64_t total, int64_t hidden) { return total <= 32 || (total <= 64 && hidden <= 16 * 256); }
 
 template <typename T, int ACT, uint32_t FM, uint32_t WAVES>

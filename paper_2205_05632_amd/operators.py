@@ -523,7 +523,7 @@ def compams_clip_gradients(gradients, max_norm: float, n: int = 1, *, scale: flo
     norms[i]) times it (0 and zeros where it is not finite: the worker takes no part).
     gradients: a matrix of n rows, or a list of them (a tensor's gradients of all workers each), in any mixture of types.
     out: the same shapes, each float32 or of its gradient's type, such as views of the step's g; None: in place.
-    max_norm: math.inf cuts nothing.  scale: takes a loss's scale back."""
+    max_norm: math.inf cuts nothing.  scale: takes a loss's scale back.  (Both are fp32 numbers and rounded to one.)"""
     alone = isinstance(gradients, torch.Tensor)
     given = [gradients] if alone else list(gradients)
     to = given if out is None else [out] if isinstance(out, torch.Tensor) else list(out)

@@ -21,7 +21,8 @@ int main() {
         b.p = base + at;
         bool shared = false;
         for (int64_t i = 0; i < a.rows; ++i)
-          for (int64_t j = 0; j < b.rows; ++j) shared |= a.bytes && b.bytes && at + j * b.ld < i * a.ld + a.bytes && i * a.ld < at + j * b.ld + b.bytes;
+          for (int64_t j = 0; a.bytes && j < b.rows; ++j)
+            shared |= b.bytes && at + j * b.ld < i * a.ld + a.bytes && i * a.ld < at + j * b.ld + b.bytes;
         const bool met = compams::meet(a, b);
         if (met == shared) ++exact;
         // only of two distances may areas be taken to meet that do not
@@ -29,6 +30,8 @@ int main() {
         else ++wrong;
       }
   const Area none = {nullptr, 3, 4, 4}, one = {base, 3, 4, 4}, far = {base, INT32_MAX, 1, INT64_C(1) << 33};
+  const Area still = {base, 3, 4, 0}, row = {base, 1, 4, 0};  // (rows that are not apart)
+  if (!compams::meet(still, row) || !compams::meet(row, still)) ++wrong;
   if (compams::meet(none, one) || compams::meet(one, none) || !compams::meet(far, one) || !compams::meet(one, far)) ++wrong;
   printf("%lld exact, %lld cautious, %lld wrong\n", (long long)exact, (long long)cautious, (long long)wrong);
   return wrong != 0;

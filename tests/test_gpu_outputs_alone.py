@@ -37,8 +37,9 @@ def clip(tensors, n, norms, factors, to=None):
     table = (ops.compams_clip_tensor * len(tensors))()
     for i, (row, t) in enumerate(zip(table, tensors)):
         o = to.get(i) if to else None
-        for k, v in {"from": t.data_ptr(), "ld_from": t.stride(0), "to": None if o is None else o.data_ptr(), "ld_to": 0 if o is None else o.stride(0),
-                     "count": t.shape[1], "from_type": kind[t.dtype], "to_type": kind[t.dtype]}.items():
+        for k, v in {"from": t.data_ptr(), "ld_from": t.stride(0), "to": None if o is None else o.data_ptr(),
+                     "ld_to": 0 if o is None else o.stride(0), "count": t.shape[1], "from_type": kind[t.dtype],
+                     "to_type": kind[t.dtype]}.items():
             setattr(row, k, v)
     a = ops.compams_clip(n=n, tensors=len(tensors), tensor=ctypes.addressof(table), max_norm=3.0, scale=0.5,
                          norms=norms.data_ptr() if norms is not None else None, factors=factors.data_ptr() if factors is not None else None)

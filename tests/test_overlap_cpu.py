@@ -107,7 +107,8 @@ def test_linear_cross_entropy_refuses_outputs_over_inputs(kw):
 
 
 def clip(n, **kw):
-    t = ops.compams_clip_tensor(**{"from": at(0), "ld_from": 100, "to": at(1), "ld_to": 100, "count": 40, "from_type": ops.F32, "to_type": ops.F32, **kw})
+    t = ops.compams_clip_tensor(**{"from": at(0), "ld_from": 100, "to": at(1), "ld_to": 100, "count": 40, "from_type": ops.F32,
+                                   "to_type": ops.F32, **kw})
     a = ops.compams_clip(n=n, tensors=1, tensor=ctypes.addressof(t), max_norm=1.0, scale=1.0, norms=at(2), factors=at(3), workspace=at(4),
                          workspace_bytes=255)
     a.table = t
