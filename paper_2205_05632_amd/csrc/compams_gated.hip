@@ -318,7 +318,9 @@ template <typename T>
 void launch_forward(ForwardArgs& a, int act, hipStream_t stream) {
   if (few_rows(a.total, a.hidden)) return launch_few<T>(a, act, stream);
   switch (tile_size({{a.total, 2 * static_cast<uint64_t>(a.hidden), 1, a.cols}}, sizeof(T) == 4)) {
-    case kTile256: launch_forward<T, 4, 2, 4, 8>(a, act, stream); break;  // (64 columns of a projection to a wavefront)
+    case kTile256:
+      if constexpr (sizeof(T) == 2) launch_forward<T, 4, 2, 4, 8>(a, act, stream);
+      break;  // (64 columns of a projection to a wavefront)
     case kTile128: launch_forward<T, 2, 2, 4, 4>(a, act, stream); break;
     default: launch_forward<T, 2, 2, 2, 2>(a, act, stream); break;
   }

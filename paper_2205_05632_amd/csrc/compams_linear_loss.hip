@@ -542,7 +542,9 @@ void launch_stats(LossArgs& a, hipStream_t stream) {
 template <typename T>
 void launch_stats(LossArgs& a, hipStream_t stream) {
   switch (tile_size({{a.total, a.vocab, 1, a.cols}}, sizeof(T) == 4)) {
-    case kTile256: launch_stats<T, 2, 4, 8, 4>(a, stream); break;
+    case kTile256:
+      if constexpr (sizeof(T) == 2) launch_stats<T, 2, 4, 8, 4>(a, stream);
+      break;
     case kTile128: launch_stats<T, 2, 2, 4, 4>(a, stream); break;
     default: launch_stats<T, 4, 1, 1, 4>(a, stream); break;
   }
@@ -565,7 +567,9 @@ void launch_piece(LossArgs& a, hipStream_t stream) {
 template <typename T>
 void launch_piece(LossArgs& a, TileSize size, hipStream_t stream) {
   switch (size) {
-    case kTile256: launch_piece<T, 2, 2, 8, 4, 64>(a, stream); break;
+    case kTile256:
+      if constexpr (sizeof(T) == 2) launch_piece<T, 2, 2, 8, 4, 64>(a, stream);
+      break;
     case kTile128: launch_piece<T, 2, 2, 4, 4>(a, stream); break;
     default: launch_piece<T, 2, 2, 2, 2>(a, stream); break;
   }

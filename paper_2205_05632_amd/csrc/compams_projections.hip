@@ -111,7 +111,9 @@ template <typename T>
 void launch(ProjectionArgs& a, hipStream_t stream) {
   switch (tile_size({{a.dx ? a.total : 0, a.cols, a.splits, static_cast<uint64_t>(a.hidden) * a.count / a.splits},
                      {a.weights ? a.hidden : 0, a.cols, static_cast<uint64_t>(a.weights) * a.n, a.rows}}, sizeof(T) == 4)) {
-    case kTile256: launch<T, 2, 2, 8, 4, 64>(a, stream); break;
+    case kTile256:
+      if constexpr (sizeof(T) == 2) launch<T, 2, 2, 8, 4, 64>(a, stream);
+      break;
     case kTile128: launch<T, 2, 2, 4, 4>(a, stream); break;
     default: launch<T, 2, 2, 2, 2>(a, stream); break;
   }

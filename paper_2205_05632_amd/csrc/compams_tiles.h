@@ -201,7 +201,12 @@ struct Tiles {
   using PlaceA = Place<T, FA, kM, STEP>;
   using PlaceB = Place<T, FB, kN, STEP>;
   static constexpr uint32_t kBytesA = PlaceA::kBytes, kBytesB = PlaceB::kBytes;
-  f32x4 sum[FM][FN];
+  // fp32 sums are formed in two levels, 64 terms and then these: they are off by the roundings of so many, not of all of them (dweight
+  // of 16384 random rows by 0.4e-6 of itself, in a row 2.2e-6).  It costs 2 to 4 % (8192 x 768 x 2048 gated forward 401 -> 414 us,
+  // projections' gradients 789 -> 804; 64 terms at a time, as a branch in the loop doubles the registers, 462), and tiles of 256, which
+  // are no faster in fp32.  Of 16-bit operands the sums stay in a row: most are rounded to 16 bits.
+  static constexpr bool kLevels = sizeof(T_) == 4;
+  f32x4 sum[FM][FN], whole[kLevels ? FM : 1][kLevels ? FN : 1];
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -215,6 +220,27 @@ struct Tiles {
   __device__ static __forceinline__ uint32_t first_n() { return wave() % WN * (FN * 16); }
   __device__ static __forceinline__ uint32_t lane_m() { return threadIdx.x & 15u; }
   __device__ static __forceinline__ uint32_t lane_n() { return (threadIdx.x >> 4 & 3u) * 4; }
+
+  // The sums of some steps join those before.  (first: what is there is what the steps' are to join)
+  __device__ __forceinline__ void join(bool first = false) {
+    if constexpr (kLevels) {
+#pragma unroll
+      for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < FN; ++j) {
+          whole[i][j] = first ? sum[i][j] : whole[i][j] + sum[i][j];
+          sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+  }
+  __device__ __forceinline__ void joined() {
+    if constexpr (kLevels) {
+#pragma unroll
+      for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < FN; ++j) sum[i][j] += whole[i][j];
+    }
+  }
 
   __device__ __forceinline__ void step(const lds_char* a, const lds_char* b) {
     const uint32_t m = first_m(), n = first_n();
@@ -256,6 +282,7 @@ struct Tiles {
         if (++at < count) pair(at, a, b, b2);
       }
     };
+    join(true);
     load(lds.a[0], lds.b[0]);
     if constexpr (CUT && (FA == kAlong || FB == kAlong)) {
       // The last step of a pair whose rows end within 16 bytes: what follows there may be anything, a NaN too.
@@ -278,6 +305,7 @@ struct Tiles {
         load(lds.a[0], lds.b[0]);
         if (first_ends(s + 1)) cut(lds.a[1], lds.b[1]);
         step(lds.a[1], lds.b[1]);
+        join();
       }
       arrived();
       lds_char *ta = lds.a[0], *tb = lds.b[0];
@@ -299,12 +327,14 @@ struct Tiles {
         arrived();
         if (s < steps) load(lds.a[0], lds.b[0]);
         step(lds.a[1], lds.b[1]);
+        join();
       }
       if (steps & 1u) {
         arrived();
         step(lds.a[0], lds.b[0]);
       }
     }
+    joined();
   }
   // What this wavefront loaded is in LDS, and so is everybody's; everybody is done with the step before.
   __device__ static __forceinline__ void arrived() {
@@ -476,7 +506,7 @@ __device__ __forceinline__ void tile_at(uint32_t id, uint32_t tall, uint32_t wid
 // sum.  The larger a tile, the higher its rate; but the compute units' shares of few large tiles are uneven, and a tile alone
 // on a compute unit has nothing beside it while it loads.  Rates of a full card, and of one tile to a compute unit, relative
 // to the first (8192 x 8192 x 768 bfloat16, TFLOP/s: 256 x 256 1340, 128 x 128 1130, 64 x 64 770; alone, 1024 x 1024 x 2048
-// and the like: 1100, 800, 375. fp32, where the matrix cores bound every size: 133, 133, 130; alone 64 x 64 100).  Launches of
+// and the like: 1100, 800, 375. fp32, where the matrix cores bound every size, 128 x 128 133, 64 x 64 130, alone 100).  Launches of
 // more than one kind of result take 256 x 128 in steps of 64 bytes for the largest, of which two and three workgroups share a
 // compute unit: one stores while another multiplies (8 x 1024 x 768 x 2048 projections' gradients 115 us, with 128 x 128 123).
 enum TileSize { kTile256, kTile128, kTile64 };
@@ -501,10 +531,10 @@ inline TileSize tile_size(std::initializer_list<Work> all, bool wide_type) {
   };
   // (the last: what a tile takes besides its products, some 2 us to load the first step and to store, as far as the others on
   // its compute unit do not hide it: 180 x 3818 x 29084 bfloat16, sums of 90 terms in 54000 tiles of 64 x 64, 564 us)
-  const double large = all.size() > 1 ? cost(256, 128, 0.97, wide_type ? 0.9 : 0.6, 2.6e6) : cost(256, 256, 1.0, 0.97, 6e6);
+  const double large = all.size() > 1 ? cost(256, 128, 0.97, 0.6, 2.6e6) : cost(256, 256, 1.0, 0.97, 6e6);
   const double middle = wide_type ? cost(128, 128, 1.0, 0.9, 0.4e6) : cost(128, 128, 0.84, 0.6, 2.6e6);
   const double small = wide_type ? cost(64, 64, 0.97, 0.75, 0.15e6) : cost(64, 64, 0.57, 0.28, 1e6);
-  if (large <= middle && large <= small) return kTile256;
+  if (!wide_type && large <= middle && large <= small) return kTile256;  // (fp32's two levels of sums fill the registers before)
   return middle <= small ? kTile128 : kTile64;
 }
 // Into how many parts the k of a result is cut whose tiles are too few for the card, each part with 1024 terms and more (fp32,
