@@ -14,7 +14,8 @@ __device__ __forceinline__ float logistic(float a) { return __builtin_amdgcn_rcp
 // The normal distribution's integral up to a, with e = exp(-a^2 / 2), which the density needs too: for z = |a| / sqrt 2,
 // erfc(z) = e p(t) / (1 + 2 z) with a polynomial in t = (z - 2) / (z + 2) (the form of Shepherd and Laframboise, "Chebyshev
 // approximation of (1 + 2 x) exp(x^2) erfc x", 1981; the coefficients by interpolation at the Chebyshev points of 0 <= z <= 10.2, as
-// fp32 off by 3.6e-8 at most, 3.1e-8 of the value).  Negative a keep their digits.  (8290 x 576 float16 backward: 51 us with the library's erfcf.)
+// fp32 off by 3.6e-8 at most, 3.1e-8 of the value).  Negative a keep their digits.  (8290 x 576 float16 backward: 51 us with the
+// library's erfcf.)
 __device__ __forceinline__ float normal_cdf(float a, float e) {
   const float z = fminf(fabsf(a) * 0.70710678118654752f, 16.0f), up = z + 2.0f, one = fmaf(2.0f, z, 1.0f);
   const float r = __builtin_amdgcn_rcpf(up * one), t = (z - 2.0f) * (r * one);

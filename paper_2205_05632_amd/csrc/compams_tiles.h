@@ -201,10 +201,10 @@ struct Tiles {
   using PlaceA = Place<T, FA, kM, STEP>;
   using PlaceB = Place<T, FB, kN, STEP>;
   static constexpr uint32_t kBytesA = PlaceA::kBytes, kBytesB = PlaceB::kBytes;
-  // fp32 sums are formed in two levels, 64 terms and then these: they are off by the roundings of so many, not of all of them (dweight
-  // of 16384 random rows by 0.4e-6 of itself, in a row 2.2e-6).  It costs 2 to 4 % (8192 x 768 x 2048 gated forward 401 -> 414 us,
-  // projections' gradients 789 -> 804; 64 terms at a time, as a branch in the loop doubles the registers, 462), and tiles of 256, which
-  // are no faster in fp32.  Of 16-bit operands the sums stay in a row: most are rounded to 16 bits.
+  // fp32 sums are formed in two levels, 64 terms and then these: they are off by the roundings of so many, not of all of them
+  // (dweight of 16000 random rows by 0.4e-6 of itself, in a row 2.3e-6).  It costs 2 to 4 % (8192 x 768 x 2048 gated forward 401 ->
+  // 414 us, projections' gradients 789 -> 804; 128 terms at a time, as a branch in the loop, take half as many registers again:
+  // 462), and tiles of 256, which are no faster in fp32.  Of 16-bit operands the sums stay in a row: most are rounded to 16 bits.
   static constexpr bool kLevels = sizeof(T_) == 4;
   f32x4 sum[FM][FN], whole[kLevels ? FM : 1][kLevels ? FN : 1];
 
